@@ -343,6 +343,127 @@ int first_set_sampling(first_ctx *ctx, int32_t top_k, float temperature, const f
 int first_sample_topk(const float *logits, int32_t B, int32_t vocab, int32_t top_k, float temperature,
                       const float *uniforms, int32_t *tokens, void *stream);
 
+/* Sampling with generation settings of its own for every row of a batch.  (The paper's settings, temperature 0.8 and
+ * top-k 10, are one case: appendix "Training and Inference Setup".)  Per row: the candidates are the tokens whose
+ * logit is above -inf (NaN counts as -inf), in descending order of their logits, equal ones (-0 = +0) in index order;
+ * their weights are exp((logit - max) / temperature), a logit equal to the maximum weighing 1.  Each filter keeps a
+ * prefix of that order:
+ *   1. top_k > 0: the first top_k candidates;  min_p > 0: those whose weight is at least min_p (the first always stays)
+ *   2. top_p < 1: of what is left, every candidate before which the weights sum to less than top_p times their total
+ *      (the first always stays)
+ * The token is the first candidate left whose cumulative weight exceeds u times the weight left.  u is the row's
+ * uniform draw; below 0 it counts as 0, at 1 and above (or NaN) as the largest float32 below 1.  temperature <= 0 (or NaN) is greedy: the
+ * lowest index among the largest logits.  A row without a candidate gets token -1 (which a later step refuses with
+ * FIRST_FLAG_BAD_TOKEN).  With top_k alone the result is first_sample_topk's, up to rounding at a weight's border.
+ * Weights are held as multiples of 2^-43 of the largest one and summed as integers: the result does not depend on the
+ * order of summation or the launch shape, and a draw that falls within that of a border may take the neighbour.
+ *   logits       dev float32 [B][row_stride], row_stride >= vocab (elements; columns beyond vocab are not read)
+ *   temperature, top_p, min_p   dev float32 [B] or NULL (= 1, 1, 0 for every row)
+ *   top_k        dev int32 [B] or NULL (= no limit)
+ *   uniforms     dev float32 [B];  tokens  dev int32 [B]
+ * first_sample is stateless (no context, no scratch; one launch on `stream`); B = 0 does nothing.
+ * first_set_sampling_rows makes every later first_decode_step and first_prefill of the context fill next_tokens this
+ * way (arrays of B entries in the step's batch order, borrowed; the caller may refresh their contents between
+ * steps, in stream order); NULL restores argmax.  The last of it and first_set_sampling holds.
+ * Errors: FIRST_E_ARG, FIRST_E_SHAPE (row_stride), FIRST_E_UNSUPPORTED (vocab > FIRST_SAMPLE_MAX_VOCAB), FIRST_E_CUDA. */
+#define FIRST_SAMPLE_MAX_VOCAB 524288
+typedef struct {
+    const float *temperature; /* dev [B] or NULL */
+    const int32_t *top_k;     /* dev [B] or NULL */
+    const float *top_p;       /* dev [B] or NULL */
+    const float *min_p;       /* dev [B] or NULL */
+    const float *uniforms;    /* dev [B]         */
+} first_sampling;
+int first_sample(const float *logits, int64_t row_stride, int32_t B, int32_t vocab, const float *temperature,
+                 const int32_t *top_k, const float *top_p, const float *min_p, const float *uniforms, int32_t *tokens,
+                 void *stream);
+int first_set_sampling_rows(first_ctx *ctx, const first_sampling *sampling);
+
+/* Low-rank adapters of many requests beside a shared projection.  The paper trains one adapter with its routers and
+ * merges it ("LoRA Compensation Module": rank 8 on attention and feed-forward); a batch whose requests were tuned for
+ * different tasks keeps them apart instead: for every row r with a = row_adapter[r] in [0, n_adapters)
+ *   y[r][f] += scales[a] * sum_j b[a][f][j] * h_j,   h_j = sum_k a[a][s*rank + j][k] * x[r][k],  s = segment of f
+ * and rows with any other id are neither read nor written.  The output features come in segments (q | k | v,
+ * gate | up), each with rows of `a` of its own: segment s covers features segments[s] .. segments[s+1]-1.
+ *   x            dev [rows][x_stride], float32 or bfloat16, k columns used
+ *   a            dev [n_adapters][n_segments*rank][k];  b  dev [n_adapters][n][rank]   (w_dtype)
+ *   scales       dev float32 [n_adapters] (alpha / rank of the usual recipe) or NULL (= 1)
+ *   row_adapter  dev int32 [rows]
+ *   segments     HOST int32 [n_segments+1]: 0 = first, n = last, increasing; inner borders multiples of 16
+ *   y            dev [rows][y_stride], float32 or bfloat16, n columns updated in place; must not overlap x
+ * Sums are float32; h is not rounded in between; y is rounded once per call.  The result does not depend on which
+ * other rows are in the batch.  rows = 0 or n_adapters = 0 does nothing.  No scratch, no wait.
+ * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides, segments), FIRST_E_UNSUPPORTED (rank not a multiple of 8 or above
+ * FIRST_LORA_MAX_RANK, k not a multiple of 8, more than FIRST_LORA_MAX_SEGMENTS segments, an inner border that is no
+ * multiple of 16; x, a, b not 16-byte aligned or rows of x not a multiple of 16 bytes apart; y not aligned to its
+ * element), FIRST_E_CUDA.
+ *
+ * first_set_adapters: from then on first_decode_step and first_prefill apply the adapters beside the projections of
+ * every layer.  All members are borrowed (scales, seq_adapter and the adapters' contents may change between steps, in
+ * stream order).  seq_adapter[b] is the adapter of batch row b (of a pool's slot b), any other id = none.
+ * The pointer-array members are HOST arrays of n_layers DEVICE pointers in the model's dtype; a NULL array, or a NULL
+ * entry, leaves that projection alone (a and b of a projection: both or neither).  Shapes per layer as first_lora's
+ * a and b: qkv segments q | k | v of d_model inputs, o one segment of Hq*hd inputs, gate_up segments gate | up of d_model
+ * inputs, down one segment of ffn_dim inputs.  With gate_up adapters the gate/up projection does not use its fused
+ * activation.  NULL removes them.
+ * Errors: FIRST_E_ARG, FIRST_E_UNSUPPORTED (rank as above; gate_up adapters when ffn_dim is no multiple of 16; a
+ * pointer that is not 16-byte aligned). */
+#define FIRST_LORA_MAX_SEGMENTS 4
+#define FIRST_LORA_MAX_RANK 128
+typedef struct {
+    int32_t n_adapters, rank;
+    const float *scales;          /* dev [n_adapters] or NULL */
+    const int32_t *seq_adapter;   /* dev [max_batch]          */
+    const void *const *qkv_a, *const *qkv_b;          /* host[L] -> dev [n][3*rank][d_model], [n][(Hq+2*Hkv)*hd][rank] */
+    const void *const *o_a, *const *o_b;              /* host[L] -> dev [n][rank][Hq*hd],     [n][d_model][rank]       */
+    const void *const *gate_up_a, *const *gate_up_b;  /* host[L] -> dev [n][2*rank][d_model], [n][2*ffn_dim][rank]     */
+    const void *const *down_a, *const *down_b;        /* host[L] -> dev [n][rank][ffn_dim],   [n][d_model][rank]       */
+} first_adapters;
+int first_lora(const void *x, int32_t x_dtype, int64_t x_stride, const void *a, const void *b, int32_t w_dtype,
+               const float *scales, const int32_t *row_adapter, int32_t n_adapters, int32_t rank, int32_t n_segments,
+               const int32_t *segments, int32_t rows, int32_t k, int32_t n, void *y, int32_t y_dtype, int64_t y_stride,
+               void *stream);
+int first_set_adapters(first_ctx *ctx, const first_adapters *adapters);
+
+/* Rotary positions on caller-owned queries and keys, in place (for callers with a prefill of their own; the step and
+ * first_prefill rotate by themselves).  Pair i of the first rot_dim elements of every head of token t turns by the
+ * angle pos[t] * inv_freq[i]: (a, b) -> (a c - b s, b c + a s), c = factor * cos, s = factor * sin; elements from
+ * rot_dim on are not touched.  Pairs are (i, i + rot_dim/2), or (2i, 2i+1) with interleaved != 0.  Angles are formed in
+ * 64 bits, so that far positions keep float32-exact cosines; products in float32, rounded once.
+ *   q, k       dev, head h of token t at t*token_stride + h*head_stride (elements), n_q_heads / n_kv_heads heads of
+ *              head_dim elements, float32 or bfloat16 (dtype); 0 heads = not given.  Every element belongs to one (token, head): rows
+ *              may not overlap, nor may q and k.
+ *   pos        dev int32 [tokens];  inv_freq  dev float64 [rot_dim/2], radians per position
+ * tokens = 0 does nothing.  No scratch, no wait.
+ * first_rope_freqs fills inv_freq (HOST float64 [rot_dim/2]) and *factor from a scheme, w_i = base^(-2i/rot_dim):
+ *   FIRST_ROPE_NONE    w_i
+ *   FIRST_ROPE_LINEAR  w_i / factor
+ *   FIRST_ROPE_LLAMA3  k w_i + (1-k) w_i / factor, k = clamp((trained_len w_i / 2 pi - low) / (high - low), 0, 1)
+ *                      (LLaMA-3.2: factor 32, low 1, high 4, trained_len 8192)
+ *   FIRST_ROPE_YARN    the same blend with k = 1 - clamp((i - lo) / max(hi - lo, 0.001), 0, 1), lo = max(floor(d(high)), 0),
+ *                      hi = min(ceil(d(low)), rot_dim - 1), d(t) = rot_dim ln(trained_len / (2 pi t)) / (2 ln base)
+ *                      (usual: low 1, high 32); *factor = 0.1 ln(factor) + 1.  Otherwise *factor = 1.
+ * first_set_rope replaces the frequencies of a context's step and prefill (pairs (i, i + head_dim/2) over the whole
+ * head): inv_freq HOST float64 [head_dim/2], finite, and factor; NULL restores base^(-2i/head_dim) of the description.
+ * Waits for the device; keys already in a cache keep the rotation they were written with.
+ * Errors: FIRST_E_ARG, FIRST_E_SHAPE (rot_dim odd or above head_dim, strides that overlap), FIRST_E_UNSUPPORTED (head_dim
+ * > 65536), FIRST_E_CAPACITY (more than 2^38 pairs), FIRST_E_STATE (first_set_rope during a stream capture), FIRST_E_CUDA. */
+#define FIRST_ROPE_NONE 0
+#define FIRST_ROPE_LINEAR 1
+#define FIRST_ROPE_LLAMA3 2
+#define FIRST_ROPE_YARN 3
+typedef struct {
+    int32_t rot_dim, scaling;  /* FIRST_ROPE_* */
+    double base, factor;       /* factor >= 1 (not read with FIRST_ROPE_NONE) */
+    double low, high;          /* LLAMA3, YARN: turns over the trained length; 0 < low < high */
+    int64_t trained_len;       /* LLAMA3, YARN: positions the model was trained on */
+} first_rope_spec;
+int first_rope_freqs(const first_rope_spec *spec, double *inv_freq, double *factor);
+int first_rope(void *q, int64_t q_token_stride, int64_t q_head_stride, int32_t n_q_heads, void *k, int64_t k_token_stride,
+               int64_t k_head_stride, int32_t n_kv_heads, int32_t dtype, int64_t tokens, int32_t head_dim, int32_t rot_dim,
+               const int32_t *pos, const double *inv_freq, float factor, int32_t interleaved, void *stream);
+int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
+
 /* Wait for `stream`, read and clear the device flag word.  Returns FIRST_OK with
  * *flags = 0, or FIRST_E_DEVICE_FLAG with the FIRST_FLAG_* bits in *flags. */
 int first_last_device_flags(first_ctx *ctx, uint32_t *flags, void *stream);

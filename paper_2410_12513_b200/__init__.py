@@ -8,9 +8,11 @@ the compiled library or without a CUDA device the calls raise.
 """
 from .binding import (FirstContext, FirstError, FirstPool, KVCache, first_set_mask_host, first_create, first_decode_step, first_destroy,
                       first_get_plan, first_last_device_flags, first_prefill, first_prefill_route, first_prefill_route_static, first_profile, first_profile_read, first_sample_topk, first_set_mask,
-                      first_set_option, first_set_sampling, first_step_trace, lib, library_path)
+                      first_lora, first_rope, first_rope_freqs, first_sample, first_set_adapters, first_set_option, first_set_rope,
+                      first_set_sampling, first_set_sampling_rows, first_step_trace, lib, library_path)
 
 __all__ = ["FirstContext", "FirstError", "FirstPool", "KVCache", "first_set_mask_host", "first_create", "first_decode_step", "first_destroy",
            "first_get_plan", "first_last_device_flags", "first_prefill", "first_prefill_route", "first_prefill_route_static", "first_profile",
            "first_profile_read", "first_sample_topk", "first_set_mask",
-           "first_set_option", "first_set_sampling", "first_step_trace", "lib", "library_path"]
+           "first_lora", "first_rope", "first_rope_freqs", "first_sample", "first_set_adapters", "first_set_option", "first_set_rope",
+           "first_set_sampling", "first_set_sampling_rows", "first_step_trace", "lib", "library_path"]

@@ -3,6 +3,7 @@ CUDA tensors.  Argument marshalling only -- no arithmetic happens here."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from pathlib import Path
 
 import torch
@@ -41,6 +42,20 @@ class KVCacheC(C.Structure):
     _fields_ = [("k", C.POINTER(C.c_void_p)), ("v", C.POINTER(C.c_void_p)), ("slab_off", C.c_void_p),
                 ("slab_cap", C.c_void_p), ("len", C.c_void_p), ("pos", C.c_void_p), ("cap_total", C.c_int64),
                 ("per_layer", C.c_int32), ("cap_total_l", C.POINTER(C.c_int64))]
+
+
+class SamplingC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "uniforms")]
+
+
+class AdaptersC(C.Structure):
+    _fields_ = [("n_adapters", C.c_int32), ("rank", C.c_int32), ("scales", C.c_void_p), ("seq_adapter", C.c_void_p)] + \
+               [(f"{t}_{m}", C.POINTER(C.c_void_p)) for t in ("qkv", "o", "gate_up", "down") for m in ("a", "b")]
+
+
+class RopeSpecC(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("trained_len", C.c_int64)]
 
 
 def library_path() -> Path:
@@ -106,6 +121,17 @@ def lib():
         L.first_selftest_wait_expiry.restype = C.c_int
         L.first_step_trace.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         L.first_step_trace.restype = C.c_int
+        p, i32, i64, f64 = C.c_void_p, C.c_int32, C.c_int64, C.c_double
+        L.first_sample.argtypes = [p, i64, i32, i32, p, p, p, p, p, p, p]
+        L.first_set_sampling_rows.argtypes = [p, C.POINTER(SamplingC)]
+        L.first_lora.argtypes = [p, i32, i64, p, p, i32, p, p, i32, i32, i32, p, i32, i32, i32, p, i32, i64, p]
+        L.first_set_adapters.argtypes = [p, C.POINTER(AdaptersC)]
+        L.first_rope_freqs.argtypes = [C.POINTER(RopeSpecC), p, p]
+        L.first_rope.argtypes = [p, i64, i64, i32, p, i64, i64, i32, i32, i64, i32, i32, p, p, C.c_float, i32, p]
+        L.first_set_rope.argtypes = [p, p, f64]
+        for name in ("first_sample", "first_set_sampling_rows", "first_lora", "first_set_adapters", "first_rope_freqs",
+                     "first_rope", "first_set_rope"):
+            getattr(L, name).restype = C.c_int
         L.first_kernel_class_count.restype = C.c_int32
         L.first_kernel_class_name.restype = C.c_char_p
         L.first_kernel_class_name.argtypes = [C.c_int32]
@@ -377,6 +403,198 @@ def first_sample_topk(logits, top_k, temperature, uniforms, tokens, stream=None)
         raise FirstError(rc, "first_sample_topk")
 
 
+def _on(t, dtype, n, what, dev):
+    """Address of a contiguous CUDA tensor of n elements (None: NULL) on device `dev`."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{what} must be a CUDA tensor of {dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous with {n} elements")
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on another device")
+    return t.data_ptr()
+
+
+def _device_of(t, what):
+    """The device index of a CUDA tensor; the calls launch on the current device, so it has to be that one."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a CUDA tensor")
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{what} is on device {dev}, not on the current one")
+    return dev
+
+
+_DTYPE_CODE = {torch.float32: FIRST_DTYPE_F32, torch.bfloat16: FIRST_DTYPE_BF16}
+
+
+def _code(t, what):
+    c = _DTYPE_CODE.get(t.dtype)
+    if c is None:
+        raise TypeError(f"{what} must be float32 or bfloat16")
+    return c
+
+
+def _rows_of(t, what):
+    """(row stride) of a matrix whose rows may be padded; elements of a row are adjacent."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be a matrix with adjacent elements in a row")
+    return t.stride(0)
+
+
+def first_sample(logits, uniforms, tokens, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """Next token of every row with settings of its own (see first.h).  logits CUDA float32 [B][vocab], rows may be
+    padded; uniforms, temperature, top_p, min_p CUDA float32 [B], top_k CUDA int32 [B]; tokens CUDA int32 [B] (output)."""
+    dev = _device_of(logits, "logits")
+    if logits.dtype != torch.float32:
+        raise TypeError("logits must be float32")
+    ld = _rows_of(logits, "logits")
+    B, V = logits.shape
+    f32, i32 = torch.float32, torch.int32
+    if uniforms is None or tokens is None:
+        raise TypeError("uniforms and tokens are required")
+    rc = lib().first_sample(logits.data_ptr(), ld, B, V, _on(temperature, f32, B, "temperature", dev), _on(top_k, i32, B, "top_k", dev),
+                            _on(top_p, f32, B, "top_p", dev), _on(min_p, f32, B, "min_p", dev),
+                            _on(uniforms, f32, B, "uniforms", dev), _on(tokens, i32, B, "tokens", dev), _stream(stream))
+    if rc:
+        raise FirstError(rc, "first_sample")
+
+
+@functools.lru_cache(maxsize=256)
+def _segment_array(segments):
+    return (C.c_int32 * len(segments))(*segments)
+
+
+def first_lora(x, a, b, row_adapter, y, scales=None, segments=None, stream=None):
+    """y[r] += scales[i] * b[i] (a[i] x[r]), i = row_adapter[r], rows with an id outside 0 .. n-1 left alone (see first.h).
+    x CUDA [rows][k], y CUDA [rows][n] (rows may be padded), float32 or bfloat16; a CUDA [adapters][segments*rank][k],
+    b CUDA [adapters][n][rank], contiguous, of one type; segments: borders of the output segments, (0, ..., n)."""
+    dev = _device_of(x, "x")
+    ldx, ldy = _rows_of(x, "x"), _rows_of(y, "y")
+    (rows, k), n = x.shape, y.shape[1]
+    if y.shape[0] != rows or a.dim() != 3 or b.dim() != 3 or a.dtype != b.dtype:
+        raise ValueError("x and y must have one row each per row of the batch; a, b three dimensions and one type")
+    segments = (0, n) if segments is None else tuple(segments)
+    adapters, _, rank = b.shape
+    if b.shape[1] != n or tuple(a.shape) != (adapters, (len(segments) - 1) * rank, k):
+        raise ValueError("a must be [adapters][segments*rank][k] and b [adapters][n][rank]")
+    if not y.is_cuda or y.get_device() != dev:
+        raise ValueError("y is on another device")
+    rc = lib().first_lora(x.data_ptr(), _code(x, "x"), ldx, _on(a, a.dtype, a.numel(), "a", dev), _on(b, b.dtype, b.numel(), "b", dev),
+                          _code(a, "a"), _on(scales, torch.float32, adapters, "scales", dev),
+                          _on(row_adapter, torch.int32, rows, "row_adapter", dev), adapters, rank, len(segments) - 1,
+                          _segment_array(segments), rows, k, n, y.data_ptr(), _code(y, "y"), ldy, _stream(stream))
+    if rc:
+        raise FirstError(rc, "first_lora")
+
+
+def first_rope_freqs(rot_dim, base, scaling="none", factor=1.0, low=1.0, high=None, trained_len=0):
+    """-> (inv_freq numpy float64 [rot_dim/2], factor on cosines and sines) of a scheme: none, linear, llama3, yarn."""
+    import numpy as np
+    kinds = {"none": 0, "linear": 1, "llama3": 2, "yarn": 3}
+    if scaling not in kinds:
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if high is None:
+        high = 32.0 if scaling == "yarn" else 4.0
+    spec = RopeSpecC(int(rot_dim), kinds[scaling], float(base), float(factor), float(low), float(high), int(trained_len))
+    inv = np.empty(max(int(rot_dim) // 2, 1), dtype=np.float64)
+    out = C.c_double(1.0)
+    rc = lib().first_rope_freqs(C.byref(spec), inv.ctypes.data, C.byref(out))
+    if rc:
+        raise FirstError(rc, "first_rope_freqs")
+    return inv, out.value
+
+
+def _heads_of(t, what):
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what} must be [tokens][heads][head_dim] with adjacent elements in a head")
+
+
+def first_rope(q, k, pos, inv_freq, factor=1.0, interleaved=False, stream=None):
+    """Rotates q CUDA [tokens][Hq][hd] and k CUDA [tokens][Hkv][hd] (or None) in place; both may be views of a larger
+    buffer.  pos CUDA int32 [tokens]; inv_freq CUDA float64 [rot/2] (rot <= hd elements of a head are rotated)."""
+    dev = _device_of(q, "q")
+    _heads_of(q, "q")
+    T, hq, hd = q.shape
+    kp, hk, ks = None, 0, (0, 0)
+    if k is not None:
+        _heads_of(k, "k")
+        if k.shape[0] != T or k.shape[2] != hd or k.dtype != q.dtype:
+            raise ValueError("q and k must agree in tokens, head size and type")
+        if not k.is_cuda or k.get_device() != dev:
+            raise ValueError("k is on another device")
+        kp, hk, ks = k.data_ptr(), k.shape[1], k.stride()
+    qs = q.stride()
+    rc = lib().first_rope(q.data_ptr(), qs[0], qs[1], hq, kp, ks[0], ks[1], hk, _code(q, "q"), T, hd, 2 * inv_freq.numel(),
+                          _on(pos, torch.int32, T, "pos", dev), _on(inv_freq, torch.float64, inv_freq.numel(), "inv_freq", dev),
+                          float(factor), int(bool(interleaved)), _stream(stream))
+    if rc:
+        raise FirstError(rc, "first_rope")
+
+
+def first_set_sampling_rows(h, uniforms=None, temperature=None, top_k=None, top_p=None, min_p=None):
+    """Per-row sampling of later steps; arrays CUDA [B], borrowed.  uniforms None restores argmax."""
+    if uniforms is None:
+        rc = lib().first_set_sampling_rows(h, None)
+    else:
+        s = SamplingC(_dev(temperature, torch.float32, "temperature"), _dev(top_k, torch.int32, "top_k"),
+                      _dev(top_p, torch.float32, "top_p"), _dev(min_p, torch.float32, "min_p"),
+                      _dev(uniforms, torch.float32, "uniforms"))
+        rc = lib().first_set_sampling_rows(h, C.byref(s))
+    if rc:
+        raise FirstError(rc, "first_set_sampling_rows")
+
+
+def first_set_adapters(h, shape, dtype, adapters=None, seq_adapter=None, scales=None):
+    """adapters: dict of per-layer lists of (a, b) pairs (None = no adapter there) under qkv, o, gate_up, down;
+    seq_adapter CUDA int32 [max_batch].  Everything is borrowed.  adapters None removes them.  Returns what to keep."""
+    if adapters is None:
+        rc = lib().first_set_adapters(h, None)
+        if rc:
+            raise FirstError(rc, "first_set_adapters")
+        return None
+    wd = torch.float32 if dtype == FIRST_DTYPE_F32 else torch.bfloat16
+    D, F, qd = shape.d_model, shape.ffn_dim, shape.n_q_heads * shape.head_dim
+    sizes = {"qkv": (3, D, qd + 2 * shape.n_kv_heads * shape.head_dim), "o": (1, qd, D), "gate_up": (2, D, 2 * F), "down": (1, F, D)}
+    if set(adapters) - set(sizes):
+        raise ValueError(f"unknown projections {sorted(set(adapters) - set(sizes))}")
+    pairs = [p for rows in adapters.values() for p in rows if p is not None]
+    if not pairs:
+        raise ValueError("no adapter given")
+    n, _, rank = pairs[0][1].shape
+    c = AdaptersC(n, rank, _dev(scales, torch.float32, "scales"), _dev(seq_adapter, torch.int32, "seq_adapter"))
+    if scales is not None and scales.numel() != n:
+        raise ValueError("scales must have one entry per adapter")
+    keep = [adapters, seq_adapter, scales]
+    for name, rows in adapters.items():
+        segs, k, out = sizes[name]
+        if len(rows) != shape.n_layers:
+            raise ValueError(f"{name}: one entry per layer")
+        for p in rows:
+            if p is not None and (tuple(p[0].shape) != (n, segs * rank, k) or tuple(p[1].shape) != (n, out, rank)):
+                raise ValueError(f"{name}: a must be [{n}][{segs * rank}][{k}] and b [{n}][{out}][{rank}]")
+        for j, m in enumerate("ab"):
+            arr = _ptr_array([None if p is None else p[j] for p in rows], wd, f"{name}.{m}")
+            keep.append(arr)
+            setattr(c, f"{name}_{m}", C.cast(arr, C.POINTER(C.c_void_p)))
+    rc = lib().first_set_adapters(h, C.byref(c))
+    if rc:
+        raise FirstError(rc, "first_set_adapters")
+    return keep
+
+
+def first_set_rope(h, inv_freq=None, factor=1.0, head_dim=None):
+    """inv_freq: HOST float64 [head_dim/2] (first_rope_freqs), or None for the description's own frequencies."""
+    import numpy as np
+    f = None if inv_freq is None else np.ascontiguousarray(np.asarray(inv_freq), dtype=np.float64)
+    if f is not None and head_dim is not None and f.size != head_dim // 2:
+        raise ValueError(f"inv_freq must have {head_dim // 2} entries")
+    rc = lib().first_set_rope(h, None if f is None else f.ctypes.data, float(factor))
+    if rc:
+        raise FirstError(rc, "first_set_rope")
+
+
 def first_profile(h, enable):
     rc = lib().first_profile(h, int(bool(enable)))
     if rc:
@@ -466,6 +684,16 @@ class FirstContext:
     def set_sampling(self, top_k, temperature, uniforms):
         self._uniforms = uniforms  # borrowed by the library until the next call
         first_set_sampling(self.h, top_k, temperature, uniforms)
+
+    def set_sampling_rows(self, uniforms=None, temperature=None, top_k=None, top_p=None, min_p=None):
+        self._sampling = (uniforms, temperature, top_k, top_p, min_p)  # borrowed by the library until the next call
+        first_set_sampling_rows(self.h, uniforms, temperature, top_k, top_p, min_p)
+
+    def set_adapters(self, adapters=None, seq_adapter=None, scales=None):
+        self._adapters = first_set_adapters(self.h, self.shape, self.dtype, adapters, seq_adapter, scales)
+
+    def set_rope(self, inv_freq=None, factor=1.0):
+        first_set_rope(self.h, inv_freq, factor, self.shape.head_dim)
 
     def selftest_wait_expiry(self, polls=1000, stream=None):
         """Runs a bounded wait that must give up; -> (what the wait returned, the abort word)."""

@@ -17,6 +17,7 @@
 #include "gemm_tc.cuh"
 #include "gemm_tc2.cuh"
 #include "gemv.cuh"
+#include "ops.h"
 #include "prefill.cuh"
 #include "router.cuh"
 #include "step.cuh"
@@ -35,11 +36,11 @@ using namespace first;
 static thread_local char g_last_cuda_error[256] = "";
 
 enum KernelClass { kClsStepBegin = 0, kClsRmsnorm, kClsGemv, kClsGemmTc, kClsRopeAppend, kClsAttn, kClsAttnCombine,
-                   kClsSiluMul, kClsStepEnd, kClsRouterScores, kClsRouterFinalize, kClsPlan, kClsPrefillAux, kNumClasses };
+                   kClsSiluMul, kClsStepEnd, kClsRouterScores, kClsRouterFinalize, kClsPlan, kClsPrefillAux, kClsLora, kNumClasses };
 static const char* const kClassNames[kNumClasses] = {"step_begin", "rmsnorm_rows", "gemv_rows", "gemm_tc",
                                                      "rope_append", "attn_split", "attn_combine", "silu_mul",
                                                      "step_end", "router_token_scores", "router_finalize",
-                                                     "plan_compact", "prefill_aux"};
+                                                     "plan_compact", "prefill_aux", "lora"};
 
 struct first_ctx {
     first_model_desc d{};
@@ -123,6 +124,17 @@ struct first_ctx {
     int sample_k = 0;
     float sample_inv_T = 1.f;
     const float* sample_u = nullptr;
+    bool sample_rows = false;  // settings of its own for every row (first_set_sampling_rows)
+    first_sampling sampling{};
+    double rope_factor = 1.0;
+    // low-rank adapters beside the projections: per target the layers' a and b (empty = none)
+    enum { kQkv = 0, kO, kGateUp, kDown, kTargets };
+    std::vector<const void*> ad_a[kTargets], ad_b[kTargets];
+    int ad_n = 0, ad_rank = 0;
+    const float* ad_scales = nullptr;
+    const int32_t* ad_seq = nullptr;   // adapter of every batch row (the caller's) ...
+    const int32_t* ad_rows = nullptr;  // ... or of every row of a prompt chunk, while one runs
+    int32_t* pf_adapter = nullptr;
     // batched prefill: per-row tables of a chunk (each prompt token is a row), an all-keep mask, the residual of
     // every sequence's last prompt token, and (allocated on first use) the per-layer token scores of the routers
     int32_t *pf_cu = nullptr, *pf_tok = nullptr, *pf_cap = nullptr, *pf_pos = nullptr, *pf_len = nullptr;
@@ -726,6 +738,43 @@ int project(first_ctx* c, cudaStream_t st, bool use_tc, const void* W, const CUt
 template <typename WT>
 int logits_tail(first_ctx* c, cudaStream_t st, int B, float* logits, int32_t* next_tokens, int32_t* pos);
 
+bool has_adapter(const first_ctx* c, int target, int l) { return c->ad_n > 0 && !c->ad_a[target].empty() && c->ad_a[target][l]; }
+
+// The adapters of layer l beside one projection: y (+)= scale * B (A x) for the rows that have one.  x as the projection
+// reads it (float32, or the bfloat16 hi/lo pair); y as it writes it (compact rows, or the residual rows idx[i]).
+int apply_adapters(first_ctx* c, cudaStream_t st, int target, int l, const float* X, const __nv_bfloat16* Xh,
+                   const __nv_bfloat16* Xl, bool pair, int K, float* y, int64_t ldy, bool scatter, const int32_t* idx,
+                   int m, const int32_t* m_dev) {
+    if (!has_adapter(c, target, l)) return FIRST_OK;
+    const int F = c->d.ffn_dim, D = c->d.d_model;
+    LoraArgs a;
+    a.x = pair ? static_cast<const void*>(Xh) : X;
+    a.x_lo = Xl;
+    a.x_kind = pair ? kLoraXPair : kLoraXF32;
+    a.ldx = K;
+    a.a = c->ad_a[target][l];
+    a.b = c->ad_b[target][l];
+    a.w_f32 = c->d.dtype == FIRST_DTYPE_F32;
+    a.scales = c->ad_scales;
+    a.adapter = c->ad_rows ? c->ad_rows : c->ad_seq;
+    a.n = c->ad_n; a.R = c->ad_rank; a.K = K;
+    switch (target) {
+        case first_ctx::kQkv: a.S = 3; a.seg[1] = c->qd; a.seg[2] = c->qd + c->kvd; a.N = c->qkvd; break;
+        case first_ctx::kGateUp: a.S = 2; a.seg[1] = F; a.N = 2 * F; break;
+        default: a.S = 1; a.N = D;
+    }
+    a.seg[a.S] = a.N;
+    a.y = y; a.ldy = ldy;
+    a.idx = idx; a.scatter = scatter;
+    a.m = m; a.m_dev = m_dev;
+    a.stamp = stamp_slot(c, kClsLora);
+    Launch guard(c, st, kClsLora);
+    const bool pdl = c->use_pdl && !c->profiling && c->pdl_next;
+    c->pdl_next = true;
+    CU_TRY(lora_launch(a, st, pdl, c->n_sm));
+    return FIRST_OK;
+}
+
 // The whole step, for one weight/cache element type.
 template <typename WT>
 int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* kv, float* logits,
@@ -744,7 +793,7 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
     }
     c->pdl_next = false;  // the first kernel of a step has no predecessor to overlap
     if ((rc = launch_k(c, st, kClsStepBegin, step_begin<WT>, dim3(B), dim3(256), 0, tokens,
-                       static_cast<const WT*>(c->embed), D, V, kv->pos, c->inv_freq, hd / 2, c->x, c->cs, c->flags)))
+                       static_cast<const WT*>(c->embed), D, V, kv->pos, c->inv_freq, hd / 2, c->rope_factor, c->x, c->cs, c->flags)))
         return rc;
 
     int S = (d.max_tokens_per_seq + 255) / 256;
@@ -779,7 +828,7 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
         __nv_bfloat16 *xh = t ? c->xh : nullptr, *xl = t ? c->xl : nullptr;
         // split-K projections reduce into float32 accumulators that the preceding norm kernel clears
         const bool zero_qkv = t;  // (cleared even when a projection ends up with one K range and plain stores)
-        const bool fused_ffn = t && c->fuse_swiglu && (F % 64 == 0) && m <= 256;
+        const bool fused_ffn = t && c->fuse_swiglu && (F % 64 == 0) && m <= 256 && !has_adapter(c, first_ctx::kGateUp, l);
         const bool zero_gu = t && !fused_ffn;
         // ---- attention half
         if ((rc = launch_k(c, st, kClsRmsnorm, rmsnorm_rows, dim3(m), dim3(norm_threads), 0, c->x, idx, m_dev, D, c->attn_norm[l],
@@ -794,6 +843,8 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
             return rc;
         if ((rc = project<WT>(c, st, t, c->wqkv[l], t ? &c->tm_wqkv[l] : nullptr, c->qkvd, D, c->xn, c->xh, c->xl, m, 0,
                               c->qkv, c->qkvd, nullptr, m_dev, true, zero_qkv)))
+            return rc;
+        if ((rc = apply_adapters(c, st, first_ctx::kQkv, l, c->xn, c->xh, c->xl, t, D, c->qkv, c->qkvd, false, idx, m, m_dev)))
             return rc;
         // The tuned attention kernel rotates q itself and appends the new token's key and value (its
         // row facts come from the norm kernel above); the general path has a kernel for that.
@@ -817,6 +868,8 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
         if ((rc = project<WT>(c, st, t, c->wo[l], t ? &c->tm_wo[l] : nullptr, D, c->qd, c->att, c->xh, c->xl, m, 1, c->x,
                               D, idx, m_dev)))
             return rc;
+        if ((rc = apply_adapters(c, st, first_ctx::kO, l, c->att, c->xh, c->xl, t, c->qd, c->x, D, true, idx, m, m_dev)))
+            return rc;
         // ---- feed-forward half (its norm kernel also advances the cache length of the rows it handles)
         if ((rc = launch_k(c, st, kClsRmsnorm, rmsnorm_rows, dim3(m), dim3(norm_threads), 0, c->x, idx, m_dev, D, c->ffn_norm[l],
                            d.rms_eps, f32, xh, xl, zero_gu ? c->gu : nullptr, 2 * F, len_l, lkv.slab_cap, static_cast<longlong2*>(nullptr), static_cast<const int32_t*>(nullptr), static_cast<const int64_t*>(nullptr), static_cast<uint32_t*>(nullptr),
@@ -831,6 +884,8 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
             if ((rc = project<WT>(c, st, t, c->w_gate_up[l], t ? &c->tm_wgu[l] : nullptr, 2 * F, D, c->xn, c->xh, c->xl,
                                   m, 0, c->gu, 2 * F, nullptr, m_dev, true, zero_gu)))
                 return rc;
+            if ((rc = apply_adapters(c, st, first_ctx::kGateUp, l, c->xn, c->xh, c->xl, t, D, c->gu, 2 * F, false, idx, m, m_dev)))
+                return rc;
             if ((rc = launch_k(c, st, kClsSiluMul, silu_mul, dim3(std::min((m * F + 255) / 256, c->n_sm * 8)),
                                dim3(256), 0, c->gu, m, m_dev, F, t ? nullptr : c->act, t ? c->acth : nullptr,
                                t ? c->actl : nullptr)))
@@ -838,6 +893,8 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
         }
         if ((rc = project<WT>(c, st, t, c->w_down[l], t ? &c->tm_wd[l] : nullptr, D, F, c->act, c->acth, c->actl, m, 1,
                               c->x, D, idx, m_dev)))
+            return rc;
+        if ((rc = apply_adapters(c, st, first_ctx::kDown, l, c->act, c->acth, c->actl, t, F, c->x, D, true, idx, m, m_dev)))
             return rc;
     }
     if (ph) return FIRST_OK;  // a prefill chunk ends here: logits are taken once, from the last prompt tokens
@@ -866,10 +923,29 @@ int logits_tail(first_ctx* c, cudaStream_t st, int B, float* logits, int32_t* ne
                               nullptr, nullptr, false)))
             return rc;
     }
+    if (next_tokens && lg && c->sample_rows) {
+        SampleArgs a;
+        a.logits = lg; a.ld = V; a.B = B; a.V = V;
+        a.temperature = c->sampling.temperature; a.top_k = c->sampling.top_k; a.top_p = c->sampling.top_p;
+        a.min_p = c->sampling.min_p; a.u = c->sampling.uniforms;
+        a.tokens = next_tokens; a.pos = pos;
+        a.stamp = stamp_slot(c, kClsStepEnd);
+        Launch guard(c, st, kClsStepEnd);
+        const bool pdl = c->use_pdl && !c->profiling && c->pdl_next;
+        c->pdl_next = true;
+        CU_TRY(sample_launch(a, st, pdl));
+        return FIRST_OK;
+    }
     if (next_tokens && lg && c->sample_k > 1)
         return launch_k(c, st, kClsStepEnd, step_end_sample, dim3(B), dim3(1024), 0, lg, V, c->sample_k, c->sample_inv_T,
                         c->sample_u, next_tokens, pos);
     return launch_k(c, st, kClsStepEnd, step_end, dim3(B), dim3(1024), 0, lg, V, next_tokens, pos);
+}
+
+std::vector<double> plain_freqs(const first_model_desc& d) {
+    std::vector<double> inv(d.head_dim / 2);
+    for (int i = 0; i < d.head_dim / 2; ++i) inv[i] = std::pow((double)d.rope_base, -2.0 * i / (double)d.head_dim);
+    return inv;
 }
 
 }  // namespace
@@ -950,7 +1026,7 @@ int first_create(const first_model_desc* desc, const first_weights* w, first_ctx
         return fail(rc);
     if (cudaMemset(c->ticket, 0, MB * d.n_kv_heads * sizeof(uint32_t)) != cudaSuccess) return fail(FIRST_E_CUDA);
     if ((rc = dev_alloc(&c->pf_cu, MB + 1)) || (rc = dev_alloc(&c->pf_tok, MB)) || (rc = dev_alloc(&c->pf_cap, MB)) ||
-        (rc = dev_alloc(&c->pf_pos, MB)) || (rc = dev_alloc(&c->pf_len, MB * d.n_layers)) ||
+        (rc = dev_alloc(&c->pf_pos, MB)) || (rc = dev_alloc(&c->pf_adapter, MB)) || (rc = dev_alloc(&c->pf_len, MB * d.n_layers)) ||
         (rc = dev_alloc(&c->pf_off, MB)) || (rc = dev_alloc(&c->pf_ones, MB * d.n_layers)) ||
         (rc = dev_alloc(&c->x_last, MB * d.d_model)))
         return fail(rc);
@@ -964,8 +1040,7 @@ int first_create(const first_model_desc* desc, const first_weights* w, first_ctx
     if (cudaStreamCreateWithFlags(&c->cap_stream, cudaStreamNonBlocking) != cudaSuccess) return fail(FIRST_E_CUDA);
     c->tok_cap = (int64_t)d.max_batch * d.max_tokens_per_seq;
     if ((rc = dev_alloc(&c->tokscore, (size_t)c->tok_cap))) return fail(rc);
-    std::vector<double> inv(d.head_dim / 2);
-    for (int i = 0; i < d.head_dim / 2; ++i) inv[i] = std::pow((double)d.rope_base, -2.0 * i / (double)d.head_dim);
+    const std::vector<double> inv = plain_freqs(d);
     if (cudaMemcpy(c->inv_freq, inv.data(), inv.size() * sizeof(double), cudaMemcpyHostToDevice) != cudaSuccess ||
         cudaMemset(c->flags, 0, sizeof(uint32_t)) != cudaSuccess)
         return fail(FIRST_E_CUDA);
@@ -978,7 +1053,7 @@ int first_destroy(first_ctx* c) {
     void* ptrs[] = {c->x, c->xn, c->qkv, c->q, c->att, c->gu, c->act, c->o_part, c->logits_int, c->tokscore,
                     c->ml_part, c->cs, c->inv_freq, c->idx, c->cnt, c->slot, c->flags, c->xh, c->xl, c->acth, c->actl, c->ticket, c->rowinfo,
                     c->pf_cu, c->pf_tok, c->pf_cap, c->pf_pos, c->pf_len, c->pf_off, c->pf_ones, c->x_last, c->pf_score,
-                    c->stamps, c->mask_dev};
+                    c->stamps, c->mask_dev, c->pf_adapter};
     for (void* p : ptrs)
         if (p) cudaFree(p);
     for (cudaEvent_t e : c->ev_pool) cudaEventDestroy(e);
@@ -1199,9 +1274,10 @@ int first_prefill(first_ctx* c, const int32_t* tokens, const int32_t* cu_seqlens
     // a chunk's keys and values before attention starts (a row attends over earlier rows of its own chunk).
     struct Restore {
         first_ctx* c; int fuse_rope;
-        ~Restore() { c->fuse_rope = fuse_rope; c->has_mask = false; }
+        ~Restore() { c->fuse_rope = fuse_rope; c->has_mask = false; c->ad_rows = nullptr; }
     } restore{c, c->fuse_rope};
     c->fuse_rope = 0;
+    c->ad_rows = c->pf_adapter;  // (a chunk's rows are prompt tokens: prefill_rows looks up their sequences' adapters)
 
     first_kv_cache vkv = *kv;
     vkv.slab_off = c->pf_off;
@@ -1221,7 +1297,7 @@ int first_prefill(first_ctx* c, const int32_t* tokens, const int32_t* cu_seqlens
         }
         FIRST_LAUNCH(kClsPrefillAux, (prefill_rows<<<(rows + 127) / 128, 128, 0, st>>>(
                                          tokens, c->pf_cu, B, (int)g0, rows, L, kv->slab_off, kv->slab_cap, c->pf_tok,
-                                         c->pf_off, c->pf_cap, c->pf_pos, c->pf_len)));
+                                         c->pf_off, c->pf_cap, c->pf_pos, c->pf_len, c->ad_n > 0 ? c->ad_seq : nullptr, c->pf_adapter)));
         if ((rc = check_launch(c))) return rc;
         const PrefillHook ph{router_w, router_b, mode, c->pf_score, total, g0};
         const int lo_rows_saved = c->tc_lo_max_rows;
@@ -1327,7 +1403,72 @@ int first_set_sampling(first_ctx* c, int32_t top_k, float temperature, const flo
     c->sample_k = greedy ? 0 : top_k;
     c->sample_inv_T = greedy ? 1.f : 1.f / temperature;
     c->sample_u = greedy ? nullptr : uniforms;
+    c->sample_rows = false;
     c->plan_version += 1;  // cached step graphs end in the previous choice of kernel and pointer
+    return FIRST_OK;
+}
+
+int first_set_sampling_rows(first_ctx* c, const first_sampling* s) {
+    if (!c || (s && !s->uniforms)) return FIRST_E_ARG;
+    if (s && c->d.vocab > kSampleMaxVocab) return FIRST_E_UNSUPPORTED;
+    c->sample_rows = s != nullptr;
+    c->sampling = s ? *s : first_sampling{};
+    c->sample_k = 0;
+    c->sample_u = nullptr;
+    c->plan_version += 1;  // cached step graphs end in the previous choice of kernel and pointers
+    return FIRST_OK;
+}
+
+int first_set_adapters(first_ctx* c, const first_adapters* ad) {
+    if (!c) return FIRST_E_ARG;
+    const first_model_desc& d = c->d;
+    if (ad) {
+        if (ad->n_adapters <= 0 || ad->rank <= 0 || !ad->seq_adapter) return FIRST_E_ARG;
+        if (ad->rank % 8 || ad->rank > kLoraMaxRank) return FIRST_E_UNSUPPORTED;
+        const void* const* const tab[first_ctx::kTargets][2] = {{ad->qkv_a, ad->qkv_b}, {ad->o_a, ad->o_b},
+                                                                {ad->gate_up_a, ad->gate_up_b}, {ad->down_a, ad->down_b}};
+        for (int t = 0; t < first_ctx::kTargets; ++t) {
+            if (!tab[t][0] != !tab[t][1]) return FIRST_E_ARG;
+            for (int l = 0; tab[t][0] && l < d.n_layers; ++l) {
+                const void *a = tab[t][0][l], *b = tab[t][1][l];
+                if (!a != !b) return FIRST_E_ARG;
+                if ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % 16) return FIRST_E_UNSUPPORTED;
+                if (a && t == first_ctx::kGateUp && d.ffn_dim % 16) return FIRST_E_UNSUPPORTED;
+            }
+        }
+        for (int t = 0; t < first_ctx::kTargets; ++t) {
+            c->ad_a[t].clear();
+            c->ad_b[t].clear();
+            if (!tab[t][0]) continue;
+            c->ad_a[t].assign(tab[t][0], tab[t][0] + d.n_layers);
+            c->ad_b[t].assign(tab[t][1], tab[t][1] + d.n_layers);
+        }
+    }
+    c->ad_n = ad ? ad->n_adapters : 0;
+    c->ad_rank = ad ? ad->rank : 0;
+    c->ad_scales = ad ? ad->scales : nullptr;
+    c->ad_seq = ad ? ad->seq_adapter : nullptr;
+    c->plan_version += 1;  // cached step graphs were recorded with the previous adapters
+    return FIRST_OK;
+}
+
+int first_set_rope(first_ctx* c, const double* inv_freq, double factor) {
+    if (!c || (inv_freq && !std::isfinite(factor))) return FIRST_E_ARG;
+    std::vector<double> inv = plain_freqs(c->d);
+    for (size_t i = 0; inv_freq && i < inv.size(); ++i) {
+        if (!std::isfinite(inv_freq[i])) return FIRST_E_ARG;
+        inv[i] = inv_freq[i];
+    }
+    // steps in flight still read the table
+    const cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaErrorStreamCaptureUnsupported) {
+        cudaGetLastError();
+        return FIRST_E_STATE;
+    }
+    CU_TRY(e);
+    CU_TRY(cudaMemcpy(c->inv_freq, inv.data(), inv.size() * sizeof(double), cudaMemcpyHostToDevice));
+    c->rope_factor = inv_freq ? factor : 1.0;
+    c->plan_version += 1;  // (the factor is a kernel argument of recorded step graphs)
     return FIRST_OK;
 }
 

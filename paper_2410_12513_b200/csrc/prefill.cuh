@@ -27,7 +27,9 @@ static __global__ void __launch_bounds__(128) prefill_rows(const int32_t* __rest
                                                            const int32_t* __restrict__ slab_cap,
                                                            int32_t* __restrict__ v_tok, int64_t* __restrict__ v_off,
                                                            int32_t* __restrict__ v_cap, int32_t* __restrict__ v_pos,
-                                                           int32_t* __restrict__ v_len) {
+                                                           int32_t* __restrict__ v_len,
+                                                           const int32_t* __restrict__ seq_adapter,
+                                                           int32_t* __restrict__ v_adapter) {
     const int r = blockIdx.x * blockDim.x + threadIdx.x;
     if (r >= rows) return;
     const int g = g0 + r, b = seq_of_token(cu, B, g), p = g - cu[b];
@@ -35,6 +37,7 @@ static __global__ void __launch_bounds__(128) prefill_rows(const int32_t* __rest
     v_off[r] = slab_off[b];
     v_cap[r] = slab_cap[b];
     v_pos[r] = p;
+    if (seq_adapter) v_adapter[r] = seq_adapter[b];
     for (int l = 0; l < L; ++l) v_len[(size_t)l * rows + r] = p;
 }
 

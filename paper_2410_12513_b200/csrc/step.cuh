@@ -8,11 +8,11 @@ namespace first {
 
 // Start of a step: residual rows from the embedding table, and the rotary cos/sin of
 // every sequence's position (same for all layers, so computed once, in float64:
-// angle = pos * base^(-2i/hd), half-split pairing).
+// angle = pos * base^(-2i/hd) or the frequencies of first_set_rope, whose factor scales both; half-split pairing).
 template <typename WT>
 __global__ void __launch_bounds__(256) step_begin(const int32_t* __restrict__ tokens, const WT* __restrict__ embed,
                                                   int D, int V, const int32_t* __restrict__ pos,
-                                                  const double* __restrict__ inv_freq, int half,
+                                                  const double* __restrict__ inv_freq, int half, double rope_factor,
                                                   float* __restrict__ x, float2* __restrict__ cs,
                                                   uint32_t* __restrict__ flags, uint64_t* stamp) {
     const Stamp stamp_guard(stamp);
@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(256) step_begin(const int32_t* __restrict__ to
     for (int i = threadIdx.x; i < half; i += blockDim.x) {
         double s, c;
         sincos(p * inv_freq[i], &s, &c);
-        cs[(size_t)b * half + i] = make_float2((float)c, (float)s);
+        cs[(size_t)b * half + i] = make_float2((float)(rope_factor * c), (float)(rope_factor * s));
     }
 }
 
