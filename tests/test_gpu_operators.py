@@ -270,11 +270,12 @@ def test_lora_on_another_stream_and_in_a_graph():
 
 # ------------------------------------------------------------------ sampling
 def _sample_ref(x, u, temp, k, p, mp):
-    """-> the tokens the definition allows: one, or a few neighbours where the draw, or the nucleus' border, is as near
-    to a weight's border as the weights' unit: each is a multiple of 2^-43 of the largest, so off by 2^-44 at most, and
-    a sum of them, as the share of the sum it is compared with, by V 2^-44: V 2^-43 together."""
+    """-> the tokens the definition allows: one, or neighbours where the draw, or the nucleus' border, is as near to a
+    weight's border as float32 weights place it.  A weight is off by at most 2^-21 of itself: the exponential 2^-22, its
+    argument's two roundings 2 * 2^-24 * 0.73, the rounding to 2^-23 of a value of at least exp(-1/2) 0.83 * 2^-23; in
+    the open last bin the last two are at most 2^-22 of that bin's own weight.  So is every sum of weights; prefix
+    sums themselves are 64-bit.  A border and the share of the sum it is compared with move by 2^-21 of the sum each."""
     V = x.size
-    eps = V * 2.0 ** -43
     x = np.where(np.isnan(x), -np.inf, x.astype(np.float64))
     order = np.lexsort((np.arange(V), -x))
     if x[order[0]] == -np.inf:
@@ -290,6 +291,7 @@ def _sample_ref(x, u, temp, k, p, mp):
         w = w[:k]
     if mp > 0:
         w = w[w >= min(mp, 1.0)]
+    eps = 2.0 ** -20 * w.sum()
     cum, below = np.cumsum(w), np.concatenate([[0.0], np.cumsum(w)[:-1]])
     one = float(np.float32(1) - np.float32(2.0 ** -24))
     u = one if not u == u else min(max(u, 0.0), one)
