@@ -9,7 +9,7 @@
 //   2. A histogram over 32 bins of (max - x) / T, half a unit wide: the sum reaches the target in one of them.
 //   3. If that bin holds many elements, it is cut into 32 parts of its range of values (and again, and, among equal
 //      values, of indices), each time keeping the part that holds the target.
-//   4. What is left, at most kList elements, goes to the first CTA's shared memory, is sorted there and summed up.
+//   4. What is left, at most kList elements, goes to every CTA's shared memory, is sorted there and summed up.
 // A histogram is private to every LANE of every warp (a bin is 32 words, a lane owns one): a bank each, no atomics, so
 // sums are the same in every run.  Weights are taken relative to that of the upper end X of their bin: exp((x - X) / T)
 // with the difference exact, as integers in units of 2^-23, which keeps float32's 24 bits; the bins' own weights and
@@ -30,8 +30,9 @@ constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kRegs = 32;            // elements a thread holds; a CTA 16384, a cluster of eight 131072 (more are re-read from L2)
 constexpr int kCluster = 8;
 constexpr int kBins = 32;
-constexpr int kList = 1024;          // elements that are sorted in shared memory (two a thread)
-constexpr int kGathers = 64;         // attempts to collect a list, at most: 3 searches of up to 12 levels each
+constexpr int kLocal = 2048;         // elements of one bin that a CTA keeps in shared memory
+constexpr int kList = kThreads;      // elements that every CTA of the cluster sorts, one a thread
+constexpr int kGathers = 64;         // lists collected for one row, at most: 3 searches of up to 16 levels each
 constexpr double kUnit = 1.0 / 8388608.0;  // 2^-23
 
 // descending: the largest logit has the smallest key; -0 has been turned into +0
@@ -44,26 +45,25 @@ __device__ __forceinline__ float value_of(uint32_t k) {
 }
 __device__ __forceinline__ float clean(float x) { return x != x ? -INFINITY : x + 0.f; }
 
-struct Best { float x; int i; };
-
-struct Result {  // of a search: where the kept prefix ends, and its weight
-    float x;     // the last kept element's value ...
-    int i;       // ... and index: elements of that value with a larger one are not kept
+struct Result {  // the last element of a kept prefix, and the prefix's weight
+    float x;
+    int i;
     double mass;
 };
 
 struct Smem {
     uint32_t hist[kWarps][kBins][32];
-    unsigned long long list[kList], sorted[kList];
-    double cum[kList];
+    float X[kBins][32];              // a bin's upper end, once per lane: the same offset as in a histogram
+    unsigned long long loc[kLocal];  // the bin being searched: this CTA's elements, value key << 32 | index
+    unsigned long long list[2][kList];  // (turn by turn: a CTA may be at the next search while another still reads)
+    unsigned long long tmp[kList];
     unsigned long long xch[2][kCluster][kBins];
     double W[kBins];                 // weight of a bin's upper end, per unit
-    float X[kBins];                  // a bin's upper end
-    Best best[kCluster], best_w[kWarps];
     double scan[kWarps];
     Result res;
-    unsigned int gcnt[kGathers];     // (first CTA) elements collected by each attempt
-    unsigned int lcnt, loff;
+    uint32_t key[2][kCluster], key_w[kWarps];
+    uint32_t gcnt[kGathers], off[kCluster];
+    uint32_t nloc, lcnt, tot;
     int hit;
     float thr;
 };
@@ -73,19 +73,27 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ uint32_t lds(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts(uint32_t a, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 
 struct Row {  // what a thread needs to know about the row
     float m, inv_T2, inv_Tl2;  // maximum; 2 / T (bins of half a unit), log2(e) / T
+    // 2^23 + bin, as the bits of a float (monotone in x, like every step of it)
+    __device__ __forceinline__ uint32_t bin_bits(float x) const {
+        return __float_as_uint(fminf((m - x) * inv_T2, (float)(kBins - 1)) + 8388608.f);
+    }
+    __device__ __forceinline__ int bin(float x) const { return (int)(bin_bits(x) & (kBins - 1)); }
+    // 2^23 + weight of x in units of 2^-23 of that of its bin's upper end X, on top of the bits of 1.0 (x - X is exact but
+    // where it does not matter; it is above 0 by a rounding at most)
+    __device__ __forceinline__ uint32_t unit_bits(float x, float X) const {
+        return __float_as_uint(ex2(fminf((x - X) * inv_Tl2, 0.f)) + 1.f);
+    }
+    __device__ __forceinline__ uint32_t units(float x, float X) const { return unit_bits(x, X) - 0x3f800000u; }
 };
-
-__device__ __forceinline__ int bin_of(float x, const Row& r) {  // (monotone in x, like every step of it)
-    return (int)(__float_as_uint(fminf((r.m - x) * r.inv_T2, (float)(kBins - 1)) + 8388608.f) & (kBins - 1));
-}
-// weight of x in units of 2^-23 of its bin's weight
-__device__ __forceinline__ uint32_t units_of(float x, float X, const Row& r) {
-    const float d = fmaxf(fminf(X - x, FLT_MAX) * r.inv_Tl2, -1.f);  // (X - x is exact but where it does not matter)
-    return __float_as_uint(ex2(-d) + 1.f) - 0x3f800000u;
-}
 
 template <bool VEC>
 struct Slice {  // this thread's elements of the row
@@ -116,26 +124,43 @@ struct Slice {  // this thread's elements of the row
 #pragma unroll
         for (int j = 0; j < kRegs; ++j) x[j] = clean(x[j]);
     }
-    // f(value, index in the row); values are clean, elements that do not exist are -inf
+    // elements beyond the registers (rows of more than 131072): f(value, index in the row)
     template <typename F>
-    __device__ __forceinline__ void each(bool infinite, F f) const {
-#pragma unroll
-        for (int j = 0; j < kRegs; ++j) f(x[j], base + local(j));
+    __device__ __forceinline__ void rest(bool infinite, F f) const {
         for (int i = kRegs * kThreads + (int)threadIdx.x; i < n; i += kThreads) {
             float v = clean(row[i]);
             if (infinite) v = v == INFINITY ? 0.f : -INFINITY;
             f(v, base + i);
         }
     }
+    // f(value, index in the row); values are clean, elements that do not exist are -inf
+    template <typename F>
+    __device__ __forceinline__ void each(bool infinite, F f) const {
+#pragma unroll
+        for (int j = 0; j < kRegs; ++j) f(x[j], base + local(j));
+        rest(infinite, f);
+    }
 };
 
-__device__ __forceinline__ unsigned long long warp_sum_u64(unsigned long long v) {
+__device__ __forceinline__ double warp_scan(double run, int lane) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+    for (int o = 1; o < 32; o <<= 1) {
+        const double v = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += v;
+    }
+    return run;
+}
+__device__ __forceinline__ uint32_t warp_scan(uint32_t run, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += v;
+    }
+    return run;
 }
 
-// grid B * C in clusters of C; one cluster per row.
+// grid B * C in clusters of C; one cluster per row.  Every decision is taken by every warp of every CTA from the same
+// numbers, so the cluster stays together without anyone telling the others.
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     const Stamp stamp_guard(p.stamp);
@@ -160,85 +185,95 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     el.load();
     const float T0 = p.temperature ? p.temperature[b] : 1.f;
 
-    // ---- maximum, and its first index
-    Best me{-INFINITY, 0x7fffffff};
-    el.each(false, [&](float x, int i) {
-        if (x > me.x) { me.x = x; me.i = i; }  // (a thread's indices ascend)
-    });
-    auto better = [](const Best& a, const Best& c) { return a.x > c.x || (a.x == c.x && a.i < c.i); };
-    auto warp_best = [&](Best v) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const Best w{__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.i, o)};
-            if (better(w, v)) v = w;
+    // the smallest of one 32-bit word per thread, over the cluster
+    auto cluster_min = [&](uint32_t v, int slot) {
+        v = __reduce_min_sync(0xffffffffu, v);
+        if (lane == 0) s.key_w[warp] = v;
+        __syncthreads();
+        if (warp == 0) {
+            v = __reduce_min_sync(0xffffffffu, lane < kWarps ? s.key_w[lane] : 0xffffffffu);
+            if (lane < C) cluster.map_shared_rank(&s.key[slot][0], lane)[rank] = v;
         }
-        return v;
+        cluster.sync();
+        return __reduce_min_sync(0xffffffffu, lane < C ? s.key[slot][lane] : 0xffffffffu);
     };
-    me = warp_best(me);
-    if (lane == 0) s.best_w[warp] = me;
-    __syncthreads();
+
+    // ---- maximum
+    float mx = -INFINITY;
+    el.each(false, [&](float x, int) { mx = fmaxf(mx, x); });
     cluster.barrier_wait();
-    if (warp == 0) {
-        me = warp_best(lane < kWarps ? s.best_w[lane] : Best{-INFINITY, 0x7fffffff});
-        if (lane < C) cluster.map_shared_rank(s.best, lane)[rank] = me;
-    }
-    cluster.sync();
-    me = warp_best(lane < C ? s.best[lane] : Best{-INFINITY, 0x7fffffff});
+    mx = value_of(cluster_min(key_of(mx), 0));
     if (rank == 0 && tid == 0 && p.pos) p.pos[b] += 1;
-    if (me.x == -INFINITY || !(T0 > 0.f)) {  // nothing to choose from, or greedy
-        if (rank == 0 && tid == 0) p.tokens[b] = me.x == -INFINITY ? -1 : me.i;
-        return;  // (nothing of another CTA's shared memory is touched after the sync)
+    if (mx == -INFINITY || !(T0 > 0.f)) {  // nothing to choose from, or greedy: the first of the largest
+        int at = 0x7fffffff;
+        if (mx > -INFINITY) {
+            el.each(false, [&](float x, int i) { at = x == mx ? min(at, i) : at; });
+            at = (int)cluster_min((uint32_t)at, 1);
+        } else {
+            at = -1;
+        }
+        if (rank == 0 && tid == 0) p.tokens[b] = at;
+        return;  // (nothing of another CTA's shared memory is touched after a sync)
     }
-    const bool infinite = me.x == INFINITY;
+    const bool infinite = mx == INFINITY;
     if (infinite) {  // infinities share all the weight: they become the only candidates
 #pragma unroll
         for (int j = 0; j < kRegs; ++j) el.x[j] = el.x[j] == INFINITY ? 0.f : -INFINITY;
-        me.x = 0.f;
+        mx = 0.f;
     }
-    const double T = fmax((double)T0, 1e-37), m = (double)me.x, inv_T = 1.0 / T;
+    const double T = fmax((double)T0, 1e-37), m = (double)mx, inv_T = 1.0 / T;
     Row r;
-    r.m = me.x;
+    r.m = mx;
     r.inv_T2 = (float)(2.0 * inv_T);
     r.inv_Tl2 = (float)(1.4426950408889634 * inv_T);
-    if (tid < kBins) {
-        const float X = T > 1e300 ? me.x : (float)fmin(fmax(m - 0.5 * (tid - 0.5) * T, -(double)FLT_MAX), (double)FLT_MAX);
-        s.X[tid] = X;
-        s.W[tid] = kUnit * exp(((double)X - m) * inv_T);
+    {
+        // two lanes' columns of a bin's upper end per thread; its weight once
+        const int bin = tid >> 4;
+        const float X = T > 1e300 ? mx : (float)fmin(fmax(m - 0.5 * (bin - 0.5) * T, -(double)FLT_MAX), (double)FLT_MAX);
+        s.X[bin][2 * (tid & 15)] = X;
+        s.X[bin][2 * (tid & 15) + 1] = X;
+        if ((tid & 15) == 0) s.W[bin] = kUnit * exp(((double)X - m) * inv_T);
     }
     // the smallest value that min_p keeps
+    float lim_x = -FLT_MAX;
     const float mp0 = p.min_p ? p.min_p[b] : 0.f;
-    if (tid == 32) {
-        float x = -FLT_MAX;
-        if (mp0 > 0.f && T < 1e300) {
+    if (mp0 > 0.f && T < 1e300) {
+        if (tid == 0) {
             const double mp = fmin((double)mp0, 1.0);
             auto kept = [&](float v) { return exp(((double)v - m) / T) >= mp; };
-            x = (float)fmax(m + T * log(mp), -(double)FLT_MAX);
+            float x = (float)fmax(m + T * log(mp), -(double)FLT_MAX);
             for (int i = 0; i < 4 && x > -FLT_MAX && kept(nextafterf(x, -INFINITY)); ++i) x = nextafterf(x, -INFINITY);
-            for (int i = 0; i < 4 && x < me.x && !kept(x); ++i) x = nextafterf(x, INFINITY);
-            x = fminf(x, me.x);
+            for (int i = 0; i < 4 && x < mx && !kept(x); ++i) x = nextafterf(x, INFINITY);
+            s.thr = fminf(x, mx) + 0.f;
         }
-        s.thr = x + 0.f;
+        __syncthreads();
+        lim_x = s.thr;
     }
     __syncthreads();
     // the kept prefix: elements above lim_x, and those equal to it with an index up to lim_i
-    float lim_x = s.thr;
-    int lim_i = 0x7fffffff;
+    constexpr int kAll = 0x7fffffff;
+    int lim_i = kAll;
     int par = 0, gathers = 0;
 
-    // Adds one lane-private histogram up over the cluster: every warp of every CTA gets the total of bin `lane`.
+    // Adds one lane-private histogram up over the cluster: every warp of every CTA gets the total of bin `lane`; the CTAs' parts
+    // stay in s.xch[par ^ 1] until the next but one.
     auto totals = [&]() {
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < kBins / kWarps; ++q) {
             const int bin = warp * (kBins / kWarps) + q;
-            unsigned long long v = 0;
+            uint32_t lo = 0, hi = 0;  // (a lane's sum has 30 bits at most)
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                v += s.hist[w][bin][lane];
+                const uint32_t v = s.hist[w][bin][lane];
                 s.hist[w][bin][lane] = 0;
+                lo += v & 0xffffu;
+                hi += v >> 16;
             }
-            v = warp_sum_u64(v);
-            if (lane < C) cluster.map_shared_rank(&s.xch[par][0][0], lane)[rank * kBins + bin] = v;
+            lo = __reduce_add_sync(0xffffffffu, lo);
+            hi = __reduce_add_sync(0xffffffffu, hi);
+            if (lane < C)
+                cluster.map_shared_rank(&s.xch[par][0][0], lane)[rank * kBins + bin] = ((unsigned long long)hi << 16) + lo;
         }
         cluster.sync();
         unsigned long long t = 0;
@@ -246,127 +281,194 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         par ^= 1;
         return t;
     };
-    uint32_t* const my_hist = &s.hist[warp][0][lane];
-
-    // A range of elements: values ka..kb (as keys, so descending), indices ia..ib once ka = kb.
-    struct Range { uint32_t ka, kb; int ia, ib; };
-    auto inside = [&](float x, int i, float xa, float xb, const Range& g) {
-        return x <= xa && x >= xb && (x != lim_x || i <= lim_i) && i >= g.ia && i <= g.ib;
+    auto largest_part = [&](int bin) {  // of the totals just taken, the largest CTA's share of a bin
+        unsigned long long v = 0;
+        for (int c = 0; c < C; ++c) v = max(v, s.xch[par ^ 1][c][bin]);
+        return (double)v;
     };
+    uint32_t* const my_hist = &s.hist[warp][0][lane];
+    const uint32_t hist_a = (uint32_t)__cvta_generic_to_shared(my_hist) - 0x4b000000u * 128u;  // + bin_bits * 128
+    const uint32_t X_a = (uint32_t)__cvta_generic_to_shared(&s.X[0][lane]) - 0x4b000000u * 128u;
 
     // The bins of the whole row up to the limit.
     auto level0 = [&](bool mass) {
-        el.each(infinite, [&](float x, int i) {
-            if (x >= lim_x && (x != lim_x || i <= lim_i)) {
-                const int bin = bin_of(x, r);
-                my_hist[bin * 32] += mass ? units_of(x, s.X[bin], r) : 1u;
-            }
-        });
+        if (mass)
+            el.each(infinite, [&](float x, int i) {
+                if (x >= lim_x && (lim_i == kAll || x != lim_x || i <= lim_i)) {
+                    const uint32_t o = r.bin_bits(x) * 128u;
+                    const uint32_t u = r.unit_bits(x, __uint_as_float(lds(X_a + o)));
+                    sts(hist_a + o, lds(hist_a + o) + u - 0x3f800000u);
+                }
+            });
+        else
+            el.each(infinite, [&](float x, int) {
+                if (x >= lim_x) {  // (top-k comes first: no limit by index yet)
+                    const uint32_t o = hist_a + r.bin_bits(x) * 128u;
+                    sts(o, lds(o) + 1u);
+                }
+            });
         return totals();
     };
-    // The values of bin j: the first and the last key with bin_of = j, searched by a whole warp (32 probes a round).
-    auto first_key = [&](int j) {  // smallest key whose bin is at least j
-        unsigned long long a = key_of(r.m), e = (unsigned long long)key_of(-FLT_MAX) + 1;  // the answer is in [a, e]
+
+    // A range of elements: values ka..kb (as keys, so descending), indices ia..ib once ka = kb.
+    struct Range { uint32_t ka, kb; int ia, ib; };
+    auto inside = [&](float x, int i, const Range& g) {  // (of an element whose value is in the range)
+        return (x != lim_x || i <= lim_i) && i >= g.ia && i <= g.ib;
+    };
+    // The smallest key whose bin is at least j.  It lies next to that of the bin's upper end: 32 probes around it nearly
+    // always hold it; if not (values near zero have finer keys), the whole range is searched, 32 probes a round.
+    auto first_key = [&](int j) -> uint32_t {
+        const uint32_t k0 = key_of(r.m), k1 = key_of(-FLT_MAX) + 1;  // the answer is in k0..k1
+        if (j <= 0) return k0;
+        if (j >= kBins) return k1;
+        {
+            const uint32_t mid = key_of(s.X[j][0] + 0.f), a = mid > k0 + 16 ? mid - 16 : k0, at = a + lane;
+            const unsigned ok = __ballot_sync(0xffffffffu, at >= k1 || r.bin(value_of(at)) >= j);
+            if (ok && (!(ok & 1u) || a == k0)) return a + __ffs(ok) - 1;
+        }
+        uint32_t a = k0, e = k1;
         while (a < e) {
-            const unsigned long long step = (e - a + 31) / 32, at = a + lane * step;
-            const unsigned ok = __ballot_sync(0xffffffffu, at >= e || bin_of(value_of((uint32_t)at), r) >= j);
-            const int f = __ffs(ok) - 1;  // (0: none true)
-            if (f < 0) { a = a + 31 * step + 1; continue; }
-            e = a + f * step < e ? a + f * step : e;
-            if (f > 0) a = a + (unsigned long long)(f - 1) * step + 1;
-            else e = a;
+            const uint32_t step = (e - a + 31) / 32;
+            const unsigned long long at = (unsigned long long)a + (unsigned long long)lane * step;
+            const unsigned ok = __ballot_sync(0xffffffffu, at >= e || r.bin(value_of((uint32_t)at)) >= j);
+            const int f = __ffs(ok) - 1;  // (-1: none)
+            if (f < 0) { a += 31 * step + 1; continue; }
+            if (f == 0) { e = a; break; }
+            e = (uint32_t)min((unsigned long long)e, (unsigned long long)a + (unsigned long long)f * step);
+            a += (f - 1) * step + 1;
         }
         return a;
     };
     auto range_of_bin = [&](int j) {
-        const unsigned long long a = first_key(j), e = first_key(j + 1);
-        return Range{(uint32_t)a, (uint32_t)(e > a ? e - 1 : a), 0, 0x7fffffff};
+        const uint32_t a = first_key(j), e = first_key(j + 1);
+        return Range{a, max(a, min(e - 1, key_of(lim_x))), 0, kAll};
     };
 
-    // Collects the elements of a range in the first CTA; returns how many there are (more than kList: not collected).
-    auto gather = [&](const Range& g) {
+    // Copies this CTA's elements of a range to s.loc (the caller knows that they fit).
+    auto compact = [&](const Range& g) {
         const float xa = value_of(g.ka), xb = value_of(g.kb);
-        if (tid == 0) s.lcnt = 0;
+        if (tid == 0) s.nloc = 0;
         __syncthreads();
-        el.each(infinite, [&](float x, int i) {
-            if (inside(x, i, xa, xb, g)) {
-                const unsigned at = atomicAdd(&s.lcnt, 1u);
-                if (at < kList) s.sorted[at] = ((unsigned long long)key_of(x) << 32) | (unsigned)i;
+        uint32_t mask = 0;
+#pragma unroll
+        for (int j = 0; j < kRegs; ++j) mask |= (el.x[j] <= xa && el.x[j] >= xb) ? 1u << j : 0u;
+        if (lim_i != kAll || g.ia > 0 || g.ib != kAll) {
+#pragma unroll
+            for (int j = 0; j < kRegs; ++j)
+                if (!inside(el.x[j], el.base + el.local(j), g)) mask &= ~(1u << j);
+        }
+        const uint32_t cnt = __popc(mask), upto = warp_scan(cnt, lane);
+        uint32_t at = 0;
+        if (lane == 31 && upto) at = atomicAdd(&s.nloc, upto);
+        at = __shfl_sync(0xffffffffu, at, 31) + upto - cnt;
+        if (__any_sync(0xffffffffu, mask != 0)) {
+#pragma unroll
+            for (int j = 0; j < kRegs; ++j)
+                if (mask & (1u << j)) {
+                    if (at < kLocal) s.loc[at] = ((unsigned long long)key_of(el.x[j]) << 32) | (unsigned)(el.base + el.local(j));
+                    ++at;
+                }
+        }
+        el.rest(infinite, [&](float x, int i) {
+            if (x <= xa && x >= xb && inside(x, i, g)) {
+                const uint32_t q = atomicAdd(&s.nloc, 1u);
+                if (q < kLocal) s.loc[q] = ((unsigned long long)key_of(x) << 32) | (unsigned)i;
             }
         });
         __syncthreads();
-        const unsigned n = s.lcnt;
-        unsigned* cnt = cluster.map_shared_rank(s.gcnt, 0) + gathers;
-        if (tid == 0 && n) s.loff = atomicAdd(cnt, n);
+    };
+    // Counts the elements of a range (the weights of the open last bin say nothing about that).
+    auto tally = [&](const Range& g, bool local, double& tot, double& part) {
+        const float xa = value_of(g.ka), xb = value_of(g.kb);
+        uint32_t n = 0;
+        if (local) {
+            for (uint32_t e = tid; e < min(s.nloc, (uint32_t)kLocal); e += kThreads) {
+                const uint32_t k = (uint32_t)(s.loc[e] >> 32);
+                const int i = (int)(uint32_t)s.loc[e];
+                n += k >= g.ka && k <= g.kb && i >= g.ia && i <= g.ib;
+            }
+        } else {
+            el.each(infinite, [&](float x, int i) { n += x <= xa && x >= xb && inside(x, i, g); });
+        }
+        my_hist[0] += n;
+        const unsigned long long t = totals();
+        tot = (double)__shfl_sync(0xffffffffu, t, 0);
+        part = largest_part(0);
+    };
+    // Brings the local elements of a range together in every CTA; returns how many there are.
+    auto gather = [&](const Range& g) {
+        if (tid == 0) s.lcnt = 0;
         __syncthreads();
-        if (n) {
-            unsigned long long* dst = cluster.map_shared_rank(s.list, 0);
-            for (unsigned e = tid; e < n && e < kList; e += kThreads)
-                if (s.loff + e < kList) dst[s.loff + e] = s.sorted[e];
+        const uint32_t nloc = min(s.nloc, (uint32_t)kLocal);
+        for (uint32_t e0 = 0; e0 < nloc; e0 += kThreads) {
+            const uint32_t e = e0 + tid;
+            const unsigned long long v = e < nloc ? s.loc[e] : ~0ull;
+            const uint32_t k = (uint32_t)(v >> 32);
+            const int i = (int)(uint32_t)v;
+            const bool in = e < nloc && k >= g.ka && k <= g.kb && i >= g.ia && i <= g.ib;
+            const unsigned who = __ballot_sync(0xffffffffu, in);
+            if (!who) continue;
+            uint32_t at = 0;
+            if (lane == 0) at = atomicAdd(&s.lcnt, (uint32_t)__popc(who));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+            if (in && at < kList) s.tmp[at] = v;
+        }
+        __syncthreads();
+        const uint32_t n = min(s.lcnt, (uint32_t)kList);
+        if (tid < C && n) s.off[tid] = atomicAdd(cluster.map_shared_rank(&s.gcnt[0], tid) + gathers, s.lcnt);
+        __syncthreads();
+        for (uint32_t e = tid; e < n * C; e += kThreads) {
+            const uint32_t c = e % C, at = s.off[c] + e / C;
+            if (at < kList) cluster.map_shared_rank(&s.list[gathers & 1][0], c)[at] = s.tmp[e / C];
         }
         cluster.sync();
-        ++gathers;
-        return *static_cast<volatile unsigned*>(cnt);
+        return (int)s.gcnt[gathers++];
     };
-    // (first CTA) Sorts the n collected elements by (value, index): every element counts those before it.
-    auto sort_list = [&](int n) {
-        __syncthreads();
-        unsigned long long k0 = tid < n ? s.list[tid] : ~0ull, k1 = tid + kThreads < n ? s.list[tid + kThreads] : ~0ull;
-        int r0 = 0, r1 = 0;
-        if (n > kThreads) {
-            for (int e = 0; e < n; ++e) {
-                const unsigned long long k = s.list[e];
-                r0 += k < k0;
-                r1 += k < k1;
+    // The n collected elements in order, element tid in thread tid: a bitonic network, over shuffles inside a warp.
+    auto sorted = [&](int n) {
+        unsigned long long k = tid < n ? s.list[(gathers & 1) ^ 1][tid] : ~0ull;  // (of the last gather)
+        int P = 32;
+        while (P < n) P *= 2;
+        for (int size = 2; size <= P; size <<= 1)
+            for (int stride = size >> 1; stride > 0; stride >>= 1) {
+                unsigned long long o;
+                if (stride >= 32) {
+                    __syncthreads();
+                    s.tmp[tid] = k;
+                    __syncthreads();
+                    o = s.tmp[tid ^ stride];
+                } else {
+                    o = __shfl_xor_sync(0xffffffffu, k, stride);
+                }
+                const bool up = (tid & size) == 0, low = (tid & stride) == 0;
+                k = (up == low) == (o < k) ? o : k;
             }
-        } else if (tid < (n + 31) / 32 * 32) {
-#pragma unroll 4
-            for (int e = 0; e < n; ++e) r0 += s.list[e] < k0;
-        }
-        if (tid < n) s.sorted[r0] = k0;
-        if (tid + kThreads < n) s.sorted[r1] = k1;
-        __syncthreads();
+        return k;
     };
-    // (first CTA) Running sums of the sorted elements' weights, on top of `before`.
-    auto sum_list = [&](int n, double before) {
-        double w[2], mine = 0.0;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int e = 2 * tid + q;
-            w[q] = 0.0;
-            if (e < n) {
-                const float x = value_of((uint32_t)(s.sorted[e] >> 32));
-                const int bin = bin_of(x, r);
-                w[q] = s.W[bin] * (double)units_of(x, s.X[bin], r);
-            }
-            mine += w[q];
+    // Running sum of the elements' weights, on top of `before`.
+    auto summed = [&](int n, unsigned long long k, double before, double& w) {
+        w = 0.0;
+        if (tid < n) {
+            const float x = value_of((uint32_t)(k >> 32));
+            const int bin = r.bin(x);
+            w = s.W[bin] * (double)r.units(x, s.X[bin][0]);
         }
-        double run = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const double v = __shfl_up_sync(0xffffffffu, run, o);
-            if (lane >= o) run += v;
-        }
+        const double run = warp_scan(w, lane);
         if (lane == 31) s.scan[warp] = run;
         __syncthreads();
-        double off = before;
-        for (int w2 = 0; w2 < warp; ++w2) off += s.scan[w2];
-        run = off + run - mine;
-        if (2 * tid < n) s.cum[2 * tid] = run + w[0];
-        if (2 * tid + 1 < n) s.cum[2 * tid + 1] = run + w[0] + w[1];
-        __syncthreads();
+        const int nw = min(warp, (n + 31) / 32);
+        for (int v = 0; v < nw; ++v) before += s.scan[v];
+        return before + run;
     };
-    // (first CTA) The first of the elements 0..n-1 whose running sum is above (strict) or at least t; the last one if none is.
-    auto first_at = [&](int n, double t, bool strict) {
-        if (tid == 0) s.hit = n - 1;
+    // The first of the elements 0..n-1 whose running sum is above (strict) or at least t; the last one if none is.
+    auto first_at = [&](int n, unsigned long long k, double run, double t, bool strict) {
+        if (tid == 0) s.hit = max(n - 1, 0);
         __syncthreads();
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int e = 2 * tid + q;
-            if (e < n && (strict ? s.cum[e] > t : s.cum[e] >= t)) { atomicMin(&s.hit, e); break; }
-        }
+        const unsigned ok = __ballot_sync(0xffffffffu, tid < n && (strict ? run > t : run >= t));
+        if (ok && lane == 0) atomicMin(&s.hit, warp * 32 + __ffs(ok) - 1);
         __syncthreads();
         const int h = s.hit;
+        if (tid == h) s.res = Result{value_of((uint32_t)(k >> 32)), (int)(uint32_t)k, run};
         __syncthreads();
         return h;
     };
@@ -375,50 +477,53 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     const float tp0 = p.top_p ? p.top_p[b] : 1.f;
     const bool nucleus = tp0 < 1.f;
     const double tp = (double)fmaxf(tp0, 0.f);
-    auto finish = [&](int e) {
-        if (tid == 0) p.tokens[b] = (int)(uint32_t)s.sorted[max(e, 0)];
-    };
-    // The other CTAs may leave once they have read what the first one holds; the first one leaves after them.
-    auto leave = [&]() {
-        cluster.barrier_arrive();
-        if (rank == 0) cluster.barrier_wait();
-    };
 
-    // Narrows a range of bin j (its elements' running sum starts at `before`) around the target until it can be
-    // collected; the first CTA then holds it sorted, with running sums.  Returns the number of elements.
-    auto narrow = [&](Range g, int j, bool by_rank, double target, bool strict, double& before, double expect) {
+    // Narrows a range of bin j around the target until its elements can be collected; `before` is the running sum in front of
+    // it, tot and part about how many elements the cluster and the fullest CTA have in it.  Returns the number collected.
+    auto narrow = [&](Range g, int j, bool by_rank, double target, bool strict, double& before, double tot, double part) {
+        bool local = false;
+        const bool open = !by_rank && j == kBins - 1;  // (weights there may be anything down to 0)
         for (int level = 0; level < 16; ++level) {
-            if (expect <= kList) {
-                const int n = (int)gather(g);
+            if (open) tally(g, local, tot, part);
+            if (!local && part <= kLocal) {
+                compact(g);
+                local = true;
+            }
+            if (local && tot <= kList) {
+                const int n = gather(g);
                 if (n <= kList) return n;
             }
             // 32 parts of its values, or of its indices where there is only one value
             const bool by_value = g.ka != g.kb;
-            if (!by_value && g.ib == 0x7fffffff) g.ib = p.V - 1;
+            if (!by_value && g.ib == kAll) g.ib = p.V - 1;
             const uint32_t lo = by_value ? g.ka : (uint32_t)g.ia, span = by_value ? g.kb - g.ka : (uint32_t)(g.ib - g.ia);
             const int sh = max(0, 32 - __clz(span) - 5);
-            const float xa = value_of(g.ka), xb = value_of(g.kb), X = s.X[j];
-            el.each(infinite, [&](float x, int i) {
-                if (inside(x, i, xa, xb, g)) {
-                    const uint32_t part = ((by_value ? key_of(x) : (uint32_t)i) - lo) >> sh;
-                    my_hist[part * 32] += by_rank ? 1u : units_of(x, X, r);
+            const float X = s.X[j][0];
+            if (local) {
+                for (uint32_t e = tid; e < min(s.nloc, (uint32_t)kLocal); e += kThreads) {
+                    const uint32_t k = (uint32_t)(s.loc[e] >> 32);
+                    const int i = (int)(uint32_t)s.loc[e];
+                    if (k >= g.ka && k <= g.kb && i >= g.ia && i <= g.ib)
+                        my_hist[(((by_value ? k : (uint32_t)i) - lo) >> sh) * 32] += by_rank ? 1u : r.units(value_of(k), X);
                 }
-            });
-            const unsigned long long t = totals();
-            const double w = by_rank ? (double)t : s.W[j] * (double)t;
-            double run = w;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double v = __shfl_up_sync(0xffffffffu, run, o);
-                if (lane >= o) run += v;
+            } else {
+                const float xa = value_of(g.ka), xb = value_of(g.kb);
+                el.each(infinite, [&](float x, int i) {
+                    if (x <= xa && x >= xb)
+                        if (inside(x, i, g))
+                            my_hist[(((by_value ? key_of(x) : (uint32_t)i) - lo) >> sh) * 32] += by_rank ? 1u : r.units(x, X);
+                });
             }
+            const unsigned long long t = totals();
+            const double w = by_rank ? (double)t : s.W[j] * (double)t, run = warp_scan(w, lane);
             const unsigned ok = __ballot_sync(0xffffffffu, t > 0 && (strict ? before + run > target : before + run >= target));
             const unsigned any = __ballot_sync(0xffffffffu, t > 0);
-            const int part = ok ? __ffs(ok) - 1 : 31 - __clz(any | 1u);
-            before += __shfl_sync(0xffffffffu, run - w, part);
-            const double tt = __shfl_sync(0xffffffffu, (double)t, part);
-            expect = by_rank ? tt : (j < kBins - 1 ? 1.7 * tt * kUnit : 0.0);  // (a weight inside a bin is at least exp(-1/2))
-            const uint32_t a = lo + ((uint32_t)part << sh), last = (uint32_t)min((unsigned long long)a + (1u << sh) - 1, (unsigned long long)lo + span);
+            const int cut = ok ? __ffs(ok) - 1 : 31 - __clz(any | 1u);
+            before += __shfl_sync(0xffffffffu, run - w, cut);
+            const double per = by_rank ? 1.0 : 1.7 * kUnit;  // elements per unit: a weight inside a bin is at least exp(-1/2)
+            tot = per * __shfl_sync(0xffffffffu, (double)t, cut);
+            part = per * largest_part(cut);
+            const uint32_t a = lo + ((uint32_t)cut << sh), last = (uint32_t)min((unsigned long long)a + (1u << sh) - 1, (unsigned long long)lo + span);
             if (by_value) { g.ka = a; g.kb = last; }
             else { g.ia = (int)a; g.ib = (int)last; }
         }
@@ -429,12 +534,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     const int k = p.top_k ? p.top_k[b] : 0;
     if (k > 0 && k < p.V) {
         const unsigned long long t = level0(false);
-        uint32_t run = (uint32_t)t;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t v = __shfl_up_sync(0xffffffffu, run, o);
-            if (lane >= o) run += v;
-        }
+        const uint32_t run = warp_scan((uint32_t)t, lane);
         const unsigned ok = __ballot_sync(0xffffffffu, run >= (uint32_t)k);
         if (ok) {  // (else there are no more than k candidates)
             const int j = __ffs(ok) - 1;
@@ -442,29 +542,29 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             Range g = range_of_bin(j);
             if (upto <= kList) {  // few enough from the top down: the rest happens in the list
                 g.ka = key_of(r.m);
-                const int n = (int)gather(g);
-                if (rank == 0) {
-                    sort_list(n);
-                    sum_list(n, 0.0);
-                    int kept = min(k, n);
-                    if (nucleus) kept = 1 + first_at(kept, tp * s.cum[kept - 1], false);
-                    finish(first_at(kept, u * s.cum[kept - 1], true));
+                compact(g);
+                const int n = gather(g);
+                const unsigned long long e = sorted(n);
+                double w;
+                const double cum = summed(n, e, 0.0, w);
+                int kept = min(k, n);
+                if (tid == kept - 1) s.res.mass = cum;
+                __syncthreads();
+                double Z = s.res.mass;
+                if (nucleus) {
+                    kept = 1 + first_at(kept, e, cum, tp * Z, false);
+                    Z = s.res.mass;
                 }
-                leave();
+                first_at(kept, e, cum, u * Z, true);
+                if (rank == 0 && tid == 0) p.tokens[b] = s.res.i;
                 return;
             }
             double before = (double)(upto - in);
-            const int n = narrow(g, j, true, (double)k, false, before, (double)in);
-            if (rank == 0) {
-                sort_list(n);
-                if (tid < C) {
-                    const unsigned long long e = s.sorted[max(0, min(n, k - (int)before) - 1)];
-                    Result* to = cluster.map_shared_rank(&s.res, tid);
-                    to->x = value_of((uint32_t)(e >> 32));
-                    to->i = (int)(uint32_t)e;
-                }
-            }
-            cluster.sync();
+            const double part = largest_part(j);
+            const int n = narrow(g, j, true, (double)k, false, before, (double)in, part);
+            const unsigned long long e = sorted(n);
+            if (tid == max(0, min(n, k - (int)before) - 1)) s.res = Result{value_of((uint32_t)(e >> 32)), (int)(uint32_t)e, 0.0};
+            __syncthreads();
             lim_x = s.res.x;
             lim_i = s.res.i;
         }
@@ -472,51 +572,32 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
 
     // ---- weights of the bins; lane j: bin j
     const unsigned long long t = level0(true);
-    const double w = s.W[lane] * (double)t;
-    double run = w;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const double v = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += v;
-    }
-    const unsigned any = __ballot_sync(0xffffffffu, t > 0);
-    double Z = __shfl_sync(0xffffffffu, run, 31);
-    // bin of the first sum that reaches a target, the sum before it, and about how many elements it has
-    auto find = [&](double target, bool strict, double& before, double& expect) {
-        const unsigned ok = __ballot_sync(0xffffffffu, t > 0 && (strict ? run > target : run >= target));
-        const int j = ok ? __ffs(ok) - 1 : 31 - __clz(any | 1u);
-        before = __shfl_sync(0xffffffffu, run - w, j);
-        expect = j < kBins - 1 ? 1.7 * kUnit * __shfl_sync(0xffffffffu, (double)t, j) : 0.0;
-        return j;
+    const double w0 = s.W[lane] * (double)t, run0 = warp_scan(w0, lane);
+    const unsigned any0 = __ballot_sync(0xffffffffu, t > 0);
+    const int par0 = par ^ 1;
+    unsigned long long most = 0;  // the fullest CTA's share of bin `lane`
+    for (int c = 0; c < C; ++c) most = max(most, s.xch[par0][c][lane]);
+    double Z = __shfl_sync(0xffffffffu, run0, 31);
+    // Element at which the running sum reaches a target: its place and the sum go to s.res.
+    auto search = [&](double target, bool strict) {
+        const unsigned ok = __ballot_sync(0xffffffffu, t > 0 && (strict ? run0 > target : run0 >= target));
+        const int j = ok ? __ffs(ok) - 1 : 31 - __clz(any0 | 1u);
+        double before = __shfl_sync(0xffffffffu, run0 - w0, j);
+        const double tot = 1.7 * kUnit * (double)__shfl_sync(0xffffffffu, t, j), part = 1.7 * kUnit * (double)__shfl_sync(0xffffffffu, most, j);
+        const int n = narrow(range_of_bin(j), j, false, target, strict, before, tot, part);
+        const unsigned long long e = sorted(n);
+        double w;
+        const double cum = summed(n, e, before, w);
+        first_at(n, e, cum, target, strict);
     };
-    double before, expect;
     if (nucleus) {
-        const int j = find(tp * Z, false, before, expect);
-        const int n = narrow(range_of_bin(j), j, false, tp * Z, false, before, expect);
-        if (rank == 0) {
-            sort_list(n);
-            sum_list(n, before);
-            const int e = max(first_at(n, tp * Z, false), 0);
-            if (tid < C) {
-                Result* to = cluster.map_shared_rank(&s.res, tid);
-                to->x = value_of((uint32_t)(s.sorted[e] >> 32));
-                to->i = (int)(uint32_t)s.sorted[e];
-                to->mass = s.cum[e];
-            }
-        }
-        cluster.sync();
+        search(tp * Z, false);
         lim_x = s.res.x;
         lim_i = s.res.i;
         Z = s.res.mass;
     }
-    const int j = find(u * Z, true, before, expect);
-    const int n = narrow(range_of_bin(j), j, false, u * Z, true, before, expect);
-    if (rank == 0) {
-        sort_list(n);
-        sum_list(n, before);
-        finish(first_at(n, u * Z, true));
-    }
-    leave();
+    search(u * Z, true);
+    if (rank == 0 && tid == 0) p.tokens[b] = s.res.i;
 }
 
 }  // namespace
