@@ -31,8 +31,10 @@ constexpr int kRegs = 32;            // elements a thread holds; a CTA 16384, a 
 constexpr int kCluster = 8;
 constexpr int kBins = 32;
 constexpr int kLocal = 2048;         // elements of one bin that a CTA keeps in shared memory
-constexpr int kList = kThreads;      // elements that every CTA of the cluster sorts, one a thread
-constexpr int kGathers = 64;         // lists collected for one row, at most: 3 searches of up to 16 levels each
+constexpr int kSlot = 64;            // elements that a CTA may put into a list ...
+constexpr int kList = kCluster * kSlot;  // ... which every CTA of the cluster sorts, one element a thread
+constexpr int kSorted = 320;         // longer lists are narrowed further first: sorting takes time with the square of them
+constexpr int kSlices = 8;           // lane-private histograms of a CTA, each shared by two warps
 constexpr double kUnit = 1.0 / 8388608.0;  // 2^-23
 
 // descending: the largest logit has the smallest key; -0 has been turned into +0
@@ -52,18 +54,18 @@ struct Result {  // the last element of a kept prefix, and the prefix's weight
 };
 
 struct Smem {
-    uint32_t hist[kWarps][kBins][32];
+    uint32_t hist[kSlices][kBins][32];
     float X[kBins][32];              // a bin's upper end, once per lane: the same offset as in a histogram
-    unsigned long long loc[kLocal];  // the bin being searched: this CTA's elements, value key << 32 | index
+    uint2 loc[kLocal];               // the bin being searched: this CTA's elements, (value, index)
     unsigned long long list[2][kList];  // (turn by turn: a CTA may be at the next search while another still reads)
-    unsigned long long tmp[kList];
+    unsigned long long tmp[kList];   // value key << 32 | index
+    uint32_t cnt[2][kCluster];
     unsigned long long xch[2][kCluster][kBins];
     double W[kBins];                 // weight of a bin's upper end, per unit
     double scan[kWarps];
     Result res;
     uint32_t key[2][kCluster], key_w[kWarps];
-    uint32_t gcnt[kGathers], off[kCluster];
-    uint32_t nloc, lcnt, tot;
+    uint32_t nloc, lcnt;
     int hit;
     float thr;
 };
@@ -73,12 +75,7 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t lds(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ void sts(uint32_t a, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
+__device__ __forceinline__ void red_add(uint32_t a, uint32_t v) { asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(a), "r"(v)); }
 
 struct Row {  // what a thread needs to know about the row
     float m, inv_T2, inv_Tl2;  // maximum; 2 / T (bins of half a unit), log2(e) / T
@@ -172,7 +169,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     {
         uint4* h = reinterpret_cast<uint4*>(s.hist);
         for (int i = tid; i < (int)(sizeof s.hist / 16); i += kThreads) h[i] = make_uint4(0, 0, 0, 0);
-        if (tid < kGathers) s.gcnt[tid] = 0;
     }
     cluster.barrier_arrive();  // (waited for before the first access to another CTA's shared memory)
     pdl_trigger();
@@ -183,7 +179,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     el.n = max(0, min(chunk, p.V - el.base));
     el.row = p.logits + (int64_t)b * p.ld + el.base;
     el.load();
-    const float T0 = p.temperature ? p.temperature[b] : 1.f;
+    const float T0 = p.temperature ? p.temperature[b] : 1.f, mp0 = p.min_p ? p.min_p[b] : 0.f;
+    const double T = fmax((double)T0, 1e-37), inv_T = 1.0 / T;
+    // a weight is at least min_p when the logit is at most this far (negative) from the maximum
+    double thr = -INFINITY;
+    if (tid == 0 && mp0 > 0.f && T < 1e300) thr = T * log(fmin((double)mp0, 1.0));
 
     // the smallest of one 32-bit word per thread, over the cluster
     auto cluster_min = [&](uint32_t v, int slot) {
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         for (int j = 0; j < kRegs; ++j) el.x[j] = el.x[j] == INFINITY ? 0.f : -INFINITY;
         mx = 0.f;
     }
-    const double T = fmax((double)T0, 1e-37), m = (double)mx, inv_T = 1.0 / T;
+    const double m = (double)mx;
     Row r;
     r.m = mx;
     r.inv_T2 = (float)(2.0 * inv_T);
@@ -233,27 +233,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         s.X[bin][2 * (tid & 15)] = X;
         s.X[bin][2 * (tid & 15) + 1] = X;
         if ((tid & 15) == 0) s.W[bin] = kUnit * exp(((double)X - m) * inv_T);
-    }
-    // the smallest value that min_p keeps
-    float lim_x = -FLT_MAX;
-    const float mp0 = p.min_p ? p.min_p[b] : 0.f;
-    if (mp0 > 0.f && T < 1e300) {
-        if (tid == 0) {
-            const double mp = fmin((double)mp0, 1.0);
-            auto kept = [&](float v) { return exp(((double)v - m) / T) >= mp; };
-            float x = (float)fmax(m + T * log(mp), -(double)FLT_MAX);
-            for (int i = 0; i < 4 && x > -FLT_MAX && kept(nextafterf(x, -INFINITY)); ++i) x = nextafterf(x, -INFINITY);
-            for (int i = 0; i < 4 && x < mx && !kept(x); ++i) x = nextafterf(x, INFINITY);
-            s.thr = fminf(x, mx) + 0.f;
-        }
-        __syncthreads();
-        lim_x = s.thr;
+        if (tid == 0) s.thr = fmaxf(__double2float_ru(m + thr), -FLT_MAX) + 0.f;
     }
     __syncthreads();
     // the kept prefix: elements above lim_x, and those equal to it with an index up to lim_i
     constexpr int kAll = 0x7fffffff;
+    float lim_x = s.thr;
     int lim_i = kAll;
-    int par = 0, gathers = 0;
+    int par = 0, turn = 0;
 
     // Adds one lane-private histogram up over the cluster: every warp of every CTA gets the total of bin `lane`; the CTAs' parts
     // stay in s.xch[par ^ 1] until the next but one.
@@ -262,9 +249,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
 #pragma unroll
         for (int q = 0; q < kBins / kWarps; ++q) {
             const int bin = warp * (kBins / kWarps) + q;
-            uint32_t lo = 0, hi = 0;  // (a lane's sum has 30 bits at most)
+            uint32_t lo = 0, hi = 0;  // (two warps' sums of a lane have 31 bits at most)
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
+            for (int w = 0; w < kSlices; ++w) {
                 const uint32_t v = s.hist[w][bin][lane];
                 s.hist[w][bin][lane] = 0;
                 lo += v & 0xffffu;
@@ -286,26 +273,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         for (int c = 0; c < C; ++c) v = max(v, s.xch[par ^ 1][c][bin]);
         return (double)v;
     };
-    uint32_t* const my_hist = &s.hist[warp][0][lane];
-    const uint32_t hist_a = (uint32_t)__cvta_generic_to_shared(my_hist) - 0x4b000000u * 128u;  // + bin_bits * 128
-    const uint32_t X_a = (uint32_t)__cvta_generic_to_shared(&s.X[0][lane]) - 0x4b000000u * 128u;
+    const uint32_t my_hist = (uint32_t)__cvta_generic_to_shared(&s.hist[warp % kSlices][0][lane]);  // + bin * 128
+    const uint32_t hist_a = my_hist - 0x4b000000u * 128u;                                              // + bin_bits * 128
+    const char* const X_a = reinterpret_cast<const char*>(&s.X[0][lane]);
 
-    // The bins of the whole row up to the limit.
+    // The bins of the whole row up to the limit.  Elements beyond it add nothing: no branches.
     auto level0 = [&](bool mass) {
         if (mass)
             el.each(infinite, [&](float x, int i) {
-                if (x >= lim_x && (lim_i == kAll || x != lim_x || i <= lim_i)) {
-                    const uint32_t o = r.bin_bits(x) * 128u;
-                    const uint32_t u = r.unit_bits(x, __uint_as_float(lds(X_a + o)));
-                    sts(hist_a + o, lds(hist_a + o) + u - 0x3f800000u);
-                }
+                const uint32_t o = r.bin_bits(x) * 128u;
+                uint32_t u = r.units(x, *reinterpret_cast<const float*>(X_a + (o & (kBins * 128u - 1u))));
+                if (!(x >= lim_x)) u = 0;
+                if (lim_i != kAll && x == lim_x && i > lim_i) u = 0;
+                red_add(hist_a + o, u);
             });
         else
-            el.each(infinite, [&](float x, int) {
-                if (x >= lim_x) {  // (top-k comes first: no limit by index yet)
-                    const uint32_t o = hist_a + r.bin_bits(x) * 128u;
-                    sts(o, lds(o) + 1u);
-                }
+            el.each(infinite, [&](float x, int) {  // (top-k comes first: no limit by index yet)
+                red_add(hist_a + r.bin_bits(x) * 128u, x >= lim_x ? 1u : 0u);
             });
         return totals();
     };
@@ -365,85 +349,87 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
 #pragma unroll
             for (int j = 0; j < kRegs; ++j)
                 if (mask & (1u << j)) {
-                    if (at < kLocal) s.loc[at] = ((unsigned long long)key_of(el.x[j]) << 32) | (unsigned)(el.base + el.local(j));
+                    if (at < kLocal) s.loc[at] = make_uint2(__float_as_uint(el.x[j]), (uint32_t)(el.base + el.local(j)));
                     ++at;
                 }
         }
         el.rest(infinite, [&](float x, int i) {
             if (x <= xa && x >= xb && inside(x, i, g)) {
                 const uint32_t q = atomicAdd(&s.nloc, 1u);
-                if (q < kLocal) s.loc[q] = ((unsigned long long)key_of(x) << 32) | (unsigned)i;
+                if (q < kLocal) s.loc[q] = make_uint2(__float_as_uint(x), (uint32_t)i);
             }
         });
         __syncthreads();
     };
+    auto local_inside = [&](const uint2& v, const Range& g, uint32_t& k, int& i) {
+        k = key_of(__uint_as_float(v.x));
+        i = (int)v.y;
+        return k >= g.ka && k <= g.kb && i >= g.ia && i <= g.ib;
+    };
     // Counts the elements of a range (the weights of the open last bin say nothing about that).
     auto tally = [&](const Range& g, bool local, double& tot, double& part) {
-        const float xa = value_of(g.ka), xb = value_of(g.kb);
-        uint32_t n = 0;
+        uint32_t n = 0, k;
+        int i;
         if (local) {
-            for (uint32_t e = tid; e < min(s.nloc, (uint32_t)kLocal); e += kThreads) {
-                const uint32_t k = (uint32_t)(s.loc[e] >> 32);
-                const int i = (int)(uint32_t)s.loc[e];
-                n += k >= g.ka && k <= g.kb && i >= g.ia && i <= g.ib;
-            }
+            for (uint32_t e = tid; e < min(s.nloc, (uint32_t)kLocal); e += kThreads) n += local_inside(s.loc[e], g, k, i);
         } else {
+            const float xa = value_of(g.ka), xb = value_of(g.kb);
             el.each(infinite, [&](float x, int i) { n += x <= xa && x >= xb && inside(x, i, g); });
         }
-        my_hist[0] += n;
+        red_add(my_hist, n);
         const unsigned long long t = totals();
         tot = (double)__shfl_sync(0xffffffffu, t, 0);
         part = largest_part(0);
     };
-    // Brings the local elements of a range together in every CTA; returns how many there are.
+    // Brings the local elements of a range together in every CTA: CTA c's go to slots 64 c .. (the caller knows that no
+    // CTA has more).
     auto gather = [&](const Range& g) {
         if (tid == 0) s.lcnt = 0;
         __syncthreads();
         const uint32_t nloc = min(s.nloc, (uint32_t)kLocal);
-        for (uint32_t e0 = 0; e0 < nloc; e0 += kThreads) {
-            const uint32_t e = e0 + tid;
-            const unsigned long long v = e < nloc ? s.loc[e] : ~0ull;
-            const uint32_t k = (uint32_t)(v >> 32);
-            const int i = (int)(uint32_t)v;
-            const bool in = e < nloc && k >= g.ka && k <= g.kb && i >= g.ia && i <= g.ib;
+        for (uint32_t e0 = warp * 32; e0 < nloc; e0 += kThreads) {
+            const uint32_t e = e0 + lane;
+            uint32_t k = 0;
+            int i = 0;
+            const bool in = e < nloc && local_inside(s.loc[e], g, k, i);
             const unsigned who = __ballot_sync(0xffffffffu, in);
             if (!who) continue;
             uint32_t at = 0;
             if (lane == 0) at = atomicAdd(&s.lcnt, (uint32_t)__popc(who));
             at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
-            if (in && at < kList) s.tmp[at] = v;
+            if (in && at < kSlot) s.tmp[at] = ((unsigned long long)k << 32) | (uint32_t)i;
         }
         __syncthreads();
-        const uint32_t n = min(s.lcnt, (uint32_t)kList);
-        if (tid < C && n) s.off[tid] = atomicAdd(cluster.map_shared_rank(&s.gcnt[0], tid) + gathers, s.lcnt);
-        __syncthreads();
-        for (uint32_t e = tid; e < n * C; e += kThreads) {
-            const uint32_t c = e % C, at = s.off[c] + e / C;
-            if (at < kList) cluster.map_shared_rank(&s.list[gathers & 1][0], c)[at] = s.tmp[e / C];
+        const uint32_t n = min(s.lcnt, (uint32_t)kSlot), c = tid / kSlot, e = tid % kSlot;
+        if (c < C) {
+            if (e < n) cluster.map_shared_rank(&s.list[turn][0], c)[rank * kSlot + e] = s.tmp[e];
+            if (e == 0) cluster.map_shared_rank(&s.cnt[turn][0], c)[rank] = n;
         }
         cluster.sync();
-        return (int)s.gcnt[gathers++];
+        turn ^= 1;
+        int all = 0;
+        for (int q = 0; q < C; ++q) all += (int)s.cnt[turn ^ 1][q];
+        return all;
     };
-    // The n collected elements in order, element tid in thread tid: a bitonic network, over shuffles inside a warp.
+    // The collected elements in order, element e in thread e: each counts those before it.
     auto sorted = [&](int n) {
-        unsigned long long k = tid < n ? s.list[(gathers & 1) ^ 1][tid] : ~0ull;  // (of the last gather)
-        int P = 32;
-        while (P < n) P *= 2;
-        for (int size = 2; size <= P; size <<= 1)
-            for (int stride = size >> 1; stride > 0; stride >>= 1) {
-                unsigned long long o;
-                if (stride >= 32) {
-                    __syncthreads();
-                    s.tmp[tid] = k;
-                    __syncthreads();
-                    o = s.tmp[tid ^ stride];
-                } else {
-                    o = __shfl_xor_sync(0xffffffffu, k, stride);
-                }
-                const bool up = (tid & size) == 0, low = (tid & stride) == 0;
-                k = (up == low) == (o < k) ? o : k;
+        const unsigned long long* list = s.list[turn ^ 1];
+        const uint32_t* cnt = s.cnt[turn ^ 1];
+        const int c0 = tid / kSlot;
+        const bool mine = c0 < C && (uint32_t)(tid % kSlot) < cnt[c0];
+        if (__any_sync(0xffffffffu, mine)) {
+            const unsigned long long k = mine ? list[tid] : ~0ull;
+            int before = 0;
+            for (int c = 0; c < C; ++c) {
+                const int m = (int)cnt[c];
+                const unsigned long long* l = list + c * kSlot;
+#pragma unroll 8
+                for (int e = 0; e < m; ++e) before += l[e] < k;
             }
-        return k;
+            if (mine) s.tmp[before] = k;
+        }
+        __syncthreads();
+        return tid < n ? s.tmp[tid] : ~0ull;
     };
     // Running sum of the elements' weights, on top of `before`.
     auto summed = [&](int n, unsigned long long k, double before, double& w) {
@@ -489,10 +475,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
                 compact(g);
                 local = true;
             }
-            if (local && tot <= kList) {
-                const int n = gather(g);
-                if (n <= kList) return n;
-            }
+            if (local && part <= kSlot && tot <= kSorted) return gather(g);
             // 32 parts of its values, or of its indices where there is only one value
             const bool by_value = g.ka != g.kb;
             if (!by_value && g.ib == kAll) g.ib = p.V - 1;
@@ -501,17 +484,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             const float X = s.X[j][0];
             if (local) {
                 for (uint32_t e = tid; e < min(s.nloc, (uint32_t)kLocal); e += kThreads) {
-                    const uint32_t k = (uint32_t)(s.loc[e] >> 32);
-                    const int i = (int)(uint32_t)s.loc[e];
-                    if (k >= g.ka && k <= g.kb && i >= g.ia && i <= g.ib)
-                        my_hist[(((by_value ? k : (uint32_t)i) - lo) >> sh) * 32] += by_rank ? 1u : r.units(value_of(k), X);
+                    uint32_t k;
+                    int i;
+                    if (local_inside(s.loc[e], g, k, i))
+                        red_add(my_hist + (((by_value ? k : (uint32_t)i) - lo) >> sh) * 128u, by_rank ? 1u : r.units(value_of(k), X));
                 }
             } else {
                 const float xa = value_of(g.ka), xb = value_of(g.kb);
                 el.each(infinite, [&](float x, int i) {
                     if (x <= xa && x >= xb)
                         if (inside(x, i, g))
-                            my_hist[(((by_value ? key_of(x) : (uint32_t)i) - lo) >> sh) * 32] += by_rank ? 1u : r.units(x, X);
+                            red_add(my_hist + (((by_value ? key_of(x) : (uint32_t)i) - lo) >> sh) * 128u, by_rank ? 1u : r.units(x, X));
                 });
             }
             const unsigned long long t = totals();
@@ -540,7 +523,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             const int j = __ffs(ok) - 1;
             const uint32_t upto = __shfl_sync(0xffffffffu, run, j), in = __shfl_sync(0xffffffffu, (uint32_t)t, j);
             Range g = range_of_bin(j);
-            if (upto <= kList) {  // few enough from the top down: the rest happens in the list
+            uint32_t most = 0;  // elements of the fullest CTA up to this bin
+            for (int c = 0; c < C; ++c)
+                most = max(most, __reduce_add_sync(0xffffffffu, lane <= j ? (uint32_t)s.xch[par ^ 1][c][lane] : 0u));
+            if (upto <= kSorted && most <= kSlot) {  // few enough from the top down: the rest happens in the list
                 g.ka = key_of(r.m);
                 compact(g);
                 const int n = gather(g);
