@@ -416,6 +416,16 @@ def _on(t, dtype, n, what, dev):
     return t.data_ptr()
 
 
+def _raw_stream(stream, dev):
+    """The stream's handle; None: the current stream of device `dev`."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev) if _RAW_STREAM else torch.cuda.current_stream(dev).cuda_stream
+
+
+_RAW_STREAM = hasattr(torch._C, "_cuda_getCurrentRawStream")  # (building a Stream object takes longer than a small call)
+
+
 def _device_of(t, what):
     """The device index of a CUDA tensor; the calls launch on the current device, so it has to be that one."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -456,7 +466,7 @@ def first_sample(logits, uniforms, tokens, temperature=None, top_k=None, top_p=N
         raise TypeError("uniforms and tokens are required")
     rc = lib().first_sample(logits.data_ptr(), ld, B, V, _on(temperature, f32, B, "temperature", dev), _on(top_k, i32, B, "top_k", dev),
                             _on(top_p, f32, B, "top_p", dev), _on(min_p, f32, B, "min_p", dev),
-                            _on(uniforms, f32, B, "uniforms", dev), _on(tokens, i32, B, "tokens", dev), _stream(stream))
+                            _on(uniforms, f32, B, "uniforms", dev), _on(tokens, i32, B, "tokens", dev), _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_sample")
 
@@ -484,7 +494,7 @@ def first_lora(x, a, b, row_adapter, y, scales=None, segments=None, stream=None)
     rc = lib().first_lora(x.data_ptr(), _code(x, "x"), ldx, _on(a, a.dtype, a.numel(), "a", dev), _on(b, b.dtype, b.numel(), "b", dev),
                           _code(a, "a"), _on(scales, torch.float32, adapters, "scales", dev),
                           _on(row_adapter, torch.int32, rows, "row_adapter", dev), adapters, rank, len(segments) - 1,
-                          _segment_array(segments), rows, k, n, y.data_ptr(), _code(y, "y"), ldy, _stream(stream))
+                          _segment_array(segments), rows, k, n, y.data_ptr(), _code(y, "y"), ldy, _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_lora")
 
@@ -528,7 +538,7 @@ def first_rope(q, k, pos, inv_freq, factor=1.0, interleaved=False, stream=None):
     qs = q.stride()
     rc = lib().first_rope(q.data_ptr(), qs[0], qs[1], hq, kp, ks[0], ks[1], hk, _code(q, "q"), T, hd, 2 * inv_freq.numel(),
                           _on(pos, torch.int32, T, "pos", dev), _on(inv_freq, torch.float64, inv_freq.numel(), "inv_freq", dev),
-                          float(factor), int(bool(interleaved)), _stream(stream))
+                          factor, bool(interleaved), _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_rope")
 

@@ -1,6 +1,23 @@
 // Low-rank adapters of many requests beside a shared projection (the paper's "LoRA Compensation Module" keeps one
 // adapter merged into the weights; here every row of a batch may have its own):
 //   y[r] += scale[a] * B_a (A_a x[r]),  a = adapter of row r.
+//
+// Bound by the adapters' bytes at few rows, by y's (read and written) at many; the products are small.  One launch does both:
+// rows of one adapter are taken together, up to TR of them (a tile), so that its A and B are read once for all of
+// them; a cluster of eight CTAs works on a tile:
+//   shrink   h = A x on the tensor cores (mma.sync m16n8k16, rank rows x batch rows: the products are far too small for
+//            128-row tcgen05 tiles), the input features split over the CTAs and their warps
+//   combine  every CTA adds the eight partial sums up from the cluster's shared memory, in a fixed order
+//   expand   y += B h, the output features split over the CTAs (and over several clusters when tiles are few; each of
+//            those computes h again, from L2)
+// All operands enter exactly: float32 values as three bfloat16 terms (8 bits each), h too; of their products those
+// below 2^-26 are left out.  How the sums are ordered depends on the sizes k, n, rank alone, so a row's result does not depend on
+// the rows around it.
+#include <algorithm>
+#include <type_traits>
+
+#include <cooperative_groups.h>
+
 #include "common.cuh"
 #include "first.h"
 #include "ops.h"
@@ -8,62 +25,440 @@
 namespace first {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ float at(const void* p, int64_t i) { return to_f32(static_cast<const T*>(p)[i]); }
+namespace cg = cooperative_groups;
 
-// One block per row: A x into shared memory (one warp per row of A), then one thread per output feature.
-template <typename WT, typename YT>
-__global__ void __launch_bounds__(256) lora_rows(const LoraArgs p) {
+constexpr int kThreads = 512, kWarps = 16, kCluster = 8;
+constexpr int kMaxRows = 1024;      // rows of a launch (the ids are sorted into tiles by every CTA)
+constexpr int kMaxIds = 4096;       // adapters that can be; with more, every row is a tile of its own
+
+// (x, y) -> packed bfloat16 pairs: term 0 the nearest bfloat16, the others what is left (nothing, of an infinity or NaN)
+template <int N>
+__device__ __forceinline__ void split(float x, float y, uint32_t (&t)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        t[i] = *reinterpret_cast<const uint32_t*>(&h);
+        const float xh = bf_lo(t[i]), yh = bf_hi(t[i]);
+        x = fabsf(xh) < INFINITY ? x - xh : 0.f;
+        y = fabsf(yh) < INFINITY ? y - yh : 0.f;
+    }
+}
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Eight (or four) consecutive elements as pairs of bfloat16, in N terms.
+template <int N, int E>
+struct Frag { uint32_t t[N][E / 2]; };
+template <typename T, int E>
+__device__ __forceinline__ Frag<sizeof(T) == 2 ? 1 : 3, E> load_frag(const T* p, bool live) {
+    Frag<sizeof(T) == 2 ? 1 : 3, E> f;
+    if constexpr (sizeof(T) == 2) {
+        if constexpr (E == 8) {
+            const uint4 v = live ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0, 0, 0, 0);
+            f.t[0][0] = v.x; f.t[0][1] = v.y; f.t[0][2] = v.z; f.t[0][3] = v.w;
+        } else {
+            const uint2 v = live ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+            f.t[0][0] = v.x; f.t[0][1] = v.y;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < E / 4; ++q) {
+            const float4 v = live ? __ldg(reinterpret_cast<const float4*>(p) + q) : make_float4(0.f, 0.f, 0.f, 0.f);
+            uint32_t t[3];
+            split(v.x, v.y, t);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) f.t[i][2 * q] = t[i];
+            split(v.z, v.w, t);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) f.t[i][2 * q + 1] = t[i];
+        }
+    }
+    return f;
+}
+
+struct Plan {
+    int tiles;          // clusters = tiles * slices
+    int slices;         // parts of the output features
+    int direct;         // 1: tile t is row t
+    int mt, ks;         // 16-row tiles of A; warps that share the input features of one
+    int h_stride;       // of a batch row's h, in bfloat16
+    int y_pairs;        // y can be accessed two features at a time
+};
+
+// XK: LoraX.  WT: type of the adapters.  TR: rows of a tile (8 or 32).
+template <int XK, typename WT, typename YT, int TR>
+__global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) lora_tiles(const LoraArgs p, const Plan pl) {
     const Stamp stamp_guard(p.stamp);
-    extern __shared__ float h[];  // [S*R]
+    constexpr int NT = TR / 8, NX = XK == kLoraXBf16 ? 1 : XK == kLoraXPair ? 2 : 3, NW = sizeof(WT) == 2 ? 1 : 3;
+    using XT = typename std::conditional<XK == kLoraXF32, float, __nv_bfloat16>::type;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ int rows_s[TR];     // the tile's rows
+    __shared__ int tile_s[3];      // adapter, which of its groups, rows
+    __shared__ int warp_s[kWarps];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
+    const int g = lane >> 2, t = lane & 3;
+    const int tile = (int)(blockIdx.x / kCluster) % pl.tiles, slice = (int)(blockIdx.x / kCluster) / pl.tiles;
     pdl_trigger();
     pdl_wait();
-    const int i = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (p.m_dev && i >= *p.m_dev) return;
-    const int s = p.idx ? p.idx[i] : i, ad = p.adapter[s];
-    if (ad < 0 || ad >= p.n) return;
-    const int M = p.S * p.R;
-    const WT* A = static_cast<const WT*>(p.a) + (int64_t)ad * M * p.K;
-    const WT* B = static_cast<const WT*>(p.b) + (int64_t)ad * p.N * p.R;
-    for (int j = warp; j < M; j += 8) {
-        float acc = 0.f;
-        for (int k = lane; k < p.K; k += 32) {
-            const int64_t e = (int64_t)i * p.ldx + k;
-            float x = p.x_kind == kLoraXF32 ? at<float>(p.x, e) : at<__nv_bfloat16>(p.x, e);
-            if (p.x_kind == kLoraXPair) x += at<__nv_bfloat16>(p.x_lo, e);
-            acc += x * to_f32(A[(int64_t)j * p.K + k]);
+    const int m = p.m_dev ? max(0, min(p.m, *p.m_dev - p.row0)) : p.m;
+    auto id_of = [&](int i) {
+        const int a = p.adapter[p.idx ? p.idx[i] : i];
+        return a >= 0 && a < p.n ? a : -1;
+    };
+
+    // ---- the tile: which adapter, which rows
+    if (pl.direct) {
+        if (tid == 0) {
+            tile_s[0] = tile < m ? id_of(tile) : -1;
+            tile_s[2] = 1;
         }
-        acc = warp_sum(acc);
-        if (lane == 0) h[j] = acc;
+        if (tid < TR) rows_s[tid] = tile;
+        __syncthreads();
+    } else if (p.m <= 32) {
+        // one warp sees all rows: every TR-th row of an adapter opens a tile, tile t belongs to the t-th of those
+        if (warp == 0) {
+            const int id = lane < m ? id_of(lane) : -1;
+            const unsigned same = __match_any_sync(0xffffffffu, id);
+            const int nth = __popc(same & ((1u << lane) - 1u));  // among its adapter's rows
+            const unsigned opens = __ballot_sync(0xffffffffu, id >= 0 && nth % TR == 0);
+            const int lead = tile < __popc(opens) ? (int)__fns(opens, 0, tile + 1) : -1;
+            if (lead < 0) {
+                if (lane == 0) tile_s[0] = -1;
+            } else {
+                const int a = __shfl_sync(0xffffffffu, id, lead), n0 = __shfl_sync(0xffffffffu, nth, lead);
+                const unsigned mine = __ballot_sync(0xffffffffu, id == a && nth >= n0 && nth < n0 + TR);
+                if (lane < TR) rows_s[lane] = lead;  // (columns beyond the tile's rows: read, never written)
+                __syncwarp();
+                if (id == a && nth >= n0 && nth < n0 + TR) rows_s[nth - n0] = lane;
+                if (lane == 0) {
+                    tile_s[0] = a;
+                    tile_s[2] = __popc(mine);
+                }
+            }
+        }
+        __syncthreads();
+    } else {
+        // rows per adapter; adapter a then has ceil(rows / TR) tiles, in the order of the ids
+        int* cnt = reinterpret_cast<int*>(smem);                    // [n]
+        int* ids = cnt + ((p.n + 3) & ~3);                          // [m]
+        for (int i = tid; i < p.n; i += kThreads) cnt[i] = 0;
+        __syncthreads();
+        for (int i = tid; i < m; i += kThreads) {
+            const int a = id_of(i);
+            ids[i] = a;
+            if (a >= 0) atomicAdd(&cnt[a], 1);
+        }
+        if (tid == 0) tile_s[0] = -1;
+        __syncthreads();
+        const int per = (p.n + kThreads - 1) / kThreads, a0 = min(p.n, tid * per), a1 = min(p.n, a0 + per);
+        int mine = 0;
+        for (int a = a0; a < a1; ++a) mine += (cnt[a] + TR - 1) / TR;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) warp_s[warp] = upto;
+        __syncthreads();
+        int before = upto - mine;
+        for (int w = 0; w < warp; ++w) before += warp_s[w];
+        if (tile >= before && tile < before + mine)
+            for (int a = a0; a < a1; ++a) {
+                const int n = (cnt[a] + TR - 1) / TR;
+                if (tile < before + n) {
+                    tile_s[0] = a;
+                    tile_s[1] = tile - before;
+                    tile_s[2] = min(TR, cnt[a] - (tile - before) * TR);
+                    break;
+                }
+                before += n;
+            }
+        __syncthreads();
+        // its rows: those of the adapter, in order, number tile_s[1] * TR and on
+        const int a = tile_s[0];
+        if (a >= 0) {
+            const int seg = (m + kWarps * 32 - 1) / (kWarps * 32) * 32, i0 = warp * seg;  // rows of a warp
+            int c = 0;
+            for (int i = i0; i < min(m, i0 + seg); i += 32) c += __popc(__ballot_sync(0xffffffffu, i + lane < m && ids[i + lane] == a));
+            if (lane == 0) warp_s[warp] = c;
+            __syncthreads();
+            int r = -tile_s[1] * TR;
+            for (int w = 0; w < warp; ++w) r += warp_s[w];
+            for (int i = i0; i < min(m, i0 + seg); i += 32) {
+                const bool is = i + lane < m && ids[i + lane] == a;
+                const unsigned who = __ballot_sync(0xffffffffu, is);
+                const int at = r + __popc(who & ((1u << lane) - 1u));
+                if (is && at >= 0 && at < TR) rows_s[at] = i + lane;
+                if (is && at == 0)
+                    for (int c = tile_s[2]; c < TR; ++c) rows_s[c] = i + lane;  // (columns beyond its rows: read, never written)
+                r += __popc(who);
+            }
+        }
+        __syncthreads();
+    }
+    const int ad = tile_s[0], live = tile_s[2];
+    if (ad < 0) return;  // (the whole cluster: nothing has been shared yet)
+
+    // ---- shrink: partial h of this CTA's input features
+    const int M = p.S * p.R, MP = pl.mt * 16;
+    float* part = reinterpret_cast<float*>(smem);                                   // [ks][MP][TR]
+    __nv_bfloat16* hs = reinterpret_cast<__nv_bfloat16*>(part + pl.ks * MP * TR);   // [S][3][TR][h_stride]
+    const int blocks = (p.K + 31) / 32;
+    const int c0 = (int)((int64_t)blocks * rank / kCluster), c1 = (int)((int64_t)blocks * (rank + 1) / kCluster);
+    for (int u = warp; u < pl.mt * pl.ks; u += kWarps) {
+        const int mt = u / pl.ks, ks = u % pl.ks;
+        const int b0 = c0 + (c1 - c0) * ks / pl.ks, b1 = c0 + (c1 - c0) * (ks + 1) / pl.ks;
+        const WT* A = static_cast<const WT*>(p.a) + (int64_t)ad * M * p.K;
+        const WT *A0 = A + (int64_t)min(mt * 16 + g, M - 1) * p.K + 8 * t, *A1 = A + (int64_t)min(mt * 16 + g + 8, M - 1) * p.K + 8 * t;
+        const XT *X[NT], *XL[NT];
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            const int64_t o = (int64_t)rows_s[q * 8 + g] * p.ldx + 8 * t;
+            X[q] = static_cast<const XT*>(p.x) + o;
+            XL[q] = XK == kLoraXPair ? static_cast<const XT*>(p.x_lo) + o : nullptr;
+        }
+        float acc[NT][4] = {};
+        constexpr int kUnroll = TR == 8 ? 4 : 2;
+#pragma unroll kUnroll
+        for (int b = b0; b < b1; ++b) {
+            const bool in = b * 32 + 8 * t < p.K;
+            const auto f0 = load_frag<WT, 8>(A0 + b * 32, in), f1 = load_frag<WT, 8>(A1 + b * 32, in);
+#pragma unroll
+            for (int q = 0; q < NT; ++q) {
+                uint32_t xf[NX][4];
+                const auto v = load_frag<XT, 8>(X[q] + b * 32, in);
+                if constexpr (XK == kLoraXPair) {
+                    const auto w = load_frag<XT, 8>(XL[q] + b * 32, in);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { xf[0][e] = v.t[0][e]; xf[1][e] = w.t[0][e]; }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NX; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) xf[i][e] = v.t[i][e];
+                }
+                // (which input features a step takes is arbitrary: a lane's eight are the same in both operands.  The tensor
+                // cores cut sums off instead of rounding them, so a chain of them stays short: 32 features, low terms first,
+                // then a float32 addition.)
+                float blk[4] = {};
+#pragma unroll
+                for (int i = NX - 1; i >= 0; --i)
+#pragma unroll
+                    for (int j = NW - 1; j >= 0; --j)
+                        if (i + j < 3)
+#pragma unroll
+                            for (int st = 0; st < 2; ++st)
+                                mma(blk, f0.t[j][2 * st], f1.t[j][2 * st], f0.t[j][2 * st + 1], f1.t[j][2 * st + 1],
+                                    xf[i][2 * st], xf[i][2 * st + 1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[q][e] += blk[e];
+            }
+        }
+        float* o = part + (ks * MP + mt * 16) * TR;
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            o[g * TR + q * 8 + 2 * t] = acc[q][0];
+            o[g * TR + q * 8 + 2 * t + 1] = acc[q][1];
+            o[(g + 8) * TR + q * 8 + 2 * t] = acc[q][2];
+            o[(g + 8) * TR + q * 8 + 2 * t + 1] = acc[q][3];
+        }
     }
     __syncthreads();
+    if (pl.ks > 1) {
+        for (int e = tid; e < MP * TR; e += kThreads) {
+            float v = part[e];
+            for (int q = 1; q < pl.ks; ++q) v += part[q * MP * TR + e];
+            part[e] = v;
+        }
+    }
+    // ---- expand, set-up: FT times 16 output features a step, features 2g and 2g+1 of each in a thread; the first step's
+    // operands are on their way while the cluster meets
+    constexpr int FT = 1;
+    using Y2 = typename std::conditional<sizeof(YT) == 4, float2, uint32_t>::type;
+    const int ft = (p.N + 16 * FT - 1) / (16 * FT), per = (ft + pl.slices * kCluster - 1) / (pl.slices * kCluster);
+    const int first = (slice * kCluster + rank) * per, last = min(ft, first + per);
+    const WT* B = static_cast<const WT*>(p.b) + (int64_t)ad * p.N * p.R;
+    YT* Y = static_cast<YT*>(p.y);
+    int64_t yo[NT][2];
+#pragma unroll
+    for (int q = 0; q < NT; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = rows_s[q * 8 + 2 * t + h];
+            yo[q][h] = q * 8 + 2 * t + h < live ? (int64_t)(p.scatter ? p.idx[i] : i) * p.ldy + 2 * g : -1;
+        }
+    const int kbs = (p.R + 15) / 16;
+    struct Step {
+        Frag<NW, 4> w[FT][2];
+        Y2 y[FT][NT][2];
+    };
+    auto weights = [&](int f, int kb, Frag<NW, 4> (&w)[2]) {  // rows f and f + 1 of B, sixteen columns
+        const bool in = kb * 16 + 4 * t < p.R;
+        w[0] = load_frag<WT, 4>(B + (int64_t)min(f, p.N - 1) * p.R + kb * 16 + 4 * t, in);
+        w[1] = load_frag<WT, 4>(B + (int64_t)min(f + 1, p.N - 1) * p.R + kb * 16 + 4 * t, in);
+    };
+    auto fetch = [&](int step, Step& d) {
+#pragma unroll
+        for (int i = 0; i < FT; ++i) {
+            const int f0 = (step * FT + i) * 16;
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (pl.y_pairs && yo[q][h] >= 0 && f0 + 2 * g + 1 < p.N) d.y[i][q][h] = *reinterpret_cast<const Y2*>(Y + yo[q][h] + f0);
+            weights(f0 + 2 * g, 0, d.w[i]);
+        }
+    };
+    Step next;
+    if (first + warp < last) fetch(first + warp, next);
+    cluster.sync();
+
+    // ---- combine: h of the tile's rows, scaled, in three terms; columns up to the next multiple of 16 are zero
     const float sc = p.scales ? p.scales[ad] : 1.f;
-    YT* y = static_cast<YT*>(p.y) + (int64_t)(p.scatter ? s : i) * p.ldy;
-    for (int f = threadIdx.x; f < p.N; f += 256) {
-        int sg = 0;
-        while (sg + 1 < p.S && f >= p.seg[sg + 1]) ++sg;
-        float acc = 0.f;
-        for (int j = 0; j < p.R; ++j) acc += to_f32(B[(int64_t)f * p.R + j]) * h[sg * p.R + j];
-        y[f] = from_f32<YT>(to_f32(y[f]) + sc * acc);
+    for (int e = tid; e < p.S * kbs * 16 * live; e += kThreads) {
+        const int sj = e / live, col = e - sj * live, s = sj / (kbs * 16), j = sj - s * (kbs * 16);
+        float v = 0.f;
+        if (j < p.R) {
+#pragma unroll
+            for (int c = 0; c < kCluster; ++c) v += cluster.map_shared_rank(part, c)[(s * p.R + j) * TR + col];
+        }
+        uint32_t t3[3];
+        split(v * sc, 0.f, t3);
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            reinterpret_cast<uint16_t*>(hs)[((s * 3 + i) * TR + col) * pl.h_stride + j] = (uint16_t)t3[i];
+    }
+    __syncthreads();
+    cluster.barrier_arrive();  // (no CTA leaves before all have read its partial sums)
+
+    // ---- expand
+    for (int step = first + warp; step < last; step += kWarps) {
+        Step cur = next;
+        if (step + kWarps < last) fetch(step + kWarps, next);
+#pragma unroll
+        for (int i = 0; i < FT; ++i) {
+            const int f0 = (step * FT + i) * 16, f = f0 + 2 * g;
+            if (f0 >= p.N) break;
+            int s = 0;
+            while (s + 1 < p.S && f0 >= p.seg[s + 1]) ++s;
+            float acc[NT][4] = {};
+            for (int kb = 0; kb < kbs; ++kb) {
+                if (kb) weights(f, kb, cur.w[i]);
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                    float blk[4] = {};
+#pragma unroll
+                    for (int k = 2; k >= 0; --k) {
+                        const uint2 h = *reinterpret_cast<const uint2*>(hs + ((s * 3 + k) * TR + q * 8 + g) * pl.h_stride + kb * 16 + 4 * t);
+#pragma unroll
+                        for (int j = NW - 1; j >= 0; --j)
+                            if (k + j < 3) mma(blk, cur.w[i][0].t[j][0], cur.w[i][1].t[j][0], cur.w[i][0].t[j][1], cur.w[i][1].t[j][1], h.x, h.y);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[q][e] += blk[e];
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (yo[q][h] < 0) continue;
+                    YT* y = Y + yo[q][h] + f0;
+                    const float d0 = acc[q][h], d1 = acc[q][2 + h];
+                    if (pl.y_pairs && f + 1 < p.N) {
+                        if constexpr (sizeof(YT) == 4)
+                            *reinterpret_cast<float2*>(y) = make_float2(cur.y[i][q][h].x + d0, cur.y[i][q][h].y + d1);
+                        else
+                            *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(bf_lo(cur.y[i][q][h]) + d0, bf_hi(cur.y[i][q][h]) + d1);
+                    } else {
+                        if (f < p.N) y[0] = from_f32<YT>(to_f32(y[0]) + d0);
+                        if (f + 1 < p.N) y[1] = from_f32<YT>(to_f32(y[1]) + d1);
+                    }
+                }
+        }
+    }
+    cluster.barrier_wait();
+}
+
+template <int XK, typename WT, typename YT, int TR>
+cudaError_t launch_tiles(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
+    Plan pl{};
+    const int M = a.S * a.R, ft = (a.N + 15) / 16;
+    // CTAs wanted: those that fit side by side, and where a tile is long work (TR = 32) a few times that, for an even end
+    const int want = TR == 8 ? 2 * n_sm : 4 * n_sm;
+    pl.direct = a.n > kMaxIds || a.m == 1;
+    pl.tiles = pl.direct ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / TR);
+    // few tiles: several clusters share one's output features, as long as each warp keeps a step of them
+    pl.slices = std::max(1, std::min((want + pl.tiles * kCluster - 1) / (pl.tiles * kCluster), ft / (kCluster * kWarps)));
+    pl.mt = (M + 15) / 16;
+    pl.ks = std::max(1, kWarps / pl.mt);
+    const int kbs = (a.R + 15) / 16;
+    pl.h_stride = 16 * (kbs | 1);  // an odd number of 32-byte units: eight batch rows' fragments meet no bank twice
+    const size_t es = sizeof(YT);
+    pl.y_pairs = reinterpret_cast<uintptr_t>(a.y) % (2 * es) == 0 && (a.m == 1 || a.ldy % 2 == 0);
+    size_t smem = (size_t)pl.ks * pl.mt * 16 * TR * 4 + (size_t)a.S * 3 * TR * pl.h_stride * 2;
+    if (!pl.direct) smem = std::max(smem, ((size_t)(a.n + 3) / 4 * 4 + a.m) * 4);
+    auto kern = lora_tiles<XK, WT, YT, TR>;
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(pl.tiles * pl.slices * kCluster);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = kCluster;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = pdl ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, a, pl);
+}
+
+template <int XK, typename WT, typename YT>
+cudaError_t launch_rows(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
+    // Tiles of 32 rows once an adapter has 16 rows on average, else of 8.
+    return a.m < 16 * (int64_t)a.n || a.m <= 32 ? launch_tiles<XK, WT, YT, 8>(a, st, pdl, n_sm) : launch_tiles<XK, WT, YT, 32>(a, st, pdl, n_sm);
+}
+
+template <typename WT, typename YT>
+cudaError_t launch_x(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
+    switch (a.x_kind) {
+        case kLoraXF32: return launch_rows<kLoraXF32, WT, YT>(a, st, pdl, n_sm);
+        case kLoraXBf16: return launch_rows<kLoraXBf16, WT, YT>(a, st, pdl, n_sm);
+        default: return launch_rows<kLoraXPair, WT, YT>(a, st, pdl, n_sm);
     }
 }
 
 }  // namespace
 
-cudaError_t lora_launch(const LoraArgs& a, cudaStream_t st, bool pdl, int) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(a.m);
-    cfg.blockDim = dim3(256);
-    cfg.dynamicSmemBytes = sizeof(float) * a.S * a.R;
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = pdl ? 1 : 0;
-    auto kern = a.w_f32 ? (a.y_f32 ? lora_rows<float, float> : lora_rows<float, __nv_bfloat16>)
-                        : (a.y_f32 ? lora_rows<__nv_bfloat16, float> : lora_rows<__nv_bfloat16, __nv_bfloat16>);
-    return cudaLaunchKernelEx(&cfg, kern, a);
+cudaError_t lora_launch(const LoraArgs& args, cudaStream_t st, bool pdl, int n_sm) {
+    LoraArgs a = args;
+    for (int r0 = 0; r0 < args.m; r0 += kMaxRows) {
+        a.m = std::min(kMaxRows, args.m - r0);
+        const size_t xe = args.x_kind == kLoraXF32 ? 4 : 2, ye = args.y_f32 ? 4 : 2;
+        a.x = static_cast<const char*>(args.x) + (size_t)r0 * args.ldx * xe;
+        a.x_lo = args.x_lo ? static_cast<const char*>(args.x_lo) + (size_t)r0 * args.ldx * xe : nullptr;
+        if (args.idx) a.idx = args.idx + r0;
+        else a.adapter = args.adapter + r0;
+        if (!args.scatter) a.y = static_cast<char*>(args.y) + (size_t)r0 * args.ldy * ye;
+        a.row0 = r0;
+        const cudaError_t e =
+            a.w_f32 ? (a.y_f32 ? launch_x<float, float>(a, st, pdl, n_sm) : launch_x<float, __nv_bfloat16>(a, st, pdl, n_sm))
+                    : (a.y_f32 ? launch_x<__nv_bfloat16, float>(a, st, pdl, n_sm) : launch_x<__nv_bfloat16, __nv_bfloat16>(a, st, pdl, n_sm));
+        if (e != cudaSuccess) return e;
+        pdl = false;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace first

@@ -27,6 +27,7 @@ struct LoraArgs {
     bool scatter = false;
     int m = 0;
     const int32_t* m_dev = nullptr;
+    int row0 = 0;                           // (set by lora_launch: rows before this piece, for m_dev)
     uint64_t* stamp = nullptr;
 };
 constexpr int kLoraMaxSegments = 4, kLoraMaxRank = 128;
