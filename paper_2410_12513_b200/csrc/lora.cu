@@ -27,7 +27,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512, kWarps = 16, kCluster = 8;
+constexpr int kThreads = 256, kWarps = 8, kCluster = 8;
+constexpr int kParts = 16;          // (16-row tile of A, share of the input features) pairs a CTA cuts its part of the shrink into, at least
 constexpr int kMaxRows = 1024;      // rows of a launch (the ids are sorted into tiles by every CTA)
 constexpr int kMaxIds = 4096;       // adapters that can be; with more, every row is a tile of its own
 
@@ -82,20 +83,20 @@ struct Plan {
     int tiles;          // clusters = tiles * slices
     int slices;         // parts of the output features
     int direct;         // 1: tile t is row t
-    int mt, ks;         // 16-row tiles of A; warps that share the input features of one
+    int mt, ks;         // 16-row tiles of A; shares that the input features of one are cut into
     int h_stride;       // of a batch row's h, in bfloat16
     int y_pairs;        // y can be accessed two features at a time
 };
 
 // XK: LoraX.  WT: type of the adapters.  TR: rows of a tile (8 or 32).
 template <int XK, typename WT, typename YT, int TR>
-__global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) lora_tiles(const LoraArgs p, const Plan pl) {
+__global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 4 : 2) lora_tiles(const LoraArgs p, const Plan pl) {
     const Stamp stamp_guard(p.stamp);
     constexpr int NT = TR / 8, NX = XK == kLoraXBf16 ? 1 : XK == kLoraXPair ? 2 : 3, NW = sizeof(WT) == 2 ? 1 : 3;
     using XT = typename std::conditional<XK == kLoraXF32, float, __nv_bfloat16>::type;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int rows_s[TR];     // the tile's rows
-    __shared__ int tile_s[3];      // adapter, which of its groups, rows
+    __shared__ int tile_s[2];      // adapter, rows
     __shared__ int warp_s[kWarps];
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
@@ -113,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) 
     if (pl.direct) {
         if (tid == 0) {
             tile_s[0] = tile < m ? id_of(tile) : -1;
-            tile_s[2] = 1;
+            tile_s[1] = 1;
         }
         if (tid < TR) rows_s[tid] = tile;
         __syncthreads();
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) 
                 if (id == a && nth >= n0 && nth < n0 + TR) rows_s[nth - n0] = lane;
                 if (lane == 0) {
                     tile_s[0] = a;
-                    tile_s[2] = __popc(mine);
+                    tile_s[1] = __popc(mine);
                 }
             }
         }
@@ -144,49 +145,45 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) 
         // rows per adapter; adapter a then has ceil(rows / TR) tiles, in the order of the ids
         int* cnt = reinterpret_cast<int*>(smem);                    // [n]
         int* ids = cnt + ((p.n + 3) & ~3);                          // [m]
+        int own[kMaxRows / kThreads];
+#pragma unroll
+        for (int q = 0; q < kMaxRows / kThreads; ++q) own[q] = tid + q * kThreads < m ? id_of(tid + q * kThreads) : -1;
         for (int i = tid; i < p.n; i += kThreads) cnt[i] = 0;
         __syncthreads();
-        for (int i = tid; i < m; i += kThreads) {
-            const int a = id_of(i);
-            ids[i] = a;
-            if (a >= 0) atomicAdd(&cnt[a], 1);
-        }
-        if (tid == 0) tile_s[0] = -1;
-        __syncthreads();
-        const int per = (p.n + kThreads - 1) / kThreads, a0 = min(p.n, tid * per), a1 = min(p.n, a0 + per);
-        int mine = 0;
-        for (int a = a0; a < a1; ++a) mine += (cnt[a] + TR - 1) / TR;
-        int upto = mine;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
+        for (int q = 0; q < kMaxRows / kThreads; ++q) {
+            if (tid + q * kThreads < m) ids[tid + q * kThreads] = own[q];
+            if (own[q] >= 0) atomicAdd(&cnt[own[q]], 1);
         }
-        if (lane == 31) warp_s[warp] = upto;
         __syncthreads();
-        int before = upto - mine;
-        for (int w = 0; w < warp; ++w) before += warp_s[w];
-        if (tile >= before && tile < before + mine)
-            for (int a = a0; a < a1; ++a) {
-                const int n = (cnt[a] + TR - 1) / TR;
-                if (tile < before + n) {
-                    tile_s[0] = a;
-                    tile_s[1] = tile - before;
-                    tile_s[2] = min(TR, cnt[a] - (tile - before) * TR);
-                    break;
-                }
-                before += n;
+        // every warp finds the tile's adapter by itself: lane l looks at adapters 32 i + l
+        int a = -1, nth = 0, rows = 0;
+        for (int a0 = 0, before = 0; a0 < p.n; a0 += 32) {
+            const int c = a0 + lane < p.n ? cnt[a0 + lane] : 0, n = (c + TR - 1) / TR;
+            int upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
             }
-        __syncthreads();
-        // its rows: those of the adapter, in order, number tile_s[1] * TR and on
-        const int a = tile_s[0];
+            const int all = __shfl_sync(0xffffffffu, upto, 31);
+            if (tile < before + all) {
+                const int l = __ffs(__ballot_sync(0xffffffffu, tile < before + upto)) - 1;
+                a = a0 + l;
+                nth = (tile - before - __shfl_sync(0xffffffffu, upto - n, l)) * TR;
+                rows = min(TR, __shfl_sync(0xffffffffu, c, l) - nth);
+                break;
+            }
+            before += all;
+        }
+        // its rows: those of the adapter, in order, number nth and on
         if (a >= 0) {
             const int seg = (m + kWarps * 32 - 1) / (kWarps * 32) * 32, i0 = warp * seg;  // rows of a warp
             int c = 0;
             for (int i = i0; i < min(m, i0 + seg); i += 32) c += __popc(__ballot_sync(0xffffffffu, i + lane < m && ids[i + lane] == a));
             if (lane == 0) warp_s[warp] = c;
             __syncthreads();
-            int r = -tile_s[1] * TR;
+            int r = -nth;
             for (int w = 0; w < warp; ++w) r += warp_s[w];
             for (int i = i0; i < min(m, i0 + seg); i += 32) {
                 const bool is = i + lane < m && ids[i + lane] == a;
@@ -194,13 +191,17 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) 
                 const int at = r + __popc(who & ((1u << lane) - 1u));
                 if (is && at >= 0 && at < TR) rows_s[at] = i + lane;
                 if (is && at == 0)
-                    for (int c = tile_s[2]; c < TR; ++c) rows_s[c] = i + lane;  // (columns beyond its rows: read, never written)
+                    for (int q = rows; q < TR; ++q) rows_s[q] = i + lane;  // (columns beyond its rows: read, never written)
                 r += __popc(who);
             }
         }
+        if (tid == 0) {
+            tile_s[0] = a;
+            tile_s[1] = rows;
+        }
         __syncthreads();
     }
-    const int ad = tile_s[0], live = tile_s[2];
+    const int ad = tile_s[0], live = tile_s[1];
     if (ad < 0) return;  // (the whole cluster: nothing has been shared yet)
 
     // ---- shrink: partial h of this CTA's input features
@@ -275,8 +276,8 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) 
             part[e] = v;
         }
     }
-    // ---- expand, set-up: FT times 16 output features a step, features 2g and 2g+1 of each in a thread; the first step's
-    // operands are on their way while the cluster meets
+    // ---- expand, set-up: FT times 16 output features a step, features 2g and 2g+1 of each in a thread; D steps' operands
+    // are on their way at a time, the first ones while the cluster meets
     constexpr int FT = 1;
     using Y2 = typename std::conditional<sizeof(YT) == 4, float2, uint32_t>::type;
     const int ft = (p.N + 16 * FT - 1) / (16 * FT), per = (ft + pl.slices * kCluster - 1) / (pl.slices * kCluster);
@@ -313,8 +314,11 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) 
             weights(f0 + 2 * g, 0, d.w[i]);
         }
     };
-    Step next;
-    if (first + warp < last) fetch(first + warp, next);
+    constexpr int D = sizeof(WT) == 4 ? 1 : TR == 8 || sizeof(YT) == 2 ? 3 : 2;  // steps in flight
+    Step ring[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (first + warp + d * kWarps < last) fetch(first + warp + d * kWarps, ring[d]);
     cluster.sync();
 
     // ---- combine: h of the tile's rows, scaled, in three terms; columns up to the next multiple of 16 are zero
@@ -336,9 +340,7 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) 
     cluster.barrier_arrive();  // (no CTA leaves before all have read its partial sums)
 
     // ---- expand
-    for (int step = first + warp; step < last; step += kWarps) {
-        Step cur = next;
-        if (step + kWarps < last) fetch(step + kWarps, next);
+    auto work = [&](int step, Step& cur) {
 #pragma unroll
         for (int i = 0; i < FT; ++i) {
             const int f0 = (step * FT + i) * 16, f = f0 + 2 * g;
@@ -380,6 +382,14 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 2 : 1) 
                     }
                 }
         }
+    };
+    for (int step = first + warp; step < last; step += D * kWarps) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int at = step + d * kWarps;
+            if (at < last) work(at, ring[d]);
+            if (at + D * kWarps < last) fetch(at + D * kWarps, ring[d]);
+        }
     }
     cluster.barrier_wait();
 }
@@ -388,14 +398,13 @@ template <int XK, typename WT, typename YT, int TR>
 cudaError_t launch_tiles(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
     Plan pl{};
     const int M = a.S * a.R, ft = (a.N + 15) / 16;
-    // CTAs wanted: those that fit side by side, and where a tile is long work (TR = 32) a few times that, for an even end
-    const int want = TR == 8 ? 2 * n_sm : 4 * n_sm;
+    const int want = (TR == 8 ? 4 : 2) * n_sm;  // CTAs that fit side by side
     pl.direct = a.n > kMaxIds || a.m == 1;
     pl.tiles = pl.direct ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / TR);
     // few tiles: several clusters share one's output features, as long as each warp keeps a step of them
     pl.slices = std::max(1, std::min((want + pl.tiles * kCluster - 1) / (pl.tiles * kCluster), ft / (kCluster * kWarps)));
     pl.mt = (M + 15) / 16;
-    pl.ks = std::max(1, kWarps / pl.mt);
+    pl.ks = std::max(1, kParts / pl.mt);
     const int kbs = (a.R + 15) / 16;
     pl.h_stride = 16 * (kbs | 1);  // an odd number of 32-byte units: eight batch rows' fragments meet no bank twice
     const size_t es = sizeof(YT);
