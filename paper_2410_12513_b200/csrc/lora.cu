@@ -79,18 +79,53 @@ __device__ __forceinline__ Frag<sizeof(T) == 2 ? 1 : 3, E> load_frag(const T* p,
     return f;
 }
 
+// Four elements of a thread's own copy.
+template <typename WT>
+__device__ __forceinline__ Frag<sizeof(WT) == 2 ? 1 : 3, 4> shared_frag(const void* p) {
+    Frag<sizeof(WT) == 2 ? 1 : 3, 4> f;
+    if constexpr (sizeof(WT) == 2) {
+        const uint2 v = *static_cast<const uint2*>(p);
+        f.t[0][0] = v.x;
+        f.t[0][1] = v.y;
+    } else {
+        const float4 v = *static_cast<const float4*>(p);
+        uint32_t a[3], b[3];
+        split(v.x, v.y, a);
+        split(v.z, v.w, b);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) { f.t[i][0] = a[i]; f.t[i][1] = b[i]; }
+    }
+    return f;
+}
+
+// 16 (8) bytes from global to shared memory in the background; with live = false zeros
+template <int N>
+__device__ __forceinline__ void copy_async(void* to, const void* from, bool live) {
+    const uint32_t a = (uint32_t)__cvta_generic_to_shared(to);
+    const int n = live ? N : 0;
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(a), "l"(from), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(a), "l"(from), "r"(n) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <typename WT, int TR>
+constexpr int ctas_per_sm() { return sizeof(WT) == 4 ? 2 : TR == 8 ? 4 : 2; }
+
 struct Plan {
     int tiles;          // clusters = tiles * slices
     int slices;         // parts of the output features
     int direct;         // 1: tile t is row t
     int mt, ks;         // 16-row tiles of A; shares that the input features of one are cut into
     int h_stride;       // of a batch row's h, in bfloat16
-    int y_pairs;        // y can be accessed two features at a time
+    int h_bytes;        // of all of h
+    int y_vec;          // y's rows are 16-byte aligned
 };
 
 // XK: LoraX.  WT: type of the adapters.  TR: rows of a tile (8 or 32).
 template <int XK, typename WT, typename YT, int TR>
-__global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 4 : 2) lora_tiles(const LoraArgs p, const Plan pl) {
+__global__ void __launch_bounds__(kThreads, ctas_per_sm<WT, TR>()) lora_tiles(const LoraArgs p, const Plan pl) {
     const Stamp stamp_guard(p.stamp);
     constexpr int NT = TR / 8, NX = XK == kLoraXBf16 ? 1 : XK == kLoraXPair ? 2 : 3, NW = sizeof(WT) == 2 ? 1 : 3;
     using XT = typename std::conditional<XK == kLoraXF32, float, __nv_bfloat16>::type;
@@ -206,8 +241,10 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 4 : 2) 
 
     // ---- shrink: partial h of this CTA's input features
     const int M = p.S * p.R, MP = pl.mt * 16;
-    float* part = reinterpret_cast<float*>(smem);                                   // [ks][MP][TR]
-    __nv_bfloat16* hs = reinterpret_cast<__nv_bfloat16*>(part + pl.ks * MP * TR);   // [S][3][TR][h_stride]
+    float* part = reinterpret_cast<float*>(smem);                              // [MP][TR]: the CTA's sum, of its first share at first
+    __nv_bfloat16* hs = reinterpret_cast<__nv_bfloat16*>(part + MP * TR);      // [S][3][TR][h_stride]
+    uint8_t* pool = reinterpret_cast<uint8_t*>(hs) + pl.h_bytes;               // the other shares, [ks - 1][MP][TR]; then the copies in flight
+    float* more = reinterpret_cast<float*>(pool);
     const int blocks = (p.K + 31) / 32;
     const int c0 = (int)((int64_t)blocks * rank / kCluster), c1 = (int)((int64_t)blocks * (rank + 1) / kCluster);
     for (int u = warp; u < pl.mt * pl.ks; u += kWarps) {
@@ -259,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 4 : 2) 
                 for (int e = 0; e < 4; ++e) acc[q][e] += blk[e];
             }
         }
-        float* o = part + (ks * MP + mt * 16) * TR;
+        float* o = (ks ? more + (ks - 1) * MP * TR : part) + mt * 16 * TR;
 #pragma unroll
         for (int q = 0; q < NT; ++q) {
             o[g * TR + q * 8 + 2 * t] = acc[q][0];
@@ -272,53 +309,85 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 4 : 2) 
     if (pl.ks > 1) {
         for (int e = tid; e < MP * TR; e += kThreads) {
             float v = part[e];
-            for (int q = 1; q < pl.ks; ++q) v += part[q * MP * TR + e];
+            for (int q = 0; q + 1 < pl.ks; ++q) v += more[q * MP * TR + e];
             part[e] = v;
         }
+        __syncthreads();
     }
-    // ---- expand, set-up: FT times 16 output features a step, features 2g and 2g+1 of each in a thread; D steps' operands
-    // are on their way at a time, the first ones while the cluster meets
-    constexpr int FT = 1;
-    using Y2 = typename std::conditional<sizeof(YT) == 4, float2, uint32_t>::type;
-    const int ft = (p.N + 16 * FT - 1) / (16 * FT), per = (ft + pl.slices * kCluster - 1) / (pl.slices * kCluster);
-    const int first = (slice * kCluster + rank) * per, last = min(ft, first + per);
-    const WT* B = static_cast<const WT*>(p.b) + (int64_t)ad * p.N * p.R;
-    YT* Y = static_cast<YT*>(p.y);
-    int64_t yo[NT][2];
-#pragma unroll
-    for (int q = 0; q < NT; ++q)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int i = rows_s[q * 8 + 2 * t + h];
-            yo[q][h] = q * 8 + 2 * t + h < live ? (int64_t)(p.scatter ? p.idx[i] : i) * p.ldy + 2 * g : -1;
+    // ---- expand, set-up: a step = 32 output features of one segment and 16 rows of the tile; as the tensor cores lay them
+    // out, a thread has eight consecutive features of the rows g and g + 8, so y moves 16 bytes at a time.  The operands of a
+    // warp's next steps are copied to shared memory in the background (each thread reads what it copied itself); the
+    // first ones are on their way while the cluster meets.
+    constexpr int HR = TR == 8 ? 1 : 2;  // 8-row halves of a 16-row tile that are used
+    constexpr int D = TR == 8 ? 2 : 3;   // steps in flight
+    int steps = 0;                       // (of 32 features)
+    for (int s = 0; s < p.S; ++s) steps += (p.seg[s + 1] - p.seg[s] + 31) / 32;
+    const int per = (steps + pl.slices * kCluster - 1) / (pl.slices * kCluster);
+    const int first = min(steps, (slice * kCluster + rank) * per), last = min(steps, first + per);
+    // with a second 16-row tile in use every other warp has that one
+    const bool two = live > 16;
+    const int q = two ? warp & 1 : 0, stride = two ? kWarps / 2 : kWarps;
+    const int mine = max(0, (last - first - (two ? warp >> 1 : warp) + stride - 1) / stride);  // this warp's steps
+    struct Place {  // of a step: its features, the end of their segment, and the segment
+        int f0, end, s;
+    };
+    auto ahead = [&](Place& at, int n) {  // n steps on
+        while (at.s < p.S) {
+            const int left = (at.end - at.f0 + 31) / 32;
+            if (n < left) {
+                at.f0 += 32 * n;
+                return;
+            }
+            n -= left;
+            if (++at.s < p.S) {
+                at.f0 = at.end;
+                at.end = p.seg[at.s + 1];
+            }
         }
+    };
+    YT* y_row[HR];  // this thread's part of its rows, or NULL
+#pragma unroll
+    for (int h = 0; h < HR; ++h) {
+        const int c = q * 16 + h * 8 + g, i = rows_s[c];
+        y_row[h] = c < live ? static_cast<YT*>(p.y) + (int64_t)(p.scatter ? p.idx[i] : i) * p.ldy + 8 * t : nullptr;
+    }
     const int kbs = (p.R + 15) / 16;
-    struct Step {
-        Frag<NW, 4> w[FT][2];
-        Y2 y[FT][NT][2];
+    constexpr int YV = sizeof(YT) / 2;  // 16-byte words of eight elements
+    struct Step {  // of one thread: y, and columns 0..15 of B (features 2j, 2j+1 of every eight in part j)
+        uint4 y[HR * YV][32];
+        typename std::conditional<sizeof(WT) == 2, uint2, uint4>::type w[4][32];
     };
-    auto weights = [&](int f, int kb, Frag<NW, 4> (&w)[2]) {  // rows f and f + 1 of B, sixteen columns
-        const bool in = kb * 16 + 4 * t < p.R;
-        w[0] = load_frag<WT, 4>(B + (int64_t)min(f, p.N - 1) * p.R + kb * 16 + 4 * t, in);
-        w[1] = load_frag<WT, 4>(B + (int64_t)min(f + 1, p.N - 1) * p.R + kb * 16 + 4 * t, in);
-    };
-    auto fetch = [&](int step, Step& d) {
+    Step* const ring = reinterpret_cast<Step*>(pool) + warp * D;
+    const WT* const B = static_cast<const WT*>(p.b) + (int64_t)ad * p.N * p.R + 4 * t;
+    const int fw = (g >> 1) * 8 + (g & 1);  // this thread's row of B in part 0
+    const bool in0 = 4 * t < p.R;           // (a rank of 8 has no columns 8..15)
+    auto w_row = [&](int f0, int j) { return B + (int64_t)min(f0 + fw + 2 * j, p.N - 1) * p.R; };
+    auto fetch = [&](const Place& at, Step& d) {
+        if (pl.y_vec && at.f0 + 8 * t + 8 <= at.end) {
 #pragma unroll
-        for (int i = 0; i < FT; ++i) {
-            const int f0 = (step * FT + i) * 16;
+            for (int h = 0; h < HR; ++h)
+                if (y_row[h])
 #pragma unroll
-            for (int q = 0; q < NT; ++q)
+                    for (int v = 0; v < YV; ++v) copy_async<16>(&d.y[h * YV + v][lane], reinterpret_cast<const uint4*>(y_row[h] + at.f0) + v, true);
+        }
+        if (at.f0 + 32 <= p.N) {
+            const WT* w = B + (int64_t)(at.f0 + fw) * p.R;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (pl.y_pairs && yo[q][h] >= 0 && f0 + 2 * g + 1 < p.N) d.y[i][q][h] = *reinterpret_cast<const Y2*>(Y + yo[q][h] + f0);
-            weights(f0 + 2 * g, 0, d.w[i]);
+            for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], in0 ? w + 2 * j * p.R : B - 4 * t, in0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], in0 ? w_row(at.f0, j) : B - 4 * t, in0);
         }
     };
-    constexpr int D = sizeof(WT) == 4 ? 1 : TR == 8 || sizeof(YT) == 2 ? 3 : 2;  // steps in flight
-    Step ring[D];
+    Place here{0, p.seg[1], 0}, next;
+    if (mine > 0) ahead(here, first + (two ? warp >> 1 : warp));
+    next = here;
 #pragma unroll
-    for (int d = 0; d < D; ++d)
-        if (first + warp + d * kWarps < last) fetch(first + warp + d * kWarps, ring[d]);
+    for (int d = 0; d < D; ++d) {
+        if (d < mine) fetch(next, ring[d]);
+        copy_commit();
+        ahead(next, stride);
+    }
     cluster.sync();
 
     // ---- combine: h of the tile's rows, scaled, in three terms; columns up to the next multiple of 16 are zero
@@ -340,76 +409,93 @@ __global__ void __launch_bounds__(kThreads, TR == 8 && sizeof(WT) == 2 ? 4 : 2) 
     cluster.barrier_arrive();  // (no CTA leaves before all have read its partial sums)
 
     // ---- expand
-    auto work = [&](int step, Step& cur) {
+    for (int n = 0, at = 0; n < mine; ++n, at = at + 1 < D ? at + 1 : 0) {
+        copy_wait<D - 1>();
+        Step& cur = ring[at];
+        const int f0 = here.f0, end = here.end;
+        float acc[4][4] = {};
+        const __nv_bfloat16* const h_tile = hs + (here.s * 3 * TR + q * 16 + g) * pl.h_stride + 4 * t;
+        for (int kb = 0; kb < kbs; ++kb) {
+            Frag<NW, 4> w[4];
 #pragma unroll
-        for (int i = 0; i < FT; ++i) {
-            const int f0 = (step * FT + i) * 16, f = f0 + 2 * g;
-            if (f0 >= p.N) break;
-            int s = 0;
-            while (s + 1 < p.S && f0 >= p.seg[s + 1]) ++s;
-            float acc[NT][4] = {};
-            for (int kb = 0; kb < kbs; ++kb) {
-                if (kb) weights(f, kb, cur.w[i]);
+            for (int j = 0; j < 4; ++j)
+                w[j] = kb ? load_frag<WT, 4>(w_row(f0, j) + kb * 16, kb * 16 + 4 * t < p.R) : shared_frag<WT>(&cur.w[j][lane]);
+            float blk[4][4] = {};
 #pragma unroll
-                for (int q = 0; q < NT; ++q) {
-                    float blk[4] = {};
+            for (int k = 2; k >= 0; --k) {
+                const __nv_bfloat16* hk = h_tile + k * TR * pl.h_stride + kb * 16;
+                const uint2 h0 = *reinterpret_cast<const uint2*>(hk);
+                const uint2 h1 = HR == 2 ? *reinterpret_cast<const uint2*>(hk + 8 * pl.h_stride) : make_uint2(0, 0);
 #pragma unroll
-                    for (int k = 2; k >= 0; --k) {
-                        const uint2 h = *reinterpret_cast<const uint2*>(hs + ((s * 3 + k) * TR + q * 8 + g) * pl.h_stride + kb * 16 + 4 * t);
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int j = NW - 1; j >= 0; --j)
-                            if (k + j < 3) mma(blk, cur.w[i][0].t[j][0], cur.w[i][1].t[j][0], cur.w[i][0].t[j][1], cur.w[i][1].t[j][1], h.x, h.y);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[q][e] += blk[e];
-                }
+                    for (int i = NW - 1; i >= 0; --i)
+                        if (k + i < 3) mma(blk[j], h0.x, h1.x, h0.y, h1.y, w[j].t[i][0], w[j].t[i][1]);
             }
 #pragma unroll
-            for (int q = 0; q < NT; ++q)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (yo[q][h] < 0) continue;
-                    YT* y = Y + yo[q][h] + f0;
-                    const float d0 = acc[q][h], d1 = acc[q][2 + h];
-                    if (pl.y_pairs && f + 1 < p.N) {
-                        if constexpr (sizeof(YT) == 4)
-                            *reinterpret_cast<float2*>(y) = make_float2(cur.y[i][q][h].x + d0, cur.y[i][q][h].y + d1);
-                        else
-                            *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(bf_lo(cur.y[i][q][h]) + d0, bf_hi(cur.y[i][q][h]) + d1);
-                    } else {
-                        if (f < p.N) y[0] = from_f32<YT>(to_f32(y[0]) + d0);
-                        if (f + 1 < p.N) y[1] = from_f32<YT>(to_f32(y[1]) + d1);
+                for (int e = 0; e < 4; ++e) acc[j][e] += blk[j][e];
+        }
+        const bool whole = pl.y_vec && f0 + 8 * t + 8 <= end;
+#pragma unroll
+        for (int h = 0; h < HR; ++h) {
+            if (!y_row[h]) continue;
+            YT* const y = y_row[h] + f0;
+            if (whole) {
+                uint4 v[YV];
+                if constexpr (sizeof(YT) == 4) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint4 o = cur.y[h * YV + i][lane];
+                        v[i] = make_uint4(__float_as_uint(__uint_as_float(o.x) + acc[2 * i][2 * h]),
+                                          __float_as_uint(__uint_as_float(o.y) + acc[2 * i][2 * h + 1]),
+                                          __float_as_uint(__uint_as_float(o.z) + acc[2 * i + 1][2 * h]),
+                                          __float_as_uint(__uint_as_float(o.w) + acc[2 * i + 1][2 * h + 1]));
                     }
+                } else {
+                    auto add = [&](uint32_t o, int j) {
+                        const __nv_bfloat162 r = __floats2bfloat162_rn(bf_lo(o) + acc[j][2 * h], bf_hi(o) + acc[j][2 * h + 1]);
+                        return *reinterpret_cast<const uint32_t*>(&r);
+                    };
+                    const uint4 o = cur.y[h][lane];
+                    v[0] = make_uint4(add(o.x, 0), add(o.y, 1), add(o.z, 2), add(o.w, 3));
                 }
-        }
-    };
-    for (int step = first + warp; step < last; step += D * kWarps) {
 #pragma unroll
-        for (int d = 0; d < D; ++d) {
-            const int at = step + d * kWarps;
-            if (at < last) work(at, ring[d]);
-            if (at + D * kWarps < last) fetch(at + D * kWarps, ring[d]);
+                for (int i = 0; i < YV; ++i) reinterpret_cast<uint4*>(y)[i] = v[i];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (f0 + 8 * t + e < end) y[e] = from_f32<YT>(to_f32(y[e]) + acc[e >> 1][2 * h + (e & 1)]);
+            }
         }
+        if (n + D < mine) fetch(next, cur);
+        copy_commit();
+        ahead(here, stride);
+        ahead(next, stride);
     }
+    copy_wait<0>();
     cluster.barrier_wait();
 }
 
 template <int XK, typename WT, typename YT, int TR>
 cudaError_t launch_tiles(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
     Plan pl{};
-    const int M = a.S * a.R, ft = (a.N + 15) / 16;
-    const int want = (TR == 8 ? 4 : 2) * n_sm;  // CTAs that fit side by side
+    const int M = a.S * a.R;
+    // At most as many tiles as: one for every row, or one ragged tile for every adapter and full ones for the rest.
     pl.direct = a.n > kMaxIds || a.m == 1;
     pl.tiles = pl.direct ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / TR);
     // few tiles: several clusters share one's output features, as long as each warp keeps a step of them
-    pl.slices = std::max(1, std::min((want + pl.tiles * kCluster - 1) / (pl.tiles * kCluster), ft / (kCluster * kWarps)));
+    const int want = ctas_per_sm<WT, TR>() * n_sm;  // CTAs that fit side by side
+    pl.slices = std::max(1, std::min((want + pl.tiles * kCluster - 1) / (pl.tiles * kCluster), a.N / (32 * kCluster * kWarps)));
     pl.mt = (M + 15) / 16;
     pl.ks = std::max(1, kParts / pl.mt);
     const int kbs = (a.R + 15) / 16;
     pl.h_stride = 16 * (kbs | 1);  // an odd number of 32-byte units: eight batch rows' fragments meet no bank twice
-    const size_t es = sizeof(YT);
-    pl.y_pairs = reinterpret_cast<uintptr_t>(a.y) % (2 * es) == 0 && (a.m == 1 || a.ldy % 2 == 0);
-    size_t smem = (size_t)pl.ks * pl.mt * 16 * TR * 4 + (size_t)a.S * 3 * TR * pl.h_stride * 2;
+    pl.y_vec = reinterpret_cast<uintptr_t>(a.y) % 16 == 0 && (a.m == 1 || a.ldy * sizeof(YT) % 16 == 0);
+    pl.h_bytes = a.S * 3 * TR * pl.h_stride * 2;
+    const size_t step = (TR == 8 ? 1 : 2) * sizeof(YT) / 2 * 512 + 4 * 32 * 4 * sizeof(WT), shares = (size_t)(pl.ks - 1) * pl.mt * 16 * TR * 4;
+    size_t smem = (size_t)pl.mt * 16 * TR * 4 + pl.h_bytes + std::max(shares, kWarps * (TR == 8 ? 2 : 3) * step);
     if (!pl.direct) smem = std::max(smem, ((size_t)(a.n + 3) / 4 * 4 + a.m) * 4);
     auto kern = lora_tiles<XK, WT, YT, TR>;
     if (smem > 40 * 1024) {
