@@ -28,7 +28,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256, kWarps = 8, kCluster = 8;
-constexpr int kParts = 16;          // (16-row tile of A, share of the input features) pairs a CTA cuts its part of the shrink into, at least
+constexpr int kParts = 8;           // (16-row tile of A, share of the input features) pairs a CTA cuts its part of the shrink into, about
 constexpr int kMaxRows = 1024;      // rows of a launch (the ids are sorted into tiles by every CTA)
 constexpr int kMaxIds = 4096;       // adapters that can be; with more, every row is a tile of its own
 
@@ -110,9 +110,6 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <typename WT, int TR>
-constexpr int ctas_per_sm() { return sizeof(WT) == 4 ? 2 : TR == 8 ? 4 : 2; }
-
 struct Plan {
     int tiles;          // clusters = tiles * slices
     int slices;         // parts of the output features
@@ -123,9 +120,10 @@ struct Plan {
     int y_vec;          // y's rows are 16-byte aligned
 };
 
-// XK: LoraX.  WT: type of the adapters.  TR: rows of a tile (8 or 32).
-template <int XK, typename WT, typename YT, int TR>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm<WT, TR>()) lora_tiles(const LoraArgs p, const Plan pl) {
+// XK: LoraX.  WT: type of the adapters.  TR: rows of a tile (8 or 32).  OCC: CTAs a
+// multiprocessor has room for (2: 128 registers a thread; 4: 64, for grids that want the room).
+template <int XK, typename WT, typename YT, int TR, int OCC>
+__global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, const Plan pl) {
     const Stamp stamp_guard(p.stamp);
     constexpr int NT = TR / 8, NX = XK == kLoraXBf16 ? 1 : XK == kLoraXPair ? 2 : 3, NW = sizeof(WT) == 2 ? 1 : 3;
     using XT = typename std::conditional<XK == kLoraXF32, float, __nv_bfloat16>::type;
@@ -260,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<WT, TR>()) lora_tiles(co
             XL[q] = XK == kLoraXPair ? static_cast<const XT*>(p.x_lo) + o : nullptr;
         }
         float acc[NT][4] = {};
-        constexpr int kUnroll = TR == 8 ? 4 : 2;
+        constexpr int kUnroll = TR == 8 && OCC == 2 ? 4 : 2;
 #pragma unroll kUnroll
         for (int b = b0; b < b1; ++b) {
             const bool in = b * 32 + 8 * t < p.K;
@@ -478,16 +476,14 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<WT, TR>()) lora_tiles(co
     cluster.barrier_wait();
 }
 
-template <int XK, typename WT, typename YT, int TR>
-cudaError_t launch_tiles(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
+template <int XK, typename WT, typename YT, int TR, int OCC>
+cudaError_t launch_tiles(const LoraArgs& a, int tiles, cudaStream_t st, bool pdl, int n_sm) {
     Plan pl{};
     const int M = a.S * a.R;
-    // At most as many tiles as: one for every row, or one ragged tile for every adapter and full ones for the rest.
     pl.direct = a.n > kMaxIds || a.m == 1;
-    pl.tiles = pl.direct ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / TR);
-    // few tiles: several clusters share one's output features, as long as each warp keeps a step of them
-    const int want = ctas_per_sm<WT, TR>() * n_sm;  // CTAs that fit side by side
-    pl.slices = std::max(1, std::min((want + pl.tiles * kCluster - 1) / (pl.tiles * kCluster), a.N / (32 * kCluster * kWarps)));
+    pl.tiles = tiles;
+    // few tiles: several clusters share one's output features, while there is room for them and a step for each warp
+    pl.slices = std::max(1, std::min(2 * n_sm / (tiles * kCluster), a.N / (32 * kCluster * kWarps)));
     pl.mt = (M + 15) / 16;
     pl.ks = std::max(1, kParts / pl.mt);
     const int kbs = (a.R + 15) / 16;
@@ -497,7 +493,7 @@ cudaError_t launch_tiles(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm)
     const size_t step = (TR == 8 ? 1 : 2) * sizeof(YT) / 2 * 512 + 4 * 32 * 4 * sizeof(WT), shares = (size_t)(pl.ks - 1) * pl.mt * 16 * TR * 4;
     size_t smem = (size_t)pl.mt * 16 * TR * 4 + pl.h_bytes + std::max(shares, kWarps * (TR == 8 ? 2 : 3) * step);
     if (!pl.direct) smem = std::max(smem, ((size_t)(a.n + 3) / 4 * 4 + a.m) * 4);
-    auto kern = lora_tiles<XK, WT, YT, TR>;
+    auto kern = lora_tiles<XK, WT, YT, TR, OCC>;
     if (smem > 40 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
         if (e != cudaSuccess) return e;
@@ -521,8 +517,17 @@ cudaError_t launch_tiles(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm)
 
 template <int XK, typename WT, typename YT>
 cudaError_t launch_rows(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
-    // Tiles of 32 rows once an adapter has 16 rows on average, else of 8.
-    return a.m < 16 * (int64_t)a.n || a.m <= 32 ? launch_tiles<XK, WT, YT, 8>(a, st, pdl, n_sm) : launch_tiles<XK, WT, YT, 32>(a, st, pdl, n_sm);
+    // Tiles of 32 rows once an adapter has 16 rows on average, else of 8.  At most as many tiles as: one for every row,
+    // or one ragged tile for every adapter and full ones for the rest.
+    const bool few = a.m < 16 * (int64_t)a.n || a.m <= 32;
+    const int TR = few ? 8 : 32;
+    const int tiles = a.n > kMaxIds || a.m == 1 ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / TR);
+    if (!few) return launch_tiles<XK, WT, YT, 32, 2>(a, tiles, st, pdl, n_sm);
+    // With 64 registers four CTAs fit on a multiprocessor instead of two, at the price of spills: 256 rows of 64 adapters
+    // (512 CTAs) 34 us against 48 with three, 32 rows of 16 adapters (160 CTAs) 12.7 against 10.9.  float32 adapters take
+    // three times the registers and stay at two.
+    if (sizeof(WT) == 2 && tiles * kCluster > 2 * n_sm) return launch_tiles<XK, WT, YT, 8, 4>(a, tiles, st, pdl, n_sm);
+    return launch_tiles<XK, WT, YT, 8, 2>(a, tiles, st, pdl, n_sm);
 }
 
 template <typename WT, typename YT>
