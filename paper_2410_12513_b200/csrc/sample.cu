@@ -5,7 +5,7 @@
 // that order, and so does a draw: the token is the first candidate whose cumulative weight exceeds u times the sum.
 // All of them are the same question -- where does a running sum (of ones, or of weights) reach a target -- and it is
 // answered without sorting the row:
-//   1. One thread-block cluster per row; the row is read once and stays in the cluster's registers.
+//   1. One thread-block cluster per row; the row is read once and stays in the cluster's shared memory.
 //   2. A histogram over 32 bins of (max - x) / T, half a unit wide: the sum reaches the target in one of them.
 //   3. If that bin holds many elements, it is cut into 32 parts of its range of values (and again, and, among equal
 //      values, of indices), each time keeping the part that holds the target.
@@ -26,26 +26,25 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kRegs = 32;            // elements a thread holds; a CTA 16384, a cluster of eight 131072 (more are re-read from L2)
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kBlock = 16;           // elements a thread looks at at a time
+constexpr int kHeld = 2 * kBlock * kThreads;  // elements that a CTA can hold in shared memory
 constexpr int kCluster = 8;
 constexpr int kBins = 32;
-constexpr int kLocal = 2048;         // elements of one bin that a CTA keeps in shared memory
-constexpr int kSlot = 64;            // elements that a CTA may put into a list ...
-constexpr int kList = kCluster * kSlot;  // ... which every CTA of the cluster sorts, one element a thread
+constexpr int kLocal = 4096;         // elements that a CTA can copy to shared memory for a search
+constexpr int kList = 512;           // elements that are sorted in every CTA of a cluster; of each CTA an equal share
 constexpr int kSorted = 320;         // longer lists are narrowed further first: sorting takes time with the square of them
-constexpr int kSlices = 8;           // lane-private histograms of a CTA, each shared by two warps
+constexpr int kSlices = 8;           // lane-private histograms of a CTA, each shared by four warps
 constexpr double kUnit = 1.0 / 8388608.0;  // 2^-23
 
-// descending: the largest logit has the smallest key; -0 has been turned into +0
+// descending: the largest logit has the smallest key; -0 equals +0
 __device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x);
+    const uint32_t b = __float_as_uint(x + 0.f);
     return (b & 0x80000000u) ? b : ~(b | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t k) {
     return __uint_as_float((k & 0x80000000u) ? k : ~(k | 0x80000000u));
 }
-__device__ __forceinline__ float clean(float x) { return x != x ? -INFINITY : x + 0.f; }
 
 struct Result {  // the last element of a kept prefix, and the prefix's weight
     float x;
@@ -56,9 +55,9 @@ struct Result {  // the last element of a kept prefix, and the prefix's weight
 struct Smem {
     uint32_t hist[kSlices][kBins][32];
     float X[kBins][32];              // a bin's upper end, once per lane: the same offset as in a histogram
-    uint2 loc[kLocal];               // the bin being searched: this CTA's elements, (value, index)
-    unsigned long long list[2][kList];  // (turn by turn: a CTA may be at the next search while another still reads)
-    unsigned long long tmp[kList];   // value key << 32 | index
+    uint2 loc[kLocal];               // this CTA's elements of the range that was copied last, (value key, index)
+    unsigned long long list[2][kList];  // value key << 32 | index; turn by turn: a CTA may be at the next search while another still reads
+    unsigned long long tmp[kList];
     uint32_t cnt[2][kCluster];
     unsigned long long xch[2][kCluster][kBins];
     double W[kBins];                 // weight of a bin's upper end, per unit
@@ -68,6 +67,7 @@ struct Smem {
     uint32_t nloc, lcnt;
     int hit;
     float thr;
+    alignas(16) float row[4];        // (HELD) the CTA's elements, as many as there are; -inf up to a multiple of a block
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -79,78 +79,91 @@ __device__ __forceinline__ void red_add(uint32_t a, uint32_t v) { asm volatile("
 
 struct Row {  // what a thread needs to know about the row
     float m, inv_T2, inv_Tl2;  // maximum; 2 / T (bins of half a unit), log2(e) / T
-    // 2^23 + bin, as the bits of a float (monotone in x, like every step of it)
+    // 2^23 + bin, as the bits of a float (monotone in x, like every step of it; NaN lands in the last bin)
     __device__ __forceinline__ uint32_t bin_bits(float x) const {
         return __float_as_uint(fminf((m - x) * inv_T2, (float)(kBins - 1)) + 8388608.f);
     }
     __device__ __forceinline__ int bin(float x) const { return (int)(bin_bits(x) & (kBins - 1)); }
-    // 2^23 + weight of x in units of 2^-23 of that of its bin's upper end X, on top of the bits of 1.0 (x - X is exact but
-    // where it does not matter; it is above 0 by a rounding at most)
-    __device__ __forceinline__ uint32_t unit_bits(float x, float X) const {
-        return __float_as_uint(ex2(fminf((x - X) * inv_Tl2, 0.f)) + 1.f);
+    // weight of x in units of 2^-23 of that of its bin's upper end X (x - X is exact but where it does not matter; it is
+    // above 0 by a rounding at most)
+    __device__ __forceinline__ uint32_t units(float x, float X) const {
+        return __float_as_uint(ex2(fminf((x - X) * inv_Tl2, 0.f)) + 1.f) - 0x3f800000u;
     }
-    __device__ __forceinline__ uint32_t units(float x, float X) const { return unit_bits(x, X) - 0x3f800000u; }
 };
 
-template <bool VEC>
-struct Slice {  // this thread's elements of the row
+// This thread's elements of the row.  HELD: the CTA keeps them in shared memory; otherwise every pass reads them again
+// (from L2).  VEC: 16-byte loads.  Elements that do not exist are -inf.
+template <bool HELD, bool VEC>
+struct Slice {
     const float* row;  // the CTA's first element
+    float* held;       // their copy
     int base, n;       // its index in the row; elements of the CTA
-    float x[kRegs];
 
-    __device__ __forceinline__ int local(int j) const {
-        return VEC ? (j >> 2) * (4 * kThreads) + 4 * (int)threadIdx.x + (j & 3) : j * kThreads + (int)threadIdx.x;
+    static __device__ __forceinline__ int place(int e) {  // of a block's element, after the block's first one of thread 0
+        return (e >> 2) * (4 * kThreads) + 4 * (int)threadIdx.x + (e & 3);
     }
-    __device__ __forceinline__ void load() {
+    __device__ __forceinline__ void load(float (&v)[kBlock], int i0) const {
 #pragma unroll
-        for (int j = 0; j < kRegs; j += VEC ? 4 : 1) {
-            const int i = local(j);
-            if constexpr (VEC) {
-                float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-                if (i + 3 < n) v = __ldcs(reinterpret_cast<const float4*>(row + i));
-                else {
-                    if (i < n) v.x = row[i];
-                    if (i + 1 < n) v.y = row[i + 1];
-                    if (i + 2 < n) v.z = row[i + 2];
-                }
-                x[j] = v.x; x[j + 1] = v.y; x[j + 2] = v.z; x[j + 3] = v.w;
-            } else {
-                x[j] = i < n ? __ldcs(row + i) : -INFINITY;
+        for (int e = 0; e < kBlock; e += 4) {
+            const int i = i0 + place(e);
+            float4 w = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            if (VEC && i + 3 < n) w = *reinterpret_cast<const float4*>(row + i);
+            else if (i < n) {
+                w.x = row[i];
+                if (i + 1 < n) w.y = row[i + 1];
+                if (i + 2 < n) w.z = row[i + 2];
+                if (i + 3 < n) w.w = row[i + 3];
+            }
+            v[e] = w.x; v[e + 1] = w.y; v[e + 2] = w.z; v[e + 3] = w.w;
+        }
+    }
+    // The first pass: f(block) of every block, which are kept (HELD).
+    template <typename F>
+    __device__ __forceinline__ void first(F f) const {
+        for (int i0 = 0; i0 < n; i0 += 2 * kBlock * kThreads) {
+            float v[2][kBlock];
+            load(v[0], i0);
+            load(v[1], i0 + kBlock * kThreads);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                f(v[q]);
+                if (HELD && i0 + q * kBlock * kThreads < n)
+#pragma unroll
+                    for (int e = 0; e < kBlock; e += 4)
+                        *reinterpret_cast<float4*>(held + i0 + q * kBlock * kThreads + place(e)) = make_float4(v[q][e], v[q][e + 1], v[q][e + 2], v[q][e + 3]);
             }
         }
-#pragma unroll
-        for (int j = 0; j < kRegs; ++j) x[j] = clean(x[j]);
     }
-    // elements beyond the registers (rows of more than 131072): f(value, index in the row)
+    // f(block, index in the row of its place 0), for every block of the CTA
     template <typename F>
-    __device__ __forceinline__ void rest(bool infinite, F f) const {
-        for (int i = kRegs * kThreads + (int)threadIdx.x; i < n; i += kThreads) {
-            float v = clean(row[i]);
-            if (infinite) v = v == INFINITY ? 0.f : -INFINITY;
-            f(v, base + i);
+    __device__ __forceinline__ void blocks(F f) const {
+        for (int i0 = 0; i0 < n; i0 += kBlock * kThreads) {
+            float v[kBlock];
+            if constexpr (HELD) {
+#pragma unroll
+                for (int e = 0; e < kBlock; e += 4) {
+                    const float4 w = *reinterpret_cast<const float4*>(held + i0 + place(e));
+                    v[e] = w.x; v[e + 1] = w.y; v[e + 2] = w.z; v[e + 3] = w.w;
+                }
+            } else {
+                load(v, i0);
+            }
+            f(v, base + i0);
         }
     }
-    // f(value, index in the row); values are clean, elements that do not exist are -inf
+    // f(value, index in the row) of every element, one by one: for what is done seldom
     template <typename F>
-    __device__ __forceinline__ void each(bool infinite, F f) const {
-#pragma unroll
-        for (int j = 0; j < kRegs; ++j) f(x[j], base + local(j));
-        rest(infinite, f);
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll 4
+        for (int i = (int)threadIdx.x; i < n; i += kThreads) f(HELD ? held[i] : row[i], base + i);
     }
 };
 
-__device__ __forceinline__ double warp_scan(double run, int lane) {
+template <typename T>
+__device__ __forceinline__ T warp_scan(T run, int lane) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const double v = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += v;
-    }
-    return run;
-}
-__device__ __forceinline__ uint32_t warp_scan(uint32_t run, int lane) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t v = __shfl_up_sync(0xffffffffu, run, o);
+        const T v = __shfl_up_sync(0xffffffffu, run, o);
         if (lane >= o) run += v;
     }
     return run;
@@ -158,8 +171,8 @@ __device__ __forceinline__ uint32_t warp_scan(uint32_t run, int lane) {
 
 // grid B * C in clusters of C; one cluster per row.  Every decision is taken by every warp of every CTA from the same
 // numbers, so the cluster stays together without anyone telling the others.
-template <bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
+template <bool HELD, bool VEC>
+__global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
     const Stamp stamp_guard(p.stamp);
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem& s = *reinterpret_cast<Smem*>(smem_raw);
@@ -173,12 +186,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     cluster.barrier_arrive();  // (waited for before the first access to another CTA's shared memory)
     pdl_trigger();
     pdl_wait();
-    Slice<VEC> el;
+    Slice<HELD, VEC> el;
     const int chunk = ((p.V + C - 1) / C + 3) / 4 * 4;
     el.base = rank * chunk;
     el.n = max(0, min(chunk, p.V - el.base));
     el.row = p.logits + (int64_t)b * p.ld + el.base;
-    el.load();
+    el.held = s.row;
     const float T0 = p.temperature ? p.temperature[b] : 1.f, mp0 = p.min_p ? p.min_p[b] : 0.f;
     const double T = fmax((double)T0, 1e-37), inv_T = 1.0 / T;
     // a weight is at least min_p when the logit is at most this far (negative) from the maximum
@@ -198,42 +211,39 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         return __reduce_min_sync(0xffffffffu, lane < C ? s.key[slot][lane] : 0xffffffffu);
     };
 
-    // ---- maximum
+    // ---- maximum (fmaxf passes NaN over)
     float mx = -INFINITY;
-    el.each(false, [&](float x, int) { mx = fmaxf(mx, x); });
+    el.first([&](const float (&v)[kBlock]) {
+#pragma unroll
+        for (int e = 0; e < kBlock; ++e) mx = fmaxf(mx, v[e]);
+    });
     cluster.barrier_wait();
     mx = value_of(cluster_min(key_of(mx), 0));
     if (rank == 0 && tid == 0 && p.pos) p.pos[b] += 1;
     if (mx == -INFINITY || !(T0 > 0.f)) {  // nothing to choose from, or greedy: the first of the largest
-        int at = 0x7fffffff;
+        int at = -1;
         if (mx > -INFINITY) {
-            el.each(false, [&](float x, int i) { at = x == mx ? min(at, i) : at; });
+            at = 0x7fffffff;
+            el.each([&](float x, int i) { at = x == mx ? min(at, i) : at; });
             at = (int)cluster_min((uint32_t)at, 1);
-        } else {
-            at = -1;
         }
         if (rank == 0 && tid == 0) p.tokens[b] = at;
         return;  // (nothing of another CTA's shared memory is touched after a sync)
     }
+    // (infinities share all the weight and are the only candidates: all in the last bin, units() is 1 there)
     const bool infinite = mx == INFINITY;
-    if (infinite) {  // infinities share all the weight: they become the only candidates
-#pragma unroll
-        for (int j = 0; j < kRegs; ++j) el.x[j] = el.x[j] == INFINITY ? 0.f : -INFINITY;
-        mx = 0.f;
-    }
     const double m = (double)mx;
     Row r;
     r.m = mx;
     r.inv_T2 = (float)(2.0 * inv_T);
     r.inv_Tl2 = (float)(1.4426950408889634 * inv_T);
     {
-        // two lanes' columns of a bin's upper end per thread; its weight once
-        const int bin = tid >> 4;
-        const float X = T > 1e300 ? mx : (float)fmin(fmax(m - 0.5 * (bin - 0.5) * T, -(double)FLT_MAX), (double)FLT_MAX);
-        s.X[bin][2 * (tid & 15)] = X;
-        s.X[bin][2 * (tid & 15) + 1] = X;
-        if ((tid & 15) == 0) s.W[bin] = kUnit * exp(((double)X - m) * inv_T);
-        if (tid == 0) s.thr = fmaxf(__double2float_ru(m + thr), -FLT_MAX) + 0.f;
+        // a lane's column of a bin's upper end per thread; its weight once
+        const int bin = warp;
+        const float X = T > 1e300 || infinite ? mx : (float)fmin(fmax(m - 0.5 * (bin - 0.5) * T, -(double)FLT_MAX), (double)FLT_MAX);
+        s.X[bin][lane] = X;
+        if (lane == 0) s.W[bin] = infinite ? kUnit : kUnit * exp(((double)X - m) * inv_T);
+        if (tid == 0) s.thr = infinite ? mx : fmaxf(__double2float_ru(m + thr), -FLT_MAX);
     }
     __syncthreads();
     // the kept prefix: elements above lim_x, and those equal to it with an index up to lim_i
@@ -249,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
 #pragma unroll
         for (int q = 0; q < kBins / kWarps; ++q) {
             const int bin = warp * (kBins / kWarps) + q;
-            uint32_t lo = 0, hi = 0;  // (two warps' sums of a lane have 31 bits at most)
+            uint32_t lo = 0, hi = 0;  // (a lane's sum has 32 bits)
 #pragma unroll
             for (int w = 0; w < kSlices; ++w) {
                 const uint32_t v = s.hist[w][bin][lane];
@@ -268,37 +278,51 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         par ^= 1;
         return t;
     };
-    auto largest_part = [&](int bin) {  // of the totals just taken, the largest CTA's share of a bin
-        unsigned long long v = 0;
-        for (int c = 0; c < C; ++c) v = max(v, s.xch[par ^ 1][c][bin]);
-        return (double)v;
+    // Of the totals just taken, the largest CTA's share of a bin.
+    auto largest_part = [&](int bin) {
+        unsigned long long most = 0;
+        for (int c = 0; c < C; ++c) most = max(most, s.xch[par ^ 1][c][bin]);
+        return (double)most;
     };
     const uint32_t my_hist = (uint32_t)__cvta_generic_to_shared(&s.hist[warp % kSlices][0][lane]);  // + bin * 128
     const uint32_t hist_a = my_hist - 0x4b000000u * 128u;                                              // + bin_bits * 128
     const char* const X_a = reinterpret_cast<const char*>(&s.X[0][lane]);
 
+    // A range of elements: values ka..kb (as keys, so descending), indices ia..ib once ka = kb.
+    struct Range { uint32_t ka, kb; int ia, ib; };
+    Range have{1, 0, 0, -1};  // what s.loc holds (nothing); from the largest value on: all that can be asked for
+    bool have_all = false;
+
     // The bins of the whole row up to the limit.  Elements beyond it add nothing: no branches.
     auto level0 = [&](bool mass) {
-        if (mass)
-            el.each(infinite, [&](float x, int i) {
-                const uint32_t o = r.bin_bits(x) * 128u;
-                uint32_t u = r.units(x, *reinterpret_cast<const float*>(X_a + (o & (kBins * 128u - 1u))));
-                if (!(x >= lim_x)) u = 0;
-                if (lim_i != kAll && x == lim_x && i > lim_i) u = 0;
-                red_add(hist_a + o, u);
+        if (have_all) {
+            const uint32_t lk = key_of(lim_x);
+            for (uint32_t e = tid; e < s.nloc; e += kThreads) {
+                const uint2 v = s.loc[e];
+                const float x = value_of(v.x);
+                if (v.x < lk || (v.x == lk && (int)v.y <= lim_i)) red_add(my_hist + r.bin(x) * 128u, r.units(x, s.X[r.bin(x)][lane]));
+            }
+        } else if (mass) {
+            el.blocks([&](const float (&v)[kBlock], int at) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < kBlock; ++e) {
+                    const float x = v[e];
+                    const uint32_t o = r.bin_bits(x) * 128u;
+                    uint32_t u = r.units(x, *reinterpret_cast<const float*>(X_a + (o & (kBins * 128u - 1u))));
+                    if (!(x >= lim_x)) u = 0;
+                    if (lim_i != kAll && x == lim_x && at + el.place(e) > lim_i) u = 0;
+                    red_add(hist_a + o, u);
+                }
             });
-        else
-            el.each(infinite, [&](float x, int) {  // (top-k comes first: no limit by index yet)
-                red_add(hist_a + r.bin_bits(x) * 128u, x >= lim_x ? 1u : 0u);
+        } else {
+            el.blocks([&](const float (&v)[kBlock], int) __attribute__((always_inline)) {  // (top-k comes first: no limit by index yet)
+#pragma unroll
+                for (int e = 0; e < kBlock; ++e) red_add(hist_a + r.bin_bits(v[e]) * 128u, v[e] >= lim_x ? 1u : 0u);
             });
+        }
         return totals();
     };
 
-    // A range of elements: values ka..kb (as keys, so descending), indices ia..ib once ka = kb.
-    struct Range { uint32_t ka, kb; int ia, ib; };
-    auto inside = [&](float x, int i, const Range& g) {  // (of an element whose value is in the range)
-        return (x != lim_x || i <= lim_i) && i >= g.ia && i <= g.ib;
-    };
     // The smallest key whose bin is at least j.  It lies next to that of the bin's upper end: 32 probes around it nearly
     // always hold it; if not (values near zero have finer keys), the whole range is searched, 32 probes a round.
     auto first_key = [&](int j) -> uint32_t {
@@ -306,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         if (j <= 0) return k0;
         if (j >= kBins) return k1;
         {
-            const uint32_t mid = key_of(s.X[j][0] + 0.f), a = mid > k0 + 16 ? mid - 16 : k0, at = a + lane;
+            const uint32_t mid = key_of(s.X[j][0]), a = mid > k0 + 16 ? mid - 16 : k0, at = a + lane;
             const unsigned ok = __ballot_sync(0xffffffffu, at >= k1 || r.bin(value_of(at)) >= j);
             if (ok && (!(ok & 1u) || a == k0)) return a + __ffs(ok) - 1;
         }
@@ -324,6 +348,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         return a;
     };
     auto range_of_bin = [&](int j) {
+        if (infinite) return Range{key_of(mx), key_of(mx), 0, kAll};
         const uint32_t a = first_key(j), e = first_key(j + 1);
         return Range{a, max(a, min(e - 1, key_of(lim_x))), 0, kAll};
     };
@@ -333,76 +358,68 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         const float xa = value_of(g.ka), xb = value_of(g.kb);
         if (tid == 0) s.nloc = 0;
         __syncthreads();
-        uint32_t mask = 0;
+        auto inside = [&](float x, int i) { return (x != lim_x || i <= lim_i) && i >= g.ia && i <= g.ib; };
+        const bool by_index = lim_i != kAll || g.ia > 0 || g.ib != kAll;
+        el.blocks([&](const float (&v)[kBlock], int first) __attribute__((always_inline)) {
+            uint32_t mask = 0;
 #pragma unroll
-        for (int j = 0; j < kRegs; ++j) mask |= (el.x[j] <= xa && el.x[j] >= xb) ? 1u << j : 0u;
-        if (lim_i != kAll || g.ia > 0 || g.ib != kAll) {
+            for (int e = 0; e < kBlock; ++e) mask |= (v[e] <= xa && v[e] >= xb) ? 1u << e : 0u;
+            if (by_index) {
 #pragma unroll
-            for (int j = 0; j < kRegs; ++j)
-                if (!inside(el.x[j], el.base + el.local(j), g)) mask &= ~(1u << j);
-        }
-        const uint32_t cnt = __popc(mask), upto = warp_scan(cnt, lane);
-        uint32_t at = 0;
-        if (lane == 31 && upto) at = atomicAdd(&s.nloc, upto);
-        at = __shfl_sync(0xffffffffu, at, 31) + upto - cnt;
-        if (__any_sync(0xffffffffu, mask != 0)) {
-#pragma unroll
-            for (int j = 0; j < kRegs; ++j)
-                if (mask & (1u << j)) {
-                    if (at < kLocal) s.loc[at] = make_uint2(__float_as_uint(el.x[j]), (uint32_t)(el.base + el.local(j)));
-                    ++at;
-                }
-        }
-        el.rest(infinite, [&](float x, int i) {
-            if (x <= xa && x >= xb && inside(x, i, g)) {
-                const uint32_t q = atomicAdd(&s.nloc, 1u);
-                if (q < kLocal) s.loc[q] = make_uint2(__float_as_uint(x), (uint32_t)i);
+                for (int e = 0; e < kBlock; ++e)
+                    if (!inside(v[e], first + el.place(e))) mask &= ~(1u << e);
+            }
+            if (!__any_sync(0xffffffffu, mask != 0)) return;
+            const uint32_t cnt = __popc(mask), upto = warp_scan(cnt, lane);
+            uint32_t at = 0;
+            if (lane == 31) at = atomicAdd(&s.nloc, upto);
+            at = __shfl_sync(0xffffffffu, at, 31) + upto - cnt;
+            for (; mask; mask &= mask - 1, ++at) {  // (few: read them once more instead of asking for each of the block)
+                const int i = first + el.place(__ffs(mask) - 1);
+                if (at < kLocal) s.loc[at] = make_uint2(key_of(HELD ? el.held[i - el.base] : el.row[i - el.base]), (uint32_t)i);
             }
         });
         __syncthreads();
+        if (tid == 0) s.nloc = min(s.nloc, (uint32_t)kLocal);
+        __syncthreads();
+        have = g;
     };
-    auto local_inside = [&](const uint2& v, const Range& g, uint32_t& k, int& i) {
-        k = key_of(__uint_as_float(v.x));
-        i = (int)v.y;
-        return k >= g.ka && k <= g.kb && i >= g.ia && i <= g.ib;
-    };
-    // Counts the elements of a range (the weights of the open last bin say nothing about that).
-    auto tally = [&](const Range& g, bool local, double& tot, double& part) {
-        uint32_t n = 0, k;
-        int i;
+    // f(key, index) of this CTA's elements of a range, from s.loc or from the row
+    auto visit = [&](const Range& g, bool local, auto f) {
         if (local) {
-            for (uint32_t e = tid; e < min(s.nloc, (uint32_t)kLocal); e += kThreads) n += local_inside(s.loc[e], g, k, i);
+            for (uint32_t e = tid; e < s.nloc; e += kThreads) {
+                const uint2 v = s.loc[e];
+                if (v.x >= g.ka && v.x <= g.kb && (int)v.y >= g.ia && (int)v.y <= g.ib) f(v.x, (int)v.y);
+            }
         } else {
-            const float xa = value_of(g.ka), xb = value_of(g.kb);
-            el.each(infinite, [&](float x, int i) { n += x <= xa && x >= xb && inside(x, i, g); });
+            el.each([&](float x, int i) {
+                const uint32_t k = key_of(x);
+                if (x == x && k >= g.ka && k <= g.kb && (x != lim_x || i <= lim_i) && i >= g.ia && i <= g.ib) f(k, i);
+            });
         }
-        red_add(my_hist, n);
-        const unsigned long long t = totals();
-        tot = (double)__shfl_sync(0xffffffffu, t, 0);
-        part = largest_part(0);
     };
-    // Brings the local elements of a range together in every CTA: CTA c's go to slots 64 c .. (the caller knows that no
-    // CTA has more).
+    // Brings the local elements of a range together in every CTA: CTA c's go to slots c * kList / C .. (the caller knows
+    // that no CTA has more).
+    const int slot = kList / C;
     auto gather = [&](const Range& g) {
         if (tid == 0) s.lcnt = 0;
         __syncthreads();
-        const uint32_t nloc = min(s.nloc, (uint32_t)kLocal);
+        const uint32_t nloc = s.nloc;
         for (uint32_t e0 = warp * 32; e0 < nloc; e0 += kThreads) {
             const uint32_t e = e0 + lane;
-            uint32_t k = 0;
-            int i = 0;
-            const bool in = e < nloc && local_inside(s.loc[e], g, k, i);
+            const uint2 v = s.loc[min(e, nloc - 1)];
+            const bool in = e < nloc && v.x >= g.ka && v.x <= g.kb && (int)v.y >= g.ia && (int)v.y <= g.ib;
             const unsigned who = __ballot_sync(0xffffffffu, in);
             if (!who) continue;
             uint32_t at = 0;
             if (lane == 0) at = atomicAdd(&s.lcnt, (uint32_t)__popc(who));
             at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
-            if (in && at < kSlot) s.tmp[at] = ((unsigned long long)k << 32) | (uint32_t)i;
+            if (in && at < slot) s.tmp[at] = ((unsigned long long)v.x << 32) | v.y;
         }
         __syncthreads();
-        const uint32_t n = min(s.lcnt, (uint32_t)kSlot), c = tid / kSlot, e = tid % kSlot;
-        if (c < C) {
-            if (e < n) cluster.map_shared_rank(&s.list[turn][0], c)[rank * kSlot + e] = s.tmp[e];
+        const uint32_t n = min(s.lcnt, (uint32_t)slot), c = tid / slot, e = tid % slot;
+        if (tid < kList) {
+            if (e < n) cluster.map_shared_rank(&s.list[turn][0], c)[rank * slot + e] = s.tmp[e];
             if (e == 0) cluster.map_shared_rank(&s.cnt[turn][0], c)[rank] = n;
         }
         cluster.sync();
@@ -413,27 +430,39 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     };
     // The collected elements in order, element e in thread e: each counts those before it.
     auto sorted = [&](int n) {
-        const unsigned long long* list = s.list[turn ^ 1];
-        const uint32_t* cnt = s.cnt[turn ^ 1];
-        const int c0 = tid / kSlot;
-        const bool mine = c0 < C && (uint32_t)(tid % kSlot) < cnt[c0];
-        if (__any_sync(0xffffffffu, mine)) {
-            const unsigned long long k = mine ? list[tid] : ~0ull;
+        unsigned long long* const list = s.list[turn ^ 1];
+        const int c0 = tid / slot, e0 = tid % slot;
+        if (tid < kList && (uint32_t)e0 < s.cnt[turn ^ 1][c0]) {  // side by side, and full to a multiple of 8
+            int to = e0;
+            for (int c = 0; c < c0; ++c) to += (int)s.cnt[turn ^ 1][c];
+            s.tmp[to] = list[tid];
+        }
+        const int n8 = (n + 7) / 8 * 8;
+        if (tid >= n && tid < n8) s.tmp[tid] = ~0ull;
+        __syncthreads();
+        // the comparisons of an element are shared by as many neighbouring threads as there are to spare
+        int P = 32;
+        while (P > 1 && P * n > kThreads) P >>= 1;
+        const int e = tid / P;
+        if (warp * 32 < P * n) {
+            const unsigned long long k = e < n ? s.tmp[e] : ~0ull;
             int before = 0;
-            for (int c = 0; c < C; ++c) {
-                const int m = (int)cnt[c];
-                const unsigned long long* l = list + c * kSlot;
-#pragma unroll 8
-                for (int e = 0; e < m; ++e) before += l[e] < k;
+            for (int q = 8 * (tid % P); q < n8; q += 8 * P) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const ulonglong2 v = reinterpret_cast<const ulonglong2*>(s.tmp + q)[i];
+                    before += (v.x < k) + (v.y < k);
+                }
             }
-            if (mine) s.tmp[before] = k;
+            for (int o = 1; o < P; o <<= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+            if (e < n && tid % P == 0) list[before] = k;
         }
         __syncthreads();
-        return tid < n ? s.tmp[tid] : ~0ull;
+        return tid < n ? list[tid] : ~0ull;
     };
     // Running sum of the elements' weights, on top of `before`.
-    auto summed = [&](int n, unsigned long long k, double before, double& w) {
-        w = 0.0;
+    auto summed = [&](int n, unsigned long long k, double before) {
+        double w = 0.0;
         if (tid < n) {
             const float x = value_of((uint32_t)(k >> 32));
             const int bin = r.bin(x);
@@ -463,143 +492,140 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     const float tp0 = p.top_p ? p.top_p[b] : 1.f;
     const bool nucleus = tp0 < 1.f;
     const double tp = (double)fmaxf(tp0, 0.f);
+    const int k = p.top_k ? p.top_k[b] : 0;
 
-    // Narrows a range of bin j around the target until its elements can be collected; `before` is the running sum in front of
-    // it, tot and part about how many elements the cluster and the fullest CTA have in it.  Returns the number collected.
-    auto narrow = [&](Range g, int j, bool by_rank, double target, bool strict, double& before, double tot, double part) {
-        bool local = false;
-        const bool open = !by_rank && j == kBins - 1;  // (weights there may be anything down to 0)
+    // Three searches at most: the k-th candidate, the border of the nucleus, the drawn token.
+    unsigned long long t = 0;      // weight (candidates) of bin `lane`
+    double w0 = 0.0, run0 = 0.0;   // of the same bin, and of all up to it
+    float most = 0.f, most_upto = 0.f;   // of the same two, the largest CTA's share (in units, about)
+    double Z = 0.0;                // weight of what is kept
+    bool weighed = false;
+    for (int stage = k > 0 && k < p.V ? 0 : 1; stage < 3; ++stage) {
+        if (stage == 1 && !nucleus) continue;
+        const bool by_rank = stage == 0, strict = stage == 2;
+        if (!weighed) {
+            t = level0(!by_rank);
+            w0 = by_rank ? (double)t : s.W[lane] * (double)t;
+            run0 = warp_scan(w0, lane);
+            Z = __shfl_sync(0xffffffffu, run0, 31);
+            weighed = !by_rank;
+            most = most_upto = 0.f;
+#pragma unroll
+            for (int c = 0; c < kCluster; ++c) {
+                const float v = c < C ? (float)s.xch[par ^ 1][c][lane] : 0.f;
+                most = fmaxf(most, v);
+                most_upto = fmaxf(most_upto, warp_scan(v, lane));
+            }
+        }
+        if (by_rank && Z <= (double)k) continue;  // no more candidates than that
+        const double target = by_rank ? (double)k : (stage == 1 ? tp : u) * Z;
+        const double per = by_rank ? 1.0 : 1.7 * kUnit;  // elements per unit: a weight inside a bin is at least exp(-1/2)
+        // the bin that holds the target
+        const unsigned ok = __ballot_sync(0xffffffffu, t > 0 && (strict ? run0 > target : run0 >= target));
+        const unsigned any = __ballot_sync(0xffffffffu, t > 0);
+        const int j = ok ? __ffs(ok) - 1 : 31 - __clz(any | 1u);
+        double before = __shfl_sync(0xffffffffu, run0 - w0, j), tot = per * __shfl_sync(0xffffffffu, (double)t, j);
+        Range g = range_of_bin(j);
+        const bool open = !by_rank && j == kBins - 1;  // (weights in the last bin may be anything down to 0: they count nothing)
+        bool local = g.ka >= have.ka && g.kb <= have.kb && have.ia == 0 && have.ib == kAll;
+        double part = per * (double)__shfl_sync(0xffffffffu, most, j);
+        if (!local && !open) {
+            // everything from the top down if it fits: then the other searches find their elements there too
+            const double upto = per * (double)__shfl_sync(0xffffffffu, most_upto, j);
+            if (upto <= kLocal) {
+                compact(Range{key_of(r.m), g.kb, 0, kAll});
+                local = true;
+                have_all = by_rank;
+                if (by_rank && __shfl_sync(0xffffffffu, run0, j) <= kSorted && upto <= slot) {
+                    // few enough from the top down: all that is left to do happens in the list
+                    const int n = gather(have);
+                    const unsigned long long e = sorted(n);
+                    const double cum = summed(n, e, 0.0);
+                    int kept = min(k, n);
+                    if (tid == kept - 1) s.res.mass = cum;
+                    __syncthreads();
+                    Z = s.res.mass;
+                    if (nucleus) {
+                        kept = 1 + first_at(kept, e, cum, tp * Z, false);
+                        Z = s.res.mass;
+                    }
+                    first_at(kept, e, cum, u * Z, true);
+                    break;
+                }
+            }
+        }
+        // Narrow the range around the target until its elements can be collected.
+        int n = 0;
         for (int level = 0; level < 16; ++level) {
-            if (open) tally(g, local, tot, part);
+            if (open) {
+                uint32_t c = 0;
+                visit(g, local, [&](uint32_t, int) { ++c; });
+                red_add(my_hist, c);
+                const unsigned long long all = totals();
+                tot = (double)__shfl_sync(0xffffffffu, all, 0);
+                part = largest_part(0);
+            }
             if (!local && part <= kLocal) {
                 compact(g);
                 local = true;
             }
-            if (local && part <= kSlot && tot <= kSorted) return gather(g);
+            if (local && part <= slot && tot <= kSorted) {
+                n = gather(g);
+                break;
+            }
             // 32 parts of its values, or of its indices where there is only one value
             const bool by_value = g.ka != g.kb;
             if (!by_value && g.ib == kAll) g.ib = p.V - 1;
             const uint32_t lo = by_value ? g.ka : (uint32_t)g.ia, span = by_value ? g.kb - g.ka : (uint32_t)(g.ib - g.ia);
             const int sh = max(0, 32 - __clz(span) - 5);
             const float X = s.X[j][0];
-            if (local) {
-                for (uint32_t e = tid; e < min(s.nloc, (uint32_t)kLocal); e += kThreads) {
-                    uint32_t k;
-                    int i;
-                    if (local_inside(s.loc[e], g, k, i))
-                        red_add(my_hist + (((by_value ? k : (uint32_t)i) - lo) >> sh) * 128u, by_rank ? 1u : r.units(value_of(k), X));
-                }
-            } else {
-                const float xa = value_of(g.ka), xb = value_of(g.kb);
-                el.each(infinite, [&](float x, int i) {
-                    if (x <= xa && x >= xb)
-                        if (inside(x, i, g))
-                            red_add(my_hist + (((by_value ? key_of(x) : (uint32_t)i) - lo) >> sh) * 128u, by_rank ? 1u : r.units(x, X));
-                });
-            }
-            const unsigned long long t = totals();
-            const double w = by_rank ? (double)t : s.W[j] * (double)t, run = warp_scan(w, lane);
-            const unsigned ok = __ballot_sync(0xffffffffu, t > 0 && (strict ? before + run > target : before + run >= target));
-            const unsigned any = __ballot_sync(0xffffffffu, t > 0);
-            const int cut = ok ? __ffs(ok) - 1 : 31 - __clz(any | 1u);
+            visit(g, local, [&](uint32_t key, int i) {
+                red_add(my_hist + (((by_value ? key : (uint32_t)i) - lo) >> sh) * 128u, by_rank ? 1u : r.units(value_of(key), X));
+            });
+            const unsigned long long tt = totals();
+            const double w = by_rank ? (double)tt : s.W[j] * (double)tt, run = warp_scan(w, lane);
+            const unsigned yes = __ballot_sync(0xffffffffu, tt > 0 && (strict ? before + run > target : before + run >= target));
+            const unsigned some = __ballot_sync(0xffffffffu, tt > 0);
+            const int cut = yes ? __ffs(yes) - 1 : 31 - __clz(some | 1u);
             before += __shfl_sync(0xffffffffu, run - w, cut);
-            const double per = by_rank ? 1.0 : 1.7 * kUnit;  // elements per unit: a weight inside a bin is at least exp(-1/2)
-            tot = per * __shfl_sync(0xffffffffu, (double)t, cut);
+            tot = per * __shfl_sync(0xffffffffu, (double)tt, cut);
             part = per * largest_part(cut);
             const uint32_t a = lo + ((uint32_t)cut << sh), last = (uint32_t)min((unsigned long long)a + (1u << sh) - 1, (unsigned long long)lo + span);
             if (by_value) { g.ka = a; g.kb = last; }
             else { g.ia = (int)a; g.ib = (int)last; }
         }
-        return 0;  // (not reached: 52 bits of value and index, five a level)
-    };
-
-    // ---- top-k: the value and index of the last candidate it keeps
-    const int k = p.top_k ? p.top_k[b] : 0;
-    if (k > 0 && k < p.V) {
-        const unsigned long long t = level0(false);
-        const uint32_t run = warp_scan((uint32_t)t, lane);
-        const unsigned ok = __ballot_sync(0xffffffffu, run >= (uint32_t)k);
-        if (ok) {  // (else there are no more than k candidates)
-            const int j = __ffs(ok) - 1;
-            const uint32_t upto = __shfl_sync(0xffffffffu, run, j), in = __shfl_sync(0xffffffffu, (uint32_t)t, j);
-            Range g = range_of_bin(j);
-            uint32_t most = 0;  // elements of the fullest CTA up to this bin
-            for (int c = 0; c < C; ++c)
-                most = max(most, __reduce_add_sync(0xffffffffu, lane <= j ? (uint32_t)s.xch[par ^ 1][c][lane] : 0u));
-            if (upto <= kSorted && most <= kSlot) {  // few enough from the top down: the rest happens in the list
-                g.ka = key_of(r.m);
-                compact(g);
-                const int n = gather(g);
-                const unsigned long long e = sorted(n);
-                double w;
-                const double cum = summed(n, e, 0.0, w);
-                int kept = min(k, n);
-                if (tid == kept - 1) s.res.mass = cum;
-                __syncthreads();
-                double Z = s.res.mass;
-                if (nucleus) {
-                    kept = 1 + first_at(kept, e, cum, tp * Z, false);
-                    Z = s.res.mass;
-                }
-                first_at(kept, e, cum, u * Z, true);
-                if (rank == 0 && tid == 0) p.tokens[b] = s.res.i;
-                return;
-            }
-            double before = (double)(upto - in);
-            const double part = largest_part(j);
-            const int n = narrow(g, j, true, (double)k, false, before, (double)in, part);
-            const unsigned long long e = sorted(n);
+        const unsigned long long e = sorted(n);
+        if (by_rank) {
             if (tid == max(0, min(n, k - (int)before) - 1)) s.res = Result{value_of((uint32_t)(e >> 32)), (int)(uint32_t)e, 0.0};
             __syncthreads();
-            lim_x = s.res.x;
-            lim_i = s.res.i;
+        } else {
+            const double cum = summed(n, e, before);
+            first_at(n, e, cum, target, strict);
         }
-    }
-
-    // ---- weights of the bins; lane j: bin j
-    const unsigned long long t = level0(true);
-    const double w0 = s.W[lane] * (double)t, run0 = warp_scan(w0, lane);
-    const unsigned any0 = __ballot_sync(0xffffffffu, t > 0);
-    const int par0 = par ^ 1;
-    unsigned long long most = 0;  // the fullest CTA's share of bin `lane`
-    for (int c = 0; c < C; ++c) most = max(most, s.xch[par0][c][lane]);
-    double Z = __shfl_sync(0xffffffffu, run0, 31);
-    // Element at which the running sum reaches a target: its place and the sum go to s.res.
-    auto search = [&](double target, bool strict) {
-        const unsigned ok = __ballot_sync(0xffffffffu, t > 0 && (strict ? run0 > target : run0 >= target));
-        const int j = ok ? __ffs(ok) - 1 : 31 - __clz(any0 | 1u);
-        double before = __shfl_sync(0xffffffffu, run0 - w0, j);
-        const double tot = 1.7 * kUnit * (double)__shfl_sync(0xffffffffu, t, j), part = 1.7 * kUnit * (double)__shfl_sync(0xffffffffu, most, j);
-        const int n = narrow(range_of_bin(j), j, false, target, strict, before, tot, part);
-        const unsigned long long e = sorted(n);
-        double w;
-        const double cum = summed(n, e, before, w);
-        first_at(n, e, cum, target, strict);
-    };
-    if (nucleus) {
-        search(tp * Z, false);
         lim_x = s.res.x;
         lim_i = s.res.i;
-        Z = s.res.mass;
+        if (stage == 1) Z = s.res.mass;
     }
-    search(u * Z, true);
     if (rank == 0 && tid == 0) p.tokens[b] = s.res.i;
 }
 
 }  // namespace
 
 cudaError_t sample_launch(const SampleArgs& a, cudaStream_t st, bool pdl) {
-    // as many CTAs as hold the row in registers (a power of two, eight at most)
+    // as many CTAs per row as hold it in shared memory (a power of two, eight at most: 262144 elements)
     int C = 1;
-    while (C < kCluster && (int64_t)C * kThreads * kRegs < a.V) C *= 2;
+    while (C < kCluster && (int64_t)C * kHeld < a.V) C *= 2;
+    const bool held = (int64_t)C * kHeld >= a.V;
+    const int chunk = ((a.V + C - 1) / C + 3) / 4 * 4, block = kBlock * kThreads;
+    const size_t smem = sizeof(Smem) + (held ? (size_t)(chunk + block - 1) / block * block * 4 : 0);
     const bool vec = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && (a.B == 1 || a.ld % 4 == 0);
-    auto kern = vec ? sample_rows<true> : sample_rows<false>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem));
+    auto kern = held ? (vec ? sample_rows<true, true> : sample_rows<true, false>) : (vec ? sample_rows<false, true> : sample_rows<false, false>);
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(a.B * C);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sizeof(Smem);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
