@@ -52,9 +52,18 @@ struct Result {  // the last element of a kept prefix, and the prefix's weight
     double mass;
 };
 
+// A range of elements: values ka..kb (as keys, so descending), indices ia..ib once ka = kb.
+struct Range { uint32_t ka, kb; int ia, ib; };
+struct Search {  // what the first warp has found out, for all
+    double target, before;  // the sum that is looked for; the sum in front of the range
+    float tot, part, upto;  // about how many elements the range has in the cluster and in its fullest CTA; in that, with all before it
+    Range g;
+    int j;                  // the range's bin, -1: nothing to search for
+    int all;                // (by rank) elements up to the bin's end
+};
+
 struct Smem {
     uint32_t hist[kSlices][kBins][32];
-    float X[kBins][32];              // a bin's upper end, once per lane: the same offset as in a histogram
     uint2 loc[kLocal];               // this CTA's elements of the range that was copied last, (value key, index)
     unsigned long long list[2][kList];  // value key << 32 | index; turn by turn: a CTA may be at the next search while another still reads
     unsigned long long tmp[kList];
@@ -63,6 +72,7 @@ struct Smem {
     double W[kBins];                 // weight of a bin's upper end, per unit
     double scan[kWarps];
     Result res;
+    Search at;
     uint32_t key[2][kCluster], key_w[kWarps];
     uint32_t nloc, lcnt;
     int hit;
@@ -79,11 +89,11 @@ __device__ __forceinline__ void red_add(uint32_t a, uint32_t v) { asm volatile("
 
 struct Row {  // what a thread needs to know about the row
     float m, inv_T2, inv_Tl2;  // maximum; 2 / T (bins of half a unit), log2(e) / T
-    // 2^23 + bin, as the bits of a float (monotone in x, like every step of it; NaN lands in the last bin)
-    __device__ __forceinline__ uint32_t bin_bits(float x) const {
-        return __float_as_uint(fminf((m - x) * inv_T2, (float)(kBins - 1)) + 8388608.f);
-    }
-    __device__ __forceinline__ int bin(float x) const { return (int)(bin_bits(x) & (kBins - 1)); }
+    float half_T, top;         // T / 2; upper end of the first bin, m + T / 4
+    // 2^23 + bin, as a float (monotone in x, like every step of it; NaN lands in the last bin)
+    __device__ __forceinline__ float bin_number(float x) const { return fminf((m - x) * inv_T2, (float)(kBins - 1)) + 8388608.f; }
+    __device__ __forceinline__ int bin(float x) const { return (int)(__float_as_uint(bin_number(x)) & (kBins - 1)); }
+    __device__ __forceinline__ float end_of(float bin) const { return fmaf(-bin, half_T, top); }  // a bin's upper end
     // weight of x in units of 2^-23 of that of its bin's upper end X (x - X is exact but where it does not matter; it is
     // above 0 by a rounding at most)
     __device__ __forceinline__ uint32_t units(float x, float X) const {
@@ -193,10 +203,12 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
     el.row = p.logits + (int64_t)b * p.ld + el.base;
     el.held = s.row;
     const float T0 = p.temperature ? p.temperature[b] : 1.f, mp0 = p.min_p ? p.min_p[b] : 0.f;
-    const double T = fmax((double)T0, 1e-37), inv_T = 1.0 / T;
+    // (from 1e30 on a temperature makes all weights equal, as far as logits go)
+    const bool flat = T0 >= 1e30f;
+    const double T = fmax((double)T0, 1e-37), inv_T = flat ? 0.0 : 1.0 / T;
     // a weight is at least min_p when the logit is at most this far (negative) from the maximum
     double thr = -INFINITY;
-    if (tid == 0 && mp0 > 0.f && T < 1e300) thr = T * log(fmin((double)mp0, 1.0));
+    if (tid == 0 && mp0 > 0.f && !flat) thr = T * log(fmin((double)mp0, 1.0));
 
     // the smallest of one 32-bit word per thread, over the cluster
     auto cluster_min = [&](uint32_t v, int slot) {
@@ -237,14 +249,10 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
     r.m = mx;
     r.inv_T2 = (float)(2.0 * inv_T);
     r.inv_Tl2 = (float)(1.4426950408889634 * inv_T);
-    {
-        // a lane's column of a bin's upper end per thread; its weight once
-        const int bin = warp;
-        const float X = T > 1e300 || infinite ? mx : (float)fmin(fmax(m - 0.5 * (bin - 0.5) * T, -(double)FLT_MAX), (double)FLT_MAX);
-        s.X[bin][lane] = X;
-        if (lane == 0) s.W[bin] = infinite ? kUnit : kUnit * exp(((double)X - m) * inv_T);
-        if (tid == 0) s.thr = infinite ? mx : fmaxf(__double2float_ru(m + thr), -FLT_MAX);
-    }
+    r.half_T = flat ? 0.f : (float)(0.5 * T);
+    r.top = flat ? mx : (float)(m + 0.25 * T);
+    if (tid < kBins) s.W[tid] = infinite ? kUnit : kUnit * exp(((double)r.end_of((float)tid) - m) * inv_T);
+    if (tid == 0) s.thr = infinite ? mx : fmaxf(__double2float_ru(m + thr), -FLT_MAX);
     __syncthreads();
     // the kept prefix: elements above lim_x, and those equal to it with an index up to lim_i
     constexpr int kAll = 0x7fffffff;
@@ -252,8 +260,8 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
     int lim_i = kAll;
     int par = 0, turn = 0;
 
-    // Adds one lane-private histogram up over the cluster: every warp of every CTA gets the total of bin `lane`; the CTAs' parts
-    // stay in s.xch[par ^ 1] until the next but one.
+    // Adds the lane-private histograms up over the cluster: the CTAs' totals of bin `lane` are in s.xch[par ^ 1][CTA][lane],
+    // until the next but one.
     auto totals = [&]() {
         __syncthreads();
 #pragma unroll
@@ -273,23 +281,21 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
                 cluster.map_shared_rank(&s.xch[par][0][0], lane)[rank * kBins + bin] = ((unsigned long long)hi << 16) + lo;
         }
         cluster.sync();
-        unsigned long long t = 0;
-        for (int c = 0; c < C; ++c) t += s.xch[par][c][lane];
         par ^= 1;
+    };
+    auto total = [&](float& most) {  // (first warp) of bin `lane`: the total, and the largest CTA's share
+        unsigned long long t = 0;
+        most = 0.f;
+        for (int c = 0; c < C; ++c) {
+            const unsigned long long v = s.xch[par ^ 1][c][lane];
+            t += v;
+            most = fmaxf(most, (float)v);
+        }
         return t;
     };
-    // Of the totals just taken, the largest CTA's share of a bin.
-    auto largest_part = [&](int bin) {
-        unsigned long long most = 0;
-        for (int c = 0; c < C; ++c) most = max(most, s.xch[par ^ 1][c][bin]);
-        return (double)most;
-    };
     const uint32_t my_hist = (uint32_t)__cvta_generic_to_shared(&s.hist[warp % kSlices][0][lane]);  // + bin * 128
-    const uint32_t hist_a = my_hist - 0x4b000000u * 128u;                                              // + bin_bits * 128
-    const char* const X_a = reinterpret_cast<const char*>(&s.X[0][lane]);
+    const uint32_t hist_a = my_hist - 0x4b000000u * 128u;                                           // + the bits of bin_number * 128
 
-    // A range of elements: values ka..kb (as keys, so descending), indices ia..ib once ka = kb.
-    struct Range { uint32_t ka, kb; int ia, ib; };
     Range have{1, 0, 0, -1};  // what s.loc holds (nothing); from the largest value on: all that can be asked for
     bool have_all = false;
 
@@ -300,27 +306,31 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
             for (uint32_t e = tid; e < s.nloc; e += kThreads) {
                 const uint2 v = s.loc[e];
                 const float x = value_of(v.x);
-                if (v.x < lk || (v.x == lk && (int)v.y <= lim_i)) red_add(my_hist + r.bin(x) * 128u, r.units(x, s.X[r.bin(x)][lane]));
+                if (v.x < lk || (v.x == lk && (int)v.y <= lim_i)) red_add(my_hist + r.bin(x) * 128u, r.units(x, r.end_of((float)r.bin(x))));
             }
-        } else if (mass) {
-            el.blocks([&](const float (&v)[kBlock], int at) __attribute__((always_inline)) {
-#pragma unroll
-                for (int e = 0; e < kBlock; ++e) {
-                    const float x = v[e];
-                    const uint32_t o = r.bin_bits(x) * 128u;
-                    uint32_t u = r.units(x, *reinterpret_cast<const float*>(X_a + (o & (kBins * 128u - 1u))));
-                    if (!(x >= lim_x)) u = 0;
-                    if (lim_i != kAll && x == lim_x && at + el.place(e) > lim_i) u = 0;
-                    red_add(hist_a + o, u);
-                }
-            });
-        } else {
+        } else if (!mass) {
             el.blocks([&](const float (&v)[kBlock], int) __attribute__((always_inline)) {  // (top-k comes first: no limit by index yet)
 #pragma unroll
-                for (int e = 0; e < kBlock; ++e) red_add(hist_a + r.bin_bits(v[e]) * 128u, v[e] >= lim_x ? 1u : 0u);
+                for (int e = 0; e < kBlock; ++e) red_add(hist_a + __float_as_uint(r.bin_number(v[e])) * 128u, v[e] >= lim_x ? 1u : 0u);
             });
+        } else {
+            el.blocks([&](const float (&v)[kBlock], int) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < kBlock; ++e) {
+                    const float n = r.bin_number(v[e]);
+                    const uint32_t u = r.units(v[e], r.end_of(n - 8388608.f));
+                    red_add(hist_a + __float_as_uint(n) * 128u, v[e] >= lim_x ? u : 0u);
+                }
+            });
+            if (lim_i != kAll) {  // equal to the limit, but behind it: their weight is taken back where it was put
+                const uint32_t at_lim = my_hist + r.bin(lim_x) * 128u, back = 0u - r.units(lim_x, r.end_of((float)r.bin(lim_x)));
+                el.blocks([&](const float (&v)[kBlock], int at) {
+                    for (int e = 0; e < kBlock; ++e)
+                        if (v[e] == lim_x && at + el.place(e) > lim_i) red_add(at_lim, back);
+                });
+            }
         }
-        return totals();
+        totals();
     };
 
     // The smallest key whose bin is at least j.  It lies next to that of the bin's upper end: 32 probes around it nearly
@@ -330,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
         if (j <= 0) return k0;
         if (j >= kBins) return k1;
         {
-            const uint32_t mid = key_of(s.X[j][0]), a = mid > k0 + 16 ? mid - 16 : k0, at = a + lane;
+            const uint32_t mid = key_of(fmaxf(r.end_of((float)j), -FLT_MAX)), a = mid > k0 + 16 ? mid - 16 : k0, at = a + lane;
             const unsigned ok = __ballot_sync(0xffffffffu, at >= k1 || r.bin(value_of(at)) >= j);
             if (ok && (!(ok & 1u) || a == k0)) return a + __ffs(ok) - 1;
         }
@@ -466,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
         if (tid < n) {
             const float x = value_of((uint32_t)(k >> 32));
             const int bin = r.bin(x);
-            w = s.W[bin] * (double)r.units(x, s.X[bin][0]);
+            w = s.W[bin] * (double)r.units(x, r.end_of((float)bin));
         }
         const double run = warp_scan(w, lane);
         if (lane == 31) s.scan[warp] = run;
@@ -494,64 +504,77 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
     const double tp = (double)fmaxf(tp0, 0.f);
     const int k = p.top_k ? p.top_k[b] : 0;
 
-    // Three searches at most: the k-th candidate, the border of the nucleus, the drawn token.
-    unsigned long long t = 0;      // weight (candidates) of bin `lane`
-    double w0 = 0.0, run0 = 0.0;   // of the same bin, and of all up to it
-    float most = 0.f, most_upto = 0.f;   // of the same two, the largest CTA's share (in units, about)
-    double Z = 0.0;                // weight of what is kept
+    // Three searches at most: the k-th candidate, the border of the nucleus, the drawn token.  The first warp of every CTA
+    // takes the decisions, from the same numbers.
+    unsigned long long t = 0;            // (first warp) weight, or candidates, of bin `lane`
+    double w0 = 0.0, run0 = 0.0;         // of the same bin, and of all up to it
+    float most = 0.f, most_upto = 0.f;   // of the same two, the largest CTA's share (in units)
+    double Z = 0.0;                      // weight of what is kept (once weighed)
     bool weighed = false;
     for (int stage = k > 0 && k < p.V ? 0 : 1; stage < 3; ++stage) {
         if (stage == 1 && !nucleus) continue;
         const bool by_rank = stage == 0, strict = stage == 2;
-        if (!weighed) {
-            t = level0(!by_rank);
-            w0 = by_rank ? (double)t : s.W[lane] * (double)t;
-            run0 = warp_scan(w0, lane);
-            Z = __shfl_sync(0xffffffffu, run0, 31);
+        const float per = by_rank ? 1.f : (float)(1.7 * kUnit);  // elements per unit: a weight inside a bin is at least exp(-1/2)
+        const bool fresh = !weighed;
+        if (fresh) {
+            level0(!by_rank);
             weighed = !by_rank;
-            most = most_upto = 0.f;
-#pragma unroll
-            for (int c = 0; c < kCluster; ++c) {
-                const float v = c < C ? (float)s.xch[par ^ 1][c][lane] : 0.f;
-                most = fmaxf(most, v);
-                most_upto = fmaxf(most_upto, warp_scan(v, lane));
-            }
         }
-        if (by_rank && Z <= (double)k) continue;  // no more candidates than that
-        const double target = by_rank ? (double)k : (stage == 1 ? tp : u) * Z;
-        const double per = by_rank ? 1.0 : 1.7 * kUnit;  // elements per unit: a weight inside a bin is at least exp(-1/2)
-        // the bin that holds the target
-        const unsigned ok = __ballot_sync(0xffffffffu, t > 0 && (strict ? run0 > target : run0 >= target));
-        const unsigned any = __ballot_sync(0xffffffffu, t > 0);
-        const int j = ok ? __ffs(ok) - 1 : 31 - __clz(any | 1u);
-        double before = __shfl_sync(0xffffffffu, run0 - w0, j), tot = per * __shfl_sync(0xffffffffu, (double)t, j);
-        Range g = range_of_bin(j);
+        if (warp == 0) {
+            if (fresh) {
+                t = total(most);
+                w0 = by_rank ? (double)t : s.W[lane] * (double)t;
+                run0 = warp_scan(w0, lane);
+                Z = __shfl_sync(0xffffffffu, run0, 31);
+                most_upto = 0.f;
+                for (int c = 0; c < C; ++c) most_upto = fmaxf(most_upto, warp_scan((float)s.xch[par ^ 1][c][lane], lane));
+            }
+            Search f;
+            f.target = by_rank ? (double)k : (stage == 1 ? tp : u) * Z;
+            // the bin that holds the target
+            const unsigned ok = __ballot_sync(0xffffffffu, t > 0 && (strict ? run0 > f.target : run0 >= f.target));
+            const unsigned any = __ballot_sync(0xffffffffu, t > 0);
+            f.j = ok ? __ffs(ok) - 1 : 31 - __clz(any | 1u);
+            f.before = __shfl_sync(0xffffffffu, run0 - w0, f.j);
+            f.tot = per * __shfl_sync(0xffffffffu, (float)t, f.j);
+            f.part = per * __shfl_sync(0xffffffffu, most, f.j);
+            f.upto = per * __shfl_sync(0xffffffffu, most_upto, f.j);
+            f.all = by_rank ? (int)__shfl_sync(0xffffffffu, run0, f.j) : 0;
+            f.g = range_of_bin(f.j);
+            if (by_rank && Z <= (double)k) f.j = -1;  // no more candidates than that
+            if (lane == 0) s.at = f;
+        }
+        __syncthreads();
+        const int j = s.at.j;
+        const double target = s.at.target;
+        Range g = s.at.g;
+        float tot = s.at.tot, part = s.at.part;
+        if (j < 0) {
+            __syncthreads();
+            continue;
+        }
         const bool open = !by_rank && j == kBins - 1;  // (weights in the last bin may be anything down to 0: they count nothing)
         bool local = g.ka >= have.ka && g.kb <= have.kb && have.ia == 0 && have.ib == kAll;
-        double part = per * (double)__shfl_sync(0xffffffffu, most, j);
-        if (!local && !open) {
-            // everything from the top down if it fits: then the other searches find their elements there too
-            const double upto = per * (double)__shfl_sync(0xffffffffu, most_upto, j);
-            if (upto <= kLocal) {
-                compact(Range{key_of(r.m), g.kb, 0, kAll});
-                local = true;
-                have_all = by_rank;
-                if (by_rank && __shfl_sync(0xffffffffu, run0, j) <= kSorted && upto <= slot) {
-                    // few enough from the top down: all that is left to do happens in the list
-                    const int n = gather(have);
-                    const unsigned long long e = sorted(n);
-                    const double cum = summed(n, e, 0.0);
-                    int kept = min(k, n);
-                    if (tid == kept - 1) s.res.mass = cum;
-                    __syncthreads();
-                    Z = s.res.mass;
-                    if (nucleus) {
-                        kept = 1 + first_at(kept, e, cum, tp * Z, false);
-                        Z = s.res.mass;
-                    }
-                    first_at(kept, e, cum, u * Z, true);
-                    break;
+        // everything from the top down if it fits: then the other searches find their elements there too
+        if (!local && !open && s.at.upto <= kLocal) {
+            compact(Range{key_of(r.m), g.kb, 0, kAll});
+            local = true;
+            have_all = by_rank;
+            if (by_rank && s.at.all <= kSorted && s.at.upto <= slot) {
+                // few enough from the top down: all that is left to do happens in the list
+                const int n = gather(have);
+                const unsigned long long e = sorted(n);
+                const double cum = summed(n, e, 0.0);
+                int kept = min(k, n);
+                if (tid == kept - 1) s.res.mass = cum;
+                __syncthreads();
+                double z = s.res.mass;
+                if (nucleus) {
+                    kept = 1 + first_at(kept, e, cum, tp * z, false);
+                    z = s.res.mass;
                 }
+                first_at(kept, e, cum, u * z, true);
+                break;
             }
         }
         // Narrow the range around the target until its elements can be collected.
@@ -561,9 +584,13 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
                 uint32_t c = 0;
                 visit(g, local, [&](uint32_t, int) { ++c; });
                 red_add(my_hist, c);
-                const unsigned long long all = totals();
-                tot = (double)__shfl_sync(0xffffffffu, all, 0);
-                part = largest_part(0);
+                totals();
+                tot = part = 0.f;
+                for (int q = 0; q < C; ++q) {
+                    const float v = (float)s.xch[par ^ 1][q][0];
+                    tot += v;
+                    part = fmaxf(part, v);
+                }
             }
             if (!local && part <= kLocal) {
                 compact(g);
@@ -578,28 +605,41 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
             if (!by_value && g.ib == kAll) g.ib = p.V - 1;
             const uint32_t lo = by_value ? g.ka : (uint32_t)g.ia, span = by_value ? g.kb - g.ka : (uint32_t)(g.ib - g.ia);
             const int sh = max(0, 32 - __clz(span) - 5);
-            const float X = s.X[j][0];
+            const float X = r.end_of((float)j);
             visit(g, local, [&](uint32_t key, int i) {
                 red_add(my_hist + (((by_value ? key : (uint32_t)i) - lo) >> sh) * 128u, by_rank ? 1u : r.units(value_of(key), X));
             });
-            const unsigned long long tt = totals();
-            const double w = by_rank ? (double)tt : s.W[j] * (double)tt, run = warp_scan(w, lane);
-            const unsigned yes = __ballot_sync(0xffffffffu, tt > 0 && (strict ? before + run > target : before + run >= target));
-            const unsigned some = __ballot_sync(0xffffffffu, tt > 0);
-            const int cut = yes ? __ffs(yes) - 1 : 31 - __clz(some | 1u);
-            before += __shfl_sync(0xffffffffu, run - w, cut);
-            tot = per * __shfl_sync(0xffffffffu, (double)tt, cut);
-            part = per * largest_part(cut);
-            const uint32_t a = lo + ((uint32_t)cut << sh), last = (uint32_t)min((unsigned long long)a + (1u << sh) - 1, (unsigned long long)lo + span);
-            if (by_value) { g.ka = a; g.kb = last; }
-            else { g.ia = (int)a; g.ib = (int)last; }
+            totals();
+            if (warp == 0) {
+                float share;
+                const unsigned long long tt = total(share);
+                const double before = s.at.before, w = by_rank ? (double)tt : s.W[j] * (double)tt, run = warp_scan(w, lane);
+                const unsigned yes = __ballot_sync(0xffffffffu, tt > 0 && (strict ? before + run > target : before + run >= target));
+                const unsigned some = __ballot_sync(0xffffffffu, tt > 0);
+                const int cut = yes ? __ffs(yes) - 1 : 31 - __clz(some | 1u);
+                const double step = __shfl_sync(0xffffffffu, run - w, cut);
+                const uint32_t a = lo + ((uint32_t)cut << sh), last = (uint32_t)min((unsigned long long)a + (1u << sh) - 1, (unsigned long long)lo + span);
+                if (by_value) { g.ka = a; g.kb = last; }
+                else { g.ia = (int)a; g.ib = (int)last; }
+                const float total_of = __shfl_sync(0xffffffffu, (float)tt, cut), share_of = __shfl_sync(0xffffffffu, share, cut);
+                if (lane == 0) {
+                    s.at.before = before + step;
+                    s.at.tot = per * total_of;
+                    s.at.part = per * share_of;
+                    s.at.g = g;
+                }
+            }
+            __syncthreads();
+            g = s.at.g;
+            tot = s.at.tot;
+            part = s.at.part;
         }
         const unsigned long long e = sorted(n);
         if (by_rank) {
-            if (tid == max(0, min(n, k - (int)before) - 1)) s.res = Result{value_of((uint32_t)(e >> 32)), (int)(uint32_t)e, 0.0};
+            if (tid == max(0, min(n, k - (int)s.at.before) - 1)) s.res = Result{value_of((uint32_t)(e >> 32)), (int)(uint32_t)e, 0.0};
             __syncthreads();
         } else {
-            const double cum = summed(n, e, before);
+            const double cum = summed(n, e, s.at.before);
             first_at(n, e, cum, target, strict);
         }
         lim_x = s.res.x;
