@@ -26,15 +26,15 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBlock = 16;           // elements a thread looks at at a time
 constexpr int kHeld = 2 * kBlock * kThreads;  // elements that a CTA can hold in shared memory
 constexpr int kCluster = 8;
 constexpr int kBins = 32;
-constexpr int kLocal = 4096;         // elements that a CTA can copy to shared memory for a search
-constexpr int kList = 512;           // elements that are sorted in every CTA of a cluster; of each CTA an equal share
-constexpr int kSorted = 320;         // longer lists are narrowed further first: sorting takes time with the square of them
-constexpr int kSlices = 8;           // lane-private histograms of a CTA, each shared by four warps
+constexpr int kLocal = 2048;         // elements that a CTA can copy to shared memory for a search
+constexpr int kList = 256;           // elements that are sorted in every CTA of a cluster; of each CTA an equal share
+constexpr int kSorted = 224;         // longer lists are narrowed further first: sorting takes time with the square of them
+constexpr int kSlices = 4;           // lane-private histograms of a CTA, each shared by four warps
 constexpr double kUnit = 1.0 / 8388608.0;  // 2^-23
 
 // descending: the largest logit has the smallest key; -0 equals +0
@@ -182,7 +182,7 @@ __device__ __forceinline__ T warp_scan(T run, int lane) {
 // grid B * C in clusters of C; one cluster per row.  Every decision is taken by every warp of every CTA from the same
 // numbers, so the cluster stays together without anyone telling the others.
 template <bool HELD, bool VEC>
-__global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
+__global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     const Stamp stamp_guard(p.stamp);
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem& s = *reinterpret_cast<Smem*>(smem_raw);
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
     };
     // Brings the local elements of a range together in every CTA: CTA c's go to slots c * kList / C .. (the caller knows
     // that no CTA has more).
-    const int slot = kList / C;
+    const int slot_bits = __ffs(kList / C) - 1, slot = 1 << slot_bits;
     auto gather = [&](const Range& g) {
         if (tid == 0) s.lcnt = 0;
         __syncthreads();
@@ -427,8 +427,8 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
             if (in && at < slot) s.tmp[at] = ((unsigned long long)v.x << 32) | v.y;
         }
         __syncthreads();
-        const uint32_t n = min(s.lcnt, (uint32_t)slot), c = tid / slot, e = tid % slot;
         if (tid < kList) {
+            const uint32_t n = min(s.lcnt, (uint32_t)slot), c = tid >> slot_bits, e = tid & (slot - 1);
             if (e < n) cluster.map_shared_rank(&s.list[turn][0], c)[rank * slot + e] = s.tmp[e];
             if (e == 0) cluster.map_shared_rank(&s.cnt[turn][0], c)[rank] = n;
         }
@@ -441,23 +441,24 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
     // The collected elements in order, element e in thread e: each counts those before it.
     auto sorted = [&](int n) {
         unsigned long long* const list = s.list[turn ^ 1];
-        const int c0 = tid / slot, e0 = tid % slot;
-        if (tid < kList && (uint32_t)e0 < s.cnt[turn ^ 1][c0]) {  // side by side, and full to a multiple of 8
-            int to = e0;
-            for (int c = 0; c < c0; ++c) to += (int)s.cnt[turn ^ 1][c];
-            s.tmp[to] = list[tid];
-        }
         const int n8 = (n + 7) / 8 * 8;
-        if (tid >= n && tid < n8) s.tmp[tid] = ~0ull;
+        if (tid < kList) {  // side by side, and full to a multiple of 8
+            const int c0 = tid >> slot_bits, e0 = tid & (slot - 1);
+            if ((uint32_t)e0 < s.cnt[turn ^ 1][c0]) {
+                int to = e0;
+                for (int c = 0; c < c0; ++c) to += (int)s.cnt[turn ^ 1][c];
+                s.tmp[to] = list[tid];
+            }
+            if (tid >= n && tid < n8) s.tmp[tid] = ~0ull;
+        }
         __syncthreads();
         // the comparisons of an element are shared by as many neighbouring threads as there are to spare
-        int P = 32;
-        while (P > 1 && P * n > kThreads) P >>= 1;
-        const int e = tid / P;
+        const int p_bits = min(5, max(0, __clz(n - 1 | 1) - __clz(kThreads / 2))), P = 1 << p_bits;  // P n <= kThreads
         if (warp * 32 < P * n) {
+            const int e = tid >> p_bits;
             const unsigned long long k = e < n ? s.tmp[e] : ~0ull;
             int before = 0;
-            for (int q = 8 * (tid % P); q < n8; q += 8 * P) {
+            for (int q = 8 * (tid & (P - 1)); q < n8; q += 8 * P) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const ulonglong2 v = reinterpret_cast<const ulonglong2*>(s.tmp + q)[i];
@@ -465,31 +466,33 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
                 }
             }
             for (int o = 1; o < P; o <<= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-            if (e < n && tid % P == 0) list[before] = k;
+            if (e < n && (tid & (P - 1)) == 0) list[before] = k;
         }
         __syncthreads();
         return tid < n ? list[tid] : ~0ull;
     };
     // Running sum of the elements' weights, on top of `before`.
     auto summed = [&](int n, unsigned long long k, double before) {
-        double w = 0.0;
-        if (tid < n) {
-            const float x = value_of((uint32_t)(k >> 32));
-            const int bin = r.bin(x);
-            w = s.W[bin] * (double)r.units(x, r.end_of((float)bin));
+        double run = 0.0;
+        if (warp * 32 < n) {
+            if (tid < n) {
+                const float x = value_of((uint32_t)(k >> 32));
+                const int bin = r.bin(x);
+                run = s.W[bin] * (double)r.units(x, r.end_of((float)bin));
+            }
+            run = warp_scan(run, lane);
+            if (lane == 31) s.scan[warp] = run;
         }
-        const double run = warp_scan(w, lane);
-        if (lane == 31) s.scan[warp] = run;
         __syncthreads();
-        const int nw = min(warp, (n + 31) / 32);
-        for (int v = 0; v < nw; ++v) before += s.scan[v];
+        if (warp * 32 < n)
+            for (int v = 0; v < warp; ++v) before += s.scan[v];
         return before + run;
     };
     // The first of the elements 0..n-1 whose running sum is above (strict) or at least t; the last one if none is.
     auto first_at = [&](int n, unsigned long long k, double run, double t, bool strict) {
         if (tid == 0) s.hit = max(n - 1, 0);
         __syncthreads();
-        const unsigned ok = __ballot_sync(0xffffffffu, tid < n && (strict ? run > t : run >= t));
+        const unsigned ok = warp * 32 < n ? __ballot_sync(0xffffffffu, tid < n && (strict ? run > t : run >= t)) : 0u;
         if (ok && lane == 0) atomicMin(&s.hit, warp * 32 + __ffs(ok) - 1);
         __syncthreads();
         const int h = s.hit;
@@ -526,8 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
                 w0 = by_rank ? (double)t : s.W[lane] * (double)t;
                 run0 = warp_scan(w0, lane);
                 Z = __shfl_sync(0xffffffffu, run0, 31);
-                most_upto = 0.f;
-                for (int c = 0; c < C; ++c) most_upto = fmaxf(most_upto, warp_scan((float)s.xch[par ^ 1][c][lane], lane));
+                most_upto = warp_scan(most, lane);  // (at most)
             }
             Search f;
             f.target = by_rank ? (double)k : (stage == 1 ? tp : u) * Z;
@@ -555,30 +557,9 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
         }
         const bool open = !by_rank && j == kBins - 1;  // (weights in the last bin may be anything down to 0: they count nothing)
         bool local = g.ka >= have.ka && g.kb <= have.kb && have.ia == 0 && have.ib == kAll;
-        // everything from the top down if it fits: then the other searches find their elements there too
-        if (!local && !open && s.at.upto <= kLocal) {
-            compact(Range{key_of(r.m), g.kb, 0, kAll});
-            local = true;
-            have_all = by_rank;
-            if (by_rank && s.at.all <= kSorted && s.at.upto <= slot) {
-                // few enough from the top down: all that is left to do happens in the list
-                const int n = gather(have);
-                const unsigned long long e = sorted(n);
-                const double cum = summed(n, e, 0.0);
-                int kept = min(k, n);
-                if (tid == kept - 1) s.res.mass = cum;
-                __syncthreads();
-                double z = s.res.mass;
-                if (nucleus) {
-                    kept = 1 + first_at(kept, e, cum, tp * z, false);
-                    z = s.res.mass;
-                }
-                first_at(kept, e, cum, u * z, true);
-                break;
-            }
-        }
         // Narrow the range around the target until its elements can be collected.
         int n = 0;
+        bool rest = false;  // few enough from the top down: all that is left to do happens in the list
         for (int level = 0; level < 16; ++level) {
             if (open) {
                 uint32_t c = 0;
@@ -593,10 +574,17 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
                 }
             }
             if (!local && part <= kLocal) {
-                compact(g);
+                // everything from the top down if it fits: then the other searches find their elements there too
+                const bool top = level == 0 && !open && s.at.upto <= kLocal;
+                compact(top ? Range{key_of(r.m), g.kb, 0, kAll} : g);
                 local = true;
+                if (top && by_rank) {
+                    have_all = true;
+                    rest = s.at.all <= kSorted && s.at.upto <= slot;
+                    if (rest) g = have;
+                }
             }
-            if (local && part <= slot && tot <= kSorted) {
+            if (local && (rest || (part <= slot && tot <= kSorted))) {
                 n = gather(g);
                 break;
             }
@@ -635,12 +623,28 @@ __global__ void __launch_bounds__(kThreads, 1) sample_rows(const SampleArgs p) {
             part = s.at.part;
         }
         const unsigned long long e = sorted(n);
-        if (by_rank) {
+        if (by_rank && !rest) {
             if (tid == max(0, min(n, k - (int)s.at.before) - 1)) s.res = Result{value_of((uint32_t)(e >> 32)), (int)(uint32_t)e, 0.0};
             __syncthreads();
         } else {
-            const double cum = summed(n, e, s.at.before);
-            first_at(n, e, cum, target, strict);
+            const double cum = summed(n, e, rest ? 0.0 : s.at.before);
+            int kept = n;
+            double at = target;
+            bool over = strict;
+            if (rest) {
+                kept = min(k, n);
+                if (tid == kept - 1) s.res.mass = cum;
+                __syncthreads();
+                double z = s.res.mass;
+                if (nucleus) {
+                    kept = 1 + first_at(kept, e, cum, tp * z, false);
+                    z = s.res.mass;
+                }
+                at = u * z;
+                over = true;
+            }
+            first_at(kept, e, cum, at, over);
+            if (rest) break;
         }
         lim_x = s.res.x;
         lim_i = s.res.i;
