@@ -31,7 +31,7 @@ constexpr int kBlock = 16;           // elements a thread looks at at a time
 constexpr int kHeld = 2 * kBlock * kThreads;  // elements that a CTA can hold in shared memory
 constexpr int kCluster = 8;
 constexpr int kBins = 32;
-constexpr int kLocal = 2048;         // elements that a CTA can copy to shared memory for a search
+constexpr int kLocal = 2560;         // elements that a CTA can copy to shared memory for a search
 constexpr int kList = 256;           // elements that are sorted in every CTA of a cluster; of each CTA an equal share
 constexpr int kSorted = 224;         // longer lists are narrowed further first: sorting takes time with the square of them
 constexpr int kSlices = 4;           // lane-private histograms of a CTA, each shared by four warps
@@ -56,10 +56,10 @@ struct Result {  // the last element of a kept prefix, and the prefix's weight
 struct Range { uint32_t ka, kb; int ia, ib; };
 struct Search {  // what the first warp has found out, for all
     double target, before;  // the sum that is looked for; the sum in front of the range
-    float tot, part, upto;  // about how many elements the range has in the cluster and in its fullest CTA; in that, with all before it
+    float tot, part;        // about how many elements (not more) the range has in the cluster and in its fullest CTA
+    float all, upto;        // the same of the range and all before it
     Range g;
     int j;                  // the range's bin, -1: nothing to search for
-    int all;                // (by rank) elements up to the bin's end
 };
 
 struct Smem {
@@ -74,7 +74,7 @@ struct Smem {
     Result res;
     Search at;
     uint32_t key[2][kCluster], key_w[kWarps];
-    uint32_t nloc, lcnt;
+    uint32_t nloc, lcnt, moved;
     int hit;
     float thr;
     alignas(16) float row[4];        // (HELD) the CTA's elements, as many as there are; -inf up to a multiple of a block
@@ -187,12 +187,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     Smem& s = *reinterpret_cast<Smem*>(smem_raw);
     cg::cluster_group cluster = cg::this_cluster();
-    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int b = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int C = (int)cluster.num_blocks();  // (CTAs that take part: 1 once the first goes on alone)
+    const int rank = (int)cluster.block_rank(), b = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     {
         uint4* h = reinterpret_cast<uint4*>(s.hist);
         for (int i = tid; i < (int)(sizeof s.hist / 16); i += kThreads) h[i] = make_uint4(0, 0, 0, 0);
     }
+    if (tid == 0) s.moved = 0;
     cluster.barrier_arrive();  // (waited for before the first access to another CTA's shared memory)
     pdl_trigger();
     pdl_wait();
@@ -260,6 +261,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     int lim_i = kAll;
     int par = 0, turn = 0;
 
+    bool solo = false;
+    auto meet = [&]() {
+        if (solo) __syncthreads();
+        else cluster.sync();
+    };
+
     // Adds the lane-private histograms up over the cluster: the CTAs' totals of bin `lane` are in s.xch[par ^ 1][CTA][lane],
     // until the next but one.
     auto totals = [&]() {
@@ -280,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             if (lane < C)
                 cluster.map_shared_rank(&s.xch[par][0][0], lane)[rank * kBins + bin] = ((unsigned long long)hi << 16) + lo;
         }
-        cluster.sync();
+        meet();
         par ^= 1;
     };
     auto total = [&](float& most) {  // (first warp) of bin `lane`: the total, and the largest CTA's share
@@ -410,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     };
     // Brings the local elements of a range together in every CTA: CTA c's go to slots c * kList / C .. (the caller knows
     // that no CTA has more).
-    const int slot_bits = __ffs(kList / C) - 1, slot = 1 << slot_bits;
+    int slot_bits = __ffs(kList / C) - 1, slot = 1 << slot_bits;
     auto gather = [&](const Range& g) {
         if (tid == 0) s.lcnt = 0;
         __syncthreads();
@@ -432,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             if (e < n) cluster.map_shared_rank(&s.list[turn][0], c)[rank * slot + e] = s.tmp[e];
             if (e == 0) cluster.map_shared_rank(&s.cnt[turn][0], c)[rank] = n;
         }
-        cluster.sync();
+        meet();
         turn ^= 1;
         int all = 0;
         for (int q = 0; q < C; ++q) all += (int)s.cnt[turn ^ 1][q];
@@ -541,7 +548,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             f.tot = per * __shfl_sync(0xffffffffu, (float)t, f.j);
             f.part = per * __shfl_sync(0xffffffffu, most, f.j);
             f.upto = per * __shfl_sync(0xffffffffu, most_upto, f.j);
-            f.all = by_rank ? (int)__shfl_sync(0xffffffffu, run0, f.j) : 0;
+            f.all = per * warp_scan((float)t, lane);
+            f.all = __shfl_sync(0xffffffffu, f.all, f.j);
             f.g = range_of_bin(f.j);
             if (by_rank && Z <= (double)k) f.j = -1;  // no more candidates than that
             if (lane == 0) s.at = f;
@@ -550,7 +558,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         const int j = s.at.j;
         const double target = s.at.target;
         Range g = s.at.g;
-        float tot = s.at.tot, part = s.at.part;
+        float tot = s.at.tot, part = solo ? tot : s.at.part;
         if (j < 0) {
             __syncthreads();
             continue;
@@ -578,9 +586,39 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
                 const bool top = level == 0 && !open && s.at.upto <= kLocal;
                 compact(top ? Range{key_of(r.m), g.kb, 0, kAll} : g);
                 local = true;
+                if (top && !solo && C > 1 && s.at.all <= kLocal) {
+                    // few enough for one CTA: the others hand over what they have and are done
+                    __syncthreads();
+                    const uint32_t n = s.nloc;
+                    uint2* const to = cluster.map_shared_rank(s.loc, 0);
+                    if (tid == 0 && rank) s.lcnt = atomicAdd(cluster.map_shared_rank(&s.moved, 0), n);
+                    __syncthreads();
+                    if (rank)  // (from the list's end: how many the first CTA has of its own is not known here)
+                        for (uint32_t e = tid; e < n && s.lcnt + e < kLocal; e += kThreads) to[kLocal - 1 - (s.lcnt + e)] = s.loc[e];
+                    cluster.sync();
+                    if (rank) return;
+                    const uint32_t own = s.nloc, moved = min(s.moved, kLocal - own);
+                    __syncthreads();
+                    // close the gap between its own and theirs
+                    uint2 keep[(kLocal + kThreads - 1) / kThreads];
+#pragma unroll
+                    for (int q = 0; q < (kLocal + kThreads - 1) / kThreads; ++q)
+                        if (tid + q * kThreads < moved) keep[q] = s.loc[kLocal - 1 - (tid + q * kThreads)];
+                    __syncthreads();
+#pragma unroll
+                    for (int q = 0; q < (kLocal + kThreads - 1) / kThreads; ++q)
+                        if (tid + q * kThreads < moved) s.loc[own + tid + q * kThreads] = keep[q];
+                    if (tid == 0) s.nloc = own + moved;
+                    __syncthreads();
+                    solo = true;
+                    C = 1;
+                    slot_bits = __ffs(kList) - 1;
+                    slot = kList;
+                    part = tot;
+                }
                 if (top && by_rank) {
                     have_all = true;
-                    rest = s.at.all <= kSorted && s.at.upto <= slot;
+                    rest = s.at.all <= kSorted && (solo ? s.at.all : s.at.upto) <= slot;
                     if (rest) g = have;
                 }
             }
