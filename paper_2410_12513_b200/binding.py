@@ -407,12 +407,12 @@ def _on(t, dtype, n, what, dev):
     """Address of a contiguous CUDA tensor of n elements (None: NULL) on device `dev`."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype:
-        raise TypeError(f"{what} must be a CUDA tensor of {dtype}")
+    if t.dtype is not dtype or t.get_device() != dev:
+        if t.dtype is not dtype or not t.is_cuda:
+            raise TypeError(f"{what} must be a CUDA tensor of {dtype}")
+        raise ValueError(f"{what} is on another device")
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous with {n} elements")
-    if t.get_device() != dev:
-        raise ValueError(f"{what} is on another device")
     return t.data_ptr()
 
 
@@ -420,10 +420,11 @@ def _raw_stream(stream, dev):
     """The stream's handle; None: the current stream of device `dev`."""
     if stream is not None:
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(dev) if _RAW_STREAM else torch.cuda.current_stream(dev).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev) if _RAW else torch.cuda.current_stream(dev).cuda_stream
 
 
-_RAW_STREAM = hasattr(torch._C, "_cuda_getCurrentRawStream")  # (building a Stream object takes longer than a small call)
+# (building a Stream object takes longer than a small call; without a CUDA build of torch neither is there)
+_RAW = hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice")
 
 
 def _device_of(t, what):
@@ -431,7 +432,7 @@ def _device_of(t, what):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a CUDA tensor")
     dev = t.get_device()
-    if dev != torch.cuda.current_device():
+    if dev != (torch._C._cuda_getDevice() if _RAW else torch.cuda.current_device()):
         raise ValueError(f"{what} is on device {dev}, not on the current one")
     return dev
 
@@ -482,19 +483,23 @@ def first_lora(x, a, b, row_adapter, y, scales=None, segments=None, stream=None)
     b CUDA [adapters][n][rank], contiguous, of one type; segments: borders of the output segments, (0, ..., n)."""
     dev = _device_of(x, "x")
     ldx, ldy = _rows_of(x, "x"), _rows_of(y, "y")
-    (rows, k), n = x.shape, y.shape[1]
-    if y.shape[0] != rows or a.dim() != 3 or b.dim() != 3 or a.dtype != b.dtype:
+    rows, k = x.shape
+    n = y.shape[1]
+    if y.shape[0] != rows or a.dim() != 3 or b.dim() != 3 or a.dtype is not b.dtype:
         raise ValueError("x and y must have one row each per row of the batch; a, b three dimensions and one type")
     segments = (0, n) if segments is None else tuple(segments)
-    adapters, _, rank = b.shape
-    if b.shape[1] != n or tuple(a.shape) != (adapters, (len(segments) - 1) * rank, k):
+    adapters, bn, rank = b.shape
+    parts = len(segments) - 1
+    if bn != n or a.shape != (adapters, parts * rank, k):
         raise ValueError("a must be [adapters][segments*rank][k] and b [adapters][n][rank]")
-    if not y.is_cuda or y.get_device() != dev:
-        raise ValueError("y is on another device")
-    rc = lib().first_lora(x.data_ptr(), _code(x, "x"), ldx, _on(a, a.dtype, a.numel(), "a", dev), _on(b, b.dtype, b.numel(), "b", dev),
-                          _code(a, "a"), _on(scales, torch.float32, adapters, "scales", dev),
-                          _on(row_adapter, torch.int32, rows, "row_adapter", dev), adapters, rank, len(segments) - 1,
-                          _segment_array(segments), rows, k, n, y.data_ptr(), _code(y, "y"), ldy, _raw_stream(stream, dev))
+    if y.get_device() != dev or a.get_device() != dev or b.get_device() != dev:
+        raise ValueError("x, y, a and b must be on one device")
+    if not (a.is_contiguous() and b.is_contiguous()):
+        raise ValueError("a and b must be contiguous")
+    rc = lib().first_lora(x.data_ptr(), _code(x, "x"), ldx, a.data_ptr(), b.data_ptr(), _code(a, "a"),
+                          _on(scales, torch.float32, adapters, "scales", dev), _on(row_adapter, torch.int32, rows, "row_adapter", dev),
+                          adapters, rank, parts, _segment_array(segments), rows, k, n, y.data_ptr(), _code(y, "y"), ldy,
+                          _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_lora")
 
@@ -532,7 +537,7 @@ def first_rope(q, k, pos, inv_freq, factor=1.0, interleaved=False, stream=None):
         _heads_of(k, "k")
         if k.shape[0] != T or k.shape[2] != hd or k.dtype != q.dtype:
             raise ValueError("q and k must agree in tokens, head size and type")
-        if not k.is_cuda or k.get_device() != dev:
+        if k.get_device() != dev:
             raise ValueError("k is on another device")
         kp, hk, ks = k.data_ptr(), k.shape[1], k.stride()
     qs = q.stride()
