@@ -32,7 +32,7 @@
  *     token scores, the internal logits row buffer of first_decode_step without `logits`).
  *   - Work is enqueued on the CUDA stream passed as `void *stream` (a cudaStream_t;
  *     NULL = the default stream).  Only first_set_mask, first_prefill, first_last_device_flags
- *     and the measurement aids wait for the stream.
+ *     and the measurement aids wait for the stream (first_set_rope for the device).
  *   - Layers are numbered from 0.  mask[b][l] is a byte, 1 = sequence b runs layer l,
  *     0 = it skips it.  All matrices are row-major; linear weights are [out][in].
  *   - dtype FIRST_DTYPE_F32: weight matrices and KV cache are float32.

@@ -647,7 +647,8 @@ class FirstContext:
     def __init__(self, shape, dtype, max_batch, max_tokens_per_seq, weights):
         if not torch.cuda.is_available():
             raise RuntimeError("a CUDA device is required; there is no CPU path")
-        self.shape, self.dtype = shape, dtype
+        self.shape, self.dtype, self.max_batch = shape, dtype, int(max_batch)
+        self._sampling = ()
         self.h, self._keep = first_create(shape, dtype, max_batch, max_tokens_per_seq, weights)
 
     def close(self):
@@ -666,6 +667,7 @@ class FirstContext:
 
     def prefill(self, tokens, cu_seqlens, kv, router_w=None, router_b=None, tau=0.5, mode=0, mask=None, scores=None,
                 logits=None, next_tokens=None, stream=None):
+        self._check_sampling(len(cu_seqlens) - 1, next_tokens)
         first_prefill(self.h, tokens, cu_seqlens, kv, router_w, router_b, tau, mode, mask, scores, logits,
                       next_tokens, stream)
 
@@ -685,6 +687,7 @@ class FirstContext:
         return first_get_plan(self.h, self.B, self.shape.n_layers)
 
     def decode_step(self, tokens, kv, logits=None, next_tokens=None, layer_inputs=None, stream=None):
+        self._check_sampling(getattr(self, "B", 0), next_tokens)
         first_decode_step(self.h, tokens, kv, logits, next_tokens, layer_inputs, stream)
 
     def device_flags(self, stream=None):
@@ -698,13 +701,22 @@ class FirstContext:
 
     def set_sampling(self, top_k, temperature, uniforms):
         self._uniforms = uniforms  # borrowed by the library until the next call
+        self._sampling = ()
         first_set_sampling(self.h, top_k, temperature, uniforms)
 
     def set_sampling_rows(self, uniforms=None, temperature=None, top_k=None, top_p=None, min_p=None):
-        self._sampling = (uniforms, temperature, top_k, top_p, min_p)  # borrowed by the library until the next call
+        """Arrays of one entry per batch row (borrowed until the next call); uniforms None restores argmax."""
         first_set_sampling_rows(self.h, uniforms, temperature, top_k, top_p, min_p)
+        self._sampling = () if uniforms is None else tuple(t for t in (uniforms, temperature, top_k, top_p, min_p) if t is not None)
+
+    def _check_sampling(self, rows, next_tokens):
+        if next_tokens is not None and any(t.numel() < rows for t in self._sampling):
+            raise ValueError(f"the sampling settings have fewer than {rows} entries")
 
     def set_adapters(self, adapters=None, seq_adapter=None, scales=None):
+        """adapters: {"qkv" | "o" | "gate_up" | "down": [(a, b) or None per layer]}; seq_adapter CUDA int32 [max_batch]."""
+        if adapters is not None and seq_adapter.numel() < self.max_batch:
+            raise ValueError(f"seq_adapter must have {self.max_batch} entries")
         self._adapters = first_set_adapters(self.h, self.shape, self.dtype, adapters, seq_adapter, scales)
 
     def set_rope(self, inv_freq=None, factor=1.0):

@@ -110,6 +110,8 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+__host__ __device__ constexpr int steps_ahead(int rows) { return rows == 8 ? 2 : 3; }
+
 struct Plan {
     int tiles;          // clusters = tiles * slices
     int slices;         // parts of the output features
@@ -317,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
     // warp's next steps are copied to shared memory in the background (each thread reads what it copied itself); the
     // first ones are on their way while the cluster meets.
     constexpr int HR = TR == 8 ? 1 : 2;  // 8-row halves of a 16-row tile that are used
-    constexpr int D = TR == 8 ? 2 : 3;   // steps in flight
+    constexpr int D = steps_ahead(TR);   // steps in flight
     int steps = 0;                       // (of 32 features)
     for (int s = 0; s < p.S; ++s) steps += (p.seg[s + 1] - p.seg[s] + 31) / 32;
     const int per = (steps + pl.slices * kCluster - 1) / (pl.slices * kCluster);
@@ -476,26 +478,32 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
     cluster.barrier_wait();
 }
 
-template <int XK, typename WT, typename YT, int TR, int OCC>
-cudaError_t launch_tiles(const LoraArgs& a, int tiles, cudaStream_t st, bool pdl, int n_sm) {
+constexpr size_t kMaxSmem = 226 * 1024;  // dynamic bytes of a CTA; the static ones (under 1 KB) come on top
+
+// Launch shape of `rows`-row tiles; the shared memory it takes (see the kernel for the parts).
+Plan plan_of(const LoraArgs& a, int rows, int tiles, int n_sm, size_t& smem) {
     Plan pl{};
-    const int M = a.S * a.R;
+    const int M = a.S * a.R, kbs = (a.R + 15) / 16, wt = a.w_f32 ? 4 : 2, yt = a.y_f32 ? 4 : 2;
     pl.direct = a.n > kMaxIds || a.m == 1;
     pl.tiles = tiles;
     // few tiles: several clusters share one's output features, while there is room for them and a step for each warp
     pl.slices = std::max(1, std::min(2 * n_sm / (tiles * kCluster), a.N / (32 * kCluster * kWarps)));
     pl.mt = (M + 15) / 16;
     pl.ks = std::max(1, kParts / pl.mt);
-    const int kbs = (a.R + 15) / 16;
     pl.h_stride = 16 * (kbs | 1);  // an odd number of 32-byte units: eight batch rows' fragments meet no bank twice
-    pl.y_vec = reinterpret_cast<uintptr_t>(a.y) % 16 == 0 && (a.m == 1 || a.ldy * sizeof(YT) % 16 == 0);
-    pl.h_bytes = a.S * 3 * TR * pl.h_stride * 2;
-    const size_t step = (TR == 8 ? 1 : 2) * sizeof(YT) / 2 * 512 + 4 * 32 * 4 * sizeof(WT), shares = (size_t)(pl.ks - 1) * pl.mt * 16 * TR * 4;
-    size_t smem = (size_t)pl.mt * 16 * TR * 4 + pl.h_bytes + std::max(shares, kWarps * (TR == 8 ? 2 : 3) * step);
+    pl.y_vec = reinterpret_cast<uintptr_t>(a.y) % 16 == 0 && (a.m == 1 || a.ldy * yt % 16 == 0);
+    pl.h_bytes = a.S * 3 * rows * pl.h_stride * 2;
+    const size_t step = (rows == 8 ? 1 : 2) * yt / 2 * 512 + 4 * 32 * 4 * wt, shares = (size_t)(pl.ks - 1) * pl.mt * 16 * rows * 4;
+    smem = (size_t)pl.mt * 16 * rows * 4 + pl.h_bytes + std::max(shares, kWarps * steps_ahead(rows) * step);
     if (!pl.direct) smem = std::max(smem, ((size_t)(a.n + 3) / 4 * 4 + a.m) * 4);
+    return pl;
+}
+
+template <int XK, typename WT, typename YT, int TR, int OCC>
+cudaError_t launch_tiles(const LoraArgs& a, const Plan& pl, size_t smem, cudaStream_t st, bool pdl) {
     auto kern = lora_tiles<XK, WT, YT, TR, OCC>;
-    if (smem > 40 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+    if (smem > 40 * 1024) {  // (always the same value: calls of other threads rely on it)
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg{};
@@ -517,17 +525,23 @@ cudaError_t launch_tiles(const LoraArgs& a, int tiles, cudaStream_t st, bool pdl
 
 template <int XK, typename WT, typename YT>
 cudaError_t launch_rows(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
-    // Tiles of 32 rows once an adapter has 16 rows on average, else of 8.  At most as many tiles as: one for every row,
-    // or one ragged tile for every adapter and full ones for the rest.
-    const bool few = a.m < 16 * (int64_t)a.n || a.m <= 32;
-    const int TR = few ? 8 : 32;
-    const int tiles = a.n > kMaxIds || a.m == 1 ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / TR);
-    if (!few) return launch_tiles<XK, WT, YT, 32, 2>(a, tiles, st, pdl, n_sm);
+    // At most as many tiles as: one for every row, or one ragged tile for every adapter and full ones for the rest.
+    auto tiles_of = [&](int rows) { return a.n > kMaxIds || a.m == 1 ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / rows); };
+    size_t smem;
+    // Tiles of 32 rows once an adapter has 16 rows on average (1024 rows of 8 adapters, gate|up: 47 us against 66 with tiles
+    // of 8), if their h fits (four segments of rank 128 do not); else of 8.
+    if (a.m >= 16 * (int64_t)a.n && a.m > 32) {
+        const Plan pl = plan_of(a, 32, tiles_of(32), n_sm, smem);
+        if (smem <= kMaxSmem) return launch_tiles<XK, WT, YT, 32, 2>(a, pl, smem, st, pdl);
+    }
+    const int tiles = tiles_of(8);
+    const Plan pl = plan_of(a, 8, tiles, n_sm, smem);
     // With 64 registers four CTAs fit on a multiprocessor instead of two, at the price of spills: 256 rows of 64 adapters
     // (512 CTAs) 34 us against 48 with three, 32 rows of 16 adapters (160 CTAs) 12.7 against 10.9.  float32 adapters take
     // three times the registers and stay at two.
-    if (sizeof(WT) == 2 && tiles * kCluster > 2 * n_sm) return launch_tiles<XK, WT, YT, 8, 4>(a, tiles, st, pdl, n_sm);
-    return launch_tiles<XK, WT, YT, 8, 2>(a, tiles, st, pdl, n_sm);
+    if constexpr (sizeof(WT) == 2)
+        if (tiles * kCluster > 2 * n_sm) return launch_tiles<XK, WT, YT, 8, 4>(a, pl, smem, st, pdl);
+    return launch_tiles<XK, WT, YT, 8, 2>(a, pl, smem, st, pdl);
 }
 
 template <typename WT, typename YT>

@@ -95,9 +95,9 @@ struct Row {  // what a thread needs to know about the row
     __device__ __forceinline__ int bin(float x) const { return (int)(__float_as_uint(bin_number(x)) & (kBins - 1)); }
     __device__ __forceinline__ float end_of(float bin) const { return fmaf(-bin, half_T, top); }  // a bin's upper end
     // weight of x in units of 2^-23 of that of its bin's upper end X (x - X is exact but where it does not matter; it is
-    // above 0 by a rounding at most)
+    // above 0 by a rounding at most): at most 2^23 - 1, so that 512 of them have 32 bits
     __device__ __forceinline__ uint32_t units(float x, float X) const {
-        return __float_as_uint(ex2(fminf((x - X) * inv_Tl2, 0.f)) + 1.f) - 0x3f800000u;
+        return __float_as_uint(ex2(fminf((x - X) * inv_Tl2, -2.5e-7f)) + 1.f) - 0x3f800000u;
     }
 };
 
@@ -702,7 +702,8 @@ cudaError_t sample_launch(const SampleArgs& a, cudaStream_t st, bool pdl) {
     const size_t smem = sizeof(Smem) + (held ? (size_t)(chunk + block - 1) / block * block * 4 : 0);
     const bool vec = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && (a.B == 1 || a.ld % 4 == 0);
     auto kern = held ? (vec ? sample_rows<true, true> : sample_rows<true, false>) : (vec ? sample_rows<false, true> : sample_rows<false, false>);
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // (always the same value: calls of other threads rely on it)
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Smem) + kHeld * 4));
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(a.B * C);

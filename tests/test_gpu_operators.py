@@ -219,6 +219,56 @@ def test_lora_padded_rows_empty_batch_and_bit_reproducible():
     assert torch.equal(none, y)
 
 
+@pytest.mark.parametrize("types", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f32", "f32", "bf16")], ids=str)
+@pytest.mark.parametrize("case", [(70, 2, 128, 264, (0, 64, 128, 192, 300)), (200, 1, 128, 72, (0, 48, 80, 97)), (1024, 64, 128, 32, (0, 33)),
+                                  (40, 4096, 8, 32, (0, 40)), (40, 4097, 8, 32, (0, 40))], ids=str)
+def test_lora_largest_ranks_segments_and_adapter_counts(case, types):
+    """What takes the most shared memory, many adapters of which few are used, and more than a CTA counts."""
+    import torch
+    from paper_2410_12513_b200 import first_lora
+    x, a, b, ids, y, g = _lora_inputs(case, *(_t(v) for v in types), 23)
+    rows, n, rank, k, seg = case
+    if n >= 4096:
+        ids.copy_(torch.tensor([0, n - 1, 17, n - 1, -1, n, 4000, 2 ** 31 - 1] * 5, dtype=torch.int32))
+    ref, mag = _lora_ref(x, a, b, ids, y, None, seg)
+    first_lora(x, a, b, ids, y, segments=seg)
+    tol = (k / 8 + rank + 24) * U32 * mag + (2.0 ** -8 * np.abs(ref) if types[1] == "bf16" else 0.0)  # (as in test_lora)
+    assert (np.abs(y.double().cpu().numpy() - ref) <= tol).all()
+
+
+def test_calls_of_several_threads_at_once():
+    """Calls of different sizes from two host threads, each on a stream of its own."""
+    import threading
+    import torch
+    from paper_2410_12513_b200 import first_lora, first_sample
+    sizes = [((48, 2, 128, 264, (0, 64, 300)), 60000), ((200, 3, 8, 512, (0, 96)), 3000)]
+    work, errors = [], []
+    for case, v in sizes:
+        x, a, b, ids, y, g = _lora_inputs(case, _t("bf16"), _t("f32"), _t("bf16"), 2)
+        want = y.clone()
+        first_lora(x, a, b, ids, want, segments=case[4])
+        lg, u = torch.randn(20, v, generator=g).cuda(), torch.rand(20, generator=g).cuda()
+        tok = torch.empty(20, dtype=torch.int32, device="cuda")
+        first_sample(lg, u, tok)
+        work.append((case, x, a, b, ids, y, want, lg, u, tok))
+    torch.cuda.synchronize()
+
+    def go(case, x, a, b, ids, y, want, lg, u, tok):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(50):
+                    got, t = y.clone(), torch.empty_like(tok)
+                    first_lora(x, a, b, ids, got, segments=case[4])
+                    first_sample(lg, u, t)
+                    assert torch.equal(got, want) and torch.equal(t, tok)
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+    threads = [threading.Thread(target=go, args=w) for w in work]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not errors, errors
+
+
 def test_lora_rows_of_other_adapters_do_not_leak_nan():
     """NaN and infinities in rows without an adapter, or in adapters no row uses, reach nothing."""
     import torch
@@ -400,6 +450,18 @@ def test_sample_ties_and_crowded_values(kind):
         _sample_check(x, u, **s)
 
 
+@pytest.mark.parametrize("V", [262144, 524288])
+def test_sample_largest_vocabularies_all_at_a_bins_upper_end(V):
+    """All candidates but one tie exactly where a histogram's bin begins, at its largest weight: sums of 2^19 of them."""
+    x = np.full((2, V), -0.25, np.float32)  # half a bin's width below the maximum: the second bin's upper end
+    x[:, 1000] = 0.0
+    u = np.array([0.31, 0.999], np.float32)
+    _sample_check(x, u)
+    _sample_check(x, u, k=np.array([V - 5, 200000]), p=np.array([0.5, 0.9]))
+    x[:, 1000] = -0.25
+    _sample_check(x, u, temp=np.full(2, np.inf))
+
+
 def test_sample_values_outside_their_ranges():
     g = np.random.default_rng(5)
     B, V = 6, 3000
@@ -538,7 +600,8 @@ def test_step_with_adapters_equals_merged_weights(bf16, targets, skip):
     pre = [oracle.prefill(oms[ids[b]], okv[b], 0, prompts[b], want_router_in=False) for b in range(B)]
 
     ctx = _ctx(shape, bf16, 64, 64, w)
-    seq = torch.tensor(ids, dtype=torch.int32, device="cuda")
+    seq = torch.full((64,), -1, dtype=torch.int32, device="cuda")
+    seq[:B] = torch.tensor(ids, dtype=torch.int32)
     ctx.set_adapters(dev, seq, torch.from_numpy(scales).cuda())
     kv = GpuKV(shape, [m + 4 for m in lens], bf16)
     logits = torch.empty((B, shape.vocab), device="cuda")
@@ -569,7 +632,7 @@ def test_step_with_adapters_equals_merged_weights(bf16, targets, skip):
         if off == "ids":
             seq.fill_(-1)
         else:
-            seq.copy_(torch.tensor(ids))
+            seq[:B] = torch.tensor(ids, dtype=torch.int32)
             ctx.set_adapters(None)
         ctx.prefill(torch.from_numpy(np.concatenate(prompts)).cuda(), cu, kv.c, logits=logits)
         err, _ = logits_check(logits.cpu().numpy(), np.stack(refs))
@@ -723,6 +786,26 @@ def test_operators_together():
         tok.copy_(nt)
     assert ctx.device_flags() == 0
     pool.close()
+
+
+def test_context_checks_the_length_of_what_it_borrows():
+    import torch
+    shape = fi.ModelShape(2, 64, 2, 2, 32, 80, 32)
+    _, kv = synthetic_caches(shape, [3, 3, 3], [9] * 3, 1, False)
+    ctx = _ctx(shape, False, 3, 9, fi.make_weights(shape, 1, False))
+    dev, _ = _adapters(shape, 2, 8, 1, False)
+    with pytest.raises(ValueError):
+        ctx.set_adapters(dev, torch.zeros(2, dtype=torch.int32, device="cuda"))
+    ctx.set_mask(torch.ones((3, 2), dtype=torch.uint8, device="cuda"))
+    ctx.set_sampling_rows(torch.zeros(2, device="cuda"))
+    tok, nxt = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        ctx.decode_step(tok, kv.c, None, nxt)
+    with pytest.raises(ValueError):
+        ctx.prefill(tok, np.array([0, 1, 2, 3], np.int32), kv.c, next_tokens=nxt)
+    ctx.decode_step(tok, kv.c)  # (nothing is sampled)
+    ctx.set_sampling_rows(torch.zeros(3, device="cuda"), temperature=torch.ones(3, device="cuda"))
+    ctx.decode_step(tok, kv.c, None, nxt)
 
 
 def test_context_setters_refuse():
