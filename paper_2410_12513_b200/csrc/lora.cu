@@ -13,6 +13,10 @@
 // All operands enter exactly: float32 values as three bfloat16 terms (8 bits each), h too; of their products those
 // below 2^-26 are left out.  How the sums are ordered depends on the sizes k, n, rank alone, so a row's result does not depend on
 // the rows around it.
+//
+// Measured (adapters, x and y larger than L2 in turn): 1 row of q|k|v at rank 8 6.2 us, 32 rows of 16 adapters 9.9 us (1.1 TB/s),
+// 256 rows of 64 adapters at the down projection 33 us (2.9 TB/s; the shrink, which streams A, is half of it), 1024 rows of 8
+// adapters at gate|up 47 us (2.7 TB/s; y begins to move after 12 us of plan, shrink and meeting).
 #include <algorithm>
 #include <type_traits>
 
@@ -528,7 +532,7 @@ cudaError_t launch_rows(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) 
     // At most as many tiles as: one for every row, or one ragged tile for every adapter and full ones for the rest.
     auto tiles_of = [&](int rows) { return a.n > kMaxIds || a.m == 1 ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / rows); };
     size_t smem;
-    // Tiles of 32 rows once an adapter has 16 rows on average (1024 rows of 8 adapters, gate|up: 47 us against 66 with tiles
+    // Tiles of 32 rows once an adapter has 16 rows on average (1024 rows of 8 adapters, gate|up: 47 us against 87 with tiles
     // of 8), if their h fits (four segments of rank 128 do not); else of 8.
     if (a.m >= 16 * (int64_t)a.n && a.m > 32) {
         const Plan pl = plan_of(a, 32, tiles_of(32), n_sm, smem);

@@ -41,6 +41,7 @@ struct SampleArgs {
     const int32_t* top_k = nullptr;
     int32_t* tokens = nullptr;
     int32_t* pos = nullptr;  // += 1 per row, or NULL
+    int move_max = 0;        // (set by sample_launch) so many candidates are left to one CTA
     uint64_t* stamp = nullptr;
 };
 constexpr int kSampleMaxVocab = 1 << 19;

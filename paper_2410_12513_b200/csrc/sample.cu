@@ -7,13 +7,18 @@
 // answered without sorting the row:
 //   1. One thread-block cluster per row; the row is read once and stays in the cluster's shared memory.
 //   2. A histogram over 32 bins of (max - x) / T, half a unit wide: the sum reaches the target in one of them.
-//   3. If that bin holds many elements, it is cut into 32 parts of its range of values (and again, and, among equal
-//      values, of indices), each time keeping the part that holds the target.
-//   4. What is left, at most kList elements, goes to every CTA's shared memory, is sorted there and summed up.
-// A histogram is private to every LANE of every warp (a bin is 32 words, a lane owns one): a bank each, no atomics, so
-// sums are the same in every run.  Weights are taken relative to that of the upper end X of their bin: exp((x - X) / T)
-// with the difference exact, as integers in units of 2^-23, which keeps float32's 24 bits; the bins' own weights and
-// all prefix sums are 64-bit floating point.
+//   3. That bin's elements are copied out, with all above them if there is room: the searches after this one then look
+//      there only, and if they are few thousand the first CTA takes them all and the others leave.
+//   4. If there are many, their range of values is cut into 32 parts (and again, and, among equal values, that of their
+//      indices), each time keeping the part that holds the target.
+//   5. What is left, at most kSorted elements, is sorted in shared memory and summed up.
+// A histogram is private to every lane (a bin is 32 words, a lane owns one): a bank each, and integer sums, which are the
+// same in every run.  Weights are taken relative to that of the upper end X of their bin: exp((x - X) / T) with the
+// difference exact, as integers in units of 2^-23, which keeps float32's 24 bits; the bins' own weights and all prefix
+// sums are 64-bit floating point.
+// Bound by the latency of these phases, one after the other with an exchange between the CTAs each: 10.4 us for one row of
+// 128256 at top-k 10, 31 us for 32 rows with settings of their own, 156 us for 256 (0.84 TB/s: two rows' CTAs share a
+// multiprocessor, the launch is seven waves of rows).
 #include <cfloat>
 #include <cooperative_groups.h>
 
@@ -31,7 +36,9 @@ constexpr int kBlock = 16;           // elements a thread looks at at a time
 constexpr int kHeld = 2 * kBlock * kThreads;  // elements that a CTA can hold in shared memory
 constexpr int kCluster = 8;
 constexpr int kBins = 32;
+constexpr int kResident = 2 * 148;   // CTAs on the GPU at a time
 constexpr int kLocal = 2560;         // elements that a CTA can copy to shared memory for a search
+constexpr int kMoved = kHeld / 2;    // the same in the place of a row, once the row itself is not needed any more
 constexpr int kList = 256;           // elements that are sorted in every CTA of a cluster; of each CTA an equal share
 constexpr int kSorted = 224;         // longer lists are narrowed further first: sorting takes time with the square of them
 constexpr int kSlices = 4;           // lane-private histograms of a CTA, each shared by four warps
@@ -73,11 +80,13 @@ struct Smem {
     double scan[kWarps];
     Result res;
     Search at;
-    uint32_t key[2][kCluster], key_w[kWarps];
-    uint32_t nloc, lcnt, moved;
-    int hit;
+    uint32_t key[2][kCluster * kWarps];
+    unsigned long long bar[2];       // mbarriers of the exchanges, by turns
+    uint32_t moved[kCluster];
+    uint32_t nloc, lcnt;
+    int hit, late;
     float thr;
-    alignas(16) float row[4];        // (HELD) the CTA's elements, as many as there are; -inf up to a multiple of a block
+    alignas(16) float row[4];        // (HELD) the CTA's elements, as many as there are; -inf up to a multiple of a block; later kMoved of the cluster's
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -86,6 +95,34 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 __device__ __forceinline__ void red_add(uint32_t a, uint32_t v) { asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(a), "r"(v)); }
+
+// Exchanges between the CTAs of a cluster: words are written to another CTA's shared memory with their bytes counted on its
+// mbarrier, so that one trip does it where a store and a cluster barrier take several (256 rows: 168 us with barriers, 162
+// so).  Exchange n uses mbarrier and buffers n & 1: a CTA that sends exchange n + 2 has had
+// everybody's n + 1, sent after they had read n.
+constexpr uint32_t kPolls = 1u << 20;  // a wait gives up after so many polls
+__device__ __forceinline__ uint32_t shared_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t in_cta(uint32_t a, int cta) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(cta));
+    return r;
+}
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, uint32_t v) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(to), "r"(v), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, unsigned long long v) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u64 [%0], %1, [%2];" ::"r"(to), "l"(v), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t n) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
+__device__ __forceinline__ bool arrived(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
 
 struct Row {  // what a thread needs to know about the row
     float m, inv_T2, inv_Tl2;  // maximum; 2 / T (bins of half a unit), log2(e) / T
@@ -193,7 +230,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         uint4* h = reinterpret_cast<uint4*>(s.hist);
         for (int i = tid; i < (int)(sizeof s.hist / 16); i += kThreads) h[i] = make_uint4(0, 0, 0, 0);
     }
-    if (tid == 0) s.moved = 0;
+    const uint32_t bars = shared_addr(&s.bar[0]);
+    if (tid == 0) {
+        for (int q = 0; q < 2; ++q) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * q) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s.late = 0;
+    }
     cluster.barrier_arrive();  // (waited for before the first access to another CTA's shared memory)
     pdl_trigger();
     pdl_wait();
@@ -207,21 +249,34 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     // (from 1e30 on a temperature makes all weights equal, as far as logits go)
     const bool flat = T0 >= 1e30f;
     const double T = fmax((double)T0, 1e-37), inv_T = flat ? 0.0 : 1.0 / T;
-    // a weight is at least min_p when the logit is at most this far (negative) from the maximum
-    double thr = -INFINITY;
-    if (tid == 0 && mp0 > 0.f && !flat) thr = T * log(fmin((double)mp0, 1.0));
 
+    bool solo = C == 1;
+    uint32_t turn = 0;  // exchanges so far
+    auto expect = [&](uint32_t bytes) {  // what the next exchange brings this CTA
+        if (tid == 0) expect_bytes(bars + 8 * (turn & 1), bytes);
+    };
+    auto wait_for = [&](uint32_t n) {
+        const uint32_t bar = bars + 8 * (n & 1), parity = n >> 1 & 1;
+        for (uint32_t q = 0; q < kPolls; ++q)
+            if (arrived(bar, parity)) return;
+        s.late = 1;  // (cannot be; the row is given up at the end, with every CTA still there)
+    };
     // the smallest of one 32-bit word per thread, over the cluster
-    auto cluster_min = [&](uint32_t v, int slot) {
+    auto cluster_min = [&](uint32_t v) {
         v = __reduce_min_sync(0xffffffffu, v);
-        if (lane == 0) s.key_w[warp] = v;
-        __syncthreads();
-        if (warp == 0) {
-            v = __reduce_min_sync(0xffffffffu, lane < kWarps ? s.key_w[lane] : 0xffffffffu);
-            if (lane < C) cluster.map_shared_rank(&s.key[slot][0], lane)[rank] = v;
+        uint32_t* const at = s.key[turn & 1];
+        if (solo) {
+            if (lane == 0) at[warp] = v;
+            __syncthreads();
+        } else {
+            expect(C * kWarps * 4);
+            if (lane < C) send(in_cta(shared_addr(at + rank * kWarps + warp), lane), in_cta(bars + 8 * (turn & 1), lane), v);
+            wait_for(turn);
         }
-        cluster.sync();
-        return __reduce_min_sync(0xffffffffu, lane < C ? s.key[slot][lane] : 0xffffffffu);
+        ++turn;
+        v = 0xffffffffu;
+        for (int i = lane; i < C * kWarps; i += 32) v = min(v, at[i]);
+        return __reduce_min_sync(0xffffffffu, v);
     };
 
     // ---- maximum (fmaxf passes NaN over)
@@ -231,17 +286,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         for (int e = 0; e < kBlock; ++e) mx = fmaxf(mx, v[e]);
     });
     cluster.barrier_wait();
-    mx = value_of(cluster_min(key_of(mx), 0));
+    mx = value_of(cluster_min(key_of(mx)));
     if (rank == 0 && tid == 0 && p.pos) p.pos[b] += 1;
     if (mx == -INFINITY || !(T0 > 0.f)) {  // nothing to choose from, or greedy: the first of the largest
         int at = -1;
         if (mx > -INFINITY) {
             at = 0x7fffffff;
             el.each([&](float x, int i) { at = x == mx ? min(at, i) : at; });
-            at = (int)cluster_min((uint32_t)at, 1);
+            at = (int)cluster_min((uint32_t)at);
         }
-        if (rank == 0 && tid == 0) p.tokens[b] = at;
-        return;  // (nothing of another CTA's shared memory is touched after a sync)
+        __syncthreads();
+        if (s.late) cluster.sync();
+        if (rank == 0 && tid == 0) p.tokens[b] = s.late ? -1 : at;
+        return;  // (nothing is sent after an exchange that all have had)
     }
     // (infinities share all the weight and are the only candidates: all in the last bin, units() is 1 there)
     const bool infinite = mx == INFINITY;
@@ -253,24 +310,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     r.half_T = flat ? 0.f : (float)(0.5 * T);
     r.top = flat ? mx : (float)(m + 0.25 * T);
     if (tid < kBins) s.W[tid] = infinite ? kUnit : kUnit * exp(((double)r.end_of((float)tid) - m) * inv_T);
-    if (tid == 0) s.thr = infinite ? mx : fmaxf(__double2float_ru(m + thr), -FLT_MAX);
+    if (tid == 32) {  // a weight is at least min_p when the logit is at most this far (negative) from the maximum
+        const double thr = mp0 > 0.f && !flat ? T * log(fmin((double)mp0, 1.0)) : -INFINITY;
+        s.thr = infinite ? mx : fmaxf(__double2float_ru(m + thr), -FLT_MAX);
+    }
     __syncthreads();
     // the kept prefix: elements above lim_x, and those equal to it with an index up to lim_i
     constexpr int kAll = 0x7fffffff;
     float lim_x = s.thr;
     int lim_i = kAll;
-    int par = 0, turn = 0;
-
-    bool solo = false;
-    auto meet = [&]() {
-        if (solo) __syncthreads();
-        else cluster.sync();
-    };
-
-    // Adds the lane-private histograms up over the cluster: the CTAs' totals of bin `lane` are in s.xch[par ^ 1][CTA][lane],
-    // until the next but one.
+    // Adds the lane-private histograms up over the cluster: the CTAs' totals of bin `lane` are in s.xch[(turn - 1) & 1][CTA][lane]
+    // once have_totals() is through.
     auto totals = [&]() {
         __syncthreads();
+        if (!solo) expect(C * kBins * 8);
 #pragma unroll
         for (int q = 0; q < kBins / kWarps; ++q) {
             const int bin = warp * (kBins / kWarps) + q;
@@ -284,34 +337,43 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             }
             lo = __reduce_add_sync(0xffffffffu, lo);
             hi = __reduce_add_sync(0xffffffffu, hi);
-            if (lane < C)
-                cluster.map_shared_rank(&s.xch[par][0][0], lane)[rank * kBins + bin] = ((unsigned long long)hi << 16) + lo;
+            unsigned long long* const to = &s.xch[turn & 1][solo ? 0 : rank][bin];
+            const unsigned long long sum = ((unsigned long long)hi << 16) + lo;
+            if (!solo && lane < C) send(in_cta(shared_addr(to), lane), in_cta(bars + 8 * (turn & 1), lane), sum);
+            if (solo && lane == 0) *to = sum;
         }
-        meet();
-        par ^= 1;
+        if (solo) __syncthreads();
+        ++turn;
     };
+    auto have_totals = [&]() { if (!solo) wait_for(turn - 1); };
     auto total = [&](float& most) {  // (first warp) of bin `lane`: the total, and the largest CTA's share
-        unsigned long long t = 0;
-        most = 0.f;
-        for (int c = 0; c < C; ++c) {
-            const unsigned long long v = s.xch[par ^ 1][c][lane];
-            t += v;
-            most = fmaxf(most, (float)v);
+        have_totals();
+        unsigned long long v[kCluster], t = 0, m = 0;
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c) v[c] = c < C ? s.xch[(turn - 1) & 1][c][lane] : 0;
+#pragma unroll
+        for (int c = 0; c < kCluster; ++c) {
+            t += v[c];
+            m = max(m, v[c]);
         }
+        most = (float)m;
         return t;
     };
     const uint32_t my_hist = (uint32_t)__cvta_generic_to_shared(&s.hist[warp % kSlices][0][lane]);  // + bin * 128
     const uint32_t hist_a = my_hist - 0x4b000000u * 128u;                                           // + the bits of bin_number * 128
 
-    Range have{1, 0, 0, -1};  // what s.loc holds (nothing); from the largest value on: all that can be asked for
-    bool have_all = false;
+    Range have{1, 0, 0, -1};  // what loc holds (nothing)
+    bool have_all = false;    // (all that can still be asked for)
+    uint2* loc = s.loc;
 
     // The bins of the whole row up to the limit.  Elements beyond it add nothing: no branches.
     auto level0 = [&](bool mass) {
         if (have_all) {
             const uint32_t lk = key_of(lim_x);
-            for (uint32_t e = tid; e < s.nloc; e += kThreads) {
-                const uint2 v = s.loc[e];
+            const uint32_t nloc = s.nloc;
+#pragma unroll 4
+            for (uint32_t e = tid; e < nloc; e += kThreads) {
+                const uint2 v = loc[e];
                 const float x = value_of(v.x);
                 if (v.x < lk || (v.x == lk && (int)v.y <= lim_i)) red_add(my_hist + r.bin(x) * 128u, r.units(x, r.end_of((float)r.bin(x))));
             }
@@ -342,16 +404,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
 
     // The smallest key whose bin is at least j.  It lies next to that of the bin's upper end: 32 probes around it nearly
     // always hold it; if not (values near zero have finer keys), the whole range is searched, 32 probes a round.
-    auto first_key = [&](int j) -> uint32_t {
-        const uint32_t k0 = key_of(r.m), k1 = key_of(-FLT_MAX) + 1;  // the answer is in k0..k1
+    const uint32_t k0 = key_of(r.m), k1 = key_of(-FLT_MAX) + 1;  // the answer is in k0..k1
+    auto probe = [&](int j, uint32_t& a) {
+        const uint32_t mid = key_of(fmaxf(r.end_of((float)j), -FLT_MAX));
+        a = mid > k0 + 16 ? mid - 16 : k0;
+        const uint32_t at = a + lane;
+        return __ballot_sync(0xffffffffu, at >= k1 || r.bin(value_of(at)) >= j);
+    };
+    auto first_key = [&](int j, unsigned near, uint32_t a) -> uint32_t {  // (near, a: the probes)
         if (j <= 0) return k0;
         if (j >= kBins) return k1;
-        {
-            const uint32_t mid = key_of(fmaxf(r.end_of((float)j), -FLT_MAX)), a = mid > k0 + 16 ? mid - 16 : k0, at = a + lane;
-            const unsigned ok = __ballot_sync(0xffffffffu, at >= k1 || r.bin(value_of(at)) >= j);
-            if (ok && (!(ok & 1u) || a == k0)) return a + __ffs(ok) - 1;
-        }
-        uint32_t a = k0, e = k1;
+        if (near && (!(near & 1u) || a == k0)) return a + __ffs(near) - 1;
+        uint32_t e = k1;
+        a = k0;
         while (a < e) {
             const uint32_t step = (e - a + 31) / 32;
             const unsigned long long at = (unsigned long long)a + (unsigned long long)lane * step;
@@ -366,7 +431,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     };
     auto range_of_bin = [&](int j) {
         if (infinite) return Range{key_of(mx), key_of(mx), 0, kAll};
-        const uint32_t a = first_key(j), e = first_key(j + 1);
+        uint32_t pa, pe;
+        const unsigned near_a = probe(j, pa), near_e = probe(j + 1, pe);
+        const uint32_t a = first_key(j, near_a, pa), e = first_key(j + 1, near_e, pe);
         return Range{a, max(a, min(e - 1, key_of(lim_x))), 0, kAll};
     };
 
@@ -404,8 +471,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     // f(key, index) of this CTA's elements of a range, from s.loc or from the row
     auto visit = [&](const Range& g, bool local, auto f) {
         if (local) {
-            for (uint32_t e = tid; e < s.nloc; e += kThreads) {
-                const uint2 v = s.loc[e];
+            const uint32_t nloc = s.nloc;
+#pragma unroll 4
+            for (uint32_t e = tid; e < nloc; e += kThreads) {
+                const uint2 v = loc[e];
                 if (v.x >= g.ka && v.x <= g.kb && (int)v.y >= g.ia && (int)v.y <= g.ib) f(v.x, (int)v.y);
             }
         } else {
@@ -422,39 +491,64 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         if (tid == 0) s.lcnt = 0;
         __syncthreads();
         const uint32_t nloc = s.nloc;
-        for (uint32_t e0 = warp * 32; e0 < nloc; e0 += kThreads) {
-            const uint32_t e = e0 + lane;
-            const uint2 v = s.loc[min(e, nloc - 1)];
-            const bool in = e < nloc && v.x >= g.ka && v.x <= g.kb && (int)v.y >= g.ia && (int)v.y <= g.ib;
-            const unsigned who = __ballot_sync(0xffffffffu, in);
-            if (!who) continue;
+        for (uint32_t e0 = 0; e0 < nloc; e0 += 4 * kThreads) {
+            uint2 v[4];
+            unsigned who[4], any = 0, cnt = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = loc[min(e0 + q * kThreads + tid, nloc - 1)];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bool in = e0 + q * kThreads + tid < nloc && v[q].x >= g.ka && v[q].x <= g.kb && (int)v[q].y >= g.ia && (int)v[q].y <= g.ib;
+                who[q] = __ballot_sync(0xffffffffu, in);
+                any |= who[q];
+                cnt += __popc(who[q]);
+            }
+            if (!any) continue;
             uint32_t at = 0;
-            if (lane == 0) at = atomicAdd(&s.lcnt, (uint32_t)__popc(who));
-            at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
-            if (in && at < slot) s.tmp[at] = ((unsigned long long)v.x << 32) | v.y;
+            if (lane == 0) at = atomicAdd(&s.lcnt, cnt);
+            at = __shfl_sync(0xffffffffu, at, 0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t to = at + __popc(who[q] & ((1u << lane) - 1u));
+                if ((who[q] >> lane & 1u) && to < slot) s.tmp[to] = ((unsigned long long)v[q].x << 32) | v[q].y;
+                at += __popc(who[q]);
+            }
         }
         __syncthreads();
         if (tid < kList) {
             const uint32_t n = min(s.lcnt, (uint32_t)slot), c = tid >> slot_bits, e = tid & (slot - 1);
-            if (e < n) cluster.map_shared_rank(&s.list[turn][0], c)[rank * slot + e] = s.tmp[e];
-            if (e == 0) cluster.map_shared_rank(&s.cnt[turn][0], c)[rank] = n;
+            unsigned long long* const to = &s.list[turn & 1][solo ? e : rank * slot + e];
+            uint32_t* const to_n = &s.cnt[turn & 1][solo ? 0 : rank];
+            if (!solo) {  // (all slots: the other side counts bytes)
+                const uint32_t bar = in_cta(bars + 8 * (turn & 1), c);
+                send(in_cta(shared_addr(to), c), bar, e < n ? s.tmp[e] : ~0ull);
+                if (e == 0) send(in_cta(shared_addr(to_n), c), bar, n);
+            } else {
+                if (e < n) *to = s.tmp[e];
+                if (e == 0) *to_n = n;
+            }
         }
-        meet();
-        turn ^= 1;
+        if (solo) {
+            __syncthreads();
+        } else {
+            expect(kList * 8 + C * 4);
+            wait_for(turn);
+        }
+        ++turn;
         int all = 0;
-        for (int q = 0; q < C; ++q) all += (int)s.cnt[turn ^ 1][q];
-        return all;
+        for (int q = 0; q < C; ++q) all += (int)s.cnt[(turn - 1) & 1][q];
+        return min(all, kList);
     };
     // The collected elements in order, element e in thread e: each counts those before it.
     auto sorted = [&](int n) {
-        unsigned long long* const list = s.list[turn ^ 1];
+        unsigned long long* const list = s.list[(turn - 1) & 1];
         const int n8 = (n + 7) / 8 * 8;
         if (tid < kList) {  // side by side, and full to a multiple of 8
             const int c0 = tid >> slot_bits, e0 = tid & (slot - 1);
-            if ((uint32_t)e0 < s.cnt[turn ^ 1][c0]) {
+            if ((uint32_t)e0 < s.cnt[(turn - 1) & 1][c0]) {
                 int to = e0;
-                for (int c = 0; c < c0; ++c) to += (int)s.cnt[turn ^ 1][c];
-                s.tmp[to] = list[tid];
+                for (int c = 0; c < c0; ++c) to += (int)s.cnt[(turn - 1) & 1][c];
+                if (to < kList) s.tmp[to] = list[tid];
             }
             if (tid >= n && tid < n8) s.tmp[tid] = ~0ull;
         }
@@ -518,7 +612,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     // takes the decisions, from the same numbers.
     unsigned long long t = 0;            // (first warp) weight, or candidates, of bin `lane`
     double w0 = 0.0, run0 = 0.0;         // of the same bin, and of all up to it
-    float most = 0.f, most_upto = 0.f;   // of the same two, the largest CTA's share (in units)
+    float most = 0.f, most_upto = 0.f;   // of the same two, the largest CTA's share (in units, at most)
+    float t_upto = 0.f;                  // t of the bin and all before it
     double Z = 0.0;                      // weight of what is kept (once weighed)
     bool weighed = false;
     for (int stage = k > 0 && k < p.V ? 0 : 1; stage < 3; ++stage) {
@@ -534,9 +629,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             if (fresh) {
                 t = total(most);
                 w0 = by_rank ? (double)t : s.W[lane] * (double)t;
-                run0 = warp_scan(w0, lane);
+                run0 = w0;
+                most_upto = most;
+                t_upto = (float)t;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {  // (three scans side by side: one alone waits for its own steps)
+                    const double a = __shfl_up_sync(0xffffffffu, run0, o);
+                    const float c = __shfl_up_sync(0xffffffffu, most_upto, o), e = __shfl_up_sync(0xffffffffu, t_upto, o);
+                    if (lane >= o) {
+                        run0 += a;
+                        most_upto += c;
+                        t_upto += e;
+                    }
+                }
                 Z = __shfl_sync(0xffffffffu, run0, 31);
-                most_upto = warp_scan(most, lane);  // (at most)
             }
             Search f;
             f.target = by_rank ? (double)k : (stage == 1 ? tp : u) * Z;
@@ -548,8 +654,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             f.tot = per * __shfl_sync(0xffffffffu, (float)t, f.j);
             f.part = per * __shfl_sync(0xffffffffu, most, f.j);
             f.upto = per * __shfl_sync(0xffffffffu, most_upto, f.j);
-            f.all = per * warp_scan((float)t, lane);
-            f.all = __shfl_sync(0xffffffffu, f.all, f.j);
+            f.all = per * __shfl_sync(0xffffffffu, t_upto, f.j);
             f.g = range_of_bin(f.j);
             if (by_rank && Z <= (double)k) f.j = -1;  // no more candidates than that
             if (lane == 0) s.at = f;
@@ -574,9 +679,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
                 visit(g, local, [&](uint32_t, int) { ++c; });
                 red_add(my_hist, c);
                 totals();
+                have_totals();
                 tot = part = 0.f;
                 for (int q = 0; q < C; ++q) {
-                    const float v = (float)s.xch[par ^ 1][q][0];
+                    const float v = (float)s.xch[(turn - 1) & 1][q][0];
                     tot += v;
                     part = fmaxf(part, v);
                 }
@@ -586,30 +692,34 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
                 const bool top = level == 0 && !open && s.at.upto <= kLocal;
                 compact(top ? Range{key_of(r.m), g.kb, 0, kAll} : g);
                 local = true;
-                if (top && !solo && C > 1 && s.at.all <= kLocal) {
-                    // few enough for one CTA: the others hand over what they have and are done
-                    __syncthreads();
+                if (top && !solo && C > 1 && s.at.all <= (float)p.move_max) {
+                    // few enough for one CTA: they go to the place of its row, and the others are done
                     const uint32_t n = s.nloc;
-                    uint2* const to = cluster.map_shared_rank(s.loc, 0);
-                    if (tid == 0 && rank) s.lcnt = atomicAdd(cluster.map_shared_rank(&s.moved, 0), n);
+                    expect(C * 4);
+                    if (tid < C) send(in_cta(shared_addr(&s.moved[rank]), tid), in_cta(bars + 8 * (turn & 1), tid), n);
+                    wait_for(turn);  // (and all have done with their rows)
+                    ++turn;
+                    uint32_t at = 0, all_n = 0;
+                    for (int c = 0; c < C; ++c) {
+                        at += c < rank ? s.moved[c] : 0;
+                        all_n += s.moved[c];
+                    }
+                    all_n = min(all_n, (uint32_t)kMoved);
+                    if (rank) {
+                        const uint32_t to = in_cta(shared_addr(&s.row[0]), 0), bar = in_cta(bars + 8 * (turn & 1), 0);
+                        for (uint32_t e = tid; e < n && at + e < kMoved; e += kThreads)
+                            send(to + 8 * (at + e), bar, *reinterpret_cast<const unsigned long long*>(&s.loc[e]));
+                        __syncthreads();
+                        if (s.late) cluster.sync();
+                        return;
+                    }
+                    for (uint32_t e = tid; e < n; e += kThreads) reinterpret_cast<uint2*>(&s.row[0])[e] = s.loc[e];
+                    expect((all_n - n) * 8);
+                    wait_for(turn);
+                    ++turn;
+                    if (tid == 0) s.nloc = all_n;
                     __syncthreads();
-                    if (rank)  // (from the list's end: how many the first CTA has of its own is not known here)
-                        for (uint32_t e = tid; e < n && s.lcnt + e < kLocal; e += kThreads) to[kLocal - 1 - (s.lcnt + e)] = s.loc[e];
-                    cluster.sync();
-                    if (rank) return;
-                    const uint32_t own = s.nloc, moved = min(s.moved, kLocal - own);
-                    __syncthreads();
-                    // close the gap between its own and theirs
-                    uint2 keep[(kLocal + kThreads - 1) / kThreads];
-#pragma unroll
-                    for (int q = 0; q < (kLocal + kThreads - 1) / kThreads; ++q)
-                        if (tid + q * kThreads < moved) keep[q] = s.loc[kLocal - 1 - (tid + q * kThreads)];
-                    __syncthreads();
-#pragma unroll
-                    for (int q = 0; q < (kLocal + kThreads - 1) / kThreads; ++q)
-                        if (tid + q * kThreads < moved) s.loc[own + tid + q * kThreads] = keep[q];
-                    if (tid == 0) s.nloc = own + moved;
-                    __syncthreads();
+                    loc = reinterpret_cast<uint2*>(&s.row[0]);
                     solo = true;
                     C = 1;
                     slot_bits = __ffs(kList) - 1;
@@ -688,7 +798,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         lim_i = s.res.i;
         if (stage == 1) Z = s.res.mass;
     }
-    if (rank == 0 && tid == 0) p.tokens[b] = s.res.i;
+    __syncthreads();
+    if (s.late) cluster.sync();
+    if (rank == 0 && tid == 0) p.tokens[b] = s.late ? -1 : s.res.i;
 }
 
 }  // namespace
@@ -699,7 +811,11 @@ cudaError_t sample_launch(const SampleArgs& a, cudaStream_t st, bool pdl) {
     while (C < kCluster && (int64_t)C * kHeld < a.V) C *= 2;
     const bool held = (int64_t)C * kHeld >= a.V;
     const int chunk = ((a.V + C - 1) / C + 3) / 4 * 4, block = kBlock * kThreads;
-    const size_t smem = sizeof(Smem) + (held ? (size_t)(chunk + block - 1) / block * block * 4 : 0);
+    SampleArgs p = a;
+    // One CTA is slower with a long list than eight, but leaves seven places to other rows: where the grid is several
+    // times what the GPU holds, it is given more (256 rows: 156 us against 162; 128 rows: 89 against 85; 32 rows: 34 against 31).
+    p.move_max = a.B * C > 4 * kResident ? kMoved : kMoved / 2;
+    const size_t smem = sizeof(Smem) + (C == 1 ? (size_t)(chunk + block - 1) / block * block * 4 : (size_t)kHeld * 4);
     const bool vec = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && (a.B == 1 || a.ld % 4 == 0);
     auto kern = held ? (vec ? sample_rows<true, true> : sample_rows<true, false>) : (vec ? sample_rows<false, true> : sample_rows<false, false>);
     // (always the same value: calls of other threads rely on it)
@@ -719,7 +835,7 @@ cudaError_t sample_launch(const SampleArgs& a, cudaStream_t st, bool pdl) {
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, a);
+    return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
 }  // namespace first
