@@ -389,6 +389,22 @@ def test_sample_mixed_settings(B, V, pad, spread):
     _sample_check(x, g.random(B).astype(np.float32), *_settings(B, g), pad=pad)
 
 
+@pytest.mark.parametrize("B", [24, 160])
+@pytest.mark.parametrize("V", [40001, 70000])
+def test_sample_long_candidate_lists(B, V):
+    """Thousands of candidates, which one CTA takes over from its cluster or not, by how many rows there are."""
+    g = np.random.default_rng(B + V)
+    x = (1.5 * g.standard_normal((B, V))).astype(np.float32)
+    t = (0.6 + 0.9 * g.random(B)).astype(np.float32)
+    k = np.where(np.arange(B) % 3 == 0, 0, g.integers(1500, 11000, B)).astype(np.int32)
+    p = np.where(np.arange(B) % 4 == 3, 1.0, 0.4 + 0.6 * g.random(B)).astype(np.float32)
+    _sample_check(x, g.random(B).astype(np.float32), t, k, p)
+    x[:, ::2] = np.round(x[:, ::2])  # half of them in large ties, at the lists' borders too
+    _sample_check(x, g.random(B).astype(np.float32), t, k, p)
+    x = np.sort(x, axis=1)           # all in the cluster's last CTA
+    _sample_check(x, g.random(B).astype(np.float32), t, k, p)
+
+
 @pytest.mark.parametrize("which", ["temp", "k", "p", "mp", "plain"])
 def test_sample_one_filter_alone(which):
     g = np.random.default_rng(3)
