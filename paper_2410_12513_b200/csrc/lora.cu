@@ -318,10 +318,11 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         }
         __syncthreads();
     }
-    // ---- expand, set-up: a step = 32 output features of one segment and 16 rows of the tile; as the tensor cores lay them
-    // out, a thread has eight consecutive features of the rows g and g + 8, so y moves 16 bytes at a time.  The operands of a
-    // warp's next steps are copied to shared memory in the background (each thread reads what it copied itself); the
-    // first ones are on their way while the cluster meets.
+    // ---- expand, set-up: a step = 32 output features of one segment and 16 rows of the tile; as the rows of B are dealt out to
+    // the tensor cores' columns, a thread has eight consecutive features of the rows g and g + 8, so y moves 16 bytes at a
+    // time.  Where y's rows are not aligned for that (`odd`; tiles of 8 rows only) it has the pairs 8j + 2t, so that a row's
+    // four threads touch neighbours (40 rows of 25433 features: 47 us, with eight apiece 94).  The operands of a warp's next steps are copied to shared memory (odd y: to L2) in the
+    // background (each thread reads what it copied itself); the first ones are on their way while the cluster meets.
     constexpr int HR = TR == 8 ? 1 : 2;  // 8-row halves of a 16-row tile that are used
     constexpr int D = steps_ahead(TR);   // steps in flight
     int steps = 0;                       // (of 32 features)
@@ -330,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
     const int first = min(steps, (slice * kCluster + rank) * per), last = min(steps, first + per);
     // with a second 16-row tile in use every other warp has that one
     const bool two = live > 16;
+    const bool odd = TR == 8 && !pl.y_vec;
     const int q = two ? warp & 1 : 0, stride = two ? kWarps / 2 : kWarps;
     const int mine = max(0, (last - first - (two ? warp >> 1 : warp) + stride - 1) / stride);  // this warp's steps
     struct Place {  // of a step: its features, the end of their segment, and the segment
@@ -353,19 +355,19 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
 #pragma unroll
     for (int h = 0; h < HR; ++h) {
         const int c = q * 16 + h * 8 + g, i = rows_s[c];
-        y_row[h] = c < live ? static_cast<YT*>(p.y) + (int64_t)(p.scatter ? p.idx[i] : i) * p.ldy + 8 * t : nullptr;
+        y_row[h] = c < live ? static_cast<YT*>(p.y) + (int64_t)(p.scatter ? p.idx[i] : i) * p.ldy + (odd ? 2 : 8) * t : nullptr;
     }
     const int kbs = (p.R + 15) / 16;
     constexpr int YV = sizeof(YT) / 2;  // 16-byte words of eight elements
-    struct Step {  // of one thread: y, and columns 0..15 of B (features 2j, 2j+1 of every eight in part j)
+    struct Step {  // of one thread: y, and columns 0..15 of B (part j: features 2j, 2j+1 of every eight; odd: the j-th eight)
         uint4 y[HR * YV][32];
         typename std::conditional<sizeof(WT) == 2, uint2, uint4>::type w[4][32];
     };
     Step* const ring = reinterpret_cast<Step*>(pool) + warp * D;
     const WT* const B = static_cast<const WT*>(p.b) + (int64_t)ad * p.N * p.R + 4 * t;
-    const int fw = (g >> 1) * 8 + (g & 1);  // this thread's row of B in part 0
+    const int fw = odd ? g : (g >> 1) * 8 + (g & 1), fj = odd ? 8 : 2;  // this thread's row of B in part 0; from part to part
     const bool in0 = 4 * t < p.R;           // (a rank of 8 has no columns 8..15)
-    auto w_row = [&](int f0, int j) { return B + (int64_t)min(f0 + fw + 2 * j, p.N - 1) * p.R; };
+    auto w_row = [&](int f0, int j) { return B + (int64_t)min(f0 + fw + fj * j, p.N - 1) * p.R; };
     auto fetch = [&](const Place& at, Step& d) {
         if (pl.y_vec && at.f0 + 8 * t + 8 <= at.end) {
 #pragma unroll
@@ -374,10 +376,12 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
 #pragma unroll
                     for (int v = 0; v < YV; ++v) copy_async<16>(&d.y[h * YV + v][lane], reinterpret_cast<const uint4*>(y_row[h] + at.f0) + v, true);
         }
+        if constexpr (TR == 8)  // (the four threads' addresses are a quarter of the step apart)
+            if (odd && y_row[0] && at.f0 + 8 * t < at.end) asm volatile("prefetch.global.L2 [%0];" ::"l"(y_row[0] + at.f0 + 6 * t));
         if (at.f0 + 32 <= p.N) {
             const WT* w = B + (int64_t)(at.f0 + fw) * p.R;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], in0 ? w + 2 * j * p.R : B - 4 * t, in0);
+            for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], in0 ? w + fj * j * p.R : B - 4 * t, in0);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], in0 ? w_row(at.f0, j) : B - 4 * t, in0);
@@ -467,6 +471,15 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
                 }
 #pragma unroll
                 for (int i = 0; i < YV; ++i) reinterpret_cast<uint4*>(y)[i] = v[i];
+            } else if constexpr (TR == 8) {
+                const int left = end - f0 - (odd ? 2 : 8) * t;  // elements up to the segment's end
+                YT o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if ((e >> 1) * fj + (e & 1) < left) o[e] = y[(e >> 1) * fj + (e & 1)];
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if ((e >> 1) * fj + (e & 1) < left) y[(e >> 1) * fj + (e & 1)] = from_f32<YT>(to_f32(o[e]) + acc[e >> 1][2 * h + (e & 1)]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -533,10 +546,11 @@ cudaError_t launch_rows(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) 
     auto tiles_of = [&](int rows) { return a.n > kMaxIds || a.m == 1 ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / rows); };
     size_t smem;
     // Tiles of 32 rows once an adapter has 16 rows on average (1024 rows of 8 adapters, gate|up: 47 us against 87 with tiles
-    // of 8), if their h fits (four segments of rank 128 do not); else of 8.
-    if (a.m >= 16 * (int64_t)a.n && a.m > 32) {
+    // of 8) and they fill the GPU (362 rows of 8 adapters, 152 CTAs: 38 us against 28 with tiles of 8), if their h fits (four
+    // segments of rank 128 do not) and y is aligned; else of 8.
+    if (a.m >= 16 * (int64_t)a.n && a.m > 32 && 2 * tiles_of(32) * kCluster > 3 * n_sm) {
         const Plan pl = plan_of(a, 32, tiles_of(32), n_sm, smem);
-        if (smem <= kMaxSmem) return launch_tiles<XK, WT, YT, 32, 2>(a, pl, smem, st, pdl);
+        if (smem <= kMaxSmem && pl.y_vec) return launch_tiles<XK, WT, YT, 32, 2>(a, pl, smem, st, pdl);
     }
     const int tiles = tiles_of(8);
     const Plan pl = plan_of(a, 8, tiles, n_sm, smem);

@@ -196,6 +196,25 @@ def test_lora_whole_numbers(case, xt, wt):
     assert np.array_equal(y.double().cpu().numpy(), ref)
 
 
+@pytest.mark.parametrize("types", [("bf16", "f32", "bf16"), ("f32", "bf16", "bf16"), ("bf16", "bf16", "f32"), ("f32", "f32", "f32")], ids=str)
+@pytest.mark.parametrize("case", [(1000, 3, 24, 264, (0, 64, 176)), (960, 1, 128, 520, (0, 48, 208)), (960, 8, 56, 1032, (0, 1000)),
+                                  (1500, 2, 8, 72, (0, 16, 32, 80, 96)), (300, 9, 40, 200, (0, 160, 431)), (700, 2, 16, 96, (0, 801))], ids=str)
+def test_lora_many_rows(case, types):
+    """Whole and ragged tiles of many rows, aligned and not; steps that end inside a segment."""
+    import torch
+    from paper_2410_12513_b200 import first_lora
+    x, a, b, ids, y, g = _lora_inputs(case, *(_t(v) for v in types), 29)
+    rows, n, rank, k, seg = case
+    scales = torch.rand(n, generator=g) * 2 - 1
+    ref, mag = _lora_ref(x, a, b, ids, y, scales, seg)
+    y0 = y.clone()
+    first_lora(x, a, b, ids, y, scales=scales.cuda(), segments=seg)
+    tol = (k / 8 + rank + 24) * U32 * mag + (2.0 ** -8 * np.abs(ref) if types[1] == "bf16" else 0.0)  # (as in test_lora)
+    assert (np.abs(y.double().cpu().numpy() - ref) <= tol).all()
+    idle = (ids < 0) | (ids >= n)
+    assert torch.equal(y[idle], y0[idle])
+
+
 def test_lora_padded_rows_empty_batch_and_bit_reproducible():
     import torch
     from paper_2410_12513_b200 import first_lora
