@@ -15,7 +15,7 @@
 // the rows around it.
 //
 // Measured (adapters, x and y larger than L2 in turn): 1 row of q|k|v at rank 8 6.2 us, 32 rows of 16 adapters 9.9 us (1.1 TB/s),
-// 256 rows of 64 adapters at the down projection 33 us (2.9 TB/s; the shrink, which streams A, is half of it), 1024 rows of 8
+// 256 rows of 64 adapters at the down projection 33 us (2.9 TB/s; the shrink, which streams A, is more than half of it), 1024 rows of 8
 // adapters at gate|up 47 us (2.7 TB/s; y begins to move after 12 us of plan, shrink and meeting).
 #include <algorithm>
 #include <type_traits>
