@@ -408,8 +408,7 @@ def test_sample_mixed_settings(B, V, pad, spread):
     _sample_check(x, g.random(B).astype(np.float32), *_settings(B, g), pad=pad)
 
 
-@pytest.mark.parametrize("B", [24, 160])
-@pytest.mark.parametrize("V", [40001, 70000])
+@pytest.mark.parametrize("B,V", [(24, 20011), (24, 40001), (160, 40001), (24, 70000), (160, 70000), (24, 140003)])
 def test_sample_long_candidate_lists(B, V):
     """Thousands of candidates, which one CTA takes over from its cluster or not, by how many rows there are."""
     g = np.random.default_rng(B + V)
