@@ -110,6 +110,10 @@ __device__ __forceinline__ void copy_async(void* to, const void* from, bool live
     if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(a), "l"(from), "r"(n) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(a), "l"(from), "r"(n) : "memory");
 }
+__device__ __forceinline__ void copy_word(void* to, int word, const void* from) {
+    const uint32_t a = (uint32_t)__cvta_generic_to_shared(to) + 4 * word;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(a), "l"(from) : "memory");
+}
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -321,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
     // ---- expand, set-up: a step = 32 output features of one segment and 16 rows of the tile; as the rows of B are dealt out to
     // the tensor cores' columns, a thread has eight consecutive features of the rows g and g + 8, so y moves 16 bytes at a
     // time.  Where y's rows are not aligned for that (`odd`; tiles of 8 rows only) it has the pairs 8j + 2t, so that a row's
-    // four threads touch neighbours (40 rows of 25433 features: 47 us, with eight apiece 94).  The operands of a warp's next steps are copied to shared memory (odd y: to L2) in the
+    // four threads touch neighbours (40 rows of 25433 features: 45 us, with eight apiece 94).  The operands of a warp's next steps are copied to shared memory (odd y partly to L2 only) in the
     // background (each thread reads what it copied itself); the first ones are on their way while the cluster meets.
     constexpr int HR = TR == 8 ? 1 : 2;  // 8-row halves of a 16-row tile that are used
     constexpr int D = steps_ahead(TR);   // steps in flight
@@ -332,6 +336,9 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
     // with a second 16-row tile in use every other warp has that one
     const bool two = live > 16;
     const bool odd = TR == 8 && !pl.y_vec;
+    // odd y word by word, where that costs no spills (63 rows of 16793 features 55 -> 49 us; with 64 registers 256 rows of down,
+    // which have nothing of it, 34 -> 36)
+    constexpr bool kWords = TR == 8 && OCC == 2 && sizeof(YT) == 4;
     const int q = two ? warp & 1 : 0, stride = two ? kWarps / 2 : kWarps;
     const int mine = max(0, (last - first - (two ? warp >> 1 : warp) + stride - 1) / stride);  // this warp's steps
     struct Place {  // of a step: its features, the end of their segment, and the segment
@@ -376,8 +383,17 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
 #pragma unroll
                     for (int v = 0; v < YV; ++v) copy_async<16>(&d.y[h * YV + v][lane], reinterpret_cast<const uint4*>(y_row[h] + at.f0) + v, true);
         }
-        if constexpr (TR == 8)  // (the four threads' addresses are a quarter of the step apart)
-            if (odd && y_row[0] && at.f0 + 8 * t < at.end) asm volatile("prefetch.global.L2 [%0];" ::"l"(y_row[0] + at.f0 + 6 * t));
+        if constexpr (TR == 8) {
+            if (odd && y_row[0]) {
+                if constexpr (kWords) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (at.f0 + 2 * t + (e >> 1) * 8 + (e & 1) < at.end) copy_word(&d.y[e >> 2][lane], e & 3, y_row[0] + at.f0 + (e >> 1) * 8 + (e & 1));
+                } else if (at.f0 + 8 * t < at.end) {  // (the four threads' addresses are a quarter of the step apart)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(y_row[0] + at.f0 + 6 * t));
+                }
+            }
+        }
         if (at.f0 + 32 <= p.N) {
             const WT* w = B + (int64_t)(at.f0 + fw) * p.R;
 #pragma unroll
@@ -423,11 +439,20 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         const int f0 = here.f0, end = here.end;
         float acc[4][4] = {};
         const __nv_bfloat16* const h_tile = hs + (here.s * 3 * TR + q * 16 + g) * pl.h_stride + 4 * t;
+        [[maybe_unused]] Frag<NW, 4> w_next[4];
         for (int kb = 0; kb < kbs; ++kb) {
             Frag<NW, 4> w[4];
+            if constexpr (TR == 8 && OCC == 2) {  // (there are registers for the next columns: 9 rows of rank 56 in float32 15 us, without 18)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = kb ? load_frag<WT, 4>(w_row(f0, j) + kb * 16, kb * 16 + 4 * t < p.R) : shared_frag<WT>(&cur.w[j][lane]);
+                for (int j = 0; j < 4; ++j) w[j] = kb ? w_next[j] : shared_frag<WT>(&cur.w[j][lane]);
+                if (kb + 1 < kbs)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w_next[j] = load_frag<WT, 4>(w_row(f0, j) + kb * 16 + 16, kb * 16 + 16 + 4 * t < p.R);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = kb ? load_frag<WT, 4>(w_row(f0, j) + kb * 16, kb * 16 + 4 * t < p.R) : shared_frag<WT>(&cur.w[j][lane]);
+            }
             float blk[4][4] = {};
 #pragma unroll
             for (int k = 2; k >= 0; --k) {
@@ -476,7 +501,10 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
                 YT o[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if ((e >> 1) * fj + (e & 1) < left) o[e] = y[(e >> 1) * fj + (e & 1)];
+                    if ((e >> 1) * fj + (e & 1) < left) {
+                        if (kWords && odd) o[e] = reinterpret_cast<const YT*>(&cur.y[(e >> 2) % (HR * YV)][lane])[e & 3];
+                        else o[e] = y[(e >> 1) * fj + (e & 1)];
+                    }
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     if ((e >> 1) * fj + (e & 1) < left) y[(e >> 1) * fj + (e & 1)] = from_f32<YT>(to_f32(o[e]) + acc[e >> 1][2 * h + (e & 1)]);
