@@ -575,11 +575,13 @@ cudaError_t launch_rows(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) 
     size_t smem;
     // Tiles of 32 rows once an adapter has 16 rows on average (1024 rows of 8 adapters, gate|up: 47 us against 87 with tiles
     // of 8) and they fill the GPU (362 rows of 8 adapters, 152 CTAs: 38 us against 28 with tiles of 8), if their h fits (four
-    // segments of rank 128 do not) and y is aligned; else of 8.
-    if (a.m >= 16 * (int64_t)a.n && a.m > 32 && 2 * tiles_of(32) * kCluster > 3 * n_sm) {
-        const Plan pl = plan_of(a, 32, tiles_of(32), n_sm, smem);
-        if (smem <= kMaxSmem && pl.y_vec) return launch_tiles<XK, WT, YT, 32, 2>(a, pl, smem, st, pdl);
-    }
+    // segments of rank 128 do not) and y is aligned; else of 8.  (x in two halves comes from the step, whose batches and
+    // prompt chunks have too few rows for them.)
+    if constexpr (XK != kLoraXPair)
+        if (a.m >= 16 * (int64_t)a.n && a.m > 32 && 2 * tiles_of(32) * kCluster > 3 * n_sm) {
+            const Plan pl = plan_of(a, 32, tiles_of(32), n_sm, smem);
+            if (smem <= kMaxSmem && pl.y_vec) return launch_tiles<XK, WT, YT, 32, 2>(a, pl, smem, st, pdl);
+        }
     const int tiles = tiles_of(8);
     const Plan pl = plan_of(a, 8, tiles, n_sm, smem);
     // With 64 registers four CTAs fit on a multiprocessor instead of two, at the price of spills: 256 rows of 64 adapters
