@@ -292,6 +292,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         int at = -1;
         if (mx > -INFINITY) {
             at = 0x7fffffff;
+            __syncthreads();  // (the row's copy was written by other threads than those that read it now)
             el.each([&](float x, int i) { at = x == mx ? min(at, i) : at; });
             at = (int)cluster_min((uint32_t)at);
         }
@@ -528,12 +529,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
                 if (e == 0) *to_n = n;
             }
         }
-        if (solo) {
-            __syncthreads();
-        } else {
-            expect(kList * 8 + C * 4);
-            wait_for(turn);
-        }
+        if (!solo) expect(kList * 8 + C * 4);
+        __syncthreads();  // (tmp is written again once the lists are there: by then every warp has sent its part of it)
+        if (!solo) wait_for(turn);
         ++turn;
         int all = 0;
         for (int q = 0; q < C; ++q) all += (int)s.cnt[(turn - 1) & 1][q];
@@ -680,6 +678,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
                 red_add(my_hist, c);
                 totals();
                 have_totals();
+                __syncthreads();  // (the histograms are counted into again: every warp has cleared its bins)
                 tot = part = 0.f;
                 for (int q = 0; q < C; ++q) {
                     const float v = (float)s.xch[(turn - 1) & 1][q][0];
@@ -717,6 +716,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
                     expect((all_n - n) * 8);
                     wait_for(turn);
                     ++turn;
+                    __syncthreads();  // (every warp has read its CTA's own count: the waits above are for other CTAs only)
                     if (tid == 0) s.nloc = all_n;
                     __syncthreads();
                     loc = reinterpret_cast<uint2*>(&s.row[0]);

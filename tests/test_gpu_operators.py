@@ -566,6 +566,27 @@ def test_sample_on_another_stream_in_a_graph_and_bit_reproducible():
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("B,V", [(200, 128256), (96, 40001), (64, 20011)])
+def test_sample_is_the_same_beside_other_work(B, V):
+    """The exchanges inside a cluster and the hand-over to one CTA while other kernels delay some of its warps: every
+    run gives the same tokens, and they are the definition's."""
+    import torch
+    g = np.random.default_rng(B)
+    x = (1.7 * g.standard_normal((B, V))).astype(np.float32)
+    u, (t, k, p, mp) = g.random(B).astype(np.float32), _settings(B, g)
+    want = _sample_check(x, u, t, k, p, mp)
+    from paper_2410_12513_b200 import first_sample
+    dev = [torch.from_numpy(np.asarray(v, dtype=d)).cuda() for v, d in ((t, np.float32), (k, np.int32), (p, np.float32), (mp, np.float32))]
+    xd, ud, tok = torch.from_numpy(x).cuda(), torch.from_numpy(u).cuda(), torch.empty(B, dtype=torch.int32, device="cuda")
+    side, noise = torch.cuda.Stream(), torch.randn(1 << 22, device="cuda")
+    for _ in range(30):
+        with torch.cuda.stream(side):
+            for _ in range(8):
+                noise.mul_(1.0000001)
+        first_sample(xd, ud, tok, *dev)
+        assert np.array_equal(tok.cpu().numpy(), want)
+
+
 # ------------------------------------------------------------------ inside the step
 ADAPTED = fi.ModelShape(3, 256, 8, 2, 64, 352, 512, 10000.0)
 
