@@ -469,14 +469,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
         __syncthreads();
         have = g;
     };
-    // f(key, index) of this CTA's elements of a range, from s.loc or from the row
+    // f(key, index) of this CTA's elements of a range, from loc or from the row.  (loc may have been filled before a top-k cut
+    // among equal logits: those behind the cut are passed over.)
     auto visit = [&](const Range& g, bool local, auto f) {
         if (local) {
-            const uint32_t nloc = s.nloc;
+            const uint32_t nloc = s.nloc, lk = key_of(lim_x);
 #pragma unroll 4
             for (uint32_t e = tid; e < nloc; e += kThreads) {
                 const uint2 v = loc[e];
-                if (v.x >= g.ka && v.x <= g.kb && (int)v.y >= g.ia && (int)v.y <= g.ib) f(v.x, (int)v.y);
+                if (v.x >= g.ka && v.x <= g.kb && (int)v.y >= g.ia && (int)v.y <= g.ib && (v.x != lk || (int)v.y <= lim_i)) f(v.x, (int)v.y);
             }
         } else {
             el.each([&](float x, int i) {
@@ -491,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     auto gather = [&](const Range& g) {
         if (tid == 0) s.lcnt = 0;
         __syncthreads();
-        const uint32_t nloc = s.nloc;
+        const uint32_t nloc = s.nloc, lk = key_of(lim_x);
         for (uint32_t e0 = 0; e0 < nloc; e0 += 4 * kThreads) {
             uint2 v[4];
             unsigned who[4], any = 0, cnt = 0;
@@ -499,7 +500,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
             for (int q = 0; q < 4; ++q) v[q] = loc[min(e0 + q * kThreads + tid, nloc - 1)];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const bool in = e0 + q * kThreads + tid < nloc && v[q].x >= g.ka && v[q].x <= g.kb && (int)v[q].y >= g.ia && (int)v[q].y <= g.ib;
+                const bool in = e0 + q * kThreads + tid < nloc && v[q].x >= g.ka && v[q].x <= g.kb && (int)v[q].y >= g.ia && (int)v[q].y <= g.ib &&
+                                (v[q].x != lk || (int)v[q].y <= lim_i);
                 who[q] = __ballot_sync(0xffffffffu, in);
                 any |= who[q];
                 cnt += __popc(who[q]);

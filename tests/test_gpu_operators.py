@@ -566,6 +566,27 @@ def test_sample_on_another_stream_in_a_graph_and_bit_reproducible():
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("V", [300, 1000, 2000, 4096, 16384, 20000, 40000, 70000, 128256])
+@pytest.mark.parametrize("top", [0, 5])
+def test_sample_top_k_cuts_a_run_of_equal_logits(V, top):
+    """The k-th candidate stands inside a run of equal logits, of hundreds to thousands in one CTA or spread over a
+    cluster, alone or below a few larger ones: those behind it are out, in every later search too."""
+    g = np.random.default_rng(V + top)
+    B = 12
+    for n in (300, 800, 2000, 2500):
+        n = min(n, V - top)
+        x = (-3.0 - g.random((B, V))).astype(np.float32)
+        for r in range(B):
+            at = np.sort(g.choice(V, n + top, replace=False)) if r % 3 else np.arange(n + top) + int(g.integers(0, V - n - top + 1))
+            x[r, at] = 0.25
+            x[r, g.choice(at, top, replace=False)] = 0.5 + 0.1 * np.arange(top, dtype=np.float32)
+        u = ((np.arange(B) + 0.37) / B).astype(np.float32)
+        for k in (1 + top, 10, 100, 225):
+            _sample_check(x, u, k=np.full(B, k))
+            _sample_check(x, u, k=np.full(B, k), p=np.full(B, 0.7))
+            _sample_check(x, u, k=np.full(B, k), temp=np.full(B, 4.0), mp=np.full(B, 0.01))
+
+
 @pytest.mark.parametrize("B,V", [(200, 128256), (96, 40001), (64, 20011)])
 def test_sample_is_the_same_beside_other_work(B, V):
     """The exchanges inside a cluster and the hand-over to one CTA while other kernels delay some of its warps: every
