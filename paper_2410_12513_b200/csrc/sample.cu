@@ -126,17 +126,22 @@ __device__ __forceinline__ bool arrived(uint32_t bar, uint32_t parity) {
 
 struct Row {  // what a thread needs to know about the row
     float m, inv_T2, inv_Tl2;  // maximum; 2 / T (bins of half a unit), log2(e) / T
-    float half_T, top;         // T / 2; upper end of the first bin, m + T / 4
+    float half_T, top;         // T / 2; upper end of the first bin, m + T / 4 - shift
+    float shift;               // what a weight's argument is measured from: 0, or m where T is a few steps of m
     // 2^23 + bin, as a float (monotone in x, like every step of it; NaN lands in the last bin)
     __device__ __forceinline__ float bin_number(float x) const { return fminf((m - x) * inv_T2, (float)(kBins - 1)) + 8388608.f; }
     __device__ __forceinline__ int bin(float x) const { return (int)(__float_as_uint(bin_number(x)) & (kBins - 1)); }
-    __device__ __forceinline__ float end_of(float bin) const { return fmaf(-bin, half_T, top); }  // a bin's upper end
-    // weight of x in units of 2^-23 of that of its bin's upper end X (x - X is exact but where it does not matter; it is
-    // above 0 by a rounding at most): at most 2^23 - 1, so that 512 of them have 32 bits
+    // a bin's upper end, above shift; rounded up, so that no element of the bin is above it
+    __device__ __forceinline__ float end_of(float bin) const { return __fmaf_ru(-bin, half_T, top); }
+    // Weight of x in units of 2^-23 of that of its bin's upper end X (x - shift - X is exact but where it does not matter; it
+    // is above 0 by a rounding at most): at most 2^23 - 1, so that 512 of them have 32 bits.
     __device__ __forceinline__ uint32_t units(float x, float X) const {
-        return __float_as_uint(ex2(fminf((x - X) * inv_Tl2, -2.5e-7f)) + 1.f) - 0x3f800000u;
+        return __float_as_uint(ex2(fminf((x - shift - X) * inv_Tl2, -2.5e-7f)) + 1.f) - 0x3f800000u;
     }
 };
+// Elements per unit of weight inside a bin (not the last), at most.  A bin is half a T wide and X lies at most two steps of
+// the row's values above it, which are T / 128 each at the most (see shift): weights are at least exp(-0.516) = 1 / 1.675.
+constexpr float kPerUnit = (float)(1.7 * kUnit);
 
 // This thread's elements of the row.  HELD: the CTA keeps them in shared memory; otherwise every pass reads them again
 // (from L2).  VEC: 16-byte loads.  Elements that do not exist are -inf.
@@ -309,8 +314,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     r.inv_T2 = (float)(2.0 * inv_T);
     r.inv_Tl2 = (float)(1.4426950408889634 * inv_T);
     r.half_T = flat ? 0.f : (float)(0.5 * T);
-    r.top = flat ? mx : (float)(m + 0.25 * T);
-    if (tid < kBins) s.W[tid] = infinite ? kUnit : kUnit * exp(((double)r.end_of((float)tid) - m) * inv_T);
+    // Where T is less than 2^-16 of the maximum, sums of both lose T's own bits: there everything is measured from the maximum,
+    // which x - m is exact for (16 T is 2^-12 of m at most; what is farther away has no weight).
+    r.shift = !flat && !infinite && T < 0x1p-16 * fabs(m) ? mx : 0.f;
+    r.top = flat ? mx : __double2float_ru(r.shift != 0.f ? 0.25 * T : m + 0.25 * T);
+    if (tid < kBins) s.W[tid] = infinite ? kUnit : kUnit * exp((r.shift != 0.f ? (double)r.end_of((float)tid) : (double)r.end_of((float)tid) - m) * inv_T);
     if (tid == 32) {  // a weight is at least min_p when the logit is at most this far (negative) from the maximum
         const double thr = mp0 > 0.f && !flat ? T * log(fmin((double)mp0, 1.0)) : -INFINITY;
         s.thr = infinite ? mx : fmaxf(__double2float_ru(m + thr), -FLT_MAX);
@@ -407,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     // always hold it; if not (values near zero have finer keys), the whole range is searched, 32 probes a round.
     const uint32_t k0 = key_of(r.m), k1 = key_of(-FLT_MAX) + 1;  // the answer is in k0..k1
     auto probe = [&](int j, uint32_t& a) {
-        const uint32_t mid = key_of(fmaxf(r.end_of((float)j), -FLT_MAX));
+        const uint32_t mid = key_of(fmaxf(r.end_of((float)j) + r.shift, -FLT_MAX));
         a = mid > k0 + 16 ? mid - 16 : k0;
         const uint32_t at = a + lane;
         return __ballot_sync(0xffffffffu, at >= k1 || r.bin(value_of(at)) >= j);
@@ -619,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     for (int stage = k > 0 && k < p.V ? 0 : 1; stage < 3; ++stage) {
         if (stage == 1 && !nucleus) continue;
         const bool by_rank = stage == 0, strict = stage == 2;
-        const float per = by_rank ? 1.f : (float)(1.7 * kUnit);  // elements per unit: a weight inside a bin is at least exp(-1/2)
+        const float per = by_rank ? 1.f : kPerUnit;
         const bool fresh = !weighed;
         if (fresh) {
             level0(!by_rank);

@@ -587,6 +587,35 @@ def test_sample_top_k_cuts_a_run_of_equal_logits(V, top):
             _sample_check(x, u, k=np.full(B, k), temp=np.full(B, 4.0), mp=np.full(B, 0.01))
 
 
+@pytest.mark.parametrize("V", [1000, 20000, 40000, 128256, 140003])
+def test_sample_temperatures_of_a_few_steps_of_the_maximum(V):
+    """Temperatures of 0.3 to 4096 steps of float32 at the maximum, with hundreds of candidates within a few of those
+    steps: what rounds at the maximum's size must not move weights, nor the room that lists of candidates need."""
+    g = np.random.default_rng(V)
+    for m in (10.0, 12.0, 33.0, 100.0, 1.0000001, -7.3, 16384.5, 1e6):
+        ulp = float(np.spacing(np.float32(abs(m))))
+        steps = np.array([0.3, 0.6, 1.0, 1.7, 2.668, 4.0, 8.0, 16.0, 30.0, 64.0, 256.0, 4096.0])
+        B = steps.size
+        temp = (steps * ulp).astype(np.float32)
+        u = np.where(np.arange(B) % 2, 0.98, g.random(B)).astype(np.float32)
+        for n, crowd in ((270, 1), (900, 1), (900, 3), (900, 40)):
+            x = np.full((B, V), m - 100 - abs(m), np.float32)
+            for r in range(B):
+                at = np.sort(g.choice(V, n + 1, replace=False)) if r % 3 else np.arange(n + 1)
+                x[r, at] = (m - ulp * np.round(np.maximum(1, steps[r] * (0.3 + 0.6 * g.random())) + g.integers(0, crowd, n + 1))).astype(np.float32)
+                x[r, at[0]] = m
+            _sample_check(x, u, temp)
+            _sample_check(x, u, temp, p=np.full(B, 0.8))
+            _sample_check(x, u, temp, k=np.full(B, 500), p=np.full(B, 0.9))
+
+
+def test_sample_hundreds_of_candidates_two_steps_below_the_maximum():
+    x = np.full((1, 1000), -100, np.float32)
+    x[0, 500] = 10
+    x[0, 100:370] = 10 - 2 * np.spacing(np.float32(10))
+    assert _sample_check(x, np.array([0.98], np.float32), np.array([2.5444e-6])) == [364]
+
+
 @pytest.mark.parametrize("B,V", [(200, 128256), (96, 40001), (64, 20011)])
 def test_sample_is_the_same_beside_other_work(B, V):
     """The exchanges inside a cluster and the hand-over to one CTA while other kernels delay some of its warps: every
