@@ -348,7 +348,7 @@ int first_sample_topk(const float *logits, int32_t B, int32_t vocab, int32_t top
  * logit is above -inf (NaN counts as -inf), in descending order of their logits, equal ones (-0 = +0) in index order;
  * their weights are exp((logit - max) / temperature), a logit equal to the maximum weighing 1.  Each filter keeps a
  * prefix of that order:
- *   1. top_k > 0: the first top_k candidates;  min_p > 0: those whose weight is at least min_p (the first always stays)
+ *   1. top_k > 0: the first top_k candidates;  min_p > 0: those whose weight is at least min_p (the first always stays: alone above 1)
  *   2. top_p < 1: of what is left, every candidate before which the weights sum to less than top_p times their total
  *      (the first always stays)
  * The token is the first candidate left whose cumulative weight exceeds u times the weight left.  u is the row's

@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     cluster.barrier_wait();
     mx = value_of(cluster_min(key_of(mx)));
     if (rank == 0 && tid == 0 && p.pos) p.pos[b] += 1;
-    if (mx == -INFINITY || !(T0 > 0.f)) {  // nothing to choose from, or greedy: the first of the largest
+    if (mx == -INFINITY || !(T0 > 0.f) || mp0 > 1.f) {  // nothing to choose from, or greedy (no weight is above 1): the first of the largest
         int at = -1;
         if (mx > -INFINITY) {
             at = 0x7fffffff;
@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
     r.top = flat ? mx : __double2float_ru(r.shift != 0.f ? 0.25 * T : m + 0.25 * T);
     if (tid < kBins) s.W[tid] = infinite ? kUnit : kUnit * exp((r.shift != 0.f ? (double)r.end_of((float)tid) : (double)r.end_of((float)tid) - m) * inv_T);
     if (tid == 32) {  // a weight is at least min_p when the logit is at most this far (negative) from the maximum
-        const double thr = mp0 > 0.f && !flat ? T * log(fmin((double)mp0, 1.0)) : -INFINITY;
+        const double thr = mp0 > 0.f && !flat ? T * log((double)mp0) : -INFINITY;
         s.thr = infinite ? mx : fmaxf(__double2float_ru(m + thr), -FLT_MAX);
     }
     __syncthreads();

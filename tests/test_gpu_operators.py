@@ -393,6 +393,17 @@ def _sample_check(x, u, temp=None, k=None, p=None, mp=None, pad=0):
     return got
 
 
+def _sample_tokens(x, u, temp=None, k=None, p=None, mp=None):
+    """The device's tokens."""
+    import torch
+    from paper_2410_12513_b200 import first_sample
+    dev = lambda v, t: None if v is None else torch.from_numpy(np.asarray(v, dtype=t)).cuda()  # noqa: E731
+    tok = torch.full((len(x),), -7, dtype=torch.int32, device="cuda")
+    first_sample(torch.from_numpy(x).cuda(), dev(u, np.float32), tok, temperature=dev(temp, np.float32), top_k=dev(k, np.int32),
+                 top_p=dev(p, np.float32), min_p=dev(mp, np.float32))
+    return tok.cpu().numpy()
+
+
 def _settings(B, g):
     return (np.where(g.random(B) < 0.1, 0.0, 0.3 + 1.5 * g.random(B)),
             np.choose(g.integers(0, 4, B), [np.zeros(B), 1 + g.integers(0, 20, B), 50 + g.integers(0, 400, B), 2000 + g.integers(0, 9000, B)]).astype(np.int32),
@@ -510,6 +521,21 @@ def test_sample_values_outside_their_ranges():
     _sample_check(x, u, p=np.array([1.0, 2.0, np.inf, 1.5, 1.0, 3.0]))
     assert (_sample_check(x, u, mp=np.array([1.0, 2.0, np.inf, 1.0, 1.5, 1.0])) == [o[0] for o in order]).all()
     _sample_check(x, u, mp=np.array([0.0, -1.0, -np.inf, np.nan, 0.0, 0.0]))
+
+
+def test_sample_min_p_above_one_keeps_the_first_candidate_alone():
+    g = np.random.default_rng(6)
+    for V in (900, 20000, 140003):
+        x = np.floor(2 * g.standard_normal((6, V))).astype(np.float32)  # ties at the largest
+        x[3] = 0.5
+        x[4, ::7] = np.inf
+        first = x.argmax(1)
+        u = np.array([0.0, 0.3, 0.6, 0.9, 0.95, 0.999], np.float32)
+        for temp in (None, np.full(6, 0.7), np.full(6, np.inf), np.full(6, 1e-6)):
+            for mp in (1.5, np.inf, float(np.nextafter(np.float32(1), np.float32(2)))):
+                assert (_sample_tokens(x, u, temp, mp=np.full(6, mp)) == first).all()
+        got = _sample_tokens(x, u, mp=np.ones(6))  # at 1 all of the largest stay
+        assert (x[np.arange(6), got] == x.max(1)).all() and (got != first).any()
 
 
 def test_sample_agrees_with_top_k_sampling_of_the_batch():
