@@ -138,14 +138,14 @@ extern "C" int first_rope(void* q, int64_t q_token_stride, int64_t q_head_stride
                           int32_t head_dim, int32_t rot_dim, const int32_t* pos, const double* inv_freq, float factor,
                           int32_t interleaved, void* stream) {
     if (tokens < 0 || n_q_heads < 0 || n_kv_heads < 0 || n_q_heads + (int64_t)n_kv_heads > 65536) return FIRST_E_ARG;
-    if ((n_q_heads > 0 && !q) || (n_kv_heads > 0 && !k) || !pos || !inv_freq) return FIRST_E_ARG;
     if (dtype != FIRST_DTYPE_F32 && dtype != FIRST_DTYPE_BF16) return FIRST_E_ARG;
     if (head_dim <= 0 || rot_dim <= 0 || rot_dim % 2 || rot_dim > head_dim) return FIRST_E_SHAPE;
     if (head_dim > 65536) return FIRST_E_UNSUPPORTED;
     if (!strides_ok(tokens, n_q_heads, head_dim, q_token_stride, q_head_stride) ||
         !strides_ok(tokens, n_kv_heads, head_dim, k_token_stride, k_head_stride))
         return FIRST_E_SHAPE;
-    if (tokens == 0 || n_q_heads + n_kv_heads == 0) return FIRST_OK;
+    if (tokens == 0 || n_q_heads + n_kv_heads == 0) return FIRST_OK;  // (an empty tensor's address may be NULL)
+    if ((n_q_heads > 0 && !q) || (n_kv_heads > 0 && !k) || !pos || !inv_freq) return FIRST_E_ARG;
     RopeArgs p{};
     p.q = q; p.k = k;
     p.q_tok = q_token_stride; p.q_head = q_head_stride; p.k_tok = k_token_stride; p.k_head = k_head_stride;

@@ -84,6 +84,15 @@ def test_rope(case, interleaved, dtype):
         assert np.array_equal(big.float().cpu().numpy()[:, hq + hk:], before[:, hq + hk:])
 
 
+def test_rope_of_an_empty_batch():
+    import torch
+    from paper_2410_12513_b200 import first_rope
+    q, k = torch.empty(0, 4, 64, device="cuda"), torch.empty(0, 2, 64, device="cuda")
+    pos, inv = torch.empty(0, dtype=torch.int32, device="cuda"), torch.ones(32, dtype=torch.float64, device="cuda")
+    first_rope(q, k, pos, inv)
+    first_rope(q, None, pos, inv, interleaved=True)
+
+
 def test_rope_on_another_stream_and_in_a_graph():
     import torch
     from paper_2410_12513_b200 import first_rope

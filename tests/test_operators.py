@@ -95,6 +95,17 @@ def test_rope_refuses():
     assert call(T=10, qt=128, qh=1279, hk=0) == SHAPE
 
 
+def test_empty_batches_need_no_addresses():
+    """An empty tensor's address is NULL: a batch of no rows does nothing, whatever the addresses are."""
+    L = _L()
+    assert L.first_rope(None, 512, 128, 4, None, 256, 128, 2, 1, 0, 128, 128, None, None, 1.0, 0, None) == 0
+    assert L.first_rope(None, 512, 128, 4, None, 0, 0, 0, 0, 0, 128, 64, None, P, 1.0, 1, None) == 0
+    assert L.first_rope(None, 0, 0, 0, None, 0, 0, 0, 0, 7, 128, 64, None, None, 1.0, 1, None) == 0
+    assert L.first_rope(None, 512, 128, 4, None, 256, 128, 2, 1, 0, 128, 129, None, None, 1.0, 0, None) == SHAPE  # other checks stay
+    assert L.first_lora(None, 1, 256, P, P, 1, None, None, 4, 8, 1, (C.c_int32 * 2)(0, 100), 0, 256, 100, None, 0, 100, None) == 0
+    assert L.first_sample(None, 100, 0, 100, None, None, None, None, None, None, None) == 0
+
+
 def test_lora_refuses():
     L = _L()
     seg = lambda *v: (C.c_int32 * len(v))(*v)  # noqa: E731
