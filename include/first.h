@@ -428,8 +428,9 @@ int first_set_adapters(first_ctx *ctx, const first_adapters *adapters);
 /* Rotary positions on caller-owned queries and keys, in place (for callers with a prefill of their own; the step and
  * first_prefill rotate by themselves).  Pair i of the first rot_dim elements of every head of token t turns by the
  * angle pos[t] * inv_freq[i]: (a, b) -> (a c - b s, b c + a s), c = factor * cos, s = factor * sin; elements from
- * rot_dim on are not touched.  Pairs are (i, i + rot_dim/2), or (2i, 2i+1) with interleaved != 0.  Angles are formed in
- * 64 bits, so that far positions keep float32-exact cosines; products in float32, rounded once.
+ * rot_dim on are not touched.  Pairs are (i, i + rot_dim/2), or (2i, 2i+1) with interleaved != 0.  Angles and factor * cos,
+ * factor * sin are formed in 64 bits and cut to float32 once, as the step's are (the same bits, for a factor that is a float32
+ * itself); products in float32, rounded once.
  *   q, k       dev, head h of token t at t*token_stride + h*head_stride (elements), n_q_heads / n_kv_heads heads of
  *              head_dim elements, float32 or bfloat16 (dtype); 0 heads = not given.  Every element belongs to one (token, head): rows
  *              may not overlap, nor may q and k.

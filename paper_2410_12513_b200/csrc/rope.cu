@@ -20,7 +20,8 @@ struct RopeArgs {
     int nv, hg;                            // vectors of pairs per head, head groups per token
     const int32_t* pos;
     const double* inv_freq;
-    float factor;
+    double factor;
+    bool shared;                           // the block's cosines and sines are computed once for all its threads
 };
 
 // One pair: (a, b) -> (a c - b s, b c + a s).
@@ -31,27 +32,45 @@ __device__ __forceinline__ void rotate(T& a, T& b, float2 cs) {
     b = from_f32<T>(y * cs.x + x * cs.y);
 }
 
-// A thread holds the cosines and sines of V pairs of one token and walks every hg-th head with them: the angle
-// (64-bit product, reduced to a fraction of a turn before it is cut to 32 bits, so that positions of millions keep
-// full accuracy) is paid once per H / hg heads.  V = 16 bytes' worth of elements where the layout allows it, else 1.
-// Bound by HBM: 32768 tokens of 32 + 8 heads of 128 in bfloat16 114 us, 5.9 TB/s (90 % of a copy); 32 tokens 3 us (launch).
+// An angle less its whole turns, to 64 bits (of angles up to 2^31; the sine's own way with large ones is a slow one).
+__device__ __forceinline__ double turned(double angle) {
+    constexpr double kTurn = 2.0 * kPi, kTurnLow = 2.4492935982947064e-16;  // 2 pi = their sum
+    const double n = rint(angle * (1.0 / kTurn));
+    return fma(-n, kTurnLow, fma(-n, kTurn, angle));
+}
+__device__ __forceinline__ float2 cos_sin(const RopeArgs& p, int64_t t, int i) {
+    double s, c;
+    sincos(turned((double)p.pos[t] * p.inv_freq[i]), &s, &c);
+    return make_float2((float)(p.factor * c), (float)(p.factor * s));
+}
+
+// A thread takes V pairs of one token and every hg-th head of them.  Their cosines and sines are those of the step, bit for bit:
+// formed in 64 bits and cut to 32 at the end.  That is some hundred instructions a pair, so a block computes those of its
+// tokens once, into shared memory.  V = 16 bytes' worth of elements where the layout allows it, else 1.
+// Bound by HBM: 32768 tokens of 32 + 8 heads of 128 in bfloat16 110.6 us, 6.1 TB/s (93 % of a copy); 32 tokens: launch.
 template <typename T, int V, bool IL>
 __global__ void __launch_bounds__(256) rope_rows(const RopeArgs p) {
-    const int64_t w = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    const int v = (int)(w % p.nv);
-    const int64_t r = w / p.nv;
-    const int g = (int)(r % p.hg);
-    const int64_t t = r / p.hg;
+    extern __shared__ __align__(16) float2 table[];
+    const int64_t w0 = (int64_t)blockIdx.x * blockDim.x;
+    const unsigned per = (unsigned)p.nv * p.hg;  // threads a token (2^31 at most)
+    const int64_t t0 = w0 / per;
+    const unsigned off = (unsigned)(w0 - t0 * per), at = off + threadIdx.x, in = at % per;
+    const int dt = (int)(at / per), g = (int)(in / p.nv), v = (int)(in % p.nv);
+    const int64_t t = t0 + dt;
+    const float2* mine;
+    if (p.shared) {
+        const int n = (int)min(p.tokens - t0, (int64_t)((off + blockDim.x - 1) / per) + 1);
+        for (int e = threadIdx.x; e < n * p.half; e += blockDim.x) table[e] = cos_sin(p, t0 + e / p.half, e % p.half);
+        mine = table + dt * p.half + v * V;
+        __syncthreads();
+    } else {
+        for (int i = 0; t < p.tokens && i < V; ++i) table[threadIdx.x * V + i] = cos_sin(p, t, v * V + i);
+        mine = table + threadIdx.x * V;
+    }
     if (t >= p.tokens) return;
     float2 cs[V];
-    const double ps = (double)p.pos[t];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const double turns = ps * p.inv_freq[v * V + i] * (0.5 / kPi);
-        float s, c;
-        sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-        cs[i] = make_float2(p.factor * c, p.factor * s);
-    }
+    for (int i = 0; i < V; ++i) cs[i] = mine[i];
     struct alignas(sizeof(T) * V) Vec { T e[V]; };
     // halves: V first members at v*V, V second members half elements on; interleaved: 2V consecutive elements
     const int o0 = IL ? 2 * v * V : v * V, o1 = IL ? o0 + V : o0 + p.half;
@@ -85,9 +104,20 @@ cudaError_t launch(RopeArgs p, bool interleaved, cudaStream_t st) {
     const int64_t one = p.tokens * p.nv * p.H, full = 148 * 2048;
     const int per = (int)(one <= full ? 1 : one / full < 8 ? one / full : 8);
     p.hg = (p.H + per - 1) / per;
+    // If an equal share of up to half as many fills whole blocks with whole tokens (or tokens with blocks), that one: a block's
+    // cosines are then all its own (the large launch: 8 groups of 5 heads 110.6 us, 5 of 8 118.7).
+    for (int h = p.hg; h <= 2 * p.hg && h <= p.H; ++h)
+        if (p.H % h == 0 && (256 % ((int64_t)p.nv * h) == 0 || (int64_t)p.nv * h % 256 == 0)) {
+            p.hg = h;
+            break;
+        }
     const int64_t blocks = (p.tokens * p.nv * p.hg + 255) / 256;
-    if (interleaved) rope_rows<T, V, true><<<(unsigned)blocks, 256, 0, st>>>(p);
-    else rope_rows<T, V, false><<<(unsigned)blocks, 256, 0, st>>>(p);
+    // tokens that a block's threads can belong to; very wide heads (from 2048 pairs on) have a block within one head
+    const int64_t most = (255 / ((int64_t)p.nv * p.hg) + 2) * p.half;
+    p.shared = most <= 4096;
+    const size_t smem = (p.shared ? most : 256 * V) * sizeof(float2);
+    if (interleaved) rope_rows<T, V, true><<<(unsigned)blocks, 256, smem, st>>>(p);
+    else rope_rows<T, V, false><<<(unsigned)blocks, 256, smem, st>>>(p);
     return cudaGetLastError();
 }
 

@@ -84,6 +84,25 @@ def test_rope(case, interleaved, dtype):
         assert np.array_equal(big.float().cpu().numpy()[:, hq + hk:], before[:, hq + hk:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("hd,rot", [(8192, 8192), (8200, 8194), (6000, 4000), (2048, 2048)])
+def test_rope_of_wide_heads(hd, rot, interleaved, dtype):
+    """Heads that are wider than a block, aligned and not."""
+    import torch
+    from paper_2410_12513_b200 import first_rope
+    g = torch.Generator().manual_seed(rot)
+    q, k = torch.randn(5, 3, hd, generator=g).to(_t(dtype)).cuda(), torch.randn(5, 1, hd, generator=g).to(_t(dtype)).cuda()
+    pos = torch.tensor([0, 1, 4097, 2 ** 31 - 1, 77], dtype=torch.int32)
+    inv = 10000.0 ** (-2.0 * np.arange(rot // 2) / rot)
+    q0, k0 = q.float().cpu().numpy(), k.float().cpu().numpy()
+    first_rope(q, k, pos.cuda(), torch.from_numpy(inv).cuda(), interleaved=interleaved)
+    for x0, x1 in ((q0, q), (k0, k)):
+        ref, mag = _rope_ref(x0, pos.numpy(), inv, 1.0, interleaved)
+        tol = 10 * U32 * mag + (2.0 ** -8 * np.abs(ref) if dtype == "bf16" else 0.0)  # (as in test_rope)
+        assert (np.abs(x1.double().cpu().numpy() - ref) <= tol).all()
+
+
 def test_rope_of_an_empty_batch():
     import torch
     from paper_2410_12513_b200 import first_rope
@@ -825,6 +844,37 @@ def test_step_with_other_frequencies(bf16, fuse):
     again = run(plain)
     if not bf16:
         assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("factor", [1.0, 1.25])
+def test_rope_turns_by_the_factors_of_the_step(factor):
+    """The key that a step appends at a position against first_rope on the key it appends at position 0 (no rotation).  The
+    second half of every key is zero, so that a rotated element is one product: equal bits are equal cosines and sines."""
+    import torch
+    from paper_2410_12513_b200 import first_rope
+    shape = fi.ModelShape(1, 64, 2, 2, 64, 80, 32, 500000.0)
+    B = 64
+    w = fi.make_weights(shape, 3, False)
+    w["wk"][0].reshape(2, 64, 64)[:, 32:] = 0.0
+    inv = 500000.0 ** (-np.arange(32) / 32.0)
+    g = np.random.default_rng(4)
+    ctx = _ctx(shape, False, B, 8, w)
+    ctx.set_mask(torch.ones((B, 1), dtype=torch.uint8, device="cuda"))
+    tok = torch.arange(B, dtype=torch.int32, device="cuda") % 32
+
+    def keys(pos):  # [B][heads][64] as appended at these positions
+        _, kv = synthetic_caches(shape, [1] * B, [4] * B, 1, False)
+        kv.pos.copy_(torch.from_numpy(pos.astype(np.int32)))
+        ctx.decode_step(tok, kv.c)
+        return kv.k[0].view(2, B, 4, 64)[:, :, 1].transpose(0, 1).contiguous()
+    base = keys(np.zeros(B))
+    ctx.set_rope(inv, factor)
+    for far in (100, 5000, 1 << 20, 2 ** 31 - 1):
+        pos = g.integers(0, far, B)
+        pos[0] = far - 1
+        q = base.clone()
+        first_rope(q, None, torch.from_numpy(pos.astype(np.int32)).cuda(), torch.from_numpy(inv).cuda(), factor=factor)
+        assert torch.equal(q, keys(pos)), far
 
 
 def test_step_with_per_row_sampling():
