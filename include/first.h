@@ -448,7 +448,7 @@ int first_set_adapters(first_ctx *ctx, const first_adapters *adapters);
  * head): inv_freq HOST float64 [head_dim/2], finite, and factor; NULL restores base^(-2i/head_dim) of the description.
  * Waits for the device; keys already in a cache keep the rotation they were written with.
  * Errors: FIRST_E_ARG, FIRST_E_SHAPE (rot_dim odd or above head_dim, strides that overlap), FIRST_E_UNSUPPORTED (head_dim
- * > 65536), FIRST_E_CAPACITY (more than 2^38 pairs), FIRST_E_STATE (first_set_rope during a stream capture), FIRST_E_CUDA. */
+ * > 65536; q or k not aligned to its element), FIRST_E_CAPACITY (more than 2^38 pairs), FIRST_E_STATE (first_set_rope during a stream capture), FIRST_E_CUDA. */
 #define FIRST_ROPE_NONE 0
 #define FIRST_ROPE_LINEAR 1
 #define FIRST_ROPE_LLAMA3 2

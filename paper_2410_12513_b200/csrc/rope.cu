@@ -185,6 +185,8 @@ extern "C" int first_rope(void* q, int64_t q_token_stride, int64_t q_head_stride
     p.pos = pos; p.inv_freq = inv_freq; p.factor = factor;
     if ((__int128)tokens * p.half * p.H > ((__int128)1 << 38)) return FIRST_E_CAPACITY;  // (grid size; 2^38 pairs = 1 TB of bfloat16)
     const int es = dtype == FIRST_DTYPE_BF16 ? 2 : 4, V = 16 / es;
+    for (const void* ptr : {n_q_heads > 0 ? q : nullptr, n_kv_heads > 0 ? k : nullptr})
+        if (reinterpret_cast<uintptr_t>(ptr) % es) return FIRST_E_UNSUPPORTED;
     auto aligned = [&](const void* ptr, int64_t ts, int64_t hs, int heads) {
         return !heads || ((reinterpret_cast<uintptr_t>(ptr) % 16) == 0 && (tokens == 1 || ts % V == 0) && (heads == 1 || hs % V == 0));
     };

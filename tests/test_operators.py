@@ -95,6 +95,12 @@ def test_rope_refuses():
     assert call(T=10, qt=128, qh=1279, hk=0) == SHAPE
 
 
+def test_rope_refuses_addresses_between_elements():
+    L = _L()
+    for dt, q, k in ((1, P + 1, P), (1, P, P + 3), (0, P + 2, P), (0, P, P + 6), (0, P + 1, P)):
+        assert L.first_rope(q, 512, 128, 4, k, 256, 128, 2, dt, 10, 128, 128, P, P, 1.0, 0, None) == UNSUPPORTED
+
+
 def test_empty_batches_need_no_addresses():
     """An empty tensor's address is NULL: a batch of no rows does nothing, whatever the addresses are."""
     L = _L()
