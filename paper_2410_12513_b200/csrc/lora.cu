@@ -14,9 +14,9 @@
 // below 2^-26 are left out.  How the sums are ordered depends on the sizes k, n, rank alone, so a row's result does not depend on
 // the rows around it.
 //
-// Measured (adapters, x and y larger than L2 in turn): 1 row of q|k|v at rank 8 6.2 us, 32 rows of 16 adapters 9.9 us (1.1 TB/s),
-// 256 rows of 64 adapters at the down projection 33 us (2.9 TB/s; the shrink, which streams A, is more than half of it), 1024 rows of 8
-// adapters at gate|up 47 us (2.7 TB/s; y begins to move after 12 us of plan, shrink and meeting).
+// Measured (on the device; adapters, x and y larger than L2 in turn): 1 row of q|k|v at rank 8 6.1 us, 32 rows of 16 adapters 9.7 us (1.2 TB/s),
+// 256 rows of 64 adapters at the down projection 33 us (3.0 TB/s; the shrink, which streams A, is more than half of it), 1024 rows of 8
+// adapters at gate|up 45 us (2.8 TB/s; y begins to move after 12 us of plan, shrink and meeting).
 #include <algorithm>
 #include <type_traits>
 
@@ -55,22 +55,30 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 
 // Eight (or four) consecutive elements as pairs of bfloat16, in N terms.
 template <int N, int E>
-struct Frag { uint32_t t[N][E / 2]; };
+struct Frag {
+    uint32_t t[N][E / 2];
+    __device__ __forceinline__ void keep_if(bool live) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) t[i][e] = live ? t[i][e] : 0;
+    }
+};
 template <typename T, int E>
-__device__ __forceinline__ Frag<sizeof(T) == 2 ? 1 : 3, E> load_frag(const T* p, bool live) {
+__device__ __forceinline__ Frag<sizeof(T) == 2 ? 1 : 3, E> load_frag(const T* p) {
     Frag<sizeof(T) == 2 ? 1 : 3, E> f;
     if constexpr (sizeof(T) == 2) {
         if constexpr (E == 8) {
-            const uint4 v = live ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0, 0, 0, 0);
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
             f.t[0][0] = v.x; f.t[0][1] = v.y; f.t[0][2] = v.z; f.t[0][3] = v.w;
         } else {
-            const uint2 v = live ? __ldg(reinterpret_cast<const uint2*>(p)) : make_uint2(0, 0);
+            const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
             f.t[0][0] = v.x; f.t[0][1] = v.y;
         }
     } else {
 #pragma unroll
         for (int q = 0; q < E / 4; ++q) {
-            const float4 v = live ? __ldg(reinterpret_cast<const float4*>(p) + q) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float4 v = __ldg(reinterpret_cast<const float4*>(p) + q);
             uint32_t t[3];
             split(v.x, v.y, t);
 #pragma unroll
@@ -110,13 +118,51 @@ __device__ __forceinline__ void copy_async(void* to, const void* from, bool live
     if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(a), "l"(from), "r"(n) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(a), "l"(from), "r"(n) : "memory");
 }
-__device__ __forceinline__ void copy_word(void* to, int word, const void* from) {
+__device__ __forceinline__ void copy_word(void* to, int word, const void* from, bool live) {
     const uint32_t a = (uint32_t)__cvta_generic_to_shared(to) + 4 * word;
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(a), "l"(from) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(a), "l"(from), "r"(live ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The tensor cores and the cluster's barriers want whole warps, so nothing between them branches on a lane's own values:
+// what a lane has no element for is loaded from an address that is good and dropped, or is a predicated instruction.
+__device__ __forceinline__ void prefetch_if(const void* p, bool live) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %1, 0;\n @p prefetch.global.L2 [%0];\n}" ::"l"(p), "r"((uint32_t)live));
+}
+template <typename T>
+__device__ __forceinline__ T load_if(const T* p, bool live) {
+    T v;
+    if constexpr (sizeof(T) == 4) {
+        uint32_t u;
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n mov.b32 %0, 0;\n @p ld.global.b32 %0, [%1];\n}" : "=r"(u) : "l"(p), "r"((uint32_t)live) : "memory");
+        memcpy(&v, &u, 4);
+    } else {
+        uint16_t u;
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n mov.b16 %0, 0;\n @p ld.global.b16 %0, [%1];\n}" : "=h"(u) : "l"(p), "r"((uint32_t)live) : "memory");
+        memcpy(&v, &u, 2);
+    }
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_if(T* p, T v, bool live) {
+    if constexpr (sizeof(T) == 4) {
+        uint32_t u;
+        memcpy(&u, &v, 4);
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n @p st.global.b32 [%0], %1;\n}" ::"l"(p), "r"(u), "r"((uint32_t)live) : "memory");
+    } else {
+        uint16_t u;
+        memcpy(&u, &v, 2);
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n @p st.global.b16 [%0], %1;\n}" ::"l"(p), "h"(u), "r"((uint32_t)live) : "memory");
+    }
+}
+__device__ __forceinline__ void store16_if(void* p, const uint4& v, bool live) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %5, 0;\n @p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n}" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z),
+                 "r"(v.w), "r"((uint32_t)live) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 __host__ __device__ constexpr int steps_ahead(int rows) { return rows == 8 ? 2 : 3; }
 
@@ -142,7 +188,8 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
     __shared__ int tile_s[2];      // adapter, rows
     __shared__ int warp_s[kWarps];
     cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
+    const int rank = (int)cluster.block_rank(), lane = threadIdx.x & 31, tid = threadIdx.x;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // (the same in every lane, for the compiler too)
     const int g = lane >> 2, t = lane & 3;
     const int tile = (int)(blockIdx.x / kCluster) % pl.tiles, slice = (int)(blockIdx.x / kCluster) / pl.tiles;
     pdl_trigger();
@@ -259,11 +306,11 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         const int mt = u / pl.ks, ks = u % pl.ks;
         const int b0 = c0 + (c1 - c0) * ks / pl.ks, b1 = c0 + (c1 - c0) * (ks + 1) / pl.ks;
         const WT* A = static_cast<const WT*>(p.a) + (int64_t)ad * M * p.K;
-        const WT *A0 = A + (int64_t)min(mt * 16 + g, M - 1) * p.K + 8 * t, *A1 = A + (int64_t)min(mt * 16 + g + 8, M - 1) * p.K + 8 * t;
+        const WT *A0 = A + (int64_t)min(mt * 16 + g, M - 1) * p.K, *A1 = A + (int64_t)min(mt * 16 + g + 8, M - 1) * p.K;
         const XT *X[NT], *XL[NT];
 #pragma unroll
         for (int q = 0; q < NT; ++q) {
-            const int64_t o = (int64_t)rows_s[q * 8 + g] * p.ldx + 8 * t;
+            const int64_t o = (int64_t)rows_s[q * 8 + g] * p.ldx;
             X[q] = static_cast<const XT*>(p.x) + o;
             XL[q] = XK == kLoraXPair ? static_cast<const XT*>(p.x_lo) + o : nullptr;
         }
@@ -271,14 +318,21 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         constexpr int kUnroll = TR == 8 && OCC == 2 ? 4 : 2;
 #pragma unroll kUnroll
         for (int b = b0; b < b1; ++b) {
-            const bool in = b * 32 + 8 * t < p.K;
-            const auto f0 = load_frag<WT, 8>(A0 + b * 32, in), f1 = load_frag<WT, 8>(A1 + b * 32, in);
+            const bool ragged = b * 32 + 32 > p.K, in = b * 32 + 8 * t < p.K;  // (what is behind the features' end: zeros)
+            const int at = min(b * 32 + 8 * t, p.K - 8);
+            auto f0 = load_frag<WT, 8>(A0 + at), f1 = load_frag<WT, 8>(A1 + at);
+            if (ragged) {
+                f0.keep_if(in);
+                f1.keep_if(in);
+            }
 #pragma unroll
             for (int q = 0; q < NT; ++q) {
                 uint32_t xf[NX][4];
-                const auto v = load_frag<XT, 8>(X[q] + b * 32, in);
+                auto v = load_frag<XT, 8>(X[q] + at);
+                if (ragged) v.keep_if(in);
                 if constexpr (XK == kLoraXPair) {
-                    const auto w = load_frag<XT, 8>(XL[q] + b * 32, in);
+                    auto w = load_frag<XT, 8>(XL[q] + at);
+                    if (ragged) w.keep_if(in);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) { xf[0][e] = v.t[0][e]; xf[1][e] = w.t[0][e]; }
                 } else {
@@ -358,11 +412,13 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
             }
         }
     };
-    YT* y_row[HR];  // this thread's part of its rows, or NULL
+    YT* y_row[HR];  // its rows
+    bool has[HR];   // (a tile may have fewer: the row is its last one then, and is left alone)
 #pragma unroll
     for (int h = 0; h < HR; ++h) {
         const int c = q * 16 + h * 8 + g, i = rows_s[c];
-        y_row[h] = c < live ? static_cast<YT*>(p.y) + (int64_t)(p.scatter ? p.idx[i] : i) * p.ldy + (odd ? 2 : 8) * t : nullptr;
+        has[h] = c < live;
+        y_row[h] = static_cast<YT*>(p.y) + (int64_t)(p.scatter ? p.idx[i] : i) * p.ldy;
     }
     const int kbs = (p.R + 15) / 16;
     constexpr int YV = sizeof(YT) / 2;  // 16-byte words of eight elements
@@ -371,36 +427,43 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         typename std::conditional<sizeof(WT) == 2, uint2, uint4>::type w[4][32];
     };
     Step* const ring = reinterpret_cast<Step*>(pool) + warp * D;
-    const WT* const B = static_cast<const WT*>(p.b) + (int64_t)ad * p.N * p.R + 4 * t;
+    const WT* const B = static_cast<const WT*>(p.b) + (int64_t)ad * p.N * p.R;
     const int fw = odd ? g : (g >> 1) * 8 + (g & 1), fj = odd ? 8 : 2;  // this thread's row of B in part 0; from part to part
     const bool in0 = 4 * t < p.R;           // (a rank of 8 has no columns 8..15)
+    const int c0w = min(4 * t, p.R - 4);
     auto w_row = [&](int f0, int j) { return B + (int64_t)min(f0 + fw + fj * j, p.N - 1) * p.R; };
+    auto w_cols = [&](int f0, int j, int kb) {  // columns 16 kb + 4 t .. + 3 of part j's row; zeros behind the last
+        auto f = load_frag<WT, 4>(w_row(f0, j) + min(kb * 16 + 4 * t, p.R - 4));
+        if (kb * 16 + 16 > p.R) f.keep_if(kb * 16 + 4 * t < p.R);
+        return f;
+    };
     auto fetch = [&](const Place& at, Step& d) {
-        if (pl.y_vec && at.f0 + 8 * t + 8 <= at.end) {
+        if (pl.y_vec && at.f0 + 32 <= at.end) {
 #pragma unroll
             for (int h = 0; h < HR; ++h)
-                if (y_row[h])
 #pragma unroll
-                    for (int v = 0; v < YV; ++v) copy_async<16>(&d.y[h * YV + v][lane], reinterpret_cast<const uint4*>(y_row[h] + at.f0) + v, true);
+                for (int v = 0; v < YV; ++v) copy_async<16>(&d.y[h * YV + v][lane], reinterpret_cast<const uint4*>(y_row[h] + at.f0 + 8 * t) + v, has[h]);
         }
         if constexpr (TR == 8) {
-            if (odd && y_row[0]) {
+            if (odd) {
                 if constexpr (kWords) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (at.f0 + 2 * t + (e >> 1) * 8 + (e & 1) < at.end) copy_word(&d.y[e >> 2][lane], e & 3, y_row[0] + at.f0 + (e >> 1) * 8 + (e & 1));
-                } else if (at.f0 + 8 * t < at.end) {  // (the four threads' addresses are a quarter of the step apart)
-                    asm volatile("prefetch.global.L2 [%0];" ::"l"(y_row[0] + at.f0 + 6 * t));
+                    for (int e = 0; e < 8; ++e) {
+                        const int f = at.f0 + 2 * t + (e >> 1) * 8 + (e & 1);
+                        copy_word(&d.y[e >> 2][lane], e & 3, y_row[0] + min(f, at.end - 1), has[0] && f < at.end);
+                    }
+                } else {  // (the four threads' addresses are a quarter of the step apart)
+                    prefetch_if(y_row[0] + at.f0 + 8 * t, has[0] && at.f0 + 8 * t < at.end);
                 }
             }
         }
         if (at.f0 + 32 <= p.N) {
-            const WT* w = B + (int64_t)(at.f0 + fw) * p.R;
+            const WT* w = B + (int64_t)(at.f0 + fw) * p.R + c0w;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], in0 ? w + fj * j * p.R : B - 4 * t, in0);
+            for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], w + fj * j * p.R, in0);
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], in0 ? w_row(at.f0, j) : B - 4 * t, in0);
+            for (int j = 0; j < 4; ++j) copy_async<4 * sizeof(WT)>(&d.w[j][lane], w_row(at.f0, j) + c0w, in0);
         }
     };
     Place here{0, p.seg[1], 0}, next;
@@ -412,7 +475,9 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         copy_commit();
         ahead(next, stride);
     }
-    cluster.sync();
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
 
     // ---- combine: h of the tile's rows, scaled, in three terms; columns up to the next multiple of 16 are zero
     const float sc = p.scales ? p.scales[ad] : 1.f;
@@ -430,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
             reinterpret_cast<uint16_t*>(hs)[((s * 3 + i) * TR + col) * pl.h_stride + j] = (uint16_t)t3[i];
     }
     __syncthreads();
-    cluster.barrier_arrive();  // (no CTA leaves before all have read its partial sums)
+    cluster_arrive();  // (no CTA leaves before all have read its partial sums)
 
     // ---- expand
     for (int n = 0, at = 0; n < mine; ++n, at = at + 1 < D ? at + 1 : 0) {
@@ -447,11 +512,11 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
                 for (int j = 0; j < 4; ++j) w[j] = kb ? w_next[j] : shared_frag<WT>(&cur.w[j][lane]);
                 if (kb + 1 < kbs)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w_next[j] = load_frag<WT, 4>(w_row(f0, j) + kb * 16 + 16, kb * 16 + 16 + 4 * t < p.R);
+                    for (int j = 0; j < 4; ++j) w_next[j] = w_cols(f0, j, kb + 1);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    w[j] = kb ? load_frag<WT, 4>(w_row(f0, j) + kb * 16, kb * 16 + 4 * t < p.R) : shared_frag<WT>(&cur.w[j][lane]);
+                    w[j] = kb ? w_cols(f0, j, kb) : shared_frag<WT>(&cur.w[j][lane]);
             }
             float blk[4][4] = {};
 #pragma unroll
@@ -470,12 +535,9 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[j][e] += blk[j][e];
         }
-        const bool whole = pl.y_vec && f0 + 8 * t + 8 <= end;
+        if (pl.y_vec && f0 + 32 <= end) {
 #pragma unroll
-        for (int h = 0; h < HR; ++h) {
-            if (!y_row[h]) continue;
-            YT* const y = y_row[h] + f0;
-            if (whole) {
+            for (int h = 0; h < HR; ++h) {
                 uint4 v[YV];
                 if constexpr (sizeof(YT) == 4) {
 #pragma unroll
@@ -495,23 +557,24 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
                     v[0] = make_uint4(add(o.x, 0), add(o.y, 1), add(o.z, 2), add(o.w, 3));
                 }
 #pragma unroll
-                for (int i = 0; i < YV; ++i) reinterpret_cast<uint4*>(y)[i] = v[i];
-            } else if constexpr (TR == 8) {
-                const int left = end - f0 - (odd ? 2 : 8) * t;  // elements up to the segment's end
+                for (int i = 0; i < YV; ++i) store16_if(reinterpret_cast<uint4*>(y_row[h] + f0 + 8 * t) + i, v[i], has[h]);
+            }
+        } else {  // a segment's last features, or rows that are not aligned: one by one
+            const int fs = TR == 8 && odd ? 8 : 2, ft = f0 + (TR == 8 && odd ? 2 : 8) * t;  // element e is feature ft + (e >> 1) * fs + (e & 1)
+#pragma unroll
+            for (int h = 0; h < HR; ++h) {
                 YT o[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if ((e >> 1) * fj + (e & 1) < left) {
-                        if (kWords && odd) o[e] = reinterpret_cast<const YT*>(&cur.y[(e >> 2) % (HR * YV)][lane])[e & 3];
-                        else o[e] = y[(e >> 1) * fj + (e & 1)];
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const int f = ft + (e >> 1) * fs + (e & 1);
+                    if (kWords && odd) o[e] = reinterpret_cast<const YT*>(&cur.y[(e >> 2) % (HR * YV)][lane])[e & 3];
+                    else o[e] = load_if(y_row[h] + f, has[h] && f < end);
+                }
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if ((e >> 1) * fj + (e & 1) < left) y[(e >> 1) * fj + (e & 1)] = from_f32<YT>(to_f32(o[e]) + acc[e >> 1][2 * h + (e & 1)]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (f0 + 8 * t + e < end) y[e] = from_f32<YT>(to_f32(y[e]) + acc[e >> 1][2 * h + (e & 1)]);
+                for (int e = 0; e < 8; ++e) {
+                    const int f = ft + (e >> 1) * fs + (e & 1);
+                    store_if(y_row[h] + f, from_f32<YT>(to_f32(o[e]) + acc[e >> 1][2 * h + (e & 1)]), has[h] && f < end);
+                }
             }
         }
         if (n + D < mine) fetch(next, cur);
@@ -520,7 +583,8 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         ahead(next, stride);
     }
     copy_wait<0>();
-    cluster.barrier_wait();
+    __syncwarp();
+    cluster_wait();
 }
 
 constexpr size_t kMaxSmem = 226 * 1024;  // dynamic bytes of a CTA; the static ones (under 1 KB) come on top

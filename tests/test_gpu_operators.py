@@ -243,6 +243,30 @@ def test_lora_many_rows(case, types):
     assert torch.equal(y[idle], y0[idle])
 
 
+@pytest.mark.parametrize("types", [("bf16", "bf16", "bf16"), ("f32", "f32", "bf16"), ("bf16", "f32", "f32"), ("f32", "f32", "f32")], ids=str)
+@pytest.mark.parametrize("n,rank,k,seg", [(8, 16, 520, (0, 1040, 2080)), (5, 24, 264, (0, 48, 1000)), (3, 8, 40, (0, 16, 2044)), (8, 16, 520, (0, 1041))], ids=str)
+def test_lora_tiles_of_every_number_of_rows(n, rank, k, seg, types):
+    """Tiles of 1 to 32 rows, some lanes of a warp without a row or a feature: every row as when it is alone, bit for bit, and
+    rows without an adapter left alone."""
+    import torch
+    from paper_2410_12513_b200 import first_lora
+    x, a, b, _, y, g = _lora_inputs((1024, n, rank, k, seg), *(_t(v) for v in types), 41)
+    scales = (torch.rand(n, generator=g) * 2 - 1).cuda()
+    for trial in range(6):
+        count = torch.randint(1, 200, (n,), generator=g)
+        count[-1] = 97 + trial
+        ids = torch.cat([torch.full((int(c),), i) for i, c in enumerate(count)] + [torch.full((1024,), -1)])[:1024]
+        ids = ids[torch.randperm(1024, generator=g)].to(torch.int32).cuda()
+        got = y.clone()
+        first_lora(x, a, b, ids, got, scales=scales, segments=seg)
+        idle = ids < 0
+        assert torch.equal(got[idle], y[idle])
+        for r in torch.randperm(1024, generator=g)[:40].tolist():
+            one = y[r:r + 1].clone()
+            first_lora(x[r:r + 1], a, b, ids[r:r + 1], one, scales=scales, segments=seg)
+            assert torch.equal(one, got[r:r + 1]), (trial, r)
+
+
 def test_lora_padded_rows_empty_batch_and_bit_reproducible():
     import torch
     from paper_2410_12513_b200 import first_lora
