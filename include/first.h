@@ -391,7 +391,8 @@ int first_set_sampling_rows(first_ctx *ctx, const first_sampling *sampling);
  *   row_adapter  dev int32 [rows]
  *   segments     HOST int32 [n_segments+1]: 0 = first, n = last, increasing; inner borders multiples of 16
  *   y            dev [rows][y_stride], float32 or bfloat16, n columns updated in place; must not overlap x
- * Sums are float32; h is not rounded in between; y is rounded once per call.  The result does not depend on which
+ * Sums are float32; h is not rounded in between; y is rounded once per call.  Infinities and NaN give what they give in
+ * float32 sums, in their own rows and features (such sums are formed one by one: slow).  The result does not depend on which
  * other rows are in the batch.  rows = 0 or n_adapters = 0 does nothing.  No scratch, no wait.
  * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides, segments), FIRST_E_UNSUPPORTED (rank not a multiple of 8 or above
  * FIRST_LORA_MAX_RANK, k not a multiple of 8, more than FIRST_LORA_MAX_SEGMENTS segments, an inner border that is no

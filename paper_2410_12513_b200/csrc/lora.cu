@@ -11,12 +11,14 @@
 //   expand   y += B h, the output features split over the CTAs (and over several clusters when tiles are few; each of
 //            those computes h again, from L2)
 // All operands enter exactly: float32 values as three bfloat16 terms (8 bits each), h too; of their products those
-// below 2^-26 are left out.  How the sums are ordered depends on the sizes k, n, rank alone, so a row's result does not depend on
+// below 2^-26 are left out.  Infinities, and float32 values that round to one in bfloat16, meet terms of zero there: a sum that
+// is not finite is formed again in plain float32.  How the sums are ordered depends on the sizes k, n, rank alone, so a row's result does not depend on
 // the rows around it.
 //
-// Measured (on the device; adapters, x and y larger than L2 in turn): 1 row of q|k|v at rank 8 6.1 us, 32 rows of 16 adapters 9.7 us (1.2 TB/s),
-// 256 rows of 64 adapters at the down projection 33 us (3.0 TB/s; the shrink, which streams A, is more than half of it), 1024 rows of 8
-// adapters at gate|up 45 us (2.8 TB/s; y begins to move after 12 us of plan, shrink and meeting).
+// Measured (on the device; adapters, x and y larger than L2 in turn): 1 row of q|k|v at rank 8 6.3 us, 32 rows of 16 adapters 10.1 us (1.1 TB/s),
+// 256 rows of 64 adapters at the down projection 33.7 us (2.9 TB/s; the shrink, which streams A, is more than half of it), 1024 rows of 8
+// adapters at gate|up 46.7 us (2.7 TB/s; y begins to move after 12 us of plan, shrink and meeting; 44.8 without the look for
+// sums that are not finite).
 #include <algorithm>
 #include <type_traits>
 
@@ -47,6 +49,23 @@ __device__ __forceinline__ void split(float x, float y, uint32_t (&t)[N]) {
         x = fabsf(xh) < INFINITY ? x - xh : 0.f;
         y = fabsf(yh) < INFINITY ? y - yh : 0.f;
     }
+}
+// The same of one value, the largest among them: a finite one has finite terms.
+__device__ __forceinline__ void split_one(float x, uint16_t (&t)[3]) {
+    constexpr float kMost = 3.3895313892515355e38f;  // of bfloat16
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const float c = fabsf(x) < INFINITY ? fminf(fmaxf(x, -kMost), kMost) : x;
+        const __nv_bfloat16 h = __float2bfloat16_rn(c);
+        t[i] = __bfloat16_as_ushort(h);
+        const float v = __bfloat162float(h);
+        x = fabsf(v) < INFINITY ? x - v : 0.f;
+    }
+}
+__device__ __forceinline__ float largest(float a, float b, float c) {  // of the absolute values; NaN where one is
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -165,6 +184,14 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 __host__ __device__ constexpr int steps_ahead(int rows) { return rows == 8 ? 2 : 3; }
+
+template <int XK>
+__device__ __forceinline__ float x_at(const LoraArgs& p, int64_t i) {
+    if constexpr (XK == kLoraXF32) return static_cast<const float*>(p.x)[i];
+    const float v = __bfloat162float(static_cast<const __nv_bfloat16*>(p.x)[i]);
+    if constexpr (XK == kLoraXPair) return fabsf(v) < INFINITY ? v + __bfloat162float(static_cast<const __nv_bfloat16*>(p.x_lo)[i]) : v;
+    return v;
+}
 
 struct Plan {
     int tiles;          // clusters = tiles * slices
@@ -487,12 +514,18 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         if (j < p.R) {
 #pragma unroll
             for (int c = 0; c < kCluster; ++c) v += cluster.map_shared_rank(part, c)[(s * p.R + j) * TR + col];
+            if (!(fabsf(v) < INFINITY)) {
+                const WT* A = static_cast<const WT*>(p.a) + ((int64_t)ad * M + s * p.R + j) * p.K;
+                const int64_t o = (int64_t)rows_s[col] * p.ldx;
+                v = 0.f;
+#pragma unroll 8
+                for (int k = 0; k < p.K; ++k) v = fmaf(to_f32(A[k]), x_at<XK>(p, o + k), v);
+            }
         }
-        uint32_t t3[3];
-        split(v * sc, 0.f, t3);
+        uint16_t t3[3];
+        split_one(v * sc, t3);
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-            reinterpret_cast<uint16_t*>(hs)[((s * 3 + i) * TR + col) * pl.h_stride + j] = (uint16_t)t3[i];
+        for (int i = 0; i < 3; ++i) reinterpret_cast<uint16_t*>(hs)[((s * 3 + i) * TR + col) * pl.h_stride + j] = t3[i];
     }
     __syncthreads();
     cluster_arrive();  // (no CTA leaves before all have read its partial sums)
@@ -535,6 +568,13 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[j][e] += blk[j][e];
         }
+        // element e of row h is feature ft + (e >> 1) * fs + (e & 1), acc[e >> 1][2 h + (e & 1)]
+        const int fs = TR == 8 && odd ? 8 : 2, ft = f0 + (TR == 8 && odd ? 2 : 8) * t;
+        bool good[HR];  // a row that is not there, or a sum that is not finite: not stored here
+#pragma unroll
+        for (int h = 0; h < HR; ++h)
+            good[h] = has[h] && largest(largest(largest(acc[0][2 * h], acc[0][2 * h + 1], acc[1][2 * h]), acc[1][2 * h + 1], acc[2][2 * h]),
+                                        largest(acc[2][2 * h + 1], acc[3][2 * h], acc[3][2 * h + 1]), 0.f) < INFINITY;
         if (pl.y_vec && f0 + 32 <= end) {
 #pragma unroll
             for (int h = 0; h < HR; ++h) {
@@ -557,10 +597,9 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
                     v[0] = make_uint4(add(o.x, 0), add(o.y, 1), add(o.z, 2), add(o.w, 3));
                 }
 #pragma unroll
-                for (int i = 0; i < YV; ++i) store16_if(reinterpret_cast<uint4*>(y_row[h] + f0 + 8 * t) + i, v[i], has[h]);
+                for (int i = 0; i < YV; ++i) store16_if(reinterpret_cast<uint4*>(y_row[h] + f0 + 8 * t) + i, v[i], good[h]);
             }
         } else {  // a segment's last features, or rows that are not aligned: one by one
-            const int fs = TR == 8 && odd ? 8 : 2, ft = f0 + (TR == 8 && odd ? 2 : 8) * t;  // element e is feature ft + (e >> 1) * fs + (e & 1)
 #pragma unroll
             for (int h = 0; h < HR; ++h) {
                 YT o[8];
@@ -573,12 +612,36 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int f = ft + (e >> 1) * fs + (e & 1);
-                    store_if(y_row[h] + f, from_f32<YT>(to_f32(o[e]) + acc[e >> 1][2 * h + (e & 1)]), has[h] && f < end);
+                    store_if(y_row[h] + f, from_f32<YT>(to_f32(o[e]) + acc[e >> 1][2 * h + (e & 1)]), good[h] && f < end);
                 }
             }
         }
         if (n + D < mine) fetch(next, cur);
         copy_commit();
+        bool again = has[0] && !good[0];
+        if constexpr (HR == 2) again = again || (has[1] && !good[1]);
+        if (__any_sync(0xffffffffu, again)) {  // (seldom: sums that are not finite, with h put together from its terms)
+#pragma unroll 1
+            for (int at_e = 0; at_e < 8 * HR; ++at_e) {
+                float v = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8 * HR; ++e) v = e == at_e ? acc[(e & 7) >> 1][2 * (e >> 3) + (e & 1)] : v;
+                const int h = at_e >> 3, f = ft + ((at_e & 7) >> 1) * fs + (at_e & 1);
+                if ((HR == 2 && h ? has[HR - 1] && !good[HR - 1] : has[0] && !good[0]) && f < end) {
+                    if (!(fabsf(v) < INFINITY)) {
+                        const __nv_bfloat16* hc = hs + (here.s * 3 * TR + q * 16 + h * 8 + g) * pl.h_stride;
+                        v = 0.f;
+                        for (int j = 0; j < p.R; ++j) {
+                            const float h0 = __bfloat162float(hc[j]), h1 = __bfloat162float(hc[TR * pl.h_stride + j]), h2 = __bfloat162float(hc[2 * TR * pl.h_stride + j]);
+                            v = fmaf(to_f32(B[(int64_t)f * p.R + j]), h0 + (h1 + h2), v);
+                        }
+                    }
+                    YT* const o = (HR == 2 && h ? y_row[HR - 1] : y_row[0]) + f;
+                    *o = from_f32<YT>(to_f32(*o) + v);
+                }
+            }
+            __syncwarp();
+        }
         ahead(here, stride);
         ahead(next, stride);
     }

@@ -361,6 +361,87 @@ def test_lora_rows_of_other_adapters_do_not_leak_nan():
     assert torch.equal(got[keep], want[keep])
 
 
+def _lora_same(got, ref, tol):
+    """NaN where the definition has NaN, its infinities, and near it elsewhere."""
+    got = got.double().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    inf = np.isinf(ref)
+    assert np.array_equal(got[inf], ref[inf])
+    ok = np.isfinite(ref)
+    assert np.isfinite(got[ok]).all() and (np.abs(got - ref)[ok] <= tol[ok]).all()
+
+
+@pytest.mark.parametrize("types", [("bf16", "f32", "bf16"), ("f32", "f32", "bf16"), ("bf16", "f32", "f32"), ("f32", "f32", "f32")], ids=str)
+@pytest.mark.parametrize("case", [(1, 1, 8, 256, (0, 128)), (23, 2, 24, 264, (0, 80, 163)), (960, 2, 56, 72, (0, 64, 1040)), (40, 3, 16, 1000, (0, 1001))], ids=str)
+@np.errstate(invalid="ignore", over="ignore")
+def test_lora_infinities_and_nan_where_the_definition_has_them(case, types):
+    """An infinity in x, in A or in B gives what the sums of the definition give, in its own rows and features only; the
+    others keep their bits."""
+    import torch
+    from paper_2410_12513_b200 import first_lora
+    rows, n, rank, k, seg = case
+    x, a, b, ids, y, _ = _lora_inputs(case, *(_t(v) for v in types), 19)
+    ids[:] = torch.arange(rows) % n
+    plain = y.clone()
+    first_lora(x, a, b, ids, plain, segments=seg)
+    inf = float("inf")
+    for where in ("x", "x two signs", "x nan", "a", "b", "b and a"):
+        x1, a1, b1 = x.clone(), a.clone(), b.clone()
+        hit = torch.zeros(rows, dtype=torch.bool, device="cuda")
+        if where[0] == "x":
+            hit[::7] = True
+            x1[::7, k // 3] = float("nan") if "nan" in where else inf
+            if "two" in where:
+                x1[::7, k - 1] = -inf
+        if "a" in where.split():
+            a1[n - 1, 3, k // 2] = -inf
+            hit |= ids == n - 1
+        if where[0] == "b":
+            b1[n - 1, seg[-1] - 2, rank - 1] = inf
+            hit |= ids == n - 1
+        ref, mag = _lora_ref(x1, a1, b1, ids, y, None, seg)
+        got = y.clone()
+        first_lora(x1, a1, b1, ids, got, segments=seg)
+        _lora_same(got, ref, (k / 8 + rank + 24) * U32 * mag)  # (as in test_lora)
+        assert torch.equal(got[~hit], plain[~hit])
+        if where == "b":
+            keep = torch.arange(seg[-1], device="cuda") != seg[-1] - 2
+            assert torch.equal(got[:, keep], plain[:, keep])
+
+
+@pytest.mark.parametrize("rows", [1, 9, 960])
+def test_lora_largest_float32_values(rows):
+    """Finite float32 values that bfloat16 rounds to an infinity, in x, A, B and in A x."""
+    import torch
+    from paper_2410_12513_b200 import first_lora
+    most = float(np.finfo(np.float32).max)
+    case = (rows, 1, 8, 40, (0, 1040))
+    for where in ("x", "a", "b", "h"):
+        x, a, b, ids, y, _ = _lora_inputs(case, _t("f32"), _t("f32"), _t("f32"), 3)
+        ids.zero_()
+        if where == "x":
+            x[:, 5] = -most
+            a *= 1e-3
+            b *= 1e-2
+        elif where == "a":
+            a[0, 2, 7] = 3.4e38
+            x *= 1e-3
+            b *= 1e-2
+        elif where == "b":
+            b[0, 33, 1] = most
+            a *= 1e-4
+        else:
+            x.zero_()
+            x[:, 0] = 1.0
+            a.zero_()
+            a[0, :, 0] = torch.tensor([3.4e38, -3.4e38, 1.0, most, 0.0, -most, 2.0, 1e38])
+            b *= 1e-2
+        ref, mag = _lora_ref(x, a, b, ids, y, None, case[4])
+        assert np.isfinite(ref).all() and np.abs(ref).max() < most / 2
+        first_lora(x, a, b, ids, y)
+        _lora_same(y, ref, (40 / 8 + 8 + 24) * U32 * mag)
+
+
 def test_lora_on_another_stream_and_in_a_graph():
     import torch
     from paper_2410_12513_b200 import first_lora
