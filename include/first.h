@@ -395,7 +395,7 @@ int first_set_sampling_rows(first_ctx *ctx, const first_sampling *sampling);
  * float32 sums, in their own rows and features (such sums are formed one by one: slow).  The result does not depend on which
  * other rows are in the batch.  rows = 0 or n_adapters = 0 does nothing.  No scratch, no wait.
  * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides, segments), FIRST_E_UNSUPPORTED (rank not a multiple of 8 or above
- * FIRST_LORA_MAX_RANK, k not a multiple of 8, more than FIRST_LORA_MAX_SEGMENTS segments, an inner border that is no
+ * FIRST_LORA_MAX_RANK, k not a multiple of 8, k or n above 2^30, more than FIRST_LORA_MAX_SEGMENTS segments, an inner border that is no
  * multiple of 16; x, a, b not 16-byte aligned or rows of x not a multiple of 16 bytes apart; y not aligned to its
  * element), FIRST_E_CUDA.
  *

@@ -36,6 +36,7 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 256, kWarps = 8, kCluster = 8;
 constexpr int kParts = 8;           // (16-row tile of A, share of the input features) pairs a CTA cuts its part of the shrink into, about
 constexpr int kMaxRows = 1024;      // rows of a launch (the ids are sorted into tiles by every CTA)
+constexpr int kMaxSize = 1 << 30;   // input, output features (numbers of them are rounded up to tiles in 32 bits)
 constexpr int kMaxIds = 4096;       // adapters that can be; with more, every row is a tile of its own
 
 // (x, y) -> packed bfloat16 pairs: term 0 the nearest bfloat16, the others what is left (nothing, of an infinity or NaN)
@@ -732,15 +733,15 @@ cudaError_t launch_x(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) {
 
 cudaError_t lora_launch(const LoraArgs& args, cudaStream_t st, bool pdl, int n_sm) {
     LoraArgs a = args;
-    for (int r0 = 0; r0 < args.m; r0 += kMaxRows) {
-        a.m = std::min(kMaxRows, args.m - r0);
+    for (int64_t r0 = 0; r0 < args.m; r0 += kMaxRows) {
+        a.m = (int)std::min<int64_t>(kMaxRows, args.m - r0);
         const size_t xe = args.x_kind == kLoraXF32 ? 4 : 2, ye = args.y_f32 ? 4 : 2;
         a.x = static_cast<const char*>(args.x) + (size_t)r0 * args.ldx * xe;
         a.x_lo = args.x_lo ? static_cast<const char*>(args.x_lo) + (size_t)r0 * args.ldx * xe : nullptr;
         if (args.idx) a.idx = args.idx + r0;
         else a.adapter = args.adapter + r0;
         if (!args.scatter) a.y = static_cast<char*>(args.y) + (size_t)r0 * args.ldy * ye;
-        a.row0 = r0;
+        a.row0 = (int)r0;
         const cudaError_t e =
             a.w_f32 ? (a.y_f32 ? launch_x<float, float>(a, st, pdl, n_sm) : launch_x<float, __nv_bfloat16>(a, st, pdl, n_sm))
                     : (a.y_f32 ? launch_x<__nv_bfloat16, float>(a, st, pdl, n_sm) : launch_x<__nv_bfloat16, __nv_bfloat16>(a, st, pdl, n_sm));
@@ -763,6 +764,7 @@ extern "C" int first_lora(const void* x, int32_t x_dtype, int64_t x_stride, cons
     if (!x || !a || !b || !row_adapter || !y || !segments) return FIRST_E_ARG;
     for (int32_t dt : {x_dtype, w_dtype, y_dtype})
         if (dt != FIRST_DTYPE_F32 && dt != FIRST_DTYPE_BF16) return FIRST_E_ARG;
+    if (k > kMaxSize || n > kMaxSize) return FIRST_E_UNSUPPORTED;
     if (n_segments > FIRST_LORA_MAX_SEGMENTS || rank > FIRST_LORA_MAX_RANK || rank % 8 || k % 8) return FIRST_E_UNSUPPORTED;
     if (segments[0] != 0 || segments[n_segments] != n) return FIRST_E_SHAPE;
     for (int i = 0; i < n_segments; ++i) {

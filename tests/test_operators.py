@@ -95,6 +95,13 @@ def test_rope_refuses():
     assert call(T=10, qt=128, qh=1279, hk=0) == SHAPE
 
 
+def test_lora_refuses_sizes_that_32_bits_cannot_round_up():
+    L = _L()
+    for k, n in ((2 ** 31 - 8, 100), (2 ** 30 + 8, 100), (256, 2 ** 31 - 1), (256, 2 ** 30 + 1)):
+        seg = (C.c_int32 * 2)(0, n)
+        assert L.first_lora(P, 1, k, P, P, 1, None, P, 4, 8, 1, seg, 1, k, n, P, 0, n, None) == UNSUPPORTED
+
+
 def test_rope_refuses_addresses_between_elements():
     L = _L()
     for dt, q, k in ((1, P + 1, P), (1, P, P + 3), (0, P + 2, P), (0, P, P + 6), (0, P + 1, P)):
