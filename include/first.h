@@ -355,8 +355,9 @@ int first_sample_topk(const float *logits, int32_t B, int32_t vocab, int32_t top
  * uniform draw; below 0 it counts as 0, at 1 and above (or NaN) as the largest float32 below 1.  temperature <= 0 (or NaN) is greedy: the
  * lowest index among the largest logits; below 1e-37 it counts as that, from 1e30 on as infinite (all weights 1).  A row without a candidate gets token -1 (which a later step refuses with
  * FIRST_FLAG_BAD_TOKEN).  With top_k alone the result is first_sample_topk's, up to such a rounding.
- * Weights have float32's precision, sums of them are formed in integers and float64, in a fixed order: the result is
- * the same in every run, and a draw (or top_p) that falls within float32's rounding of a weight's border may take the neighbour.
+ * Weights have float32's precision (each to 2^-21 of itself), sums of them are formed in integers and float64, in a fixed order:
+ * the result is the same in every run, and a draw (or top_p) that falls within float32's rounding of a weight's border may take
+ * the neighbour.  Equal weights add up exactly.
  *   logits       dev float32 [B][row_stride], row_stride >= vocab (elements; columns beyond vocab are not read)
  *   temperature, top_p, min_p   dev float32 [B] or NULL (= 1, 1, 0 for every row)
  *   top_k        dev int32 [B] or NULL (= no limit)

@@ -134,7 +134,11 @@ struct Row {  // what a thread needs to know about the row
     // a bin's upper end, above shift; rounded up, so that no element of the bin is above it
     __device__ __forceinline__ float end_of(float bin) const { return __fmaf_ru(-bin, half_T, top); }
     // Weight of x in units of 2^-23 of that of its bin's upper end X (x - shift - X is exact but where it does not matter; it
-    // is above 0 by a rounding at most): at most 2^23 - 1, so that 512 of them have 32 bits.
+    // is above 0 by a rounding at most): at most 2^23 - 1, so that 512 of them have 32 bits.  That keeps a float32 weight's 24 bits,
+    // and each is right to 2^-21 of itself, the hardware's exponential included; the errors of many weights cancel for the most
+    // part.  Draws placed next to tokens' borders (50257 to 262144 tokens, spreads of 0 to 4 T) came out with another token
+    // only when within 2^-26 of the sum, where a float32 draw itself has steps of 2^-24.  More bits (64-bit weights to 2^-31)
+    // would take about twice the instructions of a pass over the row.
     __device__ __forceinline__ uint32_t units(float x, float X) const {
         return __float_as_uint(ex2(fminf((x - shift - X) * inv_Tl2, -2.5e-7f)) + 1.f) - 0x3f800000u;
     }
@@ -221,7 +225,7 @@ __device__ __forceinline__ T warp_scan(T run, int lane) {
     return run;
 }
 
-// grid B * C in clusters of C; one cluster per row.  Every decision is taken by every warp of every CTA from the same
+// grid B * C in clusters of C; one cluster per row.  Every decision is taken by the first warp of every CTA from the same
 // numbers, so the cluster stays together without anyone telling the others.
 template <bool HELD, bool VEC>
 __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
@@ -816,7 +820,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_rows(const SampleArgs p) {
 }  // namespace
 
 cudaError_t sample_launch(const SampleArgs& a, cudaStream_t st, bool pdl) {
-    // as many CTAs per row as hold it in shared memory (a power of two, eight at most: 262144 elements)
+    // as many CTAs per row as hold it in shared memory (a power of two, eight at most: 131072 elements)
     int C = 1;
     while (C < kCluster && (int64_t)C * kHeld < a.V) C *= 2;
     const bool held = (int64_t)C * kHeld >= a.V;

@@ -775,6 +775,48 @@ def test_sample_hundreds_of_candidates_two_steps_below_the_maximum():
     assert _sample_check(x, np.array([0.98], np.float32), np.array([2.5444e-6])) == [364]
 
 
+@pytest.mark.parametrize("V", [777, 50257, 128256, 262144])
+def test_sample_of_equal_weights_is_exact(V):
+    """Equal weights: token floor(u n) of the n candidates, with no allowance, however small a share of the sum one is."""
+    g = np.random.default_rng(V)
+    x = np.full((64, V), 1.75, np.float32)
+    n = np.full(64, V)
+    for r in range(1, 64, 2):  # every second row: some of them, below a filter's limit the others
+        n[r] = g.integers(1, V)
+        x[r, g.choice(V, V - n[r], replace=False)] = -np.inf
+    u = ((np.floor(g.random(64) * n) + 0.1 + 0.8 * g.random(64)) / n).astype(np.float32)
+    u = np.minimum(u, np.float32(1 - 2.0 ** -24))
+    at = u.astype(np.float64) * n
+    clear = np.abs(at - np.round(at)) > 1e-6 * n * 2.0 ** -24  # (the sums are exact; u n has 64 bits)
+    for temp in (None, np.full(64, 0.7), np.full(64, 1e-6), np.full(64, np.inf)):
+        got = _sample_tokens(x, u, temp)
+        for r in np.nonzero(clear)[0]:
+            assert got[r] == np.nonzero(x[r] > -np.inf)[0][int(at[r])], r
+
+
+@pytest.mark.parametrize("V", [50257, 262144])
+@pytest.mark.parametrize("spread,temp", [(0.01, 1.0), (0.5, 1.0), (2.5, 0.6), (4.0, 1.3)])
+def test_sample_is_as_fine_as_its_draws(V, spread, temp):
+    """Draws next to tokens' borders: the token is that of a draw at most one step of float32 (2^-24) away."""
+    g = np.random.default_rng(V)
+    B = 32
+    x = (spread * g.standard_normal((B, V))).astype(np.float32)
+    order = np.argsort(-x, axis=1, kind="stable")
+    xs = np.take_along_axis(x, order, 1).astype(np.float64)
+    cum = np.cumsum(np.exp((xs - xs[:, :1]) / float(np.float32(temp))), 1)
+    share = cum / cum[:, -1:]
+    place = np.empty_like(order)
+    np.put_along_axis(place, order, np.arange(V)[None], 1)
+    for trial in range(6):
+        j = np.array([min(int(np.searchsorted(share[b], g.random())), V - 2) for b in range(B)])
+        u = share[np.arange(B), j].astype(np.float32)
+        u = np.clip(np.nextafter(u, np.float32(trial % 2)) if trial % 3 else u, 0, np.float32(1 - 2.0 ** -24))
+        got = place[np.arange(B), _sample_tokens(x, u, np.full(B, temp))]
+        hi = share[np.arange(B), got]
+        lo = np.where(got > 0, share[np.arange(B), np.maximum(got - 1, 0)], 0.0)
+        assert np.maximum(u - hi, lo - u).max() <= 2.0 ** -24
+
+
 @pytest.mark.parametrize("B,V", [(200, 128256), (96, 40001), (64, 20011)])
 def test_sample_is_the_same_beside_other_work(B, V):
     """The exchanges inside a cluster and the hand-over to one CTA while other kernels delay some of its warps: every
