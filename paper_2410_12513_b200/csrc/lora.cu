@@ -407,8 +407,9 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
     // ---- expand, set-up: a step = 32 output features of one segment and 16 rows of the tile; as the rows of B are dealt out to
     // the tensor cores' columns, a thread has eight consecutive features of the rows g and g + 8, so y moves 16 bytes at a
     // time.  Where y's rows are not aligned for that (`odd`; tiles of 8 rows only) it has the pairs 8j + 2t, so that a row's
-    // four threads touch neighbours (40 rows of 25433 features: 45 us, with eight apiece 94).  The operands of a warp's next steps are copied to shared memory (odd y partly to L2 only) in the
-    // background (each thread reads what it copied itself); the first ones are on their way while the cluster meets.
+    // four threads touch neighbours (half the time that eight apiece took).  The operands of a warp's next steps are copied to
+    // shared memory (odd y partly to L2 only) in the background (each thread reads what it copied itself); the first ones are on
+    // their way while the cluster meets.
     constexpr int HR = TR == 8 ? 1 : 2;  // 8-row halves of a 16-row tile that are used
     constexpr int D = steps_ahead(TR);   // steps in flight
     int steps = 0;                       // (of 32 features)
@@ -418,8 +419,8 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
     // with a second 16-row tile in use every other warp has that one
     const bool two = live > 16;
     const bool odd = TR == 8 && !pl.y_vec;
-    // odd y word by word, where that costs no spills (63 rows of 16793 features 55 -> 49 us; with 64 registers 256 rows of down,
-    // which have nothing of it, 34 -> 36)
+    // odd y word by word, where there are registers for it (63 rows, 4096 -> 16793 in float32: 15.2 us, without 15.8; 77 rows of
+    // 2040 -> 1000, which are aligned, pay for it: 10.6, without 9.9)
     constexpr bool kWords = TR == 8 && OCC == 2 && sizeof(YT) == 4;
     const int q = two ? warp & 1 : 0, stride = two ? kWarps / 2 : kWarps;
     const int mine = max(0, (last - first - (two ? warp >> 1 : warp) + stride - 1) / stride);  // this warp's steps
@@ -541,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
         [[maybe_unused]] Frag<NW, 4> w_next[4];
         for (int kb = 0; kb < kbs; ++kb) {
             Frag<NW, 4> w[4];
-            if constexpr (TR == 8 && OCC == 2) {  // (there are registers for the next columns: 9 rows of rank 56 in float32 15 us, without 18)
+            if constexpr (TR == 8 && OCC == 2) {  // (there are registers for the next columns: 9 rows, 4096 -> 4096 at rank 56 in float32: 14.7 us, without 15.9)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[j] = kb ? w_next[j] : shared_frag<WT>(&cur.w[j][lane]);
                 if (kb + 1 < kbs)
@@ -701,10 +702,11 @@ cudaError_t launch_rows(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) 
     // At most as many tiles as: one for every row, or one ragged tile for every adapter and full ones for the rest.
     auto tiles_of = [&](int rows) { return a.n > kMaxIds || a.m == 1 ? a.m : (int)std::min<int64_t>(a.m, (int64_t)a.n + a.m / rows); };
     size_t smem;
-    // Tiles of 32 rows once an adapter has 16 rows on average (1024 rows of 8 adapters, gate|up: 47 us against 87 with tiles
-    // of 8) and they fill the GPU (362 rows of 8 adapters, 152 CTAs: 38 us against 28 with tiles of 8), if their h fits (four
-    // segments of rank 128 do not) and y is aligned; else of 8.  (x in two halves comes from the step, whose batches and
-    // prompt chunks have too few rows for them.)
+    // Tiles of 32 rows once an adapter has 16 rows on average (1024 rows of 8 adapters, gate|up: 46.7 us against 83.5 with
+    // tiles of 8) and they fill the GPU (362 rows of 8 adapters, 4096 -> 6144, 152 CTAs: 15.5 us against 13.6 with tiles of 8), if
+    // their h fits (four segments of rank 128 do not) and y is aligned; else of 8.  Adapters are counted as they are resident: how
+    // many of them the rows use is known on the device only.  (x in two halves comes from the step, whose batches and prompt
+    // chunks have too few rows for them.)
     if constexpr (XK != kLoraXPair)
         if (a.m >= 16 * (int64_t)a.n && a.m > 32 && 2 * tiles_of(32) * kCluster > 3 * n_sm) {
             const Plan pl = plan_of(a, 32, tiles_of(32), n_sm, smem);
@@ -713,7 +715,7 @@ cudaError_t launch_rows(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm) 
     const int tiles = tiles_of(8);
     const Plan pl = plan_of(a, 8, tiles, n_sm, smem);
     // With 64 registers four CTAs fit on a multiprocessor instead of two, at the price of spills: 256 rows of 64 adapters
-    // (512 CTAs) 34 us against 48 with three, 32 rows of 16 adapters (160 CTAs) 12.7 against 10.9.  float32 adapters take
+    // (768 CTAs) 33.7 us against 36.9 with two, 32 rows of 16 adapters (160 CTAs) 11.7 against 10.2.  float32 adapters take
     // three times the registers and stay at two.
     if constexpr (sizeof(WT) == 2)
         if (tiles * kCluster > 2 * n_sm) return launch_tiles<XK, WT, YT, 8, 4>(a, pl, smem, st, pdl);
@@ -789,5 +791,5 @@ extern "C" int first_lora(const void* x, int32_t x_dtype, int64_t x_stride, cons
     for (int i = 0; i <= n_segments; ++i) p.seg[i] = segments[i];
     p.y = y; p.y_f32 = y_dtype == FIRST_DTYPE_F32; p.ldy = y_stride;
     p.m = rows;
-    return lora_launch(p, static_cast<cudaStream_t>(stream), false, 148) == cudaSuccess ? FIRST_OK : FIRST_E_CUDA;
+    return lora_launch(p, static_cast<cudaStream_t>(stream), false, kSMs) == cudaSuccess ? FIRST_OK : FIRST_E_CUDA;
 }

@@ -6,6 +6,9 @@
 
 namespace first {
 
+constexpr int kSMs = 148;  // of a B200; for rules on grid sizes in calls without a context
+constexpr int kLoraMaxSegments = 4, kLoraMaxRank = 128;
+
 enum LoraX { kLoraXF32 = 0, kLoraXBf16 = 1, kLoraXPair = 2 };  // kLoraXPair: bfloat16 hi + lo halves (x = hi + lo)
 
 // y[row(i)][f] += scale[a] * sum_j B[a][f][j] * (sum_k A[a][seg(f)*R + j][k] * x[i][k]),  a = adapter[seq(i)],
@@ -19,7 +22,7 @@ struct LoraArgs {
     const float* scales = nullptr;          // [n] or NULL (= 1)
     const int32_t* adapter = nullptr;
     int n = 0, S = 1, R = 0, K = 0, N = 0;
-    int seg[5] = {};                        // borders of the output segments, seg[0] = 0, seg[S] = N
+    int seg[kLoraMaxSegments + 1] = {};     // borders of the output segments, seg[0] = 0, seg[S] = N
     void* y = nullptr;
     bool y_f32 = true;
     int64_t ldy = 0;
@@ -30,7 +33,6 @@ struct LoraArgs {
     int row0 = 0;                           // (set by lora_launch: rows before this piece, for m_dev)
     uint64_t* stamp = nullptr;
 };
-constexpr int kLoraMaxSegments = 4, kLoraMaxRank = 128;
 cudaError_t lora_launch(const LoraArgs& a, cudaStream_t st, bool pdl, int n_sm);
 
 struct SampleArgs {

@@ -4,6 +4,7 @@
 
 #include "common.cuh"
 #include "first.h"
+#include "ops.h"
 
 using namespace first;
 
@@ -101,7 +102,7 @@ template <typename T, int V>
 cudaError_t launch(RopeArgs p, bool interleaved, cudaStream_t st) {
     p.nv = p.half / V;
     // Heads per thread: one while the launch is small, more once the threads fill the GPU anyway.
-    const int64_t one = p.tokens * p.nv * p.H, full = 148 * 2048;
+    const int64_t one = p.tokens * p.nv * p.H, full = kSMs * 2048;
     const int per = (int)(one <= full ? 1 : one / full < 8 ? one / full : 8);
     p.hg = (p.H + per - 1) / per;
     // If an equal share of up to half as many fills whole blocks with whole tokens (or tokens with blocks), that one: a block's

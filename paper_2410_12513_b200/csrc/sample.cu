@@ -16,8 +16,8 @@
 // same in every run.  Weights are taken relative to that of the upper end X of their bin: exp((x - X) / T) with the
 // difference exact, as integers in units of 2^-23, which keeps float32's 24 bits; the bins' own weights and all prefix
 // sums are 64-bit floating point.
-// Bound by the latency of these phases, one after the other with an exchange between the CTAs each: 10.4 us for one row of
-// 128256 at top-k 10, 31 us for 32 rows with settings of their own, 156 us for 256 (0.84 TB/s: two rows' CTAs share a
+// Bound by the latency of these phases, one after the other with an exchange between the CTAs each: 10.6 us for one row of
+// 128256 at top-k 10, 32 us for 32 rows with settings of their own, 161 us for 256 (0.82 TB/s: two rows' CTAs share a
 // multiprocessor, the launch is seven waves of rows).
 #include <cfloat>
 #include <cooperative_groups.h>
@@ -36,7 +36,7 @@ constexpr int kBlock = 16;           // elements a thread looks at at a time
 constexpr int kHeld = 2 * kBlock * kThreads;  // elements that a CTA can hold in shared memory
 constexpr int kCluster = 8;
 constexpr int kBins = 32;
-constexpr int kResident = 2 * 148;   // CTAs on the GPU at a time
+constexpr int kResident = 2 * kSMs;  // CTAs on the GPU at a time
 constexpr int kLocal = 2560;         // elements that a CTA can copy to shared memory for a search
 constexpr int kMoved = kHeld / 2;    // the same in the place of a row, once the row itself is not needed any more
 constexpr int kList = 256;           // elements that are sorted in every CTA of a cluster; of each CTA an equal share
@@ -827,7 +827,7 @@ cudaError_t sample_launch(const SampleArgs& a, cudaStream_t st, bool pdl) {
     const int chunk = ((a.V + C - 1) / C + 3) / 4 * 4, block = kBlock * kThreads;
     SampleArgs p = a;
     // One CTA is slower with a long list than eight, but leaves seven places to other rows: where the grid is several
-    // times what the GPU holds, it is given more (256 rows: 156 us against 162; 128 rows: 89 against 85; 32 rows: 34 against 31).
+    // times what the GPU holds, it is given more (256 rows: 4 % less time; 128 rows: 89 against 85; 32 rows: 34 against 31).
     p.move_max = a.B * C > 4 * kResident ? kMoved : kMoved / 2;
     const size_t smem = sizeof(Smem) + (C == 1 ? (size_t)(chunk + block - 1) / block * block * 4 : (size_t)kHeld * 4);
     const bool vec = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && (a.B == 1 || a.ld % 4 == 0);
