@@ -520,8 +520,9 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
                 const WT* A = static_cast<const WT*>(p.a) + ((int64_t)ad * M + s * p.R + j) * p.K;
                 const int64_t o = (int64_t)rows_s[col] * p.ldx;
                 v = 0.f;
-#pragma unroll 8
-                for (int k = 0; k < p.K; ++k) v = fmaf(to_f32(A[k]), x_at<XK>(p, o + k), v);
+                for (int k = 0; k < p.K && v == v; k += 8)  // (a NaN stays one: rows full of them end at once)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v = fmaf(to_f32(A[k + i]), x_at<XK>(p, o + k + i), v);
             }
         }
         uint16_t t3[3];
@@ -633,10 +634,12 @@ __global__ void __launch_bounds__(kThreads, OCC) lora_tiles(const LoraArgs p, co
                     if (!(fabsf(v) < INFINITY)) {
                         const __nv_bfloat16* hc = hs + (here.s * 3 * TR + q * 16 + h * 8 + g) * pl.h_stride;
                         v = 0.f;
-                        for (int j = 0; j < p.R; ++j) {
-                            const float h0 = __bfloat162float(hc[j]), h1 = __bfloat162float(hc[TR * pl.h_stride + j]), h2 = __bfloat162float(hc[2 * TR * pl.h_stride + j]);
-                            v = fmaf(to_f32(B[(int64_t)f * p.R + j]), h0 + (h1 + h2), v);
-                        }
+                        for (int j0 = 0; j0 < p.R && v == v; j0 += 8)
+#pragma unroll
+                            for (int j = j0; j < j0 + 8; ++j) {
+                                const float h0 = __bfloat162float(hc[j]), h1 = __bfloat162float(hc[TR * pl.h_stride + j]), h2 = __bfloat162float(hc[2 * TR * pl.h_stride + j]);
+                                v = fmaf(to_f32(B[(int64_t)f * p.R + j]), h0 + (h1 + h2), v);
+                            }
                     }
                     YT* const o = (HR == 2 && h ? y_row[HR - 1] : y_row[0]) + f;
                     *o = from_f32<YT>(to_f32(*o) + v);

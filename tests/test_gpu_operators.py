@@ -409,6 +409,23 @@ def test_lora_infinities_and_nan_where_the_definition_has_them(case, types):
             assert torch.equal(got[:, keep], plain[:, keep])
 
 
+@pytest.mark.parametrize("types", [("bf16", "bf16", "bf16"), ("f32", "f32", "f32")], ids=str)
+@pytest.mark.parametrize("rows", [1, 40, 960])
+def test_lora_rows_full_of_nan(rows, types):
+    """Every fifth row NaN from end to end: NaN there, the other rows as without them."""
+    import torch
+    from paper_2410_12513_b200 import first_lora
+    case = (rows, 2, 16, 4096, (0, 2048, 2600))
+    x, a, b, ids, y, _ = _lora_inputs(case, *(_t(v) for v in types), 8)
+    ids[:] = torch.arange(rows) % 2
+    want = y.clone()
+    first_lora(x, a, b, ids, want, segments=case[4])
+    x[::5] = float("nan")
+    first_lora(x, a, b, ids, y, segments=case[4])
+    bad = torch.arange(rows, device="cuda") % 5 == 0
+    assert y[bad].isnan().all() and torch.equal(y[~bad], want[~bad])
+
+
 @pytest.mark.parametrize("rows", [1, 9, 960])
 def test_lora_largest_float32_values(rows):
     """Finite float32 values that bfloat16 rounds to an infinity, in x, A, B and in A x."""
