@@ -15,9 +15,9 @@
 // is not finite is formed again in plain float32.  How the sums are ordered depends on the sizes k, n, rank alone, so a row's result does not depend on
 // the rows around it.
 //
-// Measured (on the device; adapters, x and y larger than L2 in turn): 1 row of q|k|v at rank 8 6.3 us, 32 rows of 16 adapters 10.1 us (1.1 TB/s),
-// 256 rows of 64 adapters at the down projection 33.7 us (2.9 TB/s; the shrink, which streams A, is more than half of it), 1024 rows of 8
-// adapters at gate|up 46.7 us (2.7 TB/s; y begins to move after 12 us of plan, shrink and meeting; 44.8 without the look for
+// Measured (on the device; adapters, x and y larger than L2 in turn): 1 row of q|k|v at rank 8 6.3 us, 32 rows of 16 adapters 9.9 us (1.1 TB/s),
+// 256 rows of 64 adapters at the down projection 34.0 us (2.9 TB/s; the shrink, which streams A, is more than half of it), 1024 rows of 8
+// adapters at gate|up 46.1 us (2.7 TB/s; y begins to move after 12 us of plan, shrink and meeting; 44.8 without the look for
 // sums that are not finite).
 #include <algorithm>
 #include <type_traits>
