@@ -69,7 +69,9 @@ extern "C" {
 #define FIRST_FLAG_WAIT_EXPIRED 8u /* a bounded wait inside a kernel gave up */
 #define FIRST_FLAG_EMPTY_SEQ 16u   /* a router call saw a sequence with no tokens */
 #define FIRST_FLAG_BAD_SEQ_TABLE 32u /* a router call saw cu_seqlens entries that are negative, decreasing or
-                                        beyond total_tokens; that sequence's mask byte and score are unwritten */
+                                        beyond total_tokens; that sequence's mask byte and score are unwritten
+                                        (calls on 8-bit caches: likewise, that sequence's rows are left alone) */
+#define FIRST_FLAG_BAD_PAGE 64u    /* a page id outside the cache; what it would hold is left out */
 
 #define FIRST_ROUTER_MEAN_OF_SIGMOID 0 /* the paper's order: rho = mean_j sigmoid(z_j) */
 #define FIRST_ROUTER_SIGMOID_OF_MEAN 1 /* pooled variant:    rho = sigmoid(mean_j z_j) */
@@ -466,6 +468,91 @@ int first_rope(void *q, int64_t q_token_stride, int64_t q_head_stride, int32_t n
                int64_t k_head_stride, int32_t n_kv_heads, int32_t dtype, int64_t tokens, int32_t head_dim, int32_t rot_dim,
                const int32_t *pos, const double *inv_freq, float factor, int32_t interleaved, void *stream);
 int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
+
+/* A paged cache in 8 bits.  One first_cache8 is one layer's: pages of `page` tokens, each holding, head by head, that many
+ * keys (and values) of head_dim 8-bit numbers, and one float32 scale a (page, head): a key is its number times its page's
+ * scale.  Sequences own lists of pages, [B][max_pages] ids, -1 = none: position t of sequence b is token t % page of page
+ * pages[b][t / page].  Two sequences may share a page that neither appends to (first_pages_* keeps count of that).  In 8
+ * bits a cache takes half of the room and, in decoding, half of the time of a bfloat16 one; rounding: half a 1/127 of the
+ * page's largest key (INT8), or 2^-4 of each value (E4M3, 3 bits of mantissa).
+ *   k, v              dev [n_pages][n_kv_heads][page][head_dim], 16-byte aligned
+ *   k_scale, v_scale  dev float32 [n_pages][n_kv_heads]
+ * page 16, 32, 64 or 128; head_dim 32, 64 or 128 (FIRST_E_UNSUPPORTED otherwise).
+ *
+ * Calls on a batch: the new tokens of sequence b are rows cu_new[b] .. cu_new[b+1]-1 of the tensors (dev int32 [B+1]; total = rows of
+ * the tensors; rows from cu_new[B] on are left alone), at most max_new of any sequence (a host value: it sizes the launch);
+ * cu_new NULL: one row a sequence (total = B).  Their positions start at len[b], the tokens that the sequence held before.  Row (t, head) of a tensor
+ * is at t*token_stride + head*head_stride (elements), head_dim adjacent elements, float32 or bfloat16 (dtype).
+ * Errors that only the device sees set bits in *flags (dev uint32 or NULL; OR-ed in, never cleared): FIRST_FLAG_BAD_SEQ_TABLE
+ * (cu_new or len cannot be, or more than max_new new tokens: that sequence is left out), FIRST_FLAG_BAD_PAGE (an id outside
+ * the cache: counts as -1), FIRST_FLAG_KV_FULL (a new token without a page is not stored).  No scratch, no wait, one launch.
+ *
+ * first_append8  stores new keys and values.  For every page and head that gains tokens: scale = max(its scale, if the page held
+ *                tokens of the sequence before, else 0; largest finite magnitude of the new ones * 1/127 (E4M3: 1/448)), in
+ *                float32; each new value is stored as the number nearest to value / scale (the exact quotient; ties to even; infinities saturate, NaN is
+ *                stored as 0); where the scale grew, earlier numbers are rounded anew, to the nearest of number * old / new.
+ * first_read8    the values of rows: row cu[b] + i of k and v takes position start[b] + i (number * scale, rounded to dtype).
+ *                A position without a page leaves its row alone and sets FIRST_FLAG_BAD_PAGE.
+ * first_attn8    attention of the new tokens (already appended): new token i of sequence b sees positions 0 .. len[b] + i;
+ *                out = sum_t softmax_t(scale * q . k_t) v_t, query head h with KV head h / (n_q_heads / n_kv_heads).
+ *                Positions without a page are not there; a row that sees nothing gives zeros.  Products and sums are
+ *                float32; weights have 11 bits of mantissa with bfloat16 q and 22 with float32 q; out is rounded once.  The
+ *                result is the same in every run and depends on nothing but the sequence itself and the launch's sizes (B, max_new, max_pages).  Meant for one token a sequence and
+ *                for drafts under verification: the cache is read once for every 32 (float32: 16) query rows of a KV head.
+ * first_copy_pages  copies pages (keys, values, scales) within the layers' caches: moves dev int32 [n_moves][3] of (layer,
+ *                from, to).  All layers alike in format and sizes.  No page may be written twice, nor be both read and
+ *                written.  A move outside the caches is left out (FIRST_FLAG_BAD_PAGE).
+ * Errors: FIRST_E_ARG, FIRST_E_SHAPE (negative strides, rows that are written overlap, total != B without cu_new, heads),
+ * FIRST_E_UNSUPPORTED (page, head_dim, alignment, more than 1024 KV heads, more than 96 layers), FIRST_E_CAPACITY (grid
+ * sizes: max_pages * page above 2^30, more than 65000 pages or 2^18 query rows a sequence, first_read8: B above 65535), FIRST_E_CUDA. */
+#define FIRST_CACHE_INT8 0
+#define FIRST_CACHE_E4M3 1
+typedef struct {
+    int32_t format;                              /* FIRST_CACHE_* */
+    int32_t n_pages, n_kv_heads, page, head_dim;
+    void *k, *v;
+    float *k_scale, *v_scale;
+} first_cache8;
+int first_append8(const first_cache8 *cache, const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v,
+                  int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, const int32_t *cu_new, int32_t total,
+                  const int32_t *pages, int32_t max_pages, const int32_t *len, int32_t B, int32_t max_new, uint32_t *flags,
+                  void *stream);
+int first_read8(const first_cache8 *cache, const int32_t *pages, int32_t max_pages, const int32_t *start, const int32_t *cu,
+                int32_t B, int32_t total, int32_t max_rows, void *k, int64_t k_token_stride, int64_t k_head_stride, void *v,
+                int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, uint32_t *flags, void *stream);
+int first_attn8(const first_cache8 *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride, int32_t n_q_heads,
+                int32_t dtype, float scale, const int32_t *cu_new, int32_t total, const int32_t *pages, int32_t max_pages,
+                const int32_t *len, int32_t B, int32_t max_new, void *out, int64_t out_token_stride, int64_t out_head_stride,
+                uint32_t *flags, void *stream);
+int first_copy_pages(const first_cache8 *layers, int32_t n_layers, const int32_t *moves, int64_t n_moves, uint32_t *flags,
+                     void *stream);
+
+/* Verification of drafted tokens.  A cheaper model (a step with more layers skipped, a lookup in the prompt) proposes tokens,
+ * the target scores them all in one pass; the tokens that come out have the target's distribution.  Per sequence, with p_i the target's
+ * distribution behind the first i drafts and q_i the one that draft i was drawn from: draft i is accepted while
+ * u_i q_i(d_i) < p_i(d_i); the token after the accepted ones is drawn from max(0, p_i - q_i) (from p_i where that is all zero), or, if every draft was
+ * accepted, from p_n: the first index whose cumulative weight exceeds draw * (sum of the weights).
+ *   target    dev float32, row i (0 .. n_draft) of sequence b at b*seq_stride + i*row_stride, vocab entries
+ *   draft     the same with n_draft rows, or NULL: every drafted token had probability 1 (q_i = 1 at d_i)
+ *   probs     0: both are logits, p = softmax(logits / temperature[b]), likewise q; -inf closes a token, NaN counts as -inf, +inf as
+ *             the largest float32; temperature <= 0 (or NaN) is greedy (p = 1 at the lowest index among the largest), below
+ *             1e-37 it counts as that, above 1e30 as that.  1: both are probabilities, taken as they are (negative and NaN as
+ *             0), temperature is not read
+ *   drafted   dev int32 [B][n_draft]; the first entry that is no token (such as -1) ends a sequence's drafts
+ *   temperature  dev float32 [B] or NULL (= 1)
+ *   uniforms  dev float32 [B][n_draft], draws dev float32 [B], each in [0,1) (below counts as 0, above or NaN as the largest
+ *             float32 below 1)
+ *   tokens    dev int32 [B][n_draft+1]: the accepted drafts, the new token (-1 if the row has no candidate), then -1
+ *   accepted  dev int32 [B]: how many drafts were accepted
+ * Sums that decide which token a draw falls on are formed in 64 bits; acceptance has float32's precision.  The result is the same in
+ * every run.  Stateless, no scratch, no wait, one launch; B = 0 does nothing.
+ * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides below vocab), FIRST_E_UNSUPPORTED (n_draft > FIRST_VERIFY_MAX_DRAFTS, vocab >
+ * FIRST_SAMPLE_MAX_VOCAB), FIRST_E_CAPACITY, FIRST_E_CUDA. */
+#define FIRST_VERIFY_MAX_DRAFTS 32
+int first_verify(const float *target, int64_t target_seq_stride, int64_t target_row_stride, const float *draft,
+                 int64_t draft_seq_stride, int64_t draft_row_stride, int32_t probs, const int32_t *drafted, int32_t B,
+                 int32_t n_draft, int32_t vocab, const float *temperature, const float *uniforms, const float *draws,
+                 int32_t *tokens, int32_t *accepted, void *stream);
 
 /* Wait for `stream`, read and clear the device flag word.  Returns FIRST_OK with
  * *flags = 0, or FIRST_E_DEVICE_FLAG with the FIRST_FLAG_* bits in *flags. */

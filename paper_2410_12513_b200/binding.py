@@ -14,7 +14,8 @@ _lib = None
 
 FIRST_DTYPE_F32, FIRST_DTYPE_BF16 = 0, 1
 MEAN_OF_SIGMOID, SIGMOID_OF_MEAN = 0, 1
-FLAG_KV_FULL, FLAG_BAD_TOKEN, FLAG_BAD_MASK, FLAG_WAIT_EXPIRED, FLAG_EMPTY_SEQ, FLAG_BAD_SEQ_TABLE = 1, 2, 4, 8, 16, 32
+FLAG_KV_FULL, FLAG_BAD_TOKEN, FLAG_BAD_MASK, FLAG_WAIT_EXPIRED, FLAG_EMPTY_SEQ, FLAG_BAD_SEQ_TABLE, FLAG_BAD_PAGE = 1, 2, 4, 8, 16, 32, 64
+CACHE_INT8, CACHE_E4M3 = 0, 1
 
 
 class FirstError(RuntimeError):
@@ -51,6 +52,11 @@ class SamplingC(C.Structure):
 class AdaptersC(C.Structure):
     _fields_ = [("n_adapters", C.c_int32), ("rank", C.c_int32), ("scales", C.c_void_p), ("seq_adapter", C.c_void_p)] + \
                [(f"{t}_{m}", C.POINTER(C.c_void_p)) for t in ("qkv", "o", "gate_up", "down") for m in ("a", "b")]
+
+
+class Cache8C(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("format", "n_pages", "n_kv_heads", "page", "head_dim")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
 
 
 class RopeSpecC(C.Structure):
@@ -129,7 +135,13 @@ def lib():
         L.first_rope_freqs.argtypes = [C.POINTER(RopeSpecC), p, p]
         L.first_rope.argtypes = [p, i64, i64, i32, p, i64, i64, i32, i32, i64, i32, i32, p, p, C.c_float, i32, p]
         L.first_set_rope.argtypes = [p, p, f64]
-        for name in ("first_sample", "first_set_sampling_rows", "first_lora", "first_set_adapters", "first_rope_freqs",
+        cache8 = C.POINTER(Cache8C)
+        L.first_append8.argtypes = [cache8, p, i64, i64, p, i64, i64, i32, p, i32, p, i32, p, i32, i32, p, p]
+        L.first_read8.argtypes = [cache8, p, i32, p, p, i32, i32, i32, p, i64, i64, p, i64, i64, i32, p, p]
+        L.first_attn8.argtypes = [cache8, p, i64, i64, i32, i32, C.c_float, p, i32, p, i32, p, i32, i32, p, i64, i64, p, p]
+        L.first_copy_pages.argtypes = [cache8, i32, p, i64, p, p]
+        L.first_verify.argtypes = [p, i64, i64, p, i64, i64, i32, p, i32, i32, i32, p, p, p, p, p, p]
+        for name in ("first_append8", "first_read8", "first_attn8", "first_copy_pages", "first_verify", "first_sample", "first_set_sampling_rows", "first_lora", "first_set_adapters", "first_rope_freqs",
                      "first_rope", "first_set_rope"):
             getattr(L, name).restype = C.c_int
         L.first_kernel_class_count.restype = C.c_int32
@@ -546,6 +558,147 @@ def first_rope(q, k, pos, inv_freq, factor=1.0, interleaved=False, stream=None):
                           factor, bool(interleaved), _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_rope")
+
+
+class Cache8:
+    """One layer's paged 8-bit cache (first_cache8 in first.h): k, v CUDA [n_pages][Hkv][page][hd] of torch.int8 or
+    torch.float8_e4m3fn, k_scale, v_scale CUDA float32 [n_pages][Hkv].  Borrowed: holds on to the tensors."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        formats = {torch.int8: CACHE_INT8, torch.float8_e4m3fn: CACHE_E4M3}
+        if k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("k and v must be [pages][heads][tokens][head_dim], alike")
+        if k.dtype not in formats or v.dtype is not k.dtype:
+            raise TypeError("k and v must be int8 or float8_e4m3fn, alike")
+        self.device = k.get_device()
+        n, heads, page, hd = k.shape
+        for t in (k, v):
+            if not t.is_cuda or t.get_device() != self.device or not t.is_contiguous():
+                raise ValueError("k and v must be contiguous, on one CUDA device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.c = Cache8C(formats[k.dtype], n, heads, page, hd, k.data_ptr(), v.data_ptr(),
+                         _on(k_scale, torch.float32, n * heads, "k_scale", self.device),
+                         _on(v_scale, torch.float32, n * heads, "v_scale", self.device))
+        self.ref = C.byref(self.c)
+
+
+def _batch8(cache, dev, pages, len_, cu, total):
+    """(cu, pages, width, len, sequences) of a call on an 8-bit cache."""
+    if cache.device != dev:
+        raise ValueError("the cache is on another device")
+    if pages.dim() != 2:
+        raise ValueError("pages must be [sequences][pages]")
+    B, width = pages.shape
+    return (_on(cu, torch.int32, B + 1, "cu", dev), _on(pages, torch.int32, B * width, "pages", dev), width,
+            _on(len_, torch.int32, B, "len", dev), B)
+
+
+def _flags_on(flags, dev):
+    return _on(flags, torch.int32, 1, "flags", dev)
+
+
+def _kv_rows(cache, k, v):
+    _heads_of(k, "k")
+    _heads_of(v, "v")
+    if k.shape != v.shape or k.dtype is not v.dtype or k.get_device() != v.get_device():
+        raise ValueError("k and v must be alike")
+    if k.shape[1] != cache.c.n_kv_heads or k.shape[2] != cache.c.head_dim:
+        raise ValueError("k and v must have the cache's heads and head size")
+
+
+def first_append8(k, v, cache, pages, len, cu_new=None, max_new=1, flags=None, stream=None):
+    """Stores new keys and values, CUDA [total][Hkv][hd] (strided views are fine), in pages of a Cache8 (see first.h).  pages
+    CUDA int32 [B][n] of page ids; len CUDA int32 [B], tokens before the new ones; cu_new CUDA int32 [B+1], rows of each sequence (None:
+    one row each); max_new: most new tokens of a sequence; flags CUDA int32 [1] or None."""
+    dev = _device_of(k, "k")
+    _kv_rows(cache, k, v)
+    total = k.shape[0]
+    cu, pp, width, lp, B = _batch8(cache, dev, pages, len, cu_new, total)
+    ks, vs = k.stride(), v.stride()
+    rc = lib().first_append8(cache.ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], _code(k, "k"), cu, total, pp,
+                             width, lp, B, max_new, _flags_on(flags, dev), _raw_stream(stream, dev))
+    if rc:
+        raise FirstError(rc, "first_append8")
+
+
+def first_read8(cache, pages, start, k, v, cu=None, max_rows=1, flags=None, stream=None):
+    """Writes the values at positions start[b] .. of every sequence to rows cu[b] .. cu[b+1]-1 of k and v (see first.h)."""
+    dev = _device_of(k, "k")
+    _kv_rows(cache, k, v)
+    total = k.shape[0]
+    cp, pp, width, sp, B = _batch8(cache, dev, pages, start, cu, total)
+    ks, vs = k.stride(), v.stride()
+    rc = lib().first_read8(cache.ref, pp, width, sp, cp, B, total, max_rows, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0],
+                           vs[1], _code(k, "k"), _flags_on(flags, dev), _raw_stream(stream, dev))
+    if rc:
+        raise FirstError(rc, "first_read8")
+
+
+def first_attn8(q, cache, pages, len, out, scale=None, cu_new=None, max_new=1, flags=None, stream=None):
+    """Attention of the new tokens' queries, CUDA [total][Hq][hd], over a Cache8 that holds their keys and values already; out
+    like q.  len, cu_new, max_new as in first_append8.  scale None: 1/sqrt(hd)."""
+    dev = _device_of(q, "q")
+    _heads_of(q, "q")
+    _heads_of(out, "out")
+    total, hq, hd = q.shape
+    if out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != dev:
+        raise ValueError("out must be like q")
+    if hd != cache.c.head_dim:
+        raise ValueError("q must have the cache's head size")
+    cu, pp, width, lp, B = _batch8(cache, dev, pages, len, cu_new, total)
+    qs, os_ = q.stride(), out.stride()
+    rc = lib().first_attn8(cache.ref, q.data_ptr(), qs[0], qs[1], hq, _code(q, "q"), hd ** -0.5 if scale is None else scale, cu,
+                           total, pp, width, lp, B, max_new, out.data_ptr(), os_[0], os_[1], _flags_on(flags, dev),
+                           _raw_stream(stream, dev))
+    if rc:
+        raise FirstError(rc, "first_attn8")
+
+
+def first_copy_pages(caches, moves, flags=None, stream=None):
+    """Copies pages within the layers' caches (a list of Cache8): moves CUDA int32 [n][3] of (layer, from, to)."""
+    dev = _device_of(moves, "moves")
+    if moves.dim() != 2 or moves.shape[1] != 3:
+        raise ValueError("moves must be [n][3]")
+    if any(c.device != dev for c in caches):
+        raise ValueError("the caches are on another device")
+    arr = (Cache8C * len(caches))(*[c.c for c in caches])
+    rc = lib().first_copy_pages(arr, len(caches), _on(moves, torch.int32, moves.numel(), "moves", dev), moves.shape[0],
+                                _flags_on(flags, dev), _raw_stream(stream, dev))
+    if rc:
+        raise FirstError(rc, "first_copy_pages")
+
+
+def first_verify(target, drafted, uniforms, draws, tokens, accepted, draft=None, temperature=None, probs=False, stream=None):
+    """Accepts or refuses drafted tokens and draws the token after them (see first.h).  target CUDA float32
+    [B][n+1][vocab], draft [B][n][vocab] or None (adjacent elements in a row): logits, or probabilities with probs;
+    drafted CUDA int32 [B][n]; uniforms CUDA float32 [B][n], draws [B]; temperature CUDA float32 [B] or None.
+    Output: tokens CUDA int32 [B][n+1], accepted CUDA int32 [B]."""
+    dev = _device_of(target, "target")
+    f32, i32 = torch.float32, torch.int32
+    if target.dim() != 3 or (target.shape[2] > 1 and target.stride(2) != 1):
+        raise ValueError("target must be [sequences][drafts + 1][vocab] with adjacent elements in a row")
+    if target.dtype is not f32:
+        raise TypeError("target must be float32")
+    B, rows, V = target.shape
+    n = rows - 1
+    if n < 0:
+        raise ValueError("target needs a row for the token after the drafts")
+    dp, ds = None, (0, 0)
+    if draft is not None:
+        if draft.dtype is not f32 or draft.get_device() != dev:
+            raise TypeError("draft must be float32, on target's device")
+        if tuple(draft.shape) != (B, n, V) or (V > 1 and draft.stride(2) != 1):
+            raise ValueError("draft must be [sequences][drafts][vocab] with adjacent elements in a row")
+        dp, ds = draft.data_ptr(), draft.stride()
+    if draws is None or tokens is None or accepted is None:
+        raise TypeError("draws, tokens and accepted are required")
+    ts = target.stride()
+    rc = lib().first_verify(target.data_ptr(), ts[0], ts[1], dp, ds[0], ds[1], bool(probs), _on(drafted, i32, B * n, "drafted", dev),
+                            B, n, V, _on(temperature, f32, B, "temperature", dev), _on(uniforms, f32, B * n, "uniforms", dev),
+                            _on(draws, f32, B, "draws", dev), _on(tokens, i32, B * rows, "tokens", dev),
+                            _on(accepted, i32, B, "accepted", dev), _raw_stream(stream, dev))
+    if rc:
+        raise FirstError(rc, "first_verify")
 
 
 def first_set_sampling_rows(h, uniforms=None, temperature=None, top_k=None, top_p=None, min_p=None):

@@ -35,7 +35,7 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     if not force and not is_stale():
         return LIB
     tmp = LIB.with_suffix(f".tmp{os.getpid()}.so")
-    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+    cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
            "-Xcompiler", "-fPIC", "-shared",
            "-I", str(ROOT / "include"), "-I", str(CSRC), *[str(s) for s in sources()], "-o", str(tmp)]
     if verbose:

@@ -1,0 +1,410 @@
+// Paged 8-bit cache: new keys and values into pages, values back out of them, and pages from place to place.
+#include <algorithm>
+
+#include "cache8.cuh"
+
+using namespace first;
+
+namespace first {
+
+int check_cache8(const first_cache8* c) {
+    if (!c || c->n_pages < 0 || c->n_kv_heads <= 0) return FIRST_E_ARG;
+    if (c->format != FIRST_CACHE_INT8 && c->format != FIRST_CACHE_E4M3) return FIRST_E_ARG;
+    if (c->n_pages > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return FIRST_E_ARG;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return FIRST_E_UNSUPPORTED;
+    if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return FIRST_E_UNSUPPORTED;
+    if (c->n_kv_heads > 1024) return FIRST_E_UNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16) return FIRST_E_UNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) % 4) return FIRST_E_UNSUPPORTED;
+    return FIRST_OK;
+}
+
+int check_seqs8(const int32_t* pages, int32_t max_pages, const int32_t* len, const int32_t* cu, int32_t B, int32_t total, int32_t max_new) {
+    if (B < 0 || total < 0 || max_pages < 0 || max_new < 0) return FIRST_E_ARG;
+    if (!cu && total != B) return FIRST_E_SHAPE;
+    if (B > 0 && total > 0 && max_new > 0 && (!len || (max_pages > 0 && !pages))) return FIRST_E_ARG;
+    return FIRST_OK;
+}
+
+// Rows that are written belong to one (token, head) each; rows that are read may repeat.
+int check_rows8(const void* p, int64_t tok, int64_t head, int32_t heads, int32_t hd, int32_t dtype, int64_t total, bool written) {
+    if (dtype != FIRST_DTYPE_F32 && dtype != FIRST_DTYPE_BF16) return FIRST_E_ARG;
+    if (tok < 0 || head < 0) return FIRST_E_SHAPE;
+    if (written && total > 0) {
+        if (heads > 1 && head < hd) return FIRST_E_SHAPE;
+        if (total > 1 && !(heads == 1 ? tok >= hd : tok >= (heads - 1) * head + hd || (tok >= hd && head >= (total - 1) * tok + hd)))
+            return FIRST_E_SHAPE;
+    }
+    if (total > 0 && !p) return FIRST_E_ARG;
+    if (reinterpret_cast<uintptr_t>(p) % (dtype == FIRST_DTYPE_F32 ? 4 : 2)) return FIRST_E_UNSUPPORTED;
+    return FIRST_OK;
+}
+
+Cache8 cache8_of(const first_cache8& c) {
+    Cache8 o;
+    o.k = static_cast<uint8_t*>(c.k);
+    o.v = static_cast<uint8_t*>(c.v);
+    o.ks = c.k_scale;
+    o.vs = c.v_scale;
+    o.n_pages = c.n_pages;
+    o.H = c.n_kv_heads;
+    for (o.shift = 4; (1 << o.shift) < c.page;) ++o.shift;
+    o.hd = c.head_dim;
+    o.e4m3 = c.format == FIRST_CACHE_E4M3;
+    return o;
+}
+
+}  // namespace first
+
+namespace {
+
+// The 8-bit value nearest to an exact quotient num / den (ties to even, saturated; NaN gives 0), in 64 bits: the quotient
+// of two float32 is nearer to a tie than 64 bits resolve only where it is one.
+template <bool E4M3>
+__device__ __noinline__ uint32_t quotient_slow(double num, double den) {
+    const double y = num / den;
+    if (!(y == y)) return 0;
+    if constexpr (E4M3) {
+        const double a = fmin(fabs(y), 448.0);
+        int e = 0;
+        frexp(a, &e);  // a in [2^(e-1), 2^e)
+        e = max(e, -5);
+        const double step = ldexp(1.0, e - 4);
+        const float r = (float)(rint(a / step) * step);
+        return __nv_cvt_float_to_fp8(y < 0 ? -r : r, __NV_SATFINITE, __NV_E4M3);
+    } else {
+        return (uint32_t)(uint8_t)(int8_t)(int)rint(fmin(fmax(y, -127.0), 127.0));
+    }
+}
+
+// The same for x / s, s given with its float32 reciprocal (0: too small for one).  x * inv is within 2^-22 of the
+// quotient: the slow way is for what that close to a tie cannot tell (1 element in some 10^4).
+template <bool E4M3>
+__device__ __forceinline__ uint32_t quotient(float x, float s, float inv) {
+    const float y = x * inv;
+    if constexpr (E4M3) {
+        const uint32_t lo = __nv_cvt_float_to_fp8(y * (1.f - 0x1p-20f), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float_to_fp8(y * (1.f + 0x1p-20f), __NV_SATFINITE, __NV_E4M3);
+        if (lo == hi && inv > 0.f && y == y) return lo;
+    } else {
+        const float c = fminf(fmaxf(y, -127.f), 127.f), r = rintf(c);
+        if (fabsf(c - r) < 0.4999f && inv > 0.f && y == y) return (uint32_t)(uint8_t)(int8_t)(int)r;
+    }
+    return s > 0.f ? quotient_slow<E4M3>((double)x, (double)s) : 0u;
+}
+
+// Eight elements of a row as float32.
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+    if constexpr (WIDE && sizeof(T) == 2) {
+        unpack8(*reinterpret_cast<const uint4*>(p), f);
+    } else if constexpr (WIDE) {
+        const float4 a = *reinterpret_cast<const float4*>(p), b = *(reinterpret_cast<const float4*>(p) + 1);
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = to_f32(p[i]);
+    }
+}
+
+constexpr int kAppendThreads = 128;
+
+// One block a (page that gains tokens, head, K or V): the largest magnitude of the new values, the page's scale, and the
+// new values rounded to it; where the scale grew the page's earlier values are rounded to it again.
+template <typename T, bool E4M3, bool WIDE>
+__global__ void __launch_bounds__(kAppendThreads) append8(const Cache8 c, const Seqs8 s, const Rows8 kr, const Rows8 vr) {
+    const Stamp stamp_guard(s.stamp);
+    pdl_trigger();
+    pdl_wait();
+    Seq8 q;
+    if (!find_seq(s, blockIdx.x, q)) return;
+    const int tid = threadIdx.x, h = blockIdx.z >> 1, hd = c.hd, page = 1 << c.shift;
+    const bool is_v = blockIdx.z & 1;
+    const int64_t first = ((int64_t)(q.before >> c.shift) + blockIdx.y) << c.shift;  // the page's first position
+    const int64_t end = (int64_t)q.before + q.n;
+    if (first >= end) return;
+    const int p = find_page(s, c.n_pages, q.seq, first >> c.shift);
+    if (p < 0) {  // no room: the tokens are left out
+        if (s.flags && tid == 0) atomicOr(s.flags, FIRST_FLAG_KV_FULL);
+        return;
+    }
+    const int lo = (int)max((int64_t)q.before - first, (int64_t)0), hi = (int)min(end - first, (int64_t)page);
+    const Rows8& r = is_v ? vr : kr;
+    // row `lo` of the page is row `row0` of the tensor
+    const T* src = static_cast<const T*>(r.p) + (q.start + first + lo - q.before) * r.tok + h * r.head;
+    uint8_t* dst = (is_v ? c.v : c.k) + ((((int64_t)p * c.H + h) << c.shift)) * hd;
+    float* scale = (is_v ? c.vs : c.ks) + (int64_t)p * c.H + h;
+    const float2* cs = s.cs && !is_v ? s.cs + (int64_t)q.seq * (hd / 2) : nullptr;
+    const int vpr = hd / 8, nv = (hi - lo) * vpr;
+    auto fetch = [&](int i, float (&f)[8]) {
+        const T* row = src + (int64_t)(i / vpr) * r.tok;
+        const int d = i % vpr * 8;
+        load8<T, WIDE>(row + d, f);
+        if (cs) {  // rotary pair (d, d + hd/2)
+            const int half = hd / 2;
+            const bool up = d >= half;
+            float g[8];
+            load8<T, WIDE>(row + (up ? d - half : d + half), g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 t = cs[(up ? d - half : d) + e];
+                f[e] = up ? f[e] * t.x + g[e] * t.y : f[e] * t.x - g[e] * t.y;
+            }
+        }
+    };
+    uint32_t amax = 0;  // (as bits: magnitudes of finite values are ordered alike)
+    for (int i = tid; i < nv; i += kAppendThreads) {
+        float f[8];
+        fetch(i, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t m = __float_as_uint(f[e]) & 0x7fffffffu;
+            amax = max(amax, m < 0x7f800000u ? m : 0u);
+        }
+    }
+    __shared__ uint32_t red[kAppendThreads / 32];
+    amax = __reduce_max_sync(0xffffffffu, amax);
+    if ((tid & 31) == 0) red[tid >> 5] = amax;
+    const float held = lo > 0 ? *scale : 0.f;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kAppendThreads / 32; ++w) amax = max(amax, red[w]);
+    const float fresh = __uint_as_float(amax) * (1.f / (E4M3 ? 448.f : 127.f));
+    const float now = held >= fresh || held != held ? held : fresh;  // (a NaN stays: what the page holds is none either)
+    const float inv = now > 1e-37f ? 1.f / now : 0.f;
+    for (int i = tid; i < nv; i += kAppendThreads) {
+        float f[8];
+        fetch(i, f);
+        uint32_t o[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e >> 2] |= quotient<E4M3>(f[e], now, inv) << (8 * (e & 3));
+        *reinterpret_cast<uint2*>(dst + (int64_t)(lo + i / vpr) * hd + i % vpr * 8) = make_uint2(o[0], o[1]);
+    }
+    if (lo > 0 && now > held) {
+        const float ratio = (float)((double)held / (double)now);
+        for (int i = tid; i < lo * hd / 4; i += kAppendThreads) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(dst) + i;
+            const uint32_t old = *w;
+            uint32_t o = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = to_value<E4M3>(old >> (8 * e) & 255u);
+                const float y = x * ratio;
+                uint32_t code;
+                bool sure;
+                if constexpr (E4M3) {
+                    code = __nv_cvt_float_to_fp8(y * (1.f - 0x1p-20f), __NV_SATFINITE, __NV_E4M3);
+                    sure = code == __nv_cvt_float_to_fp8(y * (1.f + 0x1p-20f), __NV_SATFINITE, __NV_E4M3);
+                } else {
+                    const float rr = rintf(y);
+                    code = (uint32_t)(uint8_t)(int8_t)(int)rr;
+                    sure = fabsf(y - rr) < 0.4999f;
+                }
+                if (!sure) code = quotient_slow<E4M3>((double)x * (double)held, (double)now);
+                o |= code << (8 * e);
+            }
+            *w = o;
+        }
+    }
+    if (tid == 0) *scale = now;
+}
+
+// Values of pages as rows: one thread a 16 bytes of K and of V.
+template <typename T, bool E4M3, bool WIDE>
+__global__ void __launch_bounds__(256) read8(const Cache8 c, const Seqs8 s, const Rows8 kr, const Rows8 vr) {
+    Seq8 q;
+    if (!find_seq(s, blockIdx.y, q)) return;
+    const int vpr = c.hd / 16, per = c.H * vpr;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    if (row >= q.n) return;
+    const int h = (int)(i % per) / vpr, d = (int)(i % vpr) * 16;
+    const int64_t pos = (int64_t)q.before + row;
+    const int p = find_page(s, c.n_pages, q.seq, pos >> c.shift);
+    if (p < 0) {
+        if (s.flags) atomicOr(s.flags, FIRST_FLAG_BAD_PAGE);
+        return;
+    }
+    const int64_t at = ((((int64_t)p * c.H + h) << c.shift) + (pos & ((1 << c.shift) - 1))) * c.hd + d;
+    const float scale[2] = {c.ks[(int64_t)p * c.H + h], c.vs[(int64_t)p * c.H + h]};
+    const uint4 in[2] = {*reinterpret_cast<const uint4*>(c.k + at), *reinterpret_cast<const uint4*>(c.v + at)};
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const Rows8& r = w ? vr : kr;
+        T* o = static_cast<T*>(r.p) + (q.start + row) * r.tok + h * r.head + d;
+        const uint32_t u[4] = {in[w].x, in[w].y, in[w].z, in[w].w};
+        struct alignas(16) Out { T e[16 / sizeof(T)]; };
+        Out t[sizeof(T)];
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            t[e / (16 / sizeof(T))].e[e % (16 / sizeof(T))] = from_f32<T>(to_value<E4M3>(u[e >> 2] >> (8 * (e & 3)) & 255u) * scale[w]);
+#pragma unroll
+        for (int e = 0; e < (int)sizeof(T); ++e) {
+            if constexpr (WIDE) {
+                reinterpret_cast<Out*>(o)[e] = t[e];
+            } else {
+#pragma unroll
+                for (int x = 0; x < (int)(16 / sizeof(T)); ++x) o[e * (16 / sizeof(T)) + x] = t[e].e[x];
+            }
+        }
+    }
+}
+
+constexpr int kMaxCopyLayers = 96;  // the layers' addresses travel as kernel parameters
+struct CopyArgs {
+    uint8_t *k[kMaxCopyLayers], *v[kMaxCopyLayers];
+    float *ks[kMaxCopyLayers], *vs[kMaxCopyLayers];
+    int n_pages[kMaxCopyLayers];
+    int L, H;
+    int bytes, chunks;  // of a page's K, and pieces it is cut into
+    const int32_t* moves;
+    int64_t units;
+    uint32_t* flags;
+};
+constexpr int kCopyChunk = 256 * 16 * 4;
+
+// One block a 16 KB of K or V of a move.
+__global__ void __launch_bounds__(256) copy_pages(const __grid_constant__ CopyArgs a) {
+    const int64_t unit = blockIdx.x;
+    const int piece = (int)(unit % (2 * a.chunks)), chunk = piece >> 1;
+    const int32_t* m = a.moves + unit / (2 * a.chunks) * 3;
+    const int l = m[0], from = m[1], to = m[2];
+    if (l < 0 || l >= a.L || from < 0 || to < 0 || from >= a.n_pages[l] || to >= a.n_pages[l]) {
+        if (a.flags && threadIdx.x == 0) atomicOr(a.flags, FIRST_FLAG_BAD_PAGE);
+        return;
+    }
+    if (from == to) return;
+    uint8_t* base = piece & 1 ? a.v[l] : a.k[l];
+    float* sc = piece & 1 ? a.vs[l] : a.ks[l];
+    const int64_t at = (int64_t)chunk * kCopyChunk;
+    const uint4* src = reinterpret_cast<const uint4*>(base + (int64_t)from * a.bytes + at);
+    uint4* dst = reinterpret_cast<uint4*>(base + (int64_t)to * a.bytes + at);
+    const int n = (int)min((int64_t)kCopyChunk, a.bytes - at) / 16;
+    uint4 r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((int)threadIdx.x + i * 256 < n) r[i] = src[threadIdx.x + i * 256];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((int)threadIdx.x + i * 256 < n) dst[threadIdx.x + i * 256] = r[i];
+    if (chunk == 0)
+        for (int h = threadIdx.x; h < a.H; h += 256) sc[(int64_t)to * a.H + h] = sc[(int64_t)from * a.H + h];
+}
+
+bool aligned16(const Rows8& r) {
+    const int es = r.f32 ? 4 : 2;
+    return reinterpret_cast<uintptr_t>(r.p) % 16 == 0 && r.tok * es % 16 == 0 && r.head * es % 16 == 0;
+}
+
+}  // namespace
+
+namespace first {
+
+cudaError_t append8_launch(const Cache8& c, const Seqs8& s, const Rows8& k, const Rows8& v, cudaStream_t st, bool pdl) {
+    const int pages = (int)(((int64_t)s.max_new + (1 << c.shift) - 2) / (1 << c.shift) + 1);  // that a sequence's tokens touch at most
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(s.B, s.max_new == 1 ? 1 : pages, 2 * c.H);
+    cfg.blockDim = dim3(kAppendThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = pdl ? 1 : 0;
+    const bool wide = aligned16(k) && aligned16(v);
+#define FIRST_APPEND(T, E, W) return cudaLaunchKernelEx(&cfg, append8<T, E, W>, c, s, k, v)
+    if (k.f32) {
+        if (c.e4m3) { if (wide) FIRST_APPEND(float, true, true); else FIRST_APPEND(float, true, false); }
+        else { if (wide) FIRST_APPEND(float, false, true); else FIRST_APPEND(float, false, false); }
+    }
+    if (c.e4m3) { if (wide) FIRST_APPEND(__nv_bfloat16, true, true); else FIRST_APPEND(__nv_bfloat16, true, false); }
+    if (wide) FIRST_APPEND(__nv_bfloat16, false, true); else FIRST_APPEND(__nv_bfloat16, false, false);
+#undef FIRST_APPEND
+}
+
+}  // namespace first
+
+extern "C" {
+
+int first_append8(const first_cache8* cache, const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                  int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, const int32_t* cu_new, int32_t total,
+                  const int32_t* pages, int32_t max_pages, const int32_t* len, int32_t B, int32_t max_new, uint32_t* flags,
+                  void* stream) {
+    int rc = check_cache8(cache);
+    if (rc || (rc = check_seqs8(pages, max_pages, len, cu_new, B, total, max_new)) ||
+        (rc = check_rows8(k, k_token_stride, k_head_stride, cache->n_kv_heads, cache->head_dim, dtype, total, false)) ||
+        (rc = check_rows8(v, v_token_stride, v_head_stride, cache->n_kv_heads, cache->head_dim, dtype, total, false)))
+        return rc;
+    if (B == 0 || total == 0 || max_new == 0) return FIRST_OK;
+    const Cache8 c = cache8_of(*cache);
+    if ((int64_t)max_pages * cache->page > (1 << 30) || (max_new >> c.shift) > 65000) return FIRST_E_CAPACITY;
+    Seqs8 s;
+    s.pages = pages; s.width = max_pages; s.len = len; s.cu = cu_new;
+    s.B = B; s.total = total; s.max_new = std::min(max_new, total); s.flags = flags;
+    const bool f32 = dtype == FIRST_DTYPE_F32;
+    const Rows8 kr{const_cast<void*>(k), k_token_stride, k_head_stride, f32}, vr{const_cast<void*>(v), v_token_stride, v_head_stride, f32};
+    return append8_launch(c, s, kr, vr, static_cast<cudaStream_t>(stream), false) == cudaSuccess ? FIRST_OK : FIRST_E_CUDA;
+}
+
+int first_read8(const first_cache8* cache, const int32_t* pages, int32_t max_pages, const int32_t* start, const int32_t* cu,
+                int32_t B, int32_t total, int32_t max_rows, void* k, int64_t k_token_stride, int64_t k_head_stride, void* v,
+                int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, uint32_t* flags, void* stream) {
+    int rc = check_cache8(cache);
+    if (rc || (rc = check_seqs8(pages, max_pages, start, cu, B, total, max_rows)) ||
+        (rc = check_rows8(k, k_token_stride, k_head_stride, cache->n_kv_heads, cache->head_dim, dtype, total, true)) ||
+        (rc = check_rows8(v, v_token_stride, v_head_stride, cache->n_kv_heads, cache->head_dim, dtype, total, true)))
+        return rc;
+    if (B == 0 || total == 0 || max_rows == 0) return FIRST_OK;
+    if (B > 65535 || (int64_t)max_pages * cache->page > (1 << 30)) return FIRST_E_CAPACITY;
+    const Cache8 c = cache8_of(*cache);
+    Seqs8 s;
+    s.pages = pages; s.width = max_pages; s.len = start; s.cu = cu;
+    s.B = B; s.total = total; s.max_new = std::min(max_rows, total); s.flags = flags;
+    const bool f32 = dtype == FIRST_DTYPE_F32;
+    const Rows8 kr{k, k_token_stride, k_head_stride, f32}, vr{v, v_token_stride, v_head_stride, f32};
+    const int64_t blocks = ((int64_t)s.max_new * c.H * (c.hd / 16) + 255) / 256;
+    if (blocks > 0x7fffffff) return FIRST_E_CAPACITY;
+    const dim3 grid((unsigned)blocks, B);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool wide = aligned16(kr) && aligned16(vr);
+#define FIRST_READ(T, E, W) read8<T, E, W><<<grid, 256, 0, st>>>(c, s, kr, vr)
+    if (f32) {
+        if (c.e4m3) { if (wide) FIRST_READ(float, true, true); else FIRST_READ(float, true, false); }
+        else { if (wide) FIRST_READ(float, false, true); else FIRST_READ(float, false, false); }
+    } else {
+        if (c.e4m3) { if (wide) FIRST_READ(__nv_bfloat16, true, true); else FIRST_READ(__nv_bfloat16, true, false); }
+        else { if (wide) FIRST_READ(__nv_bfloat16, false, true); else FIRST_READ(__nv_bfloat16, false, false); }
+    }
+#undef FIRST_READ
+    return cudaGetLastError() == cudaSuccess ? FIRST_OK : FIRST_E_CUDA;
+}
+
+int first_copy_pages(const first_cache8* layers, int32_t n_layers, const int32_t* moves, int64_t n_moves, uint32_t* flags,
+                     void* stream) {
+    if (!layers || n_layers <= 0 || n_moves < 0 || (n_moves > 0 && !moves)) return FIRST_E_ARG;
+    if (n_layers > kMaxCopyLayers) return FIRST_E_UNSUPPORTED;
+    CopyArgs a{};
+    for (int l = 0; l < n_layers; ++l) {
+        int rc = check_cache8(layers + l);
+        if (rc) return rc;
+        const first_cache8 &c = layers[l], &d = layers[0];
+        if (c.format != d.format || c.n_kv_heads != d.n_kv_heads || c.page != d.page || c.head_dim != d.head_dim) return FIRST_E_SHAPE;
+        a.k[l] = static_cast<uint8_t*>(c.k);
+        a.v[l] = static_cast<uint8_t*>(c.v);
+        a.ks[l] = c.k_scale;
+        a.vs[l] = c.v_scale;
+        a.n_pages[l] = c.n_pages;
+    }
+    if (n_moves == 0) return FIRST_OK;
+    a.L = n_layers;
+    a.H = layers[0].n_kv_heads;
+    a.bytes = a.H * layers[0].page * layers[0].head_dim;
+    a.chunks = (a.bytes + kCopyChunk - 1) / kCopyChunk;
+    a.moves = moves;
+    if (n_moves > (0x7fffffff / 2) / a.chunks) return FIRST_E_CAPACITY;  // (grid size)
+    a.units = n_moves * 2 * a.chunks;
+    a.flags = flags;
+    copy_pages<<<(unsigned)a.units, 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    return cudaGetLastError() == cudaSuccess ? FIRST_OK : FIRST_E_CUDA;
+}
+
+}  // extern "C"

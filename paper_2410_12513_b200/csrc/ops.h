@@ -1,8 +1,11 @@
 // Host-side launch interfaces of the operators that serve both a standalone entry point and the step: low-rank
-// adapters (lora.cu) and per-request sampling (sample.cu).  Arguments are checked by the callers.
+// adapters (lora.cu), per-request sampling (sample.cu) and the paged 8-bit cache (append8.cu, attn8.cu).  Arguments are checked by the callers.
 #pragma once
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include "first.h"
 
 namespace first {
 
@@ -48,5 +51,47 @@ struct SampleArgs {
 };
 constexpr int kSampleMaxVocab = 1 << 19;
 cudaError_t sample_launch(const SampleArgs& a, cudaStream_t st, bool pdl);
+
+// One layer of a paged 8-bit cache: pages of 2^shift tokens, [n_pages][H][2^shift][hd] bytes, one scale a (page, head).
+struct Cache8 {
+    uint8_t *k = nullptr, *v = nullptr;
+    float *ks = nullptr, *vs = nullptr;
+    int n_pages = 0, H = 0, shift = 0, hd = 0;
+    bool e4m3 = false;
+};
+// Sequences over it.  New token i of sequence b is row cu[b] + i of the caller's tensors (cu NULL: row r is the one new
+// token of sequence idx ? idx[r] : r) and has position len[b] + i.  m_dev: live rows, as in the step's kernels.
+struct Seqs8 {
+    const int32_t* pages = nullptr;  // [.][width], -1 = no page
+    int64_t width = 0;
+    const int32_t *len = nullptr, *cu = nullptr;
+    int B = 0, total = 0, max_new = 1;
+    const int32_t *idx = nullptr, *m_dev = nullptr;
+    uint32_t* flags = nullptr;       // or NULL
+    const float2* cs = nullptr;      // [.][hd/2] by sequence: rotate q and k on the way (the step), or NULL
+    uint64_t* stamp = nullptr;
+};
+struct Rows8 {                       // a tensor [tokens][heads][hd], strides in elements
+    void* p = nullptr;
+    int64_t tok = 0, head = 0;
+    bool f32 = true;
+};
+cudaError_t append8_launch(const Cache8& c, const Seqs8& s, const Rows8& k, const Rows8& v, cudaStream_t st, bool pdl);
+
+struct Attn8Args {
+    Cache8 c;
+    Seqs8 s;
+    Rows8 q, out;                    // out.p NULL: out_hi / out_lo instead (the step's bfloat16 pair), out's strides
+    __nv_bfloat16 *out_hi = nullptr, *out_lo = nullptr;
+    int G = 1;
+    float scale = 1.f;
+};
+cudaError_t attn8_launch(const Attn8Args& a, cudaStream_t st, bool pdl, int n_sm);
+
+// Checks of arguments: FIRST_OK or an error.
+int check_cache8(const first_cache8* c);
+int check_seqs8(const int32_t* pages, int32_t max_pages, const int32_t* len, const int32_t* cu, int32_t B, int32_t total, int32_t max_new);
+int check_rows8(const void* p, int64_t tok, int64_t head, int32_t heads, int32_t hd, int32_t dtype, int64_t total, bool written);
+Cache8 cache8_of(const first_cache8& c);
 
 }  // namespace first
