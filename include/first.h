@@ -523,7 +523,9 @@ int first_read8(const first_cache8 *cache, const int32_t *pages, int32_t max_pag
 int first_attn8(const first_cache8 *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride, int32_t n_q_heads,
                 int32_t dtype, float scale, const int32_t *cu_new, int32_t total, const int32_t *pages, int32_t max_pages,
                 const int32_t *len, int32_t B, int32_t max_new, void *out, int64_t out_token_stride, int64_t out_head_stride,
-                uint32_t *flags, void *stream);
+                void *workspace, int64_t workspace_bytes, uint32_t *flags, void *stream);
+int64_t first_attn8_workspace(const first_cache8 *cache, int32_t n_q_heads, int32_t dtype, int32_t total, int32_t max_pages,
+                              int32_t B, int32_t max_new);
 int first_copy_pages(const first_cache8 *layers, int32_t n_layers, const int32_t *moves, int64_t n_moves, uint32_t *flags,
                      void *stream);
 

@@ -2,6 +2,7 @@
 CUDA tensors.  Argument marshalling only -- no arithmetic happens here."""
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import functools
 from pathlib import Path
@@ -138,7 +139,9 @@ def lib():
         cache8 = C.POINTER(Cache8C)
         L.first_append8.argtypes = [cache8, p, i64, i64, p, i64, i64, i32, p, i32, p, i32, p, i32, i32, p, p]
         L.first_read8.argtypes = [cache8, p, i32, p, p, i32, i32, i32, p, i64, i64, p, i64, i64, i32, p, p]
-        L.first_attn8.argtypes = [cache8, p, i64, i64, i32, i32, C.c_float, p, i32, p, i32, p, i32, i32, p, i64, i64, p, p]
+        L.first_attn8.argtypes = [cache8, p, i64, i64, i32, i32, C.c_float, p, i32, p, i32, p, i32, i32, p, i64, i64, p, i64, p, p]
+        L.first_attn8_workspace.argtypes = [cache8, i32, i32, i32, i32, i32, i32]
+        L.first_attn8_workspace.restype = i64
         L.first_copy_pages.argtypes = [cache8, i32, p, i64, p, p]
         L.first_verify.argtypes = [p, i64, i64, p, i64, i64, i32, p, i32, i32, i32, p, p, p, p, p, p]
         for name in ("first_append8", "first_read8", "first_attn8", "first_copy_pages", "first_verify", "first_sample", "first_set_sampling_rows", "first_lora", "first_set_adapters", "first_rope_freqs",
@@ -634,9 +637,10 @@ def first_read8(cache, pages, start, k, v, cu=None, max_rows=1, flags=None, stre
         raise FirstError(rc, "first_read8")
 
 
-def first_attn8(q, cache, pages, len, out, scale=None, cu_new=None, max_new=1, flags=None, stream=None):
+def first_attn8(q, cache, pages, len, out, scale=None, cu_new=None, max_new=1, workspace=None, flags=None, stream=None):
     """Attention of the new tokens' queries, CUDA [total][Hq][hd], over a Cache8 that holds their keys and values already; out
-    like q.  len, cu_new, max_new as in first_append8.  scale None: 1/sqrt(hd)."""
+    like q.  len, cu_new, max_new as in first_append8.  scale None: 1/sqrt(hd).  workspace: a CUDA tensor to keep unfinished
+    results in (first_attn8_workspace bytes), None: one is taken from torch's allocator where there is a use for it."""
     dev = _device_of(q, "q")
     _heads_of(q, "q")
     _heads_of(out, "out")
@@ -647,9 +651,18 @@ def first_attn8(q, cache, pages, len, out, scale=None, cu_new=None, max_new=1, f
         raise ValueError("q must have the cache's head size")
     cu, pp, width, lp, B = _batch8(cache, dev, pages, len, cu_new, total)
     qs, os_ = q.stride(), out.stride()
-    rc = lib().first_attn8(cache.ref, q.data_ptr(), qs[0], qs[1], hq, _code(q, "q"), hd ** -0.5 if scale is None else scale, cu,
-                           total, pp, width, lp, B, max_new, out.data_ptr(), os_[0], os_[1], _flags_on(flags, dev),
-                           _raw_stream(stream, dev))
+    code = _code(q, "q")
+    if workspace is None:
+        need = lib().first_attn8_workspace(cache.ref, hq, code, total, width, B, max_new)
+        if need:
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on q's device")
+    room = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib().first_attn8(cache.ref, q.data_ptr(), qs[0], qs[1], hq, code, hd ** -0.5 if scale is None else scale, cu,
+                           total, pp, width, lp, B, max_new, out.data_ptr(), os_[0], os_[1],
+                           workspace.data_ptr() if room else None, room, _flags_on(flags, dev), _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_attn8")
 

@@ -14,6 +14,7 @@ int check_cache8(const first_cache8* c) {
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return FIRST_E_UNSUPPORTED;
     if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return FIRST_E_UNSUPPORTED;
     if (c->n_kv_heads > 1024) return FIRST_E_UNSUPPORTED;
+    if ((int64_t)c->n_pages * c->n_kv_heads * c->page > 0x7fffffff) return FIRST_E_CAPACITY;  // (rows are counted in 32 bits)
     if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16) return FIRST_E_UNSUPPORTED;
     if ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) % 4) return FIRST_E_UNSUPPORTED;
     return FIRST_OK;

@@ -58,14 +58,18 @@ __device__ __forceinline__ bool find_seq(const Seqs8& s, int b, Seq8& q) {
 }
 
 // Page i of a sequence, -1 where it has none; ids outside the cache raise FIRST_FLAG_BAD_PAGE.
-__device__ __forceinline__ int find_page(const Seqs8& s, int n_pages, int seq, int64_t i) {
-    if (i >= s.width) return -1;
-    const int p = s.pages[(int64_t)seq * s.width + i];
+__device__ __forceinline__ int raw_page(const Seqs8& s, int seq, int64_t i) {
+    return i < s.width ? s.pages[(int64_t)seq * s.width + i] : -1;
+}
+__device__ __forceinline__ int check_page(const Seqs8& s, int n_pages, int p) {
     if (p < -1 || p >= n_pages) {
         if (s.flags) atomicOr(s.flags, FIRST_FLAG_BAD_PAGE);
         return -1;
     }
     return p;
+}
+__device__ __forceinline__ int find_page(const Seqs8& s, int n_pages, int seq, int64_t i) {
+    return check_page(s, n_pages, raw_page(s, seq, i));
 }
 
 }  // namespace first

@@ -85,7 +85,10 @@ struct Attn8Args {
     __nv_bfloat16 *out_hi = nullptr, *out_lo = nullptr;
     int G = 1;
     float scale = 1.f;
+    float *part_o = nullptr, *part_ml = nullptr;  // room for attn8_part_floats: unfinished results, [rows][splits][hd] and [..][2]; or NULL
 };
+// Floats that a call of these sizes has a use for (0: none); rows: query rows of a KV head.
+int64_t attn8_part_floats(int64_t B, int64_t H, int64_t rows, int hd, int64_t longest, bool f32, int n_sm);
 cudaError_t attn8_launch(const Attn8Args& a, cudaStream_t st, bool pdl, int n_sm);
 
 // Checks of arguments: FIRST_OK or an error.

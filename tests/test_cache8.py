@@ -34,8 +34,8 @@ def _read(c=None, k=P, kt=128, kh=64, v=P, vt=128, vh=64, dt=1, cu=None, total=3
     return _L().first_read8(c or _cache(), pages, width, ln, cu, B, total, new, k, kt, kh, v, vt, vh, dt, None, None)
 
 
-def _attn(c=None, q=P, qt=256, qh=64, hq=4, dt=1, cu=None, total=3, pages=P, width=4, ln=P, B=3, new=1, out=P, ot=256, oh=64):
-    return _L().first_attn8(c or _cache(), q, qt, qh, hq, dt, 0.1, cu, total, pages, width, ln, B, new, out, ot, oh, None, None)
+def _attn(c=None, q=P, qt=256, qh=64, hq=4, dt=1, cu=None, total=3, pages=P, width=4, ln=P, B=3, new=1, out=P, ot=256, oh=64, ws=None, room=0):
+    return _L().first_attn8(c or _cache(), q, qt, qh, hq, dt, 0.1, cu, total, pages, width, ln, B, new, out, ot, oh, ws, room, None, None)
 
 
 @pytest.mark.parametrize("call", [_append, _read, _attn])
@@ -67,11 +67,11 @@ def test_append_and_read_refuse():
 
 
 def test_attention_refuses():
-    for kw in ({"q": None}, {"out": None}, {"hq": 0}, {"hq": -4}):
+    for kw in ({"q": None}, {"out": None}, {"hq": 0}, {"hq": -4}, {"ws": P, "room": -1}):
         assert _attn(**kw) == ARG, kw
     for kw in ({"hq": 5}, {"qt": -256}, {"qh": -64}, {"ot": 255}, {"oh": 63}, {"ot": 0}):
         assert _attn(**kw) == SHAPE, kw
-    for kw in ({"q": P + 1}, {"out": P + 1}, {"dt": 0, "q": P + 2}, {"dt": 0, "out": P + 2}):
+    for kw in ({"q": P + 1}, {"out": P + 1}, {"dt": 0, "q": P + 2}, {"dt": 0, "out": P + 2}, {"ws": P + 2, "room": 64}):
         assert _attn(**kw) == UNSUPPORTED, kw
     assert _attn(cu=P, total=1 << 20, new=1 << 20) == CAPACITY
 
