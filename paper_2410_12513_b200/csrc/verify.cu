@@ -12,7 +12,7 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 512, kWarps = kThreads / 32;  // that count; one more warp copies
 constexpr int kMaxCluster = 16, kMaxRound = 8;
 
 struct VerifyArgs {
@@ -26,10 +26,9 @@ struct VerifyArgs {
     int C, R;  // CTAs of a cluster, positions a round
 };
 
-// One row's sum over one CTA's part, relative to the part's largest value; greedy rows: value and lowest index of the largest.
+// One row's sum over some of its tokens, relative to their largest logit; greedy rows: value and lowest index of the largest.
 struct Part {
-    double sum;
-    float top;
+    float top, sum;
     int32_t at;
 };
 
@@ -38,131 +37,155 @@ __device__ __forceinline__ float logit(float x) { return x > FLT_MAX ? FLT_MAX :
 // Uniform draws as they count.
 __device__ __forceinline__ double draw(float u) { return u < 1.f ? (double)fmaxf(u, 0.f) : (double)0x1.fffffep-1f; }
 
-// exp((x - top) / T) in 64 bits: which token a draw falls on hangs on the sums of these.
-__device__ __forceinline__ double weight(float x, float top, double inv_t) {
-    x = logit(x);
-    return x == -INFINITY ? 0.0 : exp(((double)x - (double)top) * inv_t);
-}
-
 struct Scale {
     float hi, lo, floor;  // log2(e) / T in two parts; differences below `floor` weigh nothing
-    double inv_t;
+    double steps;         // 32 log2(e) / T
 };
 
-// Sum of a row's weights over [lo, hi) by one block; float32 weights (their sum only decides about acceptance, where a
-// relative error of 2^-22 moves the border of a draw by that much).
-__device__ Part row_part(const float* row, int lo, int hi, const Scale& sc, bool greedy, Part* red) {
-    const int tid = threadIdx.x;
-    float top = -INFINITY;
-    double sum = 0.0;
-    int at = 0x7fffffff;
-    auto batch = [&](const float* x, int n, const int* idx) {
-        float big = -INFINITY;
-        for (int i = 0; i < n; ++i) big = fmaxf(big, x[i]);
-        if (greedy) {
-            if (big > top || at == 0x7fffffff) {
-                for (int i = n - 1; i >= 0; --i)
-                    if (x[i] == big) at = idx[i];
-                top = big;
-            }
-            return;
-        }
-        if (big > top) {
-            sum *= top == -INFINITY ? 0.0 : exp(((double)top - (double)big) * sc.inv_t);
-            top = big;
-        }
-        float part = 0.f;
-        for (int i = 0; i < n; ++i) {
-            const float t = fmaxf(x[i] - top, sc.floor);
-            float w;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(fmaf(t, sc.hi, t * sc.lo)));
-            part += w;
-        }
-        sum += (double)part;
-    };
-    // head: up to the first 16-byte border, tail: after the last
-    const int head = min(hi - lo, (int)((4 - ((reinterpret_cast<uintptr_t>(row + lo) >> 2) & 3)) & 3));
-    const int body = (hi - lo - head) / 4, tail = lo + head + body * 4;
-    if (tid < head || (tid >= 32 && tid - 32 < hi - tail)) {
-        const int e = tid < head ? lo + tid : tail + tid - 32;
-        const float x = logit(row[e]);
-        batch(&x, 1, &e);
-    }
-    const float4* v = reinterpret_cast<const float4*>(row + lo + head);
-    constexpr int kUnroll = 4;
-    for (int i = tid; i < body; i += kUnroll * kThreads) {
-        float x[4 * kUnroll];
-        int idx[4 * kUnroll];
-#pragma unroll
-        for (int j = 0; j < kUnroll; ++j) {
-            const int k = i + j * kThreads;
-            const float4 f = k < body ? __ldg(v + k) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-            x[4 * j] = logit(f.x); x[4 * j + 1] = logit(f.y); x[4 * j + 2] = logit(f.z); x[4 * j + 3] = logit(f.w);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) idx[4 * j + e] = lo + head + 4 * k + e;
-        }
-        batch(x, 4 * kUnroll, idx);
-    }
-    // the warp's, then the block's
-    float big = warp_max(top);
-    if (greedy) {
-        at = __reduce_min_sync(0xffffffffu, top == big ? at : 0x7fffffff);
-    } else {
-        sum *= top == -INFINITY ? 0.0 : (top == big ? 1.0 : exp(((double)top - (double)big) * sc.inv_t));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    }
-    __syncthreads();  // (red may still be read)
-    if ((tid & 31) == 0) red[tid >> 5] = Part{sum, big, at};
-    __syncthreads();
-    Part all{0.0, -INFINITY, 0x7fffffff};
-    if (tid < 32) {
-        const Part q = tid < kWarps ? red[tid] : Part{0.0, -INFINITY, 0x7fffffff};
-        big = warp_max(q.top);
-        all.top = big;
-        all.at = __reduce_min_sync(0xffffffffu, q.top == big ? q.at : 0x7fffffff);
-        all.sum = greedy || q.top == -INFINITY ? 0.0 : q.sum * (q.top == big ? 1.0 : exp(((double)q.top - (double)big) * sc.inv_t));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) all.sum += __shfl_xor_sync(0xffffffffu, all.sum, o);
-    }
-    return all;  // (threads 0..31)
+// exp((x - top) / T) in float32, of logits that count.
+__device__ __forceinline__ float weight32(float x, float top, const Scale& sc) {
+    const float t = fmaxf(x - top, sc.floor);
+    float w;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(fmaf(t, sc.hi, t * sc.lo)));
+    return w;
+}
+// The same in 64 bits, to 2^-39: which token a draw falls on hangs on the sums of these.  2^(k / 32) from a table for the nearest k, the
+// rest by its Taylor series: |g| <= ln 2 / 64, g^5 / 120 < 2^-39.
+__device__ __forceinline__ double weight64(float x, float top, const Scale& sc, const double* pow32) {
+    x = logit(x);
+    const double a = ((double)x - (double)top) * sc.steps;
+    if (!(a > -32000.0)) return 0.0;
+    constexpr double kMagic = 6755399441055744.0;  // 1.5 2^52: adding it leaves the nearest whole number in the low bits
+    const double m = a + kMagic, g = (a - (m - kMagic)) * (0.69314718055994530942 / 32);
+    const int k = __double2loint(m);
+    const double s = fma(fma(fma(fma(g, 1.0 / 24, 1.0 / 6), g, 0.5), g, 1.0), g, 1.0) * pow32[k & 31];
+    return __hiloint2double(__double2hiint(s) + (k >> 5) * (1 << 20), __double2loint(s));
 }
 
-__device__ __forceinline__ double block_sum(double x, double* red) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
-    __syncthreads();
-    double s = 0.0;
-    for (int w = 0; w < kWarps; ++w) s += red[w];
+__device__ __forceinline__ Part warp_join(Part p, const Scale& sc, bool greedy) {
+    const float top = warp_max(p.top);
+    if (greedy) p.at = __reduce_min_sync(0xffffffffu, p.top == top ? p.at : 0x7fffffff);
+    else p.sum = top > -INFINITY ? warp_sum(p.sum * weight32(p.top, top, sc)) : 0.f;
+    p.top = top;
+    return p;
+}
+
+// A row's part [lo, hi) comes in pieces of kPiece tokens (whole 16 bytes of memory: what they hold of neighbouring rows is passed over) through
+// a ring in shared memory.
+constexpr int kPiece = 8192, kRing = 3, kEach = kPiece / (4 * kThreads);
+struct Span {
+    const float* from;  // 16-byte aligned
+    int off, n, pieces; // tokens of it before the part, of the part, pieces
+};
+__device__ __forceinline__ Span span_of(const float* row, int lo, int hi) {
+    Span s;
+    s.off = (int)(reinterpret_cast<uintptr_t>(row + lo) >> 2 & 3);
+    s.from = row + lo - s.off;
+    s.n = hi - lo;
+    s.pieces = s.n > 0 ? (s.off + s.n + kPiece - 1) / kPiece : 1;
     return s;
 }
+__device__ __forceinline__ uint32_t piece_bytes(const Span& s, int q) {
+    return s.n > 0 ? 16 * min(kPiece / 4, (s.off + s.n + 3) / 4 - q * (kPiece / 4)) : 0;
+}
+constexpr uint32_t kPolls = 1u << 22;
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {  // bounded: false after kPolls tries
+    for (uint32_t i = 0; i < kPolls; ++i) {
+        uint32_t ok;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+__device__ __forceinline__ void copy_piece(uint32_t dst, uint32_t bar, const Span& s, int q) {
+    const uint32_t bytes = piece_bytes(s, q);
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    if (bytes)
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     ::"r"(dst), "l"(s.from + (int64_t)q * kPiece), "r"(bytes), "r"(bar) : "memory");
+}
+template <bool GREEDY>
+__device__ __forceinline__ void add(Part& p, const float4* piece, const Span& s, int q, int lo, const Scale& sc) {
+    float f[4 * kEach];
+    const int first = q * kPiece - s.off + 4 * (int)threadIdx.x;  // of the part
+    const bool whole = q * kPiece >= s.off && (q + 1) * kPiece <= s.off + s.n;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const float4 v = piece[j * kThreads + threadIdx.x];
+        f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
+    }
+    if (!whole)
+#pragma unroll
+        for (int i = 0; i < 4 * kEach; ++i)
+            if ((unsigned)(first + i / 4 * 4 * kThreads + i % 4) >= (unsigned)s.n) f[i] = -INFINITY;
+    float big = -INFINITY;  // (a maximum passes over NaN, and so does weight32)
+#pragma unroll
+    for (int i = 0; i < 4 * kEach; ++i) big = fmaxf(big, f[i]);
+    if (big > FLT_MAX) {
+        big = FLT_MAX;
+#pragma unroll
+        for (int i = 0; i < 4 * kEach; ++i) f[i] = logit(f[i]);
+    }
+    if (GREEDY) {
+        if (big < p.top || big == -INFINITY) return;
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int i = 0; i < 4 * kEach; ++i)
+            if (f[i] == big) at = min(at, lo + first + i / 4 * 4 * kThreads + i % 4);
+        p.at = big > p.top ? at : min(at, p.at);
+        p.top = big;
+        return;
+    }
+    if (big == -INFINITY) return;
+    if (big > p.top) {
+        p.sum *= weight32(p.top, big, sc);
+        p.top = big;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4 * kEach; ++i) sum += weight32(f[i], p.top, sc);
+    p.sum += sum;
+}
 
-// One cluster a sequence.  Rounds of R positions: every row's sum and largest logit, then the decisions (taken by every
+// One cluster a sequence.  Rounds of R positions, then 2 R and so on: every row's sum and largest logit, then the decisions (taken by every
 // CTA alike), until one is refused or all are accepted; the rows of later positions are not read.  Then the new token's
 // distribution, in 64 bits, over the one row (or two) that it comes from: those rows are in L2 by now.
-__global__ void __launch_bounds__(kThreads) verify_rows(const VerifyArgs p) {
-    __shared__ Part s_part[2][kMaxRound][2], s_red[kWarps];
-    __shared__ double s_sum[kWarps], s_z[2], s_seg;
-    __shared__ int s_ok[kMaxRound], s_hit, s_found;
-    __shared__ float s_top[2];
-    __shared__ int s_at;
+__global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs p) {
+    __shared__ Part s_warp[2 * kMaxRound][kWarps], s_part[2][2 * kMaxRound];
+    __shared__ double s_sum[4][kWarps], s_all[4][kMaxCluster * kWarps], s_run[kWarps], s_pow[32], s_seg;
+    __shared__ int s_ok[kMaxRound], s_hit, s_found, s_at;
+    __shared__ float s_tops[kMaxRound][2], s_top[2];
+    extern __shared__ __align__(128) float4 s_ring[];  // [kRing][kPiece] tokens
+    __shared__ uint64_t s_bar[2 * kRing];  // pieces that are there, pieces that have been read
+    __shared__ int s_gave;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = p.C, b = blockIdx.x / C, rank = blockIdx.x % C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float temp = p.temperature ? p.temperature[b] : 1.f;
     const bool greedy = !p.probs && !(temp > 0.f);
+    // (at most 32 drafts: a lane each; the first that is no token ends them)
+    const int32_t* drafted = p.drafted + (int64_t)b * p.K;
+    const int mine = lane < p.K ? drafted[lane] : -1;
+    const double my_u = lane < p.K ? draw(p.u[(int64_t)b * p.K + lane]) : 0.0;
+    const uint32_t closed = ~__ballot_sync(0xffffffffu, mine >= 0 && mine < p.V);
+    const int valid = closed ? __ffs(closed) - 1 : 32;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring), bars = (uint32_t)__cvta_generic_to_shared(s_bar);
+    if (tid < 32) s_pow[tid] = exp2((double)tid / 32);
+    if (tid == 32) {
+        s_gave = 0;
+        for (int i = 0; i < 2 * kRing; ++i)
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bars + 8 * i), "r"(i < kRing ? 1 : kWarps) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    int slot = 0;  // of the ring, next
+    uint32_t phase = 0;
     Scale sc;
     const double t64 = (double)fminf(fmaxf(temp, 1e-37f), 1e30f);
-    sc.inv_t = 1.0 / t64;
     sc.hi = (float)(1.4426950408889634 / t64);
     sc.lo = (float)(1.4426950408889634 / t64 - (double)sc.hi);
     sc.floor = (float)(-200.0 * t64);
-    const int32_t* drafted = p.drafted + (int64_t)b * p.K;
-    // (at most 32 drafts: a lane each; the first that is no token ends them)
-    const int mine = lane < p.K ? drafted[lane] : -1;
-    const uint32_t closed = ~__ballot_sync(0xffffffffu, mine >= 0 && mine < p.V);
-    const int valid = closed ? __ffs(closed) - 1 : 32;
+    sc.steps = 32 * 1.4426950408889634 / t64;
     const int per = ((p.V + C - 1) / C + 3) & ~3, lo = min(rank * per, p.V), hi = min(lo + per, p.V);
     auto t_of = [&](int i) { return p.target + b * p.t_seq + i * p.t_row; };
     auto d_of = [&](int i) { return p.draft + b * p.d_seq + i * p.d_row; };
@@ -171,54 +194,85 @@ __global__ void __launch_bounds__(kThreads) verify_rows(const VerifyArgs p) {
         bool ok = false;
         if (lane < valid) {
             const double pd = fmax((double)t_of(lane)[mine], 0.0), qd = p.draft ? fmax((double)d_of(lane)[mine], 0.0) : 1.0;
-            ok = draw(p.u[(int64_t)b * p.K + lane]) * qd < pd;
+            ok = my_u * qd < pd;
         }
         const uint32_t refused = ~__ballot_sync(0xffffffffu, ok);
         j = refused ? __ffs(refused) - 1 : 32;
+        __syncthreads();
     } else {
+        const int sides = p.draft && !greedy ? 2 : 1;
         bool open = true;
-        for (int i0 = 0, round = 0; open; i0 += p.R, ++round) {
-            const int n = min(p.R, valid + 1 - i0);
-            for (int i = 0; i < n; ++i) {
-                Part a = row_part(t_of(i0 + i), lo, hi, sc, greedy, s_red);
-                if (tid == 0) s_part[round & 1][i][0] = a;
-                if (p.draft && !greedy && i0 + i < valid) {
-                    a = row_part(d_of(i0 + i), lo, hi, sc, false, s_red);
-                    if (tid == 0) s_part[round & 1][i][1] = a;
+        for (int i0 = 0, round = 0, n = 0; open; i0 += n, ++round) {
+            n = min(min(p.R << round, kMaxRound), valid + 1 - i0);  // (what survives a round is likely to survive the next)
+            // the drafted tokens' own logits and draws, for the decisions below
+            const int my_i = i0 + min(warp, n - 1), my_d = __shfl_sync(0xffffffffu, mine, my_i & 31);
+            const double u_i = __shfl_sync(0xffffffffu, my_u, my_i & 31);
+            float own[2] = {0.f, 0.f};
+            if (warp < n && my_i < valid && !greedy) {
+                own[0] = __ldg(t_of(my_i) + my_d);
+                if (p.draft) own[1] = __ldg(d_of(my_i) + my_d);
+            }
+            // the round's rows (target and draft in turns), piece after piece; the last warp copies them
+            const int rows = n * sides - (sides == 2 && i0 + n - 1 == valid ? 1 : 0);
+            for (int r = 0; r < rows; ++r) {
+                const Span sp = span_of(sides == 2 ? (r & 1 ? d_of(i0 + r / 2) : t_of(i0 + r / 2)) : t_of(i0 + r), lo, hi);
+                Part part{-INFINITY, 0.f, 0x7fffffff};
+                for (int q = 0; q < sp.pieces; ++q) {
+                    const uint32_t bar = bars + 8 * slot;
+                    if (warp < kWarps) {
+                        if (!bar_wait(bar, phase)) s_gave = 1;  // (the sequence's result is void)
+                        const float4* piece = s_ring + slot * (kPiece / 4);
+                        if (greedy) add<true>(part, piece, sp, q, lo, sc);
+                        else add<false>(part, piece, sp, q, lo, sc);
+                        __syncwarp();
+                        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar + 8 * kRing) : "memory");
+                    } else if (lane == 0) {
+                        if (!bar_wait(bar + 8 * kRing, phase ^ 1)) s_gave = 1;
+                        copy_piece(ring + slot * (kPiece * 4), bar, sp, q);
+                    }
+                    if (++slot == kRing) { slot = 0; phase ^= 1; }
+                }
+                if (warp < kWarps) {
+                    part = warp_join(part, sc, greedy);
+                    if (lane == 0) s_warp[r][warp] = part;
                 }
             }
+            __syncwarp();
+            __syncthreads();
+            for (int r = warp; r < rows; r += kWarps) {
+                const Part q = warp_join(lane < kWarps ? s_warp[r][lane] : Part{-INFINITY, 0.f, 0x7fffffff}, sc, greedy);
+                if (lane == 0) s_part[round & 1][r] = q;
+            }
             cluster.sync();
-            if (warp < n) {  // one warp a position
-                const int i = i0 + warp;
-                double z[2] = {0.0, 0.0};
-                float top[2] = {-INFINITY, -INFINITY};
-                int at = 0x7fffffff;
-                for (int side = 0; side < (p.draft && !greedy && i < valid ? 2 : 1); ++side) {
-                    const Part q = lane < C ? *cluster.map_shared_rank(&s_part[round & 1][warp][side], lane) : Part{0.0, -INFINITY, 0x7fffffff};
-                    top[side] = warp_max(q.top);
-                    if (side == 0) at = __reduce_min_sync(0xffffffffu, q.top == top[0] ? q.at : 0x7fffffff);
-                    z[side] = q.top == -INFINITY ? 0.0 : q.sum * exp(((double)q.top - (double)top[side]) * sc.inv_t);
+            if (warp < n) {  // one warp a position, half of it a side
+                const bool drafts = my_i < valid;
+                const int side = lane >> 4, k = lane & 15;
+                Part q{-INFINITY, 0.f, 0x7fffffff};
+                if (k < C && (side == 0 || (sides == 2 && drafts))) q = *cluster.map_shared_rank(&s_part[round & 1][warp * sides + side], k);
+                float top = q.top;
 #pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) z[side] += __shfl_xor_sync(0xffffffffu, z[side], o);
+                for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                float sum = greedy || !(top > -INFINITY) ? 0.f : q.sum * weight32(q.top, top, sc);
+                int at = q.top == top ? q.at : 0x7fffffff;
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) {
+                    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                    at = min(at, __shfl_xor_sync(0xffffffffu, at, o));
                 }
+                // u q < p with both sums multiplied out
+                const double w = sum > 0.f && drafts ? weight64(own[side], top, sc, s_pow) : 0.0;
+                const float other = __shfl_down_sync(0xffffffffu, sum, 16);
+                const double w_q = __shfl_down_sync(0xffffffffu, w, 16);
+                const float top_q = __shfl_down_sync(0xffffffffu, top, 16);
                 if (lane == 0) {
-                    bool ok = false;
-                    if (i < valid) {
-                        const int d = drafted[i];
-                        if (greedy) {
-                            ok = d == at && top[0] > -INFINITY;
-                        } else {
-                            const double pd = z[0] > 0.0 ? weight(t_of(i)[d], top[0], sc.inv_t) / z[0] : 0.0;
-                            const double qd = !p.draft ? 1.0 : z[1] > 0.0 ? weight(d_of(i)[d], top[1], sc.inv_t) / z[1] : 0.0;
-                            ok = draw(p.u[(int64_t)b * p.K + i]) * qd < pd;
-                        }
-                    }
-                    s_ok[warp] = ok;
-                }
-                __syncwarp();
-                if (lane == 0) {  // (kept for the position that turns out to be the last)
-                    s_red[warp] = Part{0.0, top[0], at};
-                    s_sum[warp] = top[1];
+                    if (!drafts) s_ok[warp] = 0;
+                    else if (greedy) s_ok[warp] = my_d == at && top > -INFINITY;
+                    else if (!p.draft) s_ok[warp] = u_i * sum < w;
+                    else s_ok[warp] = other > 0.f ? u_i * w_q * sum < w * other : w > 0.0;
+                    s_tops[warp][0] = top;
+                    s_tops[warp][1] = sides == 2 ? top_q : -INFINITY;
+                    s_warp[0][warp] = Part{top, sum, at};
+                    s_warp[1][warp] = Part{top_q, sides == 2 ? other : 0.f, 0};
                 }
             }
             __syncthreads();
@@ -226,7 +280,7 @@ __global__ void __launch_bounds__(kThreads) verify_rows(const VerifyArgs p) {
             while (i < n && s_ok[i]) ++i;
             if (i < n) {
                 j = i0 + i;
-                if (tid == 0) { s_top[0] = s_red[i].top; s_top[1] = (float)s_sum[i]; s_at = s_red[i].at; }
+                if (tid == 0) { s_top[0] = s_tops[i][0]; s_top[1] = s_tops[i][1]; s_at = s_warp[0][i].at; s_run[0] = s_warp[0][i].sum; s_run[1] = s_warp[1][i].sum; }
                 open = false;
             }
             __syncthreads();
@@ -240,97 +294,150 @@ __global__ void __launch_bounds__(kThreads) verify_rows(const VerifyArgs p) {
         const float* t = t_of(j);
         const bool refused = j < valid;
         const float* d = refused && p.draft ? d_of(j) : nullptr;
-        const int skip = refused && !p.draft ? drafted[j] : -1;
+        const int skip = refused && !p.draft ? __shfl_sync(0xffffffffu, mine, j & 31) : -1;
         const float tp = p.probs ? 0.f : s_top[0], td = p.probs ? 0.f : s_top[1];
         const bool none = !p.probs && tp == -INFINITY;
-        double ratio = 1.0;
-        if (d && !p.probs && !none) {  // both rows' sums
-            double zp = 0.0, zq = 0.0;
-            for (int e = lo + tid; e < hi; e += kThreads) {
-                zp += weight(t[e], tp, sc.inv_t);
-                if (td > -INFINITY) zq += weight(d[e], td, sc.inv_t);
-            }
-            zp = block_sum(zp, s_sum);
-            zq = block_sum(zq, s_sum);
-            if (tid == 0) { s_z[0] = zp; s_z[1] = zq; }
-            cluster.sync();
-            zp = zq = 0.0;
-            for (int k = 0; k < C; ++k) {
-                zp += cluster.map_shared_rank(s_z, k)[0];
-                zq += cluster.map_shared_rank(s_z, k)[1];
-            }
-            ratio = zq > 0.0 ? zp / zq : 0.0;
-        }
-        for (int again = 0; again < 2 && !none; ++again) {  // (a second time, from p itself, if nothing is left of p - q)
-            auto left = [&](int e) {
-                if (p.probs) {
-                    const double a = fmax((double)t[e], 0.0);
-                    if (again || !refused) return a;
-                    return d ? fmax(a - fmax((double)d[e], 0.0), 0.0) : (e == skip ? 0.0 : a);
-                }
-                const double a = weight(t[e], tp, sc.inv_t);
-                if (again || !refused) return a;
-                return d ? fmax(a - (td > -INFINITY ? ratio * weight(d[e], td, sc.inv_t) : 0.0), 0.0) : (e == skip ? 0.0 : a);
-            };
+        auto of_p = [&](float x) { return p.probs ? fmax((double)x, 0.0) : weight64(x, tp, sc, s_pow); };
+        auto of_q = [&](float x) { return p.probs ? fmax((double)x, 0.0) : td > -INFINITY ? weight64(x, td, sc, s_pow) : 0.0; };
+        // p - ratio q, ratio = sum of p / sum of q.  Which tokens have something left hardly hangs on it: those of a ratio good to float32
+        // are taken, whose sums, p's and q's apart, then give what is left with the 64-bit ratio (a token on the wrong side
+        // adds 2^-20 of its own weight at most; if no more than 2^-10 of all is left, they are taken anew by that ratio).
+        double rough = p.probs ? 1.0 : d && s_run[1] > 0.0 ? s_run[0] / s_run[1] : 0.0;
+        double ratio = rough;
+        bool sure = p.probs;
+        for (int again = 0; again < 2 && !none;) {  // (a second time, from p itself, if nothing is left of p - q)
+            const bool two = d && !again;
             // every warp of the cluster sums a run of tokens
             const int span = ((hi - lo + kWarps - 1) / kWarps + 31) & ~31, w0 = min(lo + warp * span, hi), w1 = min(w0 + span, hi);
-            double sum = 0.0;
-            for (int e = w0 + lane; e < w1; e += 32) sum += left(e);
+            double all_p = 0.0, all_q = 0.0, left_p = 0.0, left_q = 0.0;
+            constexpr int kDeep = 8;
+            for (int e0 = w0 + lane; e0 < w1; e0 += 32 * kDeep) {
+                float x[kDeep], y[kDeep];
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                for (int i = 0; i < kDeep; ++i) {
+                    const int e = e0 + 32 * i;
+                    x[i] = e < w1 ? __ldg(t + e) : p.probs ? 0.f : -INFINITY;
+                    if (two) y[i] = e < w1 ? __ldg(d + e) : p.probs ? 0.f : -INFINITY;
+                }
+#pragma unroll
+                for (int i = 0; i < kDeep; ++i) {
+                    const double vx = of_p(x[i]);
+                    if (two) {
+                        const double vy = of_q(y[i]);
+                        all_p += vx;
+                        all_q += vy;
+                        if (vx > rough * vy) { left_p += vx; left_q += vy; }
+                    } else if (e0 + 32 * i != skip || again) {
+                        left_p += vx;
+                    }
+                }
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                left_p += __shfl_xor_sync(0xffffffffu, left_p, o);
+                if (two) {
+                    left_q += __shfl_xor_sync(0xffffffffu, left_q, o);
+                    all_p += __shfl_xor_sync(0xffffffffu, all_p, o);
+                    all_q += __shfl_xor_sync(0xffffffffu, all_q, o);
+                }
+            }
             __syncthreads();
-            if (lane == 0) s_sum[warp] = sum;
+            if (lane == 0 && warp < kWarps) { s_sum[0][warp] = left_p; s_sum[1][warp] = left_q; s_sum[2][warp] = all_p; s_sum[3][warp] = all_q; }
             cluster.sync();
+            for (int r = tid; r < C * kWarps; r += kThreads + 32) {
+                const double* from = cluster.map_shared_rank(&s_sum[0][0], r / kWarps) + r % kWarps;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s_all[k][r] = from[k * kWarps];
+            }
+            __syncthreads();
             // which run: the last one that is not empty and starts at or before the target, a lane some neighbouring runs
             if (warp == 0) {
                 const int n = C * kWarps, each = (n + 31) / 32;
-                double x[kMaxCluster * kWarps / 32], part = 0.0;
+                constexpr int kMost = kMaxCluster * kWarps / 32;
+                double x[kMost], y[kMost], part = 0.0;
+                double zp = 0.0, zq = 0.0;
 #pragma unroll
-                for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
+                for (int i = 0; i < kMost; ++i) {
                     const int r = lane * each + i;
-                    x[i] = i < each && r < n ? cluster.map_shared_rank(s_sum, r / kWarps)[r % kWarps] : 0.0;
+                    x[i] = y[i] = 0.0;
+                    if (i < each && r < n) {
+                        x[i] = s_all[0][r];
+                        if (two) {
+                            y[i] = s_all[1][r];
+                            zp += s_all[2][r];
+                            zq += s_all[3][r];
+                        }
+                    }
+                }
+                if (two && !p.probs) {
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) {
+                        zp += __shfl_xor_sync(0xffffffffu, zp, o);
+                        zq += __shfl_xor_sync(0xffffffffu, zq, o);
+                    }
+                    ratio = zq > 0.0 ? zp / zq : 0.0;
+                }
+#pragma unroll
+                for (int i = 0; i < kMost; ++i) {
+                    if (two) x[i] = fmax(x[i] - ratio * y[i], 0.0);
                     part += x[i];
                 }
                 double run = part;
 #pragma unroll
                 for (int o = 1; o < 32; o *= 2) {
-                    const double y = __shfl_up_sync(0xffffffffu, run, o);
-                    if (lane >= o) run += y;
+                    const double v = __shfl_up_sync(0xffffffffu, run, o);
+                    if (lane >= o) run += v;
                 }
-                const double want = draw(p.draws[b]) * __shfl_sync(0xffffffffu, run, 31);
+                const double total = __shfl_sync(0xffffffffu, run, 31), want = draw(p.draws[b]) * total;
                 double before = __shfl_up_sync(0xffffffffu, run, 1), start = 0.0;
                 if (lane == 0) before = 0.0;
                 int found = -1;
 #pragma unroll
-                for (int i = 0; i < kMaxCluster * kWarps / 32; ++i) {
+                for (int i = 0; i < kMost; ++i) {
                     if (x[i] > 0.0 && before <= want) { found = lane * each + i; start = before; }
                     before += x[i];
                 }
                 const int last = __reduce_max_sync(0xffffffffu, found);
                 if (last >= 0 && found == last) s_seg = want - start;
-                if (lane == 0) s_found = last;
+                if (lane == 0) {
+                    s_found = two && !sure && total < 0x1p-10 * zp ? -2 : last;
+                    s_run[2] = ratio;
+                }
             }
             __syncthreads();
             const int found = s_found;
+            ratio = s_run[2];
+            if (found == -2) {
+                rough = ratio;
+                sure = true;
+                cluster.sync();  // (the sums are read before they change)
+                continue;
+            }
             if (found >= 0) {
                 if (found / kWarps == rank) {  // this CTA has the run: its threads take neighbouring tokens
                     const int f0 = min(lo + found % kWarps * span, hi), f1 = min(f0 + span, hi);
                     const int each = (span + kThreads - 1) / kThreads;
                     const int e0 = min(f0 + tid * each, f1), e1 = min(e0 + each, f1);
-                    double mine = 0.0;
-                    for (int e = e0; e < e1; ++e) mine += left(e);
-                    double run = mine;
+                    auto left = [&](int e) {
+                        const double x = of_p(__ldg(t + e));
+                        if (!two) return e == skip && !again ? 0.0 : x;
+                        const double y = of_q(__ldg(d + e));
+                        return x > rough * y ? fmax(x - ratio * y, 0.0) : 0.0;
+                    };
+                    double mine64 = 0.0;
+                    for (int e = e0; e < e1; ++e) mine64 += left(e);
+                    double run = mine64;
 #pragma unroll
                     for (int o = 1; o < 32; o *= 2) {
-                        const double y = __shfl_up_sync(0xffffffffu, run, o);
-                        if (lane >= o) run += y;
+                        const double v = __shfl_up_sync(0xffffffffu, run, o);
+                        if (lane >= o) run += v;
                     }
                     __syncthreads();
-                    if (lane == 31) s_red[warp].sum = run;
+                    if (lane == 31 && warp < kWarps) s_run[warp] = run;
                     if (tid == 0) s_at = -1, s_hit = 0x7fffffff;
                     __syncthreads();
-                    double cum = run - mine;
-                    for (int w = 0; w < warp; ++w) cum += s_red[w].sum;
+                    double cum = run - mine64;
+                    for (int w = 0; w < warp; ++w) cum += s_run[w];
                     int hit = 0x7fffffff, last = -1;
                     for (int e = e0; e < e1; ++e) {
                         const double x = left(e);
@@ -349,7 +456,8 @@ __global__ void __launch_bounds__(kThreads) verify_rows(const VerifyArgs p) {
                 token = -2;  // (written above)
                 break;
             }
-            cluster.sync();  // (the sums are read before they change)
+            cluster.sync();
+            ++again;
         }
     }
     if (rank == 0 && tid == 0) {
@@ -360,6 +468,7 @@ __global__ void __launch_bounds__(kThreads) verify_rows(const VerifyArgs p) {
         p.accepted[b] = j;
     }
     cluster.sync();  // (shared memory stays until everybody has read it)
+    if (tid == 0 && s_gave) p.accepted[b] = -1;
 }
 
 }  // namespace
@@ -388,12 +497,17 @@ extern "C" int first_verify(const float* target, int64_t target_seq_stride, int6
     a.C = 1;
     while (a.C < kMaxCluster && (int64_t)B * a.C * 2 <= 2 * kSMs && vocab > 4096 * a.C) a.C *= 2;
     a.R = B <= 8 ? kMaxRound : B <= 24 ? 2 : 1;
-    static const cudaError_t once = cudaFuncSetAttribute(verify_rows, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    constexpr int kSmem = kRing * kPiece * 4;
+    static const cudaError_t once = [] {
+        const cudaError_t e = cudaFuncSetAttribute(verify_rows, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(verify_rows, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    }();
     if (once != cudaSuccess) return FIRST_E_CUDA;
     if (B > 0x7fffffff / kMaxCluster) return FIRST_E_CAPACITY;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)B * a.C);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(kThreads + 32);
+    cfg.dynamicSmemBytes = kSmem;
     cfg.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
