@@ -504,7 +504,7 @@ int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
  *                written.  A move outside the caches is left out (FIRST_FLAG_BAD_PAGE).
  * Errors: FIRST_E_ARG, FIRST_E_SHAPE (negative strides, rows that are written overlap, total != B without cu_new, heads),
  * FIRST_E_UNSUPPORTED (page, head_dim, alignment, more than 1024 KV heads, more than 96 layers), FIRST_E_CAPACITY (grid
- * sizes: max_pages * page above 2^30, more than 65000 pages or 2^18 query rows a sequence, first_read8: B above 65535), FIRST_E_CUDA. */
+ * sizes: max_pages * page above 2^30, more than 65000 pages or 2^18 query rows a sequence, B above 65535), FIRST_E_CUDA. */
 #define FIRST_CACHE_INT8 0
 #define FIRST_CACHE_E4M3 1
 typedef struct {

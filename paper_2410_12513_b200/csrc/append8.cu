@@ -78,49 +78,142 @@ __device__ __noinline__ uint32_t quotient_slow(double num, double den) {
     }
 }
 
-// The same for x / s, s given with its float32 reciprocal (0: too small for one).  x * inv is within 2^-22 of the
-// quotient: the slow way is for what that close to a tie cannot tell (1 element in some 10^4).
-template <bool E4M3>
-__device__ __forceinline__ uint32_t quotient(float x, float s, float inv) {
-    const float y = x * inv;
-    if constexpr (E4M3) {
-        const uint32_t lo = __nv_cvt_float_to_fp8(y * (1.f - 0x1p-20f), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float_to_fp8(y * (1.f + 0x1p-20f), __NV_SATFINITE, __NV_E4M3);
-        if (lo == hi && inv > 0.f && y == y) return lo;
-    } else {
-        const float c = fminf(fmaxf(y, -127.f), 127.f), r = rintf(c);
-        if (fabsf(c - r) < 0.4999f && inv > 0.f && y == y) return (uint32_t)(uint8_t)(int8_t)(int)r;
-    }
-    return s > 0.f ? quotient_slow<E4M3>((double)x, (double)s) : 0u;
-}
-
-// Eight elements of a row as float32.
+// Eight elements of a row, as they are in memory, and as float32.
+template <typename T>
+struct Eight {
+    uint32_t w[2 * sizeof(T)];
+};
 template <typename T, bool WIDE>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
-    if constexpr (WIDE && sizeof(T) == 2) {
-        unpack8(*reinterpret_cast<const uint4*>(p), f);
-    } else if constexpr (WIDE) {
-        const float4 a = *reinterpret_cast<const float4*>(p), b = *(reinterpret_cast<const float4*>(p) + 1);
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+__device__ __forceinline__ Eight<T> load8(const T* p) {
+    Eight<T> r;
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const uint4 u = reinterpret_cast<const uint4*>(p)[i];
+            r.w[4 * i] = u.x; r.w[4 * i + 1] = u.y; r.w[4 * i + 2] = u.z; r.w[4 * i + 3] = u.w;
+        }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    } else {
+        const uint16_t* s = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = s[2 * i] | (uint32_t)s[2 * i + 1] << 16;
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ float value_of(const Eight<T>& r, int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(r.w[i]);
+    else return i & 1 ? bf_hi(r.w[i / 2]) : bf_lo(r.w[i / 2]);
+}
+// Largest magnitude so far, as float32 bits (bfloat16: two 16-bit halves side by side): magnitudes are ordered like their bits.
+template <typename T>
+__device__ __forceinline__ uint32_t larger(uint32_t m, const Eight<T>& r) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, r.w[i] & 0x7fffffffu);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = to_f32(p[i]);
+        for (int i = 0; i < 4; ++i) m = __vmaxu2(m, r.w[i] & 0x7fff7fffu);
+    }
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t largest(uint32_t m) {
+    return sizeof(T) == 4 ? m : max(m & 0xffff0000u, m << 16);
+}
+
+// Eight finite values to 8 bits at once, if none is close to a tie: x * inv is within 2^-22 of the quotient.  (|x| is at most the
+// scale's 127 or 448 times, so nothing saturates but by that much.)  false: some are.
+template <bool E4M3, typename T>
+__device__ __forceinline__ bool quotients(const Eight<T>& r, float inv, uint2& out) {
+    uint32_t o[2];
+    if constexpr (E4M3) {
+        const float lo = inv * (1.f - 0x1p-20f), hi = inv * (1.f + 0x1p-20f);
+        uint32_t diff = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t c[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float x = value_of(r, 4 * h + 2 * i), y = value_of(r, 4 * h + 2 * i + 1);
+                c[i][0] = __nv_cvt_float2_to_fp8x2(make_float2(x * lo, y * lo), __NV_SATFINITE, __NV_E4M3);
+                c[i][1] = __nv_cvt_float2_to_fp8x2(make_float2(x * hi, y * hi), __NV_SATFINITE, __NV_E4M3);
+                diff |= c[i][0] ^ c[i][1];
+            }
+            o[h] = c[0][0] | c[1][0] << 16;
+        }
+        out = make_uint2(o[0], o[1]);
+        return diff == 0;
+    } else {
+        float off = 0.f;
+        uint32_t b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = value_of(r, i) * inv, m = y + 12582912.f;  // 1.5 2^23: the nearest whole number, in the low bits
+            off = fmaxf(off, fabsf(y - (m - 12582912.f)));
+            b[i] = __float_as_uint(m);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) o[h] = __byte_perm(__byte_perm(b[4 * h], b[4 * h + 1], 0x0040), __byte_perm(b[4 * h + 2], b[4 * h + 3], 0x0040), 0x5410);
+        out = make_uint2(o[0], o[1]);
+        return off < 0.4999f;
     }
 }
 
-constexpr int kAppendThreads = 128;
+// Eight finite values exactly (out of line): where a little more and a little less than x * inv have different neighbours, x is compared
+// with the middle between the two, times the scale: a fused product and difference has the exact sign.  (bfloat16 values meet exact ties
+// often: quotients of 8-bit numbers.)
+template <bool E4M3, typename T>
+__device__ __noinline__ uint2 quotients_exact(const Eight<T> r, float s, float inv) {
+    uint32_t w[2] = {0, 0};
+    const float lo = inv * (1.f - 0x1p-20f), hi = inv * (1.f + 0x1p-20f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = value_of(r, e);
+        uint32_t a, b;
+        float va, vb;
+        if constexpr (E4M3) {
+            a = __nv_cvt_float_to_fp8(x * lo, __NV_SATFINITE, __NV_E4M3);
+            b = __nv_cvt_float_to_fp8(x * hi, __NV_SATFINITE, __NV_E4M3);
+            va = to_value<true>(a);
+            vb = to_value<true>(b);
+        } else {
+            va = rintf(x * lo);
+            vb = rintf(x * hi);
+            a = (uint32_t)(int)va & 255u;
+            b = (uint32_t)(int)vb & 255u;
+        }
+        const float d = fmaf(-0.5f * (va + vb), s, x);
+        const bool second = d == 0.f ? (a & 1u) != 0u : (d > 0.f) == (vb > va);
+        w[e >> 2] |= (a != b && second ? b : a) << (8 * (e & 3));
+    }
+    return make_uint2(w[0], w[1]);
+}
+// Eight of any values, one by one.
+template <bool E4M3, typename T>
+__device__ __noinline__ uint2 quotients_slow(const Eight<T> r, float s) {
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e >> 2] |= (s > 0.f ? quotient_slow<E4M3>((double)value_of(r, e), (double)s) : 0u) << (8 * (e & 3));
+    return make_uint2(w[0], w[1]);
+}
+
+constexpr int kAppendHold = 8;  // vectors of 8 elements that a thread keeps between the two passes
 
 // One block a (page that gains tokens, head, K or V): the largest magnitude of the new values, the page's scale, and the
-// new values rounded to it; where the scale grew the page's earlier values are rounded to it again.
-template <typename T, bool E4M3, bool WIDE>
-__global__ void __launch_bounds__(kAppendThreads) append8(const Cache8 c, const Seqs8 s, const Rows8 kr, const Rows8 vr) {
+// new values rounded to it; where the scale grew the page's earlier values are rounded to it again.  The new values are read once and stay in
+// registers.  Bound by HBM for prompts (4 x 8190 tokens of 8 heads of 128 in bfloat16: read, 8 bits written), launch for single tokens.
+template <typename T, bool E4M3, bool WIDE, int kThreads>
+__global__ void __launch_bounds__(kThreads) append8(const Cache8 c, const Seqs8 s, const Rows8 kr, const Rows8 vr) {
     const Stamp stamp_guard(s.stamp);
     pdl_trigger();
     pdl_wait();
     Seq8 q;
-    if (!find_seq(s, blockIdx.x, q)) return;
-    const int tid = threadIdx.x, h = blockIdx.z >> 1, hd = c.hd, page = 1 << c.shift;
-    const bool is_v = blockIdx.z & 1;
+    if (!find_seq(s, blockIdx.z, q)) return;
+    const int tid = threadIdx.x, h = blockIdx.x >> 1, hd = c.hd, page = 1 << c.shift;
+    const bool is_v = blockIdx.x & 1;
     const int64_t first = ((int64_t)(q.before >> c.shift) + blockIdx.y) << c.shift;  // the page's first position
     const int64_t end = (int64_t)q.before + q.n;
     if (first >= end) return;
@@ -135,55 +228,78 @@ __global__ void __launch_bounds__(kAppendThreads) append8(const Cache8 c, const 
     const T* src = static_cast<const T*>(r.p) + (q.start + first + lo - q.before) * r.tok + h * r.head;
     uint8_t* dst = (is_v ? c.v : c.k) + ((((int64_t)p * c.H + h) << c.shift)) * hd;
     float* scale = (is_v ? c.vs : c.ks) + (int64_t)p * c.H + h;
-    const float2* cs = s.cs && !is_v ? s.cs + (int64_t)q.seq * (hd / 2) : nullptr;
-    const int vpr = hd / 8, nv = (hi - lo) * vpr;
-    auto fetch = [&](int i, float (&f)[8]) {
-        const T* row = src + (int64_t)(i / vpr) * r.tok;
-        const int d = i % vpr * 8;
-        load8<T, WIDE>(row + d, f);
-        if (cs) {  // rotary pair (d, d + hd/2)
-            const int half = hd / 2;
-            const bool up = d >= half;
-            float g[8];
-            load8<T, WIDE>(row + (up ? d - half : d + half), g);
+    const float held = lo > 0 ? *scale : 0.f;
+    const int vs = hd == 128 ? 4 : hd == 64 ? 3 : 2, nv = (hi - lo) << vs;  // vectors of a row: 2^vs
+    Eight<T> x[kAppendHold];
+    uint32_t m = 0;
+    const T* from = src + (tid >> vs) * r.tok + (tid & ((1 << vs) - 1)) * 8;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float2 t = cs[(up ? d - half : d) + e];
-                f[e] = up ? f[e] * t.x + g[e] * t.y : f[e] * t.x - g[e] * t.y;
+    for (int k = 0; k < kAppendHold; ++k) {
+        const int i = tid + k * kThreads;
+        if (i < nv) x[k] = load8<T, WIDE>(from);
+        from += (kThreads >> vs) * r.tok;
+    }
+    if constexpr (sizeof(T) == 4) {
+        if (s.cs && !is_v) {  // (the step) rotary pairs (d, d + hd/2)
+            const float2* cs = s.cs + (int64_t)q.seq * (hd / 2);
+#pragma unroll
+            for (int k = 0; k < kAppendHold; ++k) {
+                const int i = tid + k * kThreads, d = (i & ((1 << vs) - 1)) * 8;
+                if (i >= nv) break;
+                const bool up = d >= hd / 2;
+                const int at = up ? d - hd / 2 : d;
+                const Eight<T> y = load8<T, WIDE>(src + (int64_t)(i >> vs) * r.tok + (up ? at : d + hd / 2));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 t = cs[at + e];
+                    const float a = __uint_as_float(x[k].w[e]), b = __uint_as_float(y.w[e]);
+                    x[k].w[e] = __float_as_uint(up ? a * t.x + b * t.y : a * t.x - b * t.y);
+                }
             }
         }
-    };
-    uint32_t amax = 0;  // (as bits: magnitudes of finite values are ordered alike)
-    for (int i = tid; i < nv; i += kAppendThreads) {
-        float f[8];
-        fetch(i, f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t m = __float_as_uint(f[e]) & 0x7fffffffu;
-            amax = max(amax, m < 0x7f800000u ? m : 0u);
-        }
     }
-    __shared__ uint32_t red[kAppendThreads / 32];
-    amax = __reduce_max_sync(0xffffffffu, amax);
+#pragma unroll
+    for (int k = 0; k < kAppendHold; ++k)
+        if (tid + k * kThreads < nv) m = larger(m, x[k]);
+    m = largest<T>(m);
+    __shared__ uint32_t red[kThreads / 32];
+    uint32_t amax = __reduce_max_sync(0xffffffffu, m);
     if ((tid & 31) == 0) red[tid >> 5] = amax;
-    const float held = lo > 0 ? *scale : 0.f;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kAppendThreads / 32; ++w) amax = max(amax, red[w]);
+    for (int w = 0; w < kThreads / 32; ++w) amax = max(amax, red[w]);
+    const bool odd = amax >= 0x7f800000u;  // not all are finite: the largest of those that are
+    if (odd) {
+        m = 0;
+        for (int k = 0; k < kAppendHold; ++k)
+            if (tid + k * kThreads < nv)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t u = __float_as_uint(value_of(x[k], e)) & 0x7fffffffu;
+                    m = max(m, u < 0x7f800000u ? u : 0u);
+                }
+        amax = __reduce_max_sync(0xffffffffu, m);
+        __syncthreads();
+        if ((tid & 31) == 0) red[tid >> 5] = amax;
+        __syncthreads();
+        for (int w = 0; w < kThreads / 32; ++w) amax = max(amax, red[w]);
+    }
     const float fresh = __uint_as_float(amax) * (1.f / (E4M3 ? 448.f : 127.f));
     const float now = held >= fresh || held != held ? held : fresh;  // (a NaN stays: what the page holds is none either)
     const float inv = now > 1e-37f ? 1.f / now : 0.f;
-    for (int i = tid; i < nv; i += kAppendThreads) {
-        float f[8];
-        fetch(i, f);
-        uint32_t o[2] = {0, 0};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e >> 2] |= quotient<E4M3>(f[e], now, inv) << (8 * (e & 3));
-        *reinterpret_cast<uint2*>(dst + (int64_t)(lo + i / vpr) * hd + i % vpr * 8) = make_uint2(o[0], o[1]);
+    for (int k = 0; k < kAppendHold; ++k) {
+        const int i = tid + k * kThreads;
+        if (i < nv) {
+            uint2 o;
+            if (odd || !(inv > 0.f)) o = quotients_slow<E4M3>(x[k], now);
+            else if (!quotients<E4M3>(x[k], inv, o)) o = quotients_exact<E4M3>(x[k], now, inv);
+            *reinterpret_cast<uint2*>(dst + lo * hd + i * 8) = o;
+        }
     }
     if (lo > 0 && now > held) {
         const float ratio = (float)((double)held / (double)now);
-        for (int i = tid; i < lo * hd / 4; i += kAppendThreads) {
+        for (int i = tid; i < lo * hd / 4; i += kThreads) {
             uint32_t* w = reinterpret_cast<uint32_t*>(dst) + i;
             const uint32_t old = *w;
             uint32_t o = 0;
@@ -303,8 +419,9 @@ namespace first {
 cudaError_t append8_launch(const Cache8& c, const Seqs8& s, const Rows8& k, const Rows8& v, cudaStream_t st, bool pdl) {
     const int pages = (int)(((int64_t)s.max_new + (1 << c.shift) - 2) / (1 << c.shift) + 1);  // that a sequence's tokens touch at most
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(s.B, s.max_new == 1 ? 1 : pages, 2 * c.H);
-    cfg.blockDim = dim3(kAppendThreads);
+    cfg.gridDim = dim3(2 * c.H, s.max_new == 1 ? 1 : pages, s.B);  // (neighbouring heads of a token run together)
+    const bool large = (c.hd << c.shift) > 128 * 8 * kAppendHold;    // a page's head in 128 threads' registers, or 256's
+    cfg.blockDim = dim3(large ? 256 : 128);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -312,7 +429,7 @@ cudaError_t append8_launch(const Cache8& c, const Seqs8& s, const Rows8& k, cons
     cfg.attrs = at;
     cfg.numAttrs = pdl ? 1 : 0;
     const bool wide = aligned16(k) && aligned16(v);
-#define FIRST_APPEND(T, E, W) return cudaLaunchKernelEx(&cfg, append8<T, E, W>, c, s, k, v)
+#define FIRST_APPEND(T, E, W) return large ? cudaLaunchKernelEx(&cfg, append8<T, E, W, 256>, c, s, k, v) : cudaLaunchKernelEx(&cfg, append8<T, E, W, 128>, c, s, k, v)
     if (k.f32) {
         if (c.e4m3) { if (wide) FIRST_APPEND(float, true, true); else FIRST_APPEND(float, true, false); }
         else { if (wide) FIRST_APPEND(float, false, true); else FIRST_APPEND(float, false, false); }
@@ -337,7 +454,7 @@ int first_append8(const first_cache8* cache, const void* k, int64_t k_token_stri
         return rc;
     if (B == 0 || total == 0 || max_new == 0) return FIRST_OK;
     const Cache8 c = cache8_of(*cache);
-    if ((int64_t)max_pages * cache->page > (1 << 30) || (max_new >> c.shift) > 65000) return FIRST_E_CAPACITY;
+    if (B > 65535 || (int64_t)max_pages * cache->page > (1 << 30) || (max_new >> c.shift) > 65000) return FIRST_E_CAPACITY;
     Seqs8 s;
     s.pages = pages; s.width = max_pages; s.len = len; s.cu = cu_new;
     s.B = B; s.total = total; s.max_new = std::min(max_new, total); s.flags = flags;
