@@ -265,7 +265,7 @@ int first_get_plan(first_ctx *ctx, int32_t *idx, int32_t *cnt, int32_t *slot);
  * with mask 0 leave x, the slab and len untouched.  logits[b] = lm_head . RMSNorm(x).
  * Then pos[b] += 1.
  *   tokens        dev int32 [B]
- *   kv            host struct; see first_kv_cache
+ *   kv            host struct; see first_kv_cache.  NULL: the pages of first_set_pages
  *   logits        dev float32 [B][vocab], or NULL
  *   next_tokens   dev int32 [B] or NULL: argmax of the logits row, lowest index on ties (or a
  *                 sampled token, see first_set_sampling)
@@ -528,6 +528,53 @@ int64_t first_attn8_workspace(const first_cache8 *cache, int32_t n_q_heads, int3
                               int32_t B, int32_t max_new);
 int first_copy_pages(const first_cache8 *layers, int32_t n_layers, const int32_t *moves, int64_t n_moves, uint32_t *flags,
                      void *stream);
+
+/* Pages of 8-bit caches handed out to sequences whose membership changes ("Inference for FiRST", item 2: every layer has lists of
+ * its own, a skipped (sequence, layer) has no page).  A sequence has a slot (its batch row) and, in every layer it keeps, the
+ * pages that its tokens need; forks share pages, and a page that two sequences hold is copied before one of them appends to
+ * it.  The bookkeeping is on the host; first_pages_commit brings the device's tables up to date.  All commits of a manager, and the calls on its
+ * cache, belong on one stream; pages freed since the last commit may be handed out again by the next one.
+ *
+ * first_pages_create  max_seqs <= max_batch slots of at most max_pages pages a layer; layers host [L], alike in format and sizes (n_pages may
+ *                     differ), borrowed.  Allocates the device tables.
+ * first_pages_join    a sequence enters: mask_row host uint8 [L].  src != NULL: the next commit takes over its first n_tokens keys and values from
+ *                     sequence src_seq of a slab cache (per_layer = 0, of the model's dtype, such as a first_prefill call filled; it has to
+ *                     stay as it is until then); src == NULL: n_tokens = 0.
+ * first_pages_fork    a new slot with the same tokens.  Fork and trim speak of tokens that are there: FIRST_E_STATE while an import, or tokens that the
+ *                     sequence was extended by, wait for the commit.
+ * first_pages_extend  the sequence (slot -1: every one) is about to gain n_new tokens: pages for them, all or nothing.  After the next commit first_decode_step or
+ *                     first_append8 (on len as it stands) stores them; that step advances len by itself, after first_append8 a trim does.
+ * first_pages_trim    the sequence goes back to its first n_tokens tokens (after drafts were refused); pages behind them are
+ *                     freed.  The next commit sets len and pos to n_tokens (which may be all of them: after first_append8).
+ * first_pages_leave   frees slot and pages.
+ * first_pages_commit  copies shared pages that are about to change, updates the tables, imports, and sets the step's plan (first_set_mask_host
+ *                     over all max_seqs rows).  FIRST_E_STATE during a stream capture.
+ * first_pages_compact commits, moves the highest pages in use to holes below them, and commits again: afterwards pages held = highest + 1.
+ * first_pages_kv      len, pos, slab_cap as the step reads them (k, v: the pages; not a slab cache for other calls)
+ * first_pages_layer   one layer's cache, page table (dev [max_seqs][max_pages]) and lengths (dev [max_seqs]), for first_append8 / first_attn8 on rows of
+ *                     their own; any pointer may be NULL
+ * first_pages_stats   per layer: pages in use, the highest id in use (-1: none); live sequences (any pointer may be NULL)
+ * first_pages_tokens  the sequence's tokens, by the host's count
+ * first_set_pages     first_decode_step with kv == NULL then appends to and attends over this manager's pages (its plan must be the last commit's; free rows need a
+ *                     valid token id).  NULL: none.  The manager has to outlive the setting; commit before its first step.
+ * Errors: FIRST_E_ARG, FIRST_E_SHAPE (layers differ, or from the model), FIRST_E_CAPACITY (no slot, no pages: nothing is taken then),
+ * FIRST_E_STATE (free slot), FIRST_E_UNSUPPORTED (more than 96 layers), FIRST_E_CUDA. */
+typedef struct first_pages first_pages;
+int first_pages_create(first_ctx *ctx, int32_t max_seqs, int32_t max_pages, const first_cache8 *layers, first_pages **out);
+int first_pages_destroy(first_pages *pages);
+int first_pages_join(first_pages *pages, const uint8_t *mask_row, const first_kv_cache *src, int32_t src_seq, int32_t n_tokens,
+                     int32_t *slot);
+int first_pages_fork(first_pages *pages, int32_t slot, int32_t *new_slot);
+int first_pages_extend(first_pages *pages, int32_t slot, int32_t n_new);
+int first_pages_trim(first_pages *pages, int32_t slot, int32_t n_tokens);
+int first_pages_leave(first_pages *pages, int32_t slot);
+int first_pages_commit(first_pages *pages, void *stream);
+int first_pages_compact(first_pages *pages, void *stream);
+int first_pages_kv(first_pages *pages, first_kv_cache *out);
+int first_pages_layer(first_pages *pages, int32_t layer, first_cache8 *cache, const int32_t **table, int32_t *max_pages, int32_t **len);
+int first_pages_stats(first_pages *pages, int32_t *pages_held, int32_t *highest, int32_t *live);
+int first_pages_tokens(const first_pages *pages, int32_t slot, int32_t *tokens);
+int first_set_pages(first_ctx *ctx, first_pages *pages);
 
 /* Verification of drafted tokens.  A cheaper model (a step with more layers skipped, a lookup in the prompt) proposes tokens,
  * the target scores them all in one pass; the tokens that come out have the target's distribution.  Per sequence, with p_i the target's

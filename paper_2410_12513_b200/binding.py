@@ -136,7 +136,21 @@ def lib():
         L.first_rope_freqs.argtypes = [C.POINTER(RopeSpecC), p, p]
         L.first_rope.argtypes = [p, i64, i64, i32, p, i64, i64, i32, i32, i64, i32, i32, p, p, C.c_float, i32, p]
         L.first_set_rope.argtypes = [p, p, f64]
-        cache8 = C.POINTER(Cache8C)
+        cache8, pi32 = C.POINTER(Cache8C), C.POINTER(C.c_int32)
+        L.first_pages_create.argtypes = [p, i32, i32, cache8, C.POINTER(C.c_void_p)]
+        L.first_pages_destroy.argtypes = [p]
+        L.first_pages_join.argtypes = [p, p, C.POINTER(KVCacheC), i32, i32, pi32]
+        L.first_pages_fork.argtypes = [p, i32, pi32]
+        L.first_pages_extend.argtypes = [p, i32, i32]
+        L.first_pages_trim.argtypes = [p, i32, i32]
+        L.first_pages_leave.argtypes = [p, i32]
+        L.first_pages_commit.argtypes = [p, p]
+        L.first_pages_compact.argtypes = [p, p]
+        L.first_pages_kv.argtypes = [p, C.POINTER(KVCacheC)]
+        L.first_pages_layer.argtypes = [p, i32, cache8, C.POINTER(C.c_void_p), pi32, C.POINTER(C.c_void_p)]
+        L.first_pages_stats.argtypes = [p, p, p, pi32]
+        L.first_pages_tokens.argtypes = [p, i32, pi32]
+        L.first_set_pages.argtypes = [p, p]
         L.first_append8.argtypes = [cache8, p, i64, i64, p, i64, i64, i32, p, i32, p, i32, p, i32, i32, p, p]
         L.first_read8.argtypes = [cache8, p, i32, p, p, i32, i32, i32, p, i64, i64, p, i64, i64, i32, p, p]
         L.first_attn8.argtypes = [cache8, p, i64, i64, i32, i32, C.c_float, p, i32, p, i32, p, i32, i32, p, i64, i64, p, i64, p, p]
@@ -144,7 +158,10 @@ def lib():
         L.first_attn8_workspace.restype = i64
         L.first_copy_pages.argtypes = [cache8, i32, p, i64, p, p]
         L.first_verify.argtypes = [p, i64, i64, p, i64, i64, i32, p, i32, i32, i32, p, p, p, p, p, p]
-        for name in ("first_append8", "first_read8", "first_attn8", "first_copy_pages", "first_verify", "first_sample", "first_set_sampling_rows", "first_lora", "first_set_adapters", "first_rope_freqs",
+        for name in ("first_pages_create", "first_pages_destroy", "first_pages_join", "first_pages_fork", "first_pages_extend",
+                     "first_pages_trim", "first_pages_leave", "first_pages_commit", "first_pages_compact", "first_pages_kv",
+                     "first_pages_layer", "first_pages_stats", "first_pages_tokens", "first_set_pages",
+                     "first_append8", "first_read8", "first_attn8", "first_copy_pages", "first_verify", "first_sample", "first_set_sampling_rows", "first_lora", "first_set_adapters", "first_rope_freqs",
                      "first_rope", "first_set_rope"):
             getattr(L, name).restype = C.c_int
         L.first_kernel_class_count.restype = C.c_int32
@@ -364,6 +381,105 @@ class FirstPool:
         return held, big, live.value
 
 
+class FirstPages:
+    """Pages of the layers' 8-bit caches (a list of Cache8, borrowed) handed out to sequences (first_pages_* in first.h)."""
+
+    def __init__(self, ctx, max_seqs, max_pages, caches):
+        self._ctx, self.caches = ctx, list(caches)
+        self.B, self.L, self.max_pages, self.h = int(max_seqs), len(self.caches), int(max_pages), None
+        if self.L != ctx.shape.n_layers:
+            raise ValueError(f"one cache a layer: {ctx.shape.n_layers}")
+        arr = (Cache8C * self.L)(*[c.c for c in self.caches])
+        h = C.c_void_p()
+        rc = lib().first_pages_create(ctx.h, self.B, self.max_pages, arr, C.byref(h))
+        if rc:
+            raise FirstError(rc, "first_pages_create")
+        self.h = h
+
+    def close(self):
+        if self.h:
+            if getattr(self._ctx, "_pages", None) is self and self._ctx.h is not None:
+                self._ctx.set_pages(None)
+            lib().first_pages_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _call(self, name, *args):
+        rc = getattr(lib(), name)(self.h, *args)
+        if rc:
+            raise FirstError(rc, name)
+
+    def join(self, mask_row, src=None, src_seq=0, n_tokens=0):
+        import numpy as np
+        m = np.ascontiguousarray(np.asarray(mask_row), dtype=np.uint8)
+        if m.size != self.L:
+            raise ValueError(f"mask_row must have {self.L} entries")
+        slot = C.c_int32(-1)
+        self._call("first_pages_join", m.ctypes.data, C.byref(src.c) if src is not None else None, int(src_seq), int(n_tokens), C.byref(slot))
+        return slot.value
+
+    def fork(self, slot):
+        out = C.c_int32(-1)
+        self._call("first_pages_fork", int(slot), C.byref(out))
+        return out.value
+
+    def extend(self, n_new=1, slot=-1):
+        self._call("first_pages_extend", int(slot), int(n_new))
+
+    def trim(self, slot, n_tokens):
+        self._call("first_pages_trim", int(slot), int(n_tokens))
+
+    def leave(self, slot):
+        self._call("first_pages_leave", int(slot))
+
+    def commit(self, stream=None):
+        self._call("first_pages_commit", _stream(stream))
+        self._ctx.B = self.B
+
+    def compact(self, stream=None):
+        self._call("first_pages_compact", _stream(stream))
+        self._ctx.B = self.B
+
+    def tokens(self, slot):
+        n = C.c_int32(0)
+        self._call("first_pages_tokens", int(slot), C.byref(n))
+        return n.value
+
+    def stats(self):
+        """-> (pages in use per layer, highest page in use per layer, live sequences)."""
+        import numpy as np
+        held, top, live = np.zeros(self.L, np.int32), np.zeros(self.L, np.int32), C.c_int32(0)
+        self._call("first_pages_stats", held.ctypes.data, top.ctypes.data, C.byref(live))
+        return held, top, live.value
+
+    def layer(self, layer):
+        """-> (Cache8, page table, lengths) of a layer, as CUDA int32 tensors [max_seqs][max_pages] and [max_seqs] that view the manager's own."""
+        table, ln = C.c_void_p(), C.c_void_p()
+        self._call("first_pages_layer", int(layer), None, C.byref(table), None, C.byref(ln))
+        return self.caches[layer], _view_i32(table.value, (self.B, self.max_pages), self), _view_i32(ln.value, (self.B,), self)
+
+
+class _DeviceArray:
+    def __init__(self, address, shape, owner):
+        self.owner = owner  # (a view keeps the manager alive)
+        self.__cuda_array_interface__ = {"shape": shape, "typestr": "<i4", "data": (address, False), "version": 2}
+
+
+def _view_i32(address, shape, owner):
+    return torch.as_tensor(_DeviceArray(address, shape, owner), device="cuda")
+
+
+def first_set_pages(h, pages=None):
+    rc = lib().first_set_pages(h, None if pages is None else pages.h)
+    if rc:
+        raise FirstError(rc, "first_set_pages")
+
+
 def first_get_plan(h, B, L):
     import numpy as np
     idx = np.empty((L, B), dtype=np.int32)
@@ -376,7 +492,7 @@ def first_get_plan(h, B, L):
 
 
 def first_decode_step(h, tokens, kv: KVCache, logits=None, next_tokens=None, layer_inputs=None, stream=None):
-    rc = lib().first_decode_step(h, _dev(tokens, torch.int32, "tokens"), C.byref(kv.c),
+    rc = lib().first_decode_step(h, _dev(tokens, torch.int32, "tokens"), None if kv is None else C.byref(kv.c),
                                  _dev(logits, torch.float32, "logits"),
                                  _dev(next_tokens, torch.int32, "next_tokens"),
                                  _dev(layer_inputs, torch.float32, "layer_inputs"), _stream(stream))
@@ -884,6 +1000,11 @@ class FirstContext:
         if adapters is not None and seq_adapter.numel() < self.max_batch:
             raise ValueError(f"seq_adapter must have {self.max_batch} entries")
         self._adapters = first_set_adapters(self.h, self.shape, self.dtype, adapters, seq_adapter, scales)
+
+    def set_pages(self, pages=None):
+        """Steps with kv=None run over this FirstPages (kept alive until the next call)."""
+        first_set_pages(self.h, pages)
+        self._pages = pages
 
     def set_rope(self, inv_freq=None, factor=1.0):
         first_set_rope(self.h, inv_freq, factor, self.shape.head_dim)

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kThreads) append8(const Cache8 c, const Seqs8 
     const int lo = (int)max((int64_t)q.before - first, (int64_t)0), hi = (int)min(end - first, (int64_t)page);
     const Rows8& r = is_v ? vr : kr;
     // row `lo` of the page is row `row0` of the tensor
-    const T* src = static_cast<const T*>(r.p) + (q.start + first + lo - q.before) * r.tok + h * r.head;
+    const T* src = static_cast<const T*>(r.p) + ((s.row_off ? *s.row_off : 0) + q.start + first + lo - q.before) * r.tok + h * r.head;
     uint8_t* dst = (is_v ? c.v : c.k) + ((((int64_t)p * c.H + h) << c.shift)) * hd;
     float* scale = (is_v ? c.vs : c.ks) + (int64_t)p * c.H + h;
     const float held = lo > 0 ? *scale : 0.f;

@@ -45,8 +45,8 @@ struct Seq8 {
 __device__ __forceinline__ bool find_seq(const Seqs8& s, int b, Seq8& q) {
     if (s.m_dev && b >= __ldg(s.m_dev)) return false;
     q.seq = s.idx ? s.idx[b] : b;
-    q.start = s.cu ? s.cu[b] : b;
-    const int64_t n = s.cu ? (int64_t)s.cu[b + 1] - q.start : 1;
+    q.start = s.cu ? s.cu[b] : b * s.each;
+    const int64_t n = s.cu ? (int64_t)s.cu[b + 1] - q.start : s.each;
     q.before = s.len[q.seq];
     if (n == 0 && q.start >= 0 && q.start <= s.total) return false;
     if (q.start < 0 || n < 0 || q.start + n > s.total || n > s.max_new || q.before < 0 || q.before > 0x7fffffff - n) {

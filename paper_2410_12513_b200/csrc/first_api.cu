@@ -18,6 +18,7 @@
 #include "gemm_tc2.cuh"
 #include "gemv.cuh"
 #include "ops.h"
+#include "pages.h"
 #include "prefill.cuh"
 #include "router.cuh"
 #include "step.cuh"
@@ -135,6 +136,7 @@ struct first_ctx {
     const int32_t* ad_seq = nullptr;   // adapter of every batch row (the caller's) ...
     const int32_t* ad_rows = nullptr;  // ... or of every row of a prompt chunk, while one runs
     int32_t* pf_adapter = nullptr;
+    const first_pages* pages = nullptr;  // the 8-bit pages of steps without a slab cache (first_set_pages)
     // batched prefill: per-row tables of a chunk (each prompt token is a row), an all-keep mask, the residual of
     // every sequence's last prompt token, and (allocated on first use) the per-layer token scores of the routers
     int32_t *pf_cu = nullptr, *pf_tok = nullptr, *pf_cap = nullptr, *pf_pos = nullptr, *pf_len = nullptr;
@@ -529,7 +531,7 @@ struct LayerKv {
 };
 LayerKv layer_kv(const first_kv_cache* kv, int l, int B) {
     if (!kv->per_layer) return {kv->slab_off, kv->slab_cap, kv->cap_total};
-    return {kv->slab_off + (size_t)l * B, kv->slab_cap + (size_t)l * B, kv->cap_total_l[l]};
+    return {kv->slab_off + (size_t)l * B, kv->slab_cap + (size_t)l * B, kv->cap_total_l ? kv->cap_total_l[l] : 0};
 }
 
 template <typename KT, int HD>
@@ -775,10 +777,54 @@ int apply_adapters(first_ctx* c, cudaStream_t st, int target, int l, const float
     return FIRST_OK;
 }
 
+// Rotate, append and attend over 8-bit pages: from the QKV projection's output to the attention output.
+int paged_attention(first_ctx* c, cudaStream_t st, const PagedView& v, int l, int m, const int32_t* len_l, const int32_t* idx,
+                    const int32_t* m_dev, float qscale, float* out, __nv_bfloat16* out_hi, __nv_bfloat16* out_lo) {
+    const first_model_desc& d = c->d;
+    Seqs8 s;
+    s.pages = v.pages + (int64_t)l * v.B * v.max_pages;
+    s.width = v.max_pages;
+    s.len = len_l;
+    s.B = s.total = m;
+    s.idx = idx; s.m_dev = m_dev;
+    s.flags = c->flags;
+    s.cs = c->cs;
+    const int64_t row = c->qkvd, hd = d.head_dim;
+    auto pdl = [&] {
+        const bool p = c->use_pdl && !c->profiling && c->pdl_next;
+        c->pdl_next = true;
+        return p;
+    };
+    const Cache8 cache = cache8_of(v.layers[l]);
+    {
+        s.stamp = stamp_slot(c, kClsRopeAppend);
+        Launch guard(c, st, kClsRopeAppend);
+        CU_TRY(append8_launch(cache, s, Rows8{c->qkv + c->qd, row, hd, true}, Rows8{c->qkv + c->qd + c->kvd, row, hd, true}, st, pdl()));
+    }
+    Attn8Args a;
+    a.c = cache;
+    a.s = s;
+    a.s.stamp = stamp_slot(c, kClsAttn);
+    a.q = Rows8{c->qkv, row, hd, true};
+    a.out = Rows8{out, c->qd, hd, true};
+    a.out_hi = out_hi; a.out_lo = out_lo;
+    a.G = c->group;
+    a.scale = qscale;
+    const int64_t parts = attn8_part_floats(m, d.n_kv_heads, c->group, (int)hd, (int64_t)v.max_pages << cache.shift, true, c->n_sm) / (hd + 2);
+    if (parts > 0 && parts <= (int64_t)d.max_batch * d.n_q_heads * c->max_splits) {
+        a.part_o = c->o_part;
+        a.part_ml = reinterpret_cast<float*>(c->ml_part);
+    }
+    Launch guard(c, st, kClsAttn);
+    CU_TRY(attn8_launch(a, st, pdl(), c->n_sm));
+    return FIRST_OK;
+}
+
 // The whole step, for one weight/cache element type.
 template <typename WT>
 int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* kv, float* logits,
-                     int32_t* next_tokens, float* layer_inputs, cudaStream_t st, const PrefillHook* ph = nullptr) {
+                     int32_t* next_tokens, float* layer_inputs, cudaStream_t st, const PrefillHook* ph = nullptr,
+                     const PagedView* paged = nullptr) {
     const first_model_desc& d = c->d;
     const int B = c->B, D = d.d_model, F = d.ffn_dim, V = d.vocab, L = d.n_layers, hd = d.head_dim;
     constexpr bool kBf16 = std::is_same<WT, __nv_bfloat16>::value;
@@ -800,7 +846,7 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
     S = std::max(1, std::min(S, kSimpleSplitsMax));
     const float qscale = 1.0f / std::sqrt((float)hd);
     const int norm_threads = std::max(32, std::min(c->norm_threads_max, (D / 4 + 31) / 32 * 32));  // at most norm_threads_max threads, a float4 or two each
-    const bool mma_attn = kBf16 && c->tc_ready && (hd == 64 || hd == 128) && c->attn_simple <= 0;
+    const bool mma_attn = !paged && kBf16 && c->tc_ready && (hd == 64 || hd == 128) && c->attn_simple <= 0;
     const bool fuse_rope = mma_attn && c->fuse_rope;
     // prompt chunks: consecutive rows are consecutive tokens of a sequence and may share attention work items
     const bool route_here = ph && ph->router_w;
@@ -848,14 +894,17 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
             return rc;
         // The tuned attention kernel rotates q itself and appends the new token's key and value (its
         // row facts come from the norm kernel above); the general path has a kernel for that.
-        if (!fuse_rope &&
+        if (paged) {
+            if ((rc = paged_attention(c, st, *paged, l, m, len_l, idx, m_dev, qscale, t ? nullptr : c->att, xh, xl))) return rc;
+        } else if (!fuse_rope &&
             (rc = launch_k(c, st, kClsRopeAppend, rope_append<WT>, dim3((d.n_q_heads + 2 * d.n_kv_heads + 7) / 8, m), dim3(hd / 2, 8),
                            0, c->qkv, idx, m_dev, d.n_q_heads, d.n_kv_heads, hd, c->cs, qscale, c->q,
                            static_cast<WT*>(kv->k[l]), static_cast<WT*>(kv->v[l]), lkv.cap_total, lkv.slab_off,
                            lkv.slab_cap, len_l, c->flags, mma_attn ? c->rowinfo : nullptr, pair_rows,
                            d.max_tokens_per_seq)))
             return rc;
-        if (mma_attn) {
+        if (paged) {
+        } else if (mma_attn) {
             if ((rc = launch_attn_mma(c, st, m, kv->k[l], kv->v[l], &lkv, len_l, idx, t ? nullptr : c->att, xh, xl,
                                       fuse_rope, qscale, pair_rows, m_dev)))
                 return rc;
@@ -873,7 +922,7 @@ int decode_step_impl(first_ctx* c, const int32_t* tokens, const first_kv_cache* 
         // ---- feed-forward half (its norm kernel also advances the cache length of the rows it handles)
         if ((rc = launch_k(c, st, kClsRmsnorm, rmsnorm_rows, dim3(m), dim3(norm_threads), 0, c->x, idx, m_dev, D, c->ffn_norm[l],
                            d.rms_eps, f32, xh, xl, zero_gu ? c->gu : nullptr, 2 * F, len_l, lkv.slab_cap, static_cast<longlong2*>(nullptr), static_cast<const int32_t*>(nullptr), static_cast<const int64_t*>(nullptr), static_cast<uint32_t*>(nullptr),
-                           static_cast<const float*>(nullptr), static_cast<const float*>(nullptr), 0, static_cast<float*>(nullptr), d.max_tokens_per_seq)))
+                           static_cast<const float*>(nullptr), static_cast<const float*>(nullptr), 0, static_cast<float*>(nullptr), paged ? 1 << 30 : d.max_tokens_per_seq)))
             return rc;
         if (fused_ffn) {
             // gate/up projection with silu(gate)*up applied in its epilogue: the activation is written once
@@ -1152,11 +1201,22 @@ int first_get_plan(first_ctx* c, int32_t* idx, int32_t* cnt, int32_t* slot) {
 
 int first_decode_step(first_ctx* c, const int32_t* tokens, const first_kv_cache* kv, float* logits,
                       int32_t* next_tokens, float* layer_inputs, void* stream) {
-    if (!c || !tokens || !kv) return FIRST_E_ARG;
+    if (!c || !tokens || (!kv && !c->pages)) return FIRST_E_ARG;
     if (!c->has_mask) return FIRST_E_STATE;
+    first_kv_cache of_pages{};
+    PagedView view;
+    const PagedView* paged = nullptr;
+    if (!kv) {
+        view = paged_view(c->pages);
+        if (view.B != c->B) return FIRST_E_STATE;  // (the plan is not that of the manager's last commit)
+        first_pages_kv(const_cast<first_pages*>(c->pages), &of_pages);
+        of_pages.per_layer = 1;  // (capacities by layer; there are no slabs)
+        kv = &of_pages;
+        paged = &view;
+    }
     if (!kv->k || !kv->v || !kv->slab_off || !kv->slab_cap || !kv->len || !kv->pos) return FIRST_E_ARG;
-    if (kv->per_layer ? !kv->cap_total_l : kv->cap_total <= 0) return FIRST_E_ARG;
-    for (int l = 0; l < c->d.n_layers; ++l) {
+    if (!paged && (kv->per_layer ? !kv->cap_total_l : kv->cap_total <= 0)) return FIRST_E_ARG;
+    for (int l = 0; !paged && l < c->d.n_layers; ++l) {
         if (c->cnt_h[l] == 0) continue;
         if (!kv->k[l] || !kv->v[l]) return FIRST_E_ARG;
         if (kv->per_layer && kv->cap_total_l[l] <= 0) return FIRST_E_ARG;
@@ -1164,8 +1224,8 @@ int first_decode_step(first_ctx* c, const int32_t* tokens, const first_kv_cache*
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     auto run = [&](cudaStream_t s) {
         if (c->d.dtype == FIRST_DTYPE_BF16)
-            return decode_step_impl<__nv_bfloat16>(c, tokens, kv, logits, next_tokens, layer_inputs, s);
-        return decode_step_impl<float>(c, tokens, kv, logits, next_tokens, layer_inputs, s);
+            return decode_step_impl<__nv_bfloat16>(c, tokens, kv, logits, next_tokens, layer_inputs, s, nullptr, paged);
+        return decode_step_impl<float>(c, tokens, kv, logits, next_tokens, layer_inputs, s, nullptr, paged);
     };
     if (!logits && next_tokens && !c->logits_int) {  // allocate outside any capture
         int rc = dev_alloc(&c->logits_int, (size_t)c->d.max_batch * c->d.vocab);
@@ -1182,7 +1242,8 @@ int first_decode_step(first_ctx* c, const int32_t* tokens, const first_kv_cache*
     key.push_back(kv->slab_off); key.push_back(kv->slab_cap); key.push_back(kv->len); key.push_back(kv->pos);
     key.push_back(reinterpret_cast<const void*>(static_cast<uintptr_t>(kv->cap_total)));
     key.push_back(reinterpret_cast<const void*>(static_cast<uintptr_t>(kv->per_layer)));
-    if (kv->per_layer)
+    key.push_back(paged ? view.pages : nullptr);
+    if (kv->per_layer && !paged)
         for (int l = 0; l < c->d.n_layers; ++l)
             key.push_back(reinterpret_cast<const void*>(static_cast<uintptr_t>(kv->cap_total_l[l])));
     key.push_back(reinterpret_cast<const void*>(static_cast<uintptr_t>(c->plan_version)));  // options, sampling
@@ -1449,6 +1510,18 @@ int first_set_adapters(first_ctx* c, const first_adapters* ad) {
     c->ad_scales = ad ? ad->scales : nullptr;
     c->ad_seq = ad ? ad->seq_adapter : nullptr;
     c->plan_version += 1;  // cached step graphs were recorded with the previous adapters
+    return FIRST_OK;
+}
+
+int first_set_pages(first_ctx* c, first_pages* pages) {
+    if (!c) return FIRST_E_ARG;
+    if (pages) {
+        const PagedView v = paged_view(pages);
+        if (v.layers[0].n_kv_heads != c->d.n_kv_heads || v.layers[0].head_dim != c->d.head_dim) return FIRST_E_SHAPE;
+        if (v.B > c->d.max_batch) return FIRST_E_CAPACITY;
+    }
+    c->pages = pages;
+    c->plan_version += 1;  // (recorded step graphs hold the caches' addresses)
     return FIRST_OK;
 }
 

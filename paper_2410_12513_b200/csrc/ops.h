@@ -66,6 +66,8 @@ struct Seqs8 {
     int64_t width = 0;
     const int32_t *len = nullptr, *cu = nullptr;
     int B = 0, total = 0, max_new = 1;
+    int each = 1;                    // without cu: new tokens of every sequence
+    const int64_t* row_off = nullptr;  // dev, or NULL: the sequence's rows start that much later (one sequence alone)
     const int32_t *idx = nullptr, *m_dev = nullptr;
     uint32_t* flags = nullptr;       // or NULL
     const float2* cs = nullptr;      // [.][hd/2] by sequence: rotate q and k on the way (the step), or NULL
