@@ -156,7 +156,7 @@ def lib():
         L.first_attn8.argtypes = [cache8, p, i64, i64, i32, i32, C.c_float, p, i32, p, i32, p, i32, i32, p, i64, i64, p, i64, p, p]
         L.first_attn8_workspace.argtypes = [cache8, i32, i32, i32, i32, i32, i32]
         L.first_attn8_workspace.restype = i64
-        L.first_copy_pages.argtypes = [cache8, i32, p, i64, p, p]
+        L.first_copy_pages.argtypes = [p, i32, p, i64, p, p]
         L.first_verify.argtypes = [p, i64, i64, p, i64, i64, i32, p, i32, i32, i32, p, p, p, p, p, p]
         for name in ("first_pages_create", "first_pages_destroy", "first_pages_join", "first_pages_fork", "first_pages_extend",
                      "first_pages_trim", "first_pages_leave", "first_pages_commit", "first_pages_compact", "first_pages_kv",
@@ -698,10 +698,12 @@ class Cache8:
         self.c = Cache8C(formats[k.dtype], n, heads, page, hd, k.data_ptr(), v.data_ptr(),
                          _on(k_scale, torch.float32, n * heads, "k_scale", self.device),
                          _on(v_scale, torch.float32, n * heads, "v_scale", self.device))
-        self.ref = C.byref(self.c)
+        self.ref, self.raw = C.byref(self.c), bytes(self.c)
+        self.heads, self.head_dim = heads, hd
+        self.sizes = (formats[k.dtype], n, heads, page, hd)
 
 
-def _batch8(cache, dev, pages, len_, cu, total):
+def _batch8(cache, dev, pages, len_, cu):
     """(cu, pages, width, len, sequences) of a call on an 8-bit cache."""
     if cache.device != dev:
         raise ValueError("the cache is on another device")
@@ -712,17 +714,18 @@ def _batch8(cache, dev, pages, len_, cu, total):
             _on(len_, torch.int32, B, "len", dev), B)
 
 
-def _flags_on(flags, dev):
-    return _on(flags, torch.int32, 1, "flags", dev)
-
-
-def _kv_rows(cache, k, v):
-    _heads_of(k, "k")
-    _heads_of(v, "v")
-    if k.shape != v.shape or k.dtype is not v.dtype or k.get_device() != v.get_device():
-        raise ValueError("k and v must be alike")
-    if k.shape[1] != cache.c.n_kv_heads or k.shape[2] != cache.c.head_dim:
+def _kv_rows(cache, k, v, dev):
+    """(rows, strides of k, strides of v, dtype code) of two tensors [rows][Hkv][hd].  (Sizes and strides are fetched once: the
+    checks of a small call take as long as the call.)"""
+    shape, ks, vs = k.shape, k.stride(), v.stride()
+    if len(shape) != 3 or v.shape != shape or k.dtype is not v.dtype or v.get_device() != dev:
+        raise ValueError("k and v must be [rows][heads][head_dim], alike, on one device")
+    rows, heads, hd = shape
+    if (ks[2] != 1 or vs[2] != 1) and hd > 1:
+        raise ValueError("k and v must have adjacent elements in a head")
+    if heads != cache.heads or hd != cache.head_dim:
         raise ValueError("k and v must have the cache's heads and head size")
+    return rows, ks, vs, _code(k, "k")
 
 
 def first_append8(k, v, cache, pages, len, cu_new=None, max_new=1, flags=None, stream=None):
@@ -730,12 +733,10 @@ def first_append8(k, v, cache, pages, len, cu_new=None, max_new=1, flags=None, s
     CUDA int32 [B][n] of page ids; len CUDA int32 [B], tokens before the new ones; cu_new CUDA int32 [B+1], rows of each sequence (None:
     one row each); max_new: most new tokens of a sequence; flags CUDA int32 [1] or None."""
     dev = _device_of(k, "k")
-    _kv_rows(cache, k, v)
-    total = k.shape[0]
-    cu, pp, width, lp, B = _batch8(cache, dev, pages, len, cu_new, total)
-    ks, vs = k.stride(), v.stride()
-    rc = lib().first_append8(cache.ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], _code(k, "k"), cu, total, pp,
-                             width, lp, B, max_new, _flags_on(flags, dev), _raw_stream(stream, dev))
+    total, ks, vs, code = _kv_rows(cache, k, v, dev)
+    cu, pp, width, lp, B = _batch8(cache, dev, pages, len, cu_new)
+    rc = lib().first_append8(cache.ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], code, cu, total, pp, width, lp, B,
+                             max_new, _on(flags, torch.int32, 1, "flags", dev), _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_append8")
 
@@ -743,14 +744,17 @@ def first_append8(k, v, cache, pages, len, cu_new=None, max_new=1, flags=None, s
 def first_read8(cache, pages, start, k, v, cu=None, max_rows=1, flags=None, stream=None):
     """Writes the values at positions start[b] .. of every sequence to rows cu[b] .. cu[b+1]-1 of k and v (see first.h)."""
     dev = _device_of(k, "k")
-    _kv_rows(cache, k, v)
-    total = k.shape[0]
-    cp, pp, width, sp, B = _batch8(cache, dev, pages, start, cu, total)
-    ks, vs = k.stride(), v.stride()
-    rc = lib().first_read8(cache.ref, pp, width, sp, cp, B, total, max_rows, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0],
-                           vs[1], _code(k, "k"), _flags_on(flags, dev), _raw_stream(stream, dev))
+    total, ks, vs, code = _kv_rows(cache, k, v, dev)
+    cp, pp, width, sp, B = _batch8(cache, dev, pages, start, cu)
+    rc = lib().first_read8(cache.ref, pp, width, sp, cp, B, total, max_rows, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+                           code, _on(flags, torch.int32, 1, "flags", dev), _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_read8")
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace8(sizes, n_q_heads, code, total, width, B, max_new):
+    return lib().first_attn8_workspace(C.byref(Cache8C(*sizes, 16, 16, 16, 16)), n_q_heads, code, total, width, B, max_new)
 
 
 def first_attn8(q, cache, pages, len, out, scale=None, cu_new=None, max_new=1, workspace=None, flags=None, stream=None):
@@ -758,27 +762,28 @@ def first_attn8(q, cache, pages, len, out, scale=None, cu_new=None, max_new=1, w
     like q.  len, cu_new, max_new as in first_append8.  scale None: 1/sqrt(hd).  workspace: a CUDA tensor to keep unfinished
     results in (first_attn8_workspace bytes), None: one is taken from torch's allocator where there is a use for it."""
     dev = _device_of(q, "q")
-    _heads_of(q, "q")
-    _heads_of(out, "out")
-    total, hq, hd = q.shape
-    if out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != dev:
+    shape, qs, os_ = q.shape, q.stride(), out.stride()
+    if out.shape != shape or out.dtype is not q.dtype or out.get_device() != dev:
         raise ValueError("out must be like q")
-    if hd != cache.c.head_dim:
+    if q.dim() != 3 or ((qs[2] != 1 or os_[2] != 1) and shape[2] > 1):
+        raise ValueError("q and out must be [rows][heads][head_dim] with adjacent elements in a head")
+    total, hq, hd = shape
+    if hd != cache.head_dim:
         raise ValueError("q must have the cache's head size")
-    cu, pp, width, lp, B = _batch8(cache, dev, pages, len, cu_new, total)
-    qs, os_ = q.stride(), out.stride()
-    code = _code(q, "q")
+    cu, pp, width, lp, B = _batch8(cache, dev, pages, len, cu_new)
+    code, room = _code(q, "q"), 0
     if workspace is None:
-        need = lib().first_attn8_workspace(cache.ref, hq, code, total, width, B, max_new)
-        if need:
+        room = _workspace8(cache.sizes, hq, code, total, width, B, max_new)
+        if room:
             with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    elif workspace.get_device() != dev or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous, on q's device")
-    room = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib().first_attn8(cache.ref, q.data_ptr(), qs[0], qs[1], hq, code, hd ** -0.5 if scale is None else scale, cu,
-                           total, pp, width, lp, B, max_new, out.data_ptr(), os_[0], os_[1],
-                           workspace.data_ptr() if room else None, room, _flags_on(flags, dev), _raw_stream(stream, dev))
+                workspace = torch.empty(room, dtype=torch.uint8, device=q.device)
+    else:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous, on q's device")
+        room = workspace.numel() * workspace.element_size()
+    rc = lib().first_attn8(cache.ref, q.data_ptr(), qs[0], qs[1], hq, code, hd ** -0.5 if scale is None else scale, cu, total, pp, width,
+                           lp, B, max_new, out.data_ptr(), os_[0], os_[1], workspace.data_ptr() if room else None, room,
+                           _on(flags, torch.int32, 1, "flags", dev), _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_attn8")
 
@@ -788,11 +793,12 @@ def first_copy_pages(caches, moves, flags=None, stream=None):
     dev = _device_of(moves, "moves")
     if moves.dim() != 2 or moves.shape[1] != 3:
         raise ValueError("moves must be [n][3]")
-    if any(c.device != dev for c in caches):
+    here = [c.raw for c in caches if c.device == dev]
+    if len(here) != len(caches):
         raise ValueError("the caches are on another device")
-    arr = (Cache8C * len(caches))(*[c.c for c in caches])
+    arr = b"".join(here)  # (an array of first_cache8)
     rc = lib().first_copy_pages(arr, len(caches), _on(moves, torch.int32, moves.numel(), "moves", dev), moves.shape[0],
-                                _flags_on(flags, dev), _raw_stream(stream, dev))
+                                _on(flags, torch.int32, 1, "flags", dev), _raw_stream(stream, dev))
     if rc:
         raise FirstError(rc, "first_copy_pages")
 
@@ -804,7 +810,8 @@ def first_verify(target, drafted, uniforms, draws, tokens, accepted, draft=None,
     Output: tokens CUDA int32 [B][n+1], accepted CUDA int32 [B]."""
     dev = _device_of(target, "target")
     f32, i32 = torch.float32, torch.int32
-    if target.dim() != 3 or (target.shape[2] > 1 and target.stride(2) != 1):
+    ts = target.stride()
+    if len(ts) != 3 or (ts[2] != 1 and target.shape[2] > 1):
         raise ValueError("target must be [sequences][drafts + 1][vocab] with adjacent elements in a row")
     if target.dtype is not f32:
         raise TypeError("target must be float32")
@@ -816,12 +823,12 @@ def first_verify(target, drafted, uniforms, draws, tokens, accepted, draft=None,
     if draft is not None:
         if draft.dtype is not f32 or draft.get_device() != dev:
             raise TypeError("draft must be float32, on target's device")
-        if tuple(draft.shape) != (B, n, V) or (V > 1 and draft.stride(2) != 1):
+        ds = draft.stride()
+        if draft.shape != (B, n, V) or (ds[2] != 1 and V > 1):
             raise ValueError("draft must be [sequences][drafts][vocab] with adjacent elements in a row")
-        dp, ds = draft.data_ptr(), draft.stride()
+        dp = draft.data_ptr()
     if draws is None or tokens is None or accepted is None:
         raise TypeError("draws, tokens and accepted are required")
-    ts = target.stride()
     rc = lib().first_verify(target.data_ptr(), ts[0], ts[1], dp, ds[0], ds[1], bool(probs), _on(drafted, i32, B * n, "drafted", dev),
                             B, n, V, _on(temperature, f32, B, "temperature", dev), _on(uniforms, f32, B * n, "uniforms", dev),
                             _on(draws, f32, B, "draws", dev), _on(tokens, i32, B * rows, "tokens", dev),

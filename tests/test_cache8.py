@@ -86,7 +86,7 @@ def test_copies_refuse():
         for i, kv in enumerate(layers):
             for name, value in kv:
                 setattr(arr[i], name, value)
-        return L.first_copy_pages(arr, len(layers) if n is None else n, moves, count, None, None)
+        return L.first_copy_pages(C.byref(arr), len(layers) if n is None else n, moves, count, None, None)
     assert call(count=0) == OK and call(count=0, moves=None) == OK
     assert call(n=0) == ARG and call(moves=None) == ARG and call(count=-1) == ARG
     assert L.first_copy_pages(None, 1, P, 1, None, None) == ARG
