@@ -109,17 +109,17 @@ __device__ __forceinline__ void put(const Attn8Args& p, int64_t row, int head, i
 __device__ __forceinline__ int64_t part_of(int b, int h, int r, int rows, int H) { return ((int64_t)b * H + h) * rows + r; }
 
 template <int NT>
-constexpr int kGroups = NT <= 2 ? 2 : 1;  // groups of 16 tokens a step
+constexpr int kGroups = NT <= 3 ? 2 : 1;  // groups of 16 tokens a step
 template <int NT>
 constexpr int kRing = 4 / kGroups<NT>;    // steps that a warp has room for: one in use, the others on their way
 template <int HD, int NT>
 constexpr int kStepBytes = 2 * 16 * kGroups<NT> * HD;
 
 // Integers: a query element in parts of 8 bits, base 256, for products with K as it is: as a multiple of some 2^-14 of its
-// row's largest (2 parts; bfloat16) or 2^-22 (3; float32).  E4M3 has no products of its own on this path, K becomes halves
+// row's largest (2 parts; bfloat16) or 2^-30 (4; float32).  E4M3 has no products of its own on this path, K becomes halves
 // (exactly); a query row is scaled by a power of two into their range and takes one (bfloat16's 8 bits fit) or, PER 1, two (hi + lo).
 template <bool E4M3, bool F32>
-constexpr int kParts = E4M3 ? 2 : F32 ? 3 : 2;
+constexpr int kParts = E4M3 ? 2 : F32 ? 4 : 2;
 
 // A cluster takes a tile of query rows (tokens x query heads of a KV head) of one sequence; its CTAs and their warps take
 // its tokens in turns and join (maximum, sum, output) at the end, over shared memory and then over the cluster's.  The
@@ -544,49 +544,63 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
                     pb[u][n][x] = transpose8(*reinterpret_cast<uint32_t*>(&v));
                 }
         }
-        // ---- O += V' P, two steps of 16 of hd at a time
+        // ---- O += V' P, two steps of 16 of hd at a time.  float32: a step's products are added up apart (the tensor cores cut what they add
+        // to a long sum: 1.0e-6 of the result against 3e-7 at 8192 tokens); so are, scaled, those of a page whose scale is far below the largest.
+        auto turned = [&](int u, int w, uint32_t (&x)[2][4]) {
+            uint32_t v[4];  // [step][tokens 0.. | 8..]
+            if (u == 0 && kAhead) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+                for (int y = 0; y < 4; ++y) v[y] = v0[kAhead ? w / 2 : 0][y];
+            } else {
+                blocks_turned(v_in + u * 16 * HD + k_off[w / 2], v);
+            }
+            if (special) {  // what lies behind the last token, or on no page, is not a value
 #pragma unroll
-            for (int w = 0; w < kSteps; w += 2) {
-                uint32_t v[4];  // [step][tokens 0.. | 8..]
-                if (u == 0 && kAhead) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) v[x] = v0[kAhead ? w / 2 : 0][x];
-                } else {
-                    blocks_turned(v_in + u * 16 * HD + k_off[w / 2], v);
+                for (int y = 0; y < 4; ++y) {
+                    const int t = tb + 16 * u + 2 * c + 8 * (y & 1);
+                    if (!(have >> u & 1u) || t >= end) v[y] = 0u;
+                    else if (t + 1 >= end) v[y] &= 0xffffu;
                 }
-                if (special) {  // what lies behind the last token, or on no page, is not a value
+            }
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int t = tb + 16 * u + 2 * c + 8 * (x & 1);
-                        if (!(have >> u & 1u) || t >= end) v[x] = 0u;
-                        else if (t + 1 >= end) v[x] &= 0xffffu;
-                    }
-                }
-                uint32_t x[2][4];
+            for (int y = 0; y < 2; ++y) {
+                v_halves<E4M3>(v[2 * y], x[y][0], x[y][1]);
+                v_halves<E4M3>(v[2 * y + 1], x[y][2], x[y][3]);
+            }
+        };
+        if (!F32 && !apart) {
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    v_halves<E4M3>(v[2 * y], x[y][0], x[y][1]);
-                    v_halves<E4M3>(v[2 * y + 1], x[y][2], x[y][3]);
-                }
-                if (!apart) {
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int w = 0; w < kSteps; w += 2) {
+                    uint32_t x[2][4];
+                    turned(u, w, x);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int y = 0; y < 2; ++y) mma(o[n][w + y], x[y][0], x[y][1], x[y][2], x[y][3], pb[u][n][0], pb[u][n][1]);
-                } else {
+                }
+        } else {
+#pragma unroll
+            for (int w = 0; w < kSteps; w += 2) {
+                float t[NT][2][4];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    uint32_t x[2][4];
+                    turned(u, w, x);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
-                            float t[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma(t, x[y][0], x[y][1], x[y][2], x[y][3], pb[u][n][0], pb[u][n][1]);
+                            if (u == 0 || apart) t[n][y][0] = t[n][y][1] = t[n][y][2] = t[n][y][3] = 0.f;
+                            mma(t[n][y], x[y][0], x[y][1], x[y][2], x[y][3], pb[u][n][0], pb[u][n][1]);
+                            if (apart || u == U - 1)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) o[n][w + y][e] = fmaf(t[e], vr[u], o[n][w + y][e]);
+                                for (int e = 0; e < 4; ++e) o[n][w + y][e] = apart ? fmaf(t[n][y][e], vr[u], o[n][w + y][e]) : o[n][w + y][e] + t[n][y][e];
                         }
                 }
             }
+        }
         __syncwarp();  // (the step's room is free)
     }
     __syncthreads();  // (the ring becomes O's)
