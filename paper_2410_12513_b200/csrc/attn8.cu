@@ -151,7 +151,8 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
     __shared__ float s_rs[kRows], s_inv[kRows];
     __shared__ int s_len[kMaxSorted], s_mine;
     const Stamp stamp_guard(p.s.stamp);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    const int tid = threadIdx.x, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // (so that the compiler knows it, and what hangs on it, as the warp's)
     const int rank = blockIdx.x % S, z_of = blockIdx.x / S % Z, h = blockIdx.x / (S * Z);  // a sequence and head has Z clusters
     const uint32_t aligned = ((uint32_t)__cvta_generic_to_shared(s_dynamic) + 1023u) & ~1023u;
     float* const s_part = reinterpret_cast<float*>(s_dynamic + (aligned - (uint32_t)__cvta_generic_to_shared(s_dynamic)));

@@ -51,17 +51,30 @@ __device__ __forceinline__ float weight32(float x, float top, const Scale& sc) {
 }
 // The same in 64 bits, to 2^-39: which token a draw falls on hangs on the sums of these.  2^(k / 32) from a table for the nearest k, the
 // rest by its Taylor series: |g| <= ln 2 / 64, g^5 / 120 < 2^-39.
-__device__ __forceinline__ double weight64(float x, float top, const Scale& sc, const double* pow32) {
+template <typename Table>
+__device__ __forceinline__ double weight64(float x, float top, const Scale& sc, Table&& pow32) {
     x = logit(x);
     const double a = ((double)x - (double)top) * sc.steps;
-    if (!(a > -32000.0)) return 0.0;
     constexpr double kMagic = 6755399441055744.0;  // 1.5 2^52: adding it leaves the nearest whole number in the low bits
     const double m = a + kMagic, g = (a - (m - kMagic)) * (0.69314718055994530942 / 32);
     const int k = __double2loint(m);
-    const double s = fma(fma(fma(fma(g, 1.0 / 24, 1.0 / 6), g, 0.5), g, 1.0), g, 1.0) * pow32[k & 31];
-    return __hiloint2double(__double2hiint(s) + (k >> 5) * (1 << 20), __double2loint(s));
+    const double s = fma(fma(fma(fma(g, 1.0 / 24, 1.0 / 6), g, 0.5), g, 1.0), g, 1.0) * pow32(k & 31);
+    return a > -32000.0 ? __hiloint2double(__double2hiint(s) + (k >> 5) * (1 << 20), __double2loint(s)) : 0.0;
 }
 
+__device__ __forceinline__ double warp_sum64(double x) {
+#pragma unroll 1
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+__device__ __forceinline__ double warp_scan64(double x) {
+#pragma unroll 1
+    for (int o = 1; o < 32; o *= 2) {
+        const double v = __shfl_up_sync(0xffffffffu, x, o);
+        if ((int)(threadIdx.x & 31) >= o) x += v;
+    }
+    return x;
+}
 __device__ __forceinline__ Part warp_join(Part p, const Scale& sc, bool greedy) {
     const float top = warp_max(p.top);
     if (greedy) p.at = __reduce_min_sync(0xffffffffu, p.top == top ? p.at : 0x7fffffff);
@@ -160,7 +173,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
     __shared__ uint64_t s_bar[2 * kRing];  // pieces that are there, pieces that have been read
     __shared__ int s_gave;
     cg::cluster_group cluster = cg::this_cluster();
-    const int C = p.C, b = blockIdx.x / C, rank = blockIdx.x % C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = p.C, b = blockIdx.x / C, rank = blockIdx.x % C, tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // (so that the compiler knows it as the warp's)
     const float temp = p.temperature ? p.temperature[b] : 1.f;
     const bool greedy = !p.probs && !(temp > 0.f);
     // (at most 32 drafts: a lane each; the first that is no token ends them)
@@ -170,7 +183,11 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
     const uint32_t closed = ~__ballot_sync(0xffffffffu, mine >= 0 && mine < p.V);
     const int valid = closed ? __ffs(closed) - 1 : 32;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring), bars = (uint32_t)__cvta_generic_to_shared(s_bar);
-    if (tid < 32) s_pow[tid] = exp2((double)tid / 32);
+    const double my_pow = exp2((double)lane / 32);
+    if (tid < 32) s_pow[tid] = my_pow;
+    // 2^(k/32): from shared memory, or, where the whole warp asks, from its lanes (random places of a small table meet in its banks)
+    auto from_table = [&](int k) { return s_pow[k]; };
+    auto from_lanes = [&](int k) { return __shfl_sync(0xffffffffu, my_pow, k); };
     if (tid == 32) {
         s_gave = 0;
         for (int i = 0; i < 2 * kRing; ++i)
@@ -260,7 +277,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
                     at = min(at, __shfl_xor_sync(0xffffffffu, at, o));
                 }
                 // u q < p with both sums multiplied out
-                const double w = sum > 0.f && drafts ? weight64(own[side], top, sc, s_pow) : 0.0;
+                const double w = sum > 0.f && drafts ? weight64(own[side], top, sc, from_table) : 0.0;
                 const float other = __shfl_down_sync(0xffffffffu, sum, 16);
                 const double w_q = __shfl_down_sync(0xffffffffu, w, 16);
                 const float top_q = __shfl_down_sync(0xffffffffu, top, 16);
@@ -297,8 +314,8 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
         const int skip = refused && !p.draft ? __shfl_sync(0xffffffffu, mine, j & 31) : -1;
         const float tp = p.probs ? 0.f : s_top[0], td = p.probs ? 0.f : s_top[1];
         const bool none = !p.probs && tp == -INFINITY;
-        auto of_p = [&](float x) { return p.probs ? fmax((double)x, 0.0) : weight64(x, tp, sc, s_pow); };
-        auto of_q = [&](float x) { return p.probs ? fmax((double)x, 0.0) : td > -INFINITY ? weight64(x, td, sc, s_pow) : 0.0; };
+        auto of_p = [&](float x, auto& pow32) { return p.probs ? fmax((double)x, 0.0) : weight64(x, tp, sc, pow32); };
+        auto of_q = [&](float x, auto& pow32) { return p.probs ? fmax((double)x, 0.0) : td > -INFINITY ? weight64(x, td, sc, pow32) : 0.0; };
         // p - ratio q, ratio = sum of p / sum of q.  Which tokens have something left hardly hangs on it: those of a ratio good to float32
         // are taken, whose sums, p's and q's apart, then give what is left with the 64-bit ratio (a token on the wrong side
         // adds 2^-20 of its own weight at most; if no more than 2^-10 of all is left, they are taken anew by that ratio).
@@ -308,94 +325,74 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
         for (int again = 0; again < 2 && !none;) {  // (a second time, from p itself, if nothing is left of p - q)
             const bool two = d && !again;
             // every warp of the cluster sums a run of tokens
+            constexpr int kDeep = 4;
             const int span = ((hi - lo + kWarps - 1) / kWarps + 31) & ~31, w0 = min(lo + warp * span, hi), w1 = min(w0 + span, hi);
-            double all_p = 0.0, all_q = 0.0, left_p = 0.0, left_q = 0.0;
-            constexpr int kDeep = 8;
-            for (int e0 = w0 + lane; e0 < w1; e0 += 32 * kDeep) {
+            double sums[4] = {0.0, 0.0, 0.0, 0.0};  // p and q of the tokens that have something left, of all
+#pragma unroll 1
+            for (int base = w0; base < w1; base += 32 * kDeep) {
+                const int e0 = base + lane;
                 float x[kDeep], y[kDeep];
 #pragma unroll
                 for (int i = 0; i < kDeep; ++i) {
                     const int e = e0 + 32 * i;
                     x[i] = e < w1 ? __ldg(t + e) : p.probs ? 0.f : -INFINITY;
-                    if (two) y[i] = e < w1 ? __ldg(d + e) : p.probs ? 0.f : -INFINITY;
+                    y[i] = two && e < w1 ? __ldg(d + e) : p.probs ? 0.f : -INFINITY;
                 }
 #pragma unroll
                 for (int i = 0; i < kDeep; ++i) {
-                    const double vx = of_p(x[i]);
-                    if (two) {
-                        const double vy = of_q(y[i]);
-                        all_p += vx;
-                        all_q += vy;
-                        if (vx > rough * vy) { left_p += vx; left_q += vy; }
-                    } else if (e0 + 32 * i != skip || again) {
-                        left_p += vx;
+                    const double vx = of_p(x[i], from_lanes), vy = two ? of_q(y[i], from_lanes) : 0.0;
+                    sums[2] += vx;
+                    sums[3] += vy;
+                    if (two ? vx > rough * vy : e0 + 32 * i != skip || again) {
+                        sums[0] += vx;
+                        sums[1] += vy;
                     }
                 }
             }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                left_p += __shfl_xor_sync(0xffffffffu, left_p, o);
-                if (two) {
-                    left_q += __shfl_xor_sync(0xffffffffu, left_q, o);
-                    all_p += __shfl_xor_sync(0xffffffffu, all_p, o);
-                    all_q += __shfl_xor_sync(0xffffffffu, all_q, o);
-                }
-            }
+            for (int k = 0; k < 4; ++k) sums[k] = warp_sum64(sums[k]);
             __syncthreads();
-            if (lane == 0 && warp < kWarps) { s_sum[0][warp] = left_p; s_sum[1][warp] = left_q; s_sum[2][warp] = all_p; s_sum[3][warp] = all_q; }
+            if (lane == 0 && warp < kWarps)
+                for (int k = 0; k < 4; ++k) s_sum[k][warp] = sums[k];
             cluster.sync();
+            const int each_run = (C * kWarps + 31) / 32;
             for (int r = tid; r < C * kWarps; r += kThreads + 32) {
                 const double* from = cluster.map_shared_rank(&s_sum[0][0], r / kWarps) + r % kWarps;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) s_all[k][r] = from[k * kWarps];
+                for (int k = 0; k < 4; ++k) s_all[k][r % each_run * 32 + r / each_run] = from[k * kWarps];  // (a lane's runs a row apart: other banks)
             }
             __syncthreads();
-            // which run: the last one that is not empty and starts at or before the target, a lane some neighbouring runs
+            // which run: the last one that is not empty and starts at or before the target, a lane some neighbouring runs.  (What runs
+            // once is kept short: fetching instructions is what takes the time here.)
             if (warp == 0) {
-                const int n = C * kWarps, each = (n + 31) / 32;
-                constexpr int kMost = kMaxCluster * kWarps / 32;
-                double x[kMost], y[kMost], part = 0.0;
+                const int n = max(0, min(each_run, C * kWarps - lane * each_run));  // of the lane
                 double zp = 0.0, zq = 0.0;
-#pragma unroll
-                for (int i = 0; i < kMost; ++i) {
-                    const int r = lane * each + i;
-                    x[i] = y[i] = 0.0;
-                    if (i < each && r < n) {
-                        x[i] = s_all[0][r];
-                        if (two) {
-                            y[i] = s_all[1][r];
-                            zp += s_all[2][r];
-                            zq += s_all[3][r];
-                        }
-                    }
-                }
                 if (two && !p.probs) {
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) {
-                        zp += __shfl_xor_sync(0xffffffffu, zp, o);
-                        zq += __shfl_xor_sync(0xffffffffu, zq, o);
+#pragma unroll 1
+                    for (int r = 0; r < n; ++r) {
+                        zp += s_all[2][r * 32 + lane];
+                        zq += s_all[3][r * 32 + lane];
                     }
+                    zp = warp_sum64(zp);
+                    zq = warp_sum64(zq);
                     ratio = zq > 0.0 ? zp / zq : 0.0;
                 }
-#pragma unroll
-                for (int i = 0; i < kMost; ++i) {
-                    if (two) x[i] = fmax(x[i] - ratio * y[i], 0.0);
-                    part += x[i];
-                }
-                double run = part;
-#pragma unroll
-                for (int o = 1; o < 32; o *= 2) {
-                    const double v = __shfl_up_sync(0xffffffffu, run, o);
-                    if (lane >= o) run += v;
-                }
+                auto left = [&](int r) {
+                    const double x = s_all[0][r * 32 + lane];
+                    return two ? fmax(x - ratio * s_all[1][r * 32 + lane], 0.0) : x;
+                };
+                double part = 0.0;
+#pragma unroll 1
+                for (int r = 0; r < n; ++r) part += left(r);
+                const double run = warp_scan64(part);
                 const double total = __shfl_sync(0xffffffffu, run, 31), want = draw(p.draws[b]) * total;
-                double before = __shfl_up_sync(0xffffffffu, run, 1), start = 0.0;
-                if (lane == 0) before = 0.0;
+                double before = run - part, start = 0.0;
                 int found = -1;
-#pragma unroll
-                for (int i = 0; i < kMost; ++i) {
-                    if (x[i] > 0.0 && before <= want) { found = lane * each + i; start = before; }
-                    before += x[i];
+#pragma unroll 1
+                for (int r = 0; r < n; ++r) {
+                    const double x = left(r);
+                    if (x > 0.0 && before <= want) { found = lane * each_run + r; start = before; }
+                    before += x;
                 }
                 const int last = __reduce_max_sync(0xffffffffu, found);
                 if (last >= 0 && found == last) s_seg = want - start;
@@ -419,26 +416,24 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
                     const int each = (span + kThreads - 1) / kThreads;
                     const int e0 = min(f0 + tid * each, f1), e1 = min(e0 + each, f1);
                     auto left = [&](int e) {
-                        const double x = of_p(__ldg(t + e));
+                        const double x = of_p(__ldg(t + e), from_table);
                         if (!two) return e == skip && !again ? 0.0 : x;
-                        const double y = of_q(__ldg(d + e));
+                        const double y = of_q(__ldg(d + e), from_table);
                         return x > rough * y ? fmax(x - ratio * y, 0.0) : 0.0;
                     };
                     double mine64 = 0.0;
+#pragma unroll 1
                     for (int e = e0; e < e1; ++e) mine64 += left(e);
-                    double run = mine64;
-#pragma unroll
-                    for (int o = 1; o < 32; o *= 2) {
-                        const double v = __shfl_up_sync(0xffffffffu, run, o);
-                        if (lane >= o) run += v;
-                    }
+                    const double run = warp_scan64(mine64);
                     __syncthreads();
                     if (lane == 31 && warp < kWarps) s_run[warp] = run;
                     if (tid == 0) s_at = -1, s_hit = 0x7fffffff;
                     __syncthreads();
                     double cum = run - mine64;
+#pragma unroll 1
                     for (int w = 0; w < warp; ++w) cum += s_run[w];
                     int hit = 0x7fffffff, last = -1;
+#pragma unroll 1
                     for (int e = e0; e < e1; ++e) {
                         const double x = left(e);
                         cum += x;
