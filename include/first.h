@@ -485,7 +485,7 @@ int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
  * is at t*token_stride + head*head_stride (elements), head_dim adjacent elements, float32 or bfloat16 (dtype).
  * Errors that only the device sees set bits in *flags (dev uint32 or NULL; OR-ed in, never cleared): FIRST_FLAG_BAD_SEQ_TABLE
  * (cu_new or len cannot be, or more than max_new new tokens: that sequence is left out), FIRST_FLAG_BAD_PAGE (an id outside
- * the cache: counts as -1), FIRST_FLAG_KV_FULL (a new token without a page is not stored).  No scratch, no wait, one launch.
+ * the cache: counts as -1), FIRST_FLAG_KV_FULL (a new token without a page is not stored).  No scratch, no wait, one launch (first_attn8 over a workspace: two).
  *
  * first_append8  stores new keys and values.  For every page and head that gains tokens: scale = max(its scale, if the page held
  *                tokens of the sequence before, else 0; largest finite magnitude of the new ones * 1/127 (E4M3: 1/448)), in
@@ -497,8 +497,11 @@ int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
  *                out = sum_t softmax_t(scale * q . k_t) v_t, query head h with KV head h / (n_q_heads / n_kv_heads).
  *                Positions without a page are not there; a row that sees nothing gives zeros.  Products and sums are
  *                float32; weights have 11 bits of mantissa with bfloat16 q and 22 with float32 q; out is rounded once.  The
- *                result is the same in every run and depends on nothing but the sequence itself and the launch's sizes (B, max_new, max_pages).  Meant for one token a sequence and
- *                for drafts under verification: the cache is read once for every 32 (float32: 16) query rows of a KV head.
+ *                result is the same in every run and depends on nothing but the sequence itself and the launch's sizes (B, max_new, max_pages).  Meant
+ *                for one token a sequence and for drafts under verification: the cache is read once for every 32 (float32: 16) query rows of a KV
+ *                head.  workspace (dev, 4-byte aligned, or NULL): few long sequences are cut among more of the GPU if it has
+ *                first_attn8_workspace bytes (host; 0: there is no use for one), and then take a second launch.  Calls that may overlap need workspaces of their own.
+ *                A bounded wait that gives up sets FIRST_FLAG_WAIT_EXPIRED; the result is then undefined.
  * first_copy_pages  copies pages (keys, values, scales) within the layers' caches: moves dev int32 [n_moves][3] of (layer,
  *                from, to).  All layers alike in format and sizes.  No page may be written twice, nor be both read and
  *                written.  A move outside the caches is left out (FIRST_FLAG_BAD_PAGE).
@@ -594,8 +597,9 @@ int first_set_pages(first_ctx *ctx, first_pages *pages);
  *   tokens    dev int32 [B][n_draft+1]: the accepted drafts, the new token (-1 if the row has no candidate), then -1
  *   accepted  dev int32 [B]: how many drafts were accepted
  * Sums that decide which token a draw falls on are formed in 64 bits; acceptance has float32's precision.  The result is the same in
- * every run.  Stateless, no scratch, no wait, one launch; B = 0 does nothing.
- * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides below vocab), FIRST_E_UNSUPPORTED (n_draft > FIRST_VERIFY_MAX_DRAFTS, vocab >
+ * every run.  (Rows are fetched in whole 16 bytes: up to 12 bytes before and behind a row are read, never used.)  Stateless, no scratch, no
+ * wait, one launch; B = 0 does nothing.  accepted[b] = -1: a bounded wait inside the kernel gave up, the sequence's result is void.
+ * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides below vocab), FIRST_E_UNSUPPORTED (alignment, n_draft > FIRST_VERIFY_MAX_DRAFTS, vocab >
  * FIRST_SAMPLE_MAX_VOCAB), FIRST_E_CAPACITY, FIRST_E_CUDA. */
 #define FIRST_VERIFY_MAX_DRAFTS 32
 int first_verify(const float *target, int64_t target_seq_stride, int64_t target_row_stride, const float *draft,

@@ -779,10 +779,9 @@ cudaError_t launch(const Attn8Args& a, const Plan& plan, cudaStream_t st, bool p
     constexpr int kRows = NT * 4 * PER;
     constexpr int kSmem = kWarps * std::max(kRows * (HD + 16) * 4, kRing<NT> * kStepBytes<HD, NT>) + 1024;
     auto kern = attn8<HD, NT, PER, F32, E4M3, kWarps>;
-    static const cudaError_t once = [&] {
-        return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    }();
-    if (once != cudaSuccess) return once;
+    static std::atomic<uint64_t> done{0};
+    const cudaError_t ready = allow_launch(kern, kSmem, false, done);
+    if (ready != cudaSuccess) return ready;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(S * Z * a.c.H), (unsigned)a.s.B, (unsigned)(((int64_t)a.s.max_new * a.G + kRows - 1) / kRows));
     cfg.blockDim = dim3(32 * kWarps);

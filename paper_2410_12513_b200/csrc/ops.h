@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "first.h"
 
 namespace first {
@@ -51,6 +53,21 @@ struct SampleArgs {
 };
 constexpr int kSampleMaxVocab = 1 << 19;
 cudaError_t sample_launch(const SampleArgs& a, cudaStream_t st, bool pdl);
+
+// A kernel's limits are a device's: sets its dynamic shared memory (and clusters of more than 8 CTAs) on the current device, once each.  `done`:
+// a bit a device, static beside the kernel.
+template <typename K>
+cudaError_t allow_launch(K kern, int smem, bool large_clusters, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && large_clusters) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
 
 // One layer of a paged 8-bit cache: pages of 2^shift tokens, [n_pages][H][2^shift][hd] bytes, one scale a (page, head).
 struct Cache8 {

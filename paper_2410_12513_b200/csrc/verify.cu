@@ -479,6 +479,7 @@ extern "C" int first_verify(const float* target, int64_t target_seq_stride, int6
     if (!target || !draws || !tokens || !accepted || (n_draft > 0 && (!drafted || !uniforms))) return FIRST_E_ARG;
     if ((n_draft > 0 && target_row_stride < vocab) || (draft && n_draft > 1 && draft_row_stride < vocab)) return FIRST_E_SHAPE;
     if (B > 1 && (target_seq_stride < vocab || (draft && n_draft > 0 && draft_seq_stride < vocab))) return FIRST_E_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(target) | reinterpret_cast<uintptr_t>(draft)) % 4) return FIRST_E_UNSUPPORTED;
     VerifyArgs a{};
     a.target = target; a.draft = n_draft > 0 ? draft : nullptr;
     a.t_seq = target_seq_stride; a.t_row = target_row_stride; a.d_seq = draft_seq_stride; a.d_row = draft_row_stride;
@@ -493,11 +494,8 @@ extern "C" int first_verify(const float* target, int64_t target_seq_stride, int6
     while (a.C < kMaxCluster && (int64_t)B * a.C * 2 <= 2 * kSMs && vocab > 4096 * a.C) a.C *= 2;
     a.R = B <= 8 ? kMaxRound : B <= 24 ? 2 : 1;
     constexpr int kSmem = kRing * kPiece * 4;
-    static const cudaError_t once = [] {
-        const cudaError_t e = cudaFuncSetAttribute(verify_rows, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        return e != cudaSuccess ? e : cudaFuncSetAttribute(verify_rows, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    }();
-    if (once != cudaSuccess) return FIRST_E_CUDA;
+    static std::atomic<uint64_t> done{0};
+    if (allow_launch(verify_rows, kSmem, true, done) != cudaSuccess) return FIRST_E_CUDA;
     if (B > 0x7fffffff / kMaxCluster) return FIRST_E_CAPACITY;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)B * a.C);

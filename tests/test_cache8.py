@@ -107,5 +107,5 @@ def test_verify_refuses():
         assert call(**kw) == ARG, kw
     for kw in ({"ts": 999}, {"tr": 999}, {"ds": 999}, {"dr": 999}, {"ts": -4000}, {"dr": -1}):
         assert call(**kw) == SHAPE, kw
-    for kw in ({"n": 33}, {"V": 524289}):
+    for kw in ({"n": 33}, {"V": 524289}, {"target": P + 2}, {"draft": P + 1}):
         assert call(**kw) == UNSUPPORTED, kw

@@ -323,7 +323,7 @@ ATTN = [  # lengths with the new ones, new ones, KV heads, group, hd, page, layo
     ([100, 1, 64, 65], [1] * 4, 8, 3, 128, 32, "fused"), ([5, 200, 0, 130], [5, 3, 0, 1], 2, 2, 128, 128, "odd"),
     ([40, 600], [8, 6], 1, 8, 128, 16, "heads_first"), ([300, 77], [33, 40], 2, 1, 64, 64, "own"), ([150], [100], 1, 4, 32, 32, "own"),
     ([2500, 3, 900], [2, 2, 2], 4, 8, 64, 64, "fused"), ([129, 128, 127], [1, 2, 4], 2, 5, 128, 128, "own"), ([4096, 5000], [4, 1], 1, 4, 128, 64, "odd"),
-    ([64] * 40, [1] * 40, 8, 4, 128, 64, "own"), ([20], [20], 3, 7, 64, 16, "own")]
+    ([64] * 40, [1] * 40, 8, 4, 128, 64, "own"), ([20], [20], 3, 7, 64, 16, "own"), ([1 + i % 40 for i in range(300)], [1] * 300, 1, 2, 32, 16, "own")]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -398,6 +398,37 @@ def test_attention_over_missing_pages(dtype):
     flags.zero_()
     first_attn8(q.cuda(), cache.c, _dev(pages), _dev(np.array([-1, 2, 2, 2, 2 ** 31 - 1], np.int32)), out, flags=flags)
     assert int(flags) & BAD_TABLE and (out[0] == 5.0).all() and (out[4] == 5.0).all() and (out[2] != 5.0).any()
+
+
+@pytest.mark.parametrize("n", [1, 3])
+@pytest.mark.parametrize("fmt,dtype", [("int8", "f32"), ("e4m3", "bf16")])
+def test_attention_over_a_workspace(fmt, dtype, n):
+    """Few long sequences: cut among more of the GPU where there is room for unfinished results, whatever it holds; without enough
+    room the call does without."""
+    import torch
+    from paper_2410_12513_b200 import first_attn8
+    from paper_2410_12513_b200.binding import _workspace8
+    H, G, hd, page, total = 1, 4, 128, 64, [20000, 9000, 70]
+    rng = np.random.default_rng(n)
+    need = [-(-t // page) for t in total]
+    cache = Cache(n, sum(need), H, page, hd, fmt)
+    cache.fill(n, 0.5)
+    pages = _tables(rng, need, cache.n)
+    q = (torch.randn(3 * n, H * G, hd, generator=torch.Generator().manual_seed(n)) * 2).to(_t(dtype))
+    cu = _dev(np.arange(4, dtype=np.int32) * n)
+    before = _dev(np.array(total, np.int32) - n)
+    room = _workspace8(cache.c.sizes, H * G, 0 if dtype == "f32" else 1, 3 * n, pages.shape[1], 3, n)
+    assert room > 0
+    outs = []
+    for ws in (None, torch.full((room // 4,), math.nan, device="cuda"), torch.empty(2, device="cuda")):
+        out = torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda")
+        first_attn8(q.cuda(), cache.c, _dev(pages), before, out, cu_new=cu, max_new=n, workspace=ws)
+        outs.append(out)
+        for b in range(3):
+            want, size, peak = attention(cache, q[b * n:b * n + n].double().numpy(), pages[b], total[b], n, hd ** -0.5)
+            err = np.abs(out[b * n:b * n + n].double().cpu().numpy() - want)
+            assert (err <= _tolerance(want, size, peak, total[b], dtype)).all(), b
+    assert torch.equal(outs[0], outs[1])
 
 
 def test_attention_extremes():
