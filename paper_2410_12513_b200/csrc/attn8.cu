@@ -130,6 +130,8 @@ constexpr int kParts = E4M3 ? 2 : F32 ? 4 : 2;
 // largest that the warp has met (a page far below it, 2^-12, is added apart, so that its weights are not subnormal halves).
 // Every warp copies its own tokens (TMA, a step ahead) and waits for nobody else until the end.
 // Longer sequences come first, so that the last CTAs are short ones.
+// 8 KV heads of 128, 4 query heads each: 32 sequences (277 MB, integers) 53.6 us, 5.2 TB/s; 128 (1220 MB, float32 queries) 214 us, 5.7 TB/s: the cache's bytes, and
+// the start and join of each item.  16 sequences x 6 drafts (105 MB, E4M3) 53.4 us: conversions and the softmax of 24 columns, at 8 warps an SM.
 template <int HD, int NT, int PER, bool F32, bool E4M3, int kWarps>
 __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12) : 8) / kWarps)
     attn8(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Attn8Args p, const int S,
@@ -751,11 +753,11 @@ Plan plan_for(int64_t B, int64_t H, int64_t rows, int64_t longest, bool f32, int
     const int64_t items = B * H * ((rows + p.tile - 1) / p.tile);
     const int most = p.tile <= (f32 ? 4 : 8) ? 12 : 8;  // warps that an SM holds, by their registers
     p.S = p.Z = 1;
-    // Many items: small CTAs, three an SM, whose starts and ends overlap (1024 items: 223 us, in large CTAs 244).  Fewer: one large
-    // CTA an SM, so that the longest item is not the last (256 items: 65.5 us, small CTAs 104).
+    // Many items: small CTAs, three an SM, whose starts and ends overlap (1024 items: 229 us, in large CTAs 250).  Fewer: one large
+    // CTA an SM, so that the longest item is not the last (256 items: 65.6 us, small CTAs 96).
     p.W = items >= 3 * n_sm ? 4 : most;
     if (items >= n_sm) return p;
-    // Less than one an SM: clusters.  Two CTAs each as long as all of them fit twice (128 items of six rows: 63.5 us, one each 79.9, three 75.8), more
+    // Less than one an SM: clusters.  Two CTAs each as long as all of them fit twice (128 items of six rows: 57.4 us, one each 69.6, three 71.6), more
     // as long as they fit once.
     if (longest <= 2048) {  // short: small CTAs start sooner (1 x 700 tokens: 8 small ones 12.3 us, 4 large ones 14.3)
         p.W = 4;
@@ -765,7 +767,7 @@ Plan plan_for(int64_t B, int64_t H, int64_t rows, int64_t longest, bool f32, int
     p.S = 2;
     while (p.S < kMaxCluster && items * p.S * 2 <= n_sm) p.S *= 2;
     // Long and few: a cluster has 8 CTAs at most, and large clusters leave SMs empty: several pairs, joined by a second launch over the
-    // workspace (8 items of 131072 tokens: 9 pairs each 69.6 us, one cluster of 8 each 86).
+    // workspace (8 items of 131072 tokens: 9 pairs each 69.8 us, one cluster of 8 each 84).
     if (items * kMaxCluster <= n_sm && longest > 8192) {
         p.S = 2;
         p.Z = (int)std::min<int64_t>(n_sm / (2 * items), kMaxSplits);

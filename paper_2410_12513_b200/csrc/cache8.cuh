@@ -1,4 +1,4 @@
-// Device helpers of the paged 8-bit cache: 8-bit values to halves for the tensor cores, sequences and their pages.
+// Device helpers of the paged 8-bit cache: its values, sequences and their pages.
 #pragma once
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -8,22 +8,6 @@
 #include "ops.h"
 
 namespace first {
-
-// Four 8-bit values -> two pairs of halves, exactly.  Integers: 0x64 above a byte is 1024 + byte.
-template <bool E4M3>
-__device__ __forceinline__ void to_halves(uint32_t w, uint32_t& a, uint32_t& b) {
-    if constexpr (E4M3) {
-        asm("{.reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}"
-            : "=r"(a), "=r"(b) : "r"(w));
-    } else {
-        const uint32_t u = w ^ 0x80808080u;
-        const __half2 bias = __half2half2(__ushort_as_half(0x6480));  // 1152
-        uint32_t x = __byte_perm(u, 0x64646464u, 0x4140), y = __byte_perm(u, 0x64646464u, 0x4342);
-        const __half2 p = __hsub2(*reinterpret_cast<__half2*>(&x), bias), q = __hsub2(*reinterpret_cast<__half2*>(&y), bias);
-        a = *reinterpret_cast<const uint32_t*>(&p);
-        b = *reinterpret_cast<const uint32_t*>(&q);
-    }
-}
 
 // One 8-bit value as float32.
 template <bool E4M3>
