@@ -490,10 +490,11 @@ extern "C" int first_verify(const float* target, int64_t target_seq_stride, int6
     a.tokens = tokens; a.accepted = accepted;
     a.B = B; a.K = n_draft; a.V = vocab;
     a.probs = probs != 0;
-    // CTAs a sequence: two a multiprocessor in all (more where that leaves most idle); positions a round: all where there are few sequences, as the
-    // GPU has room for them at once, else one, so that rows behind a refusal are not read
+    // CTAs a sequence: two a multiprocessor in all, what that has room for (24 x 5 of 50257: 8 each 37 us, 16 each 49), or up to three while clusters are
+    // small, as many sequences end early and the next ones shorten the last (180 x 4 of 64000: one each 186 us, two each 121; 80 x 3 of 32000: 57, 49).  Positions a
+    // round: all where there are few sequences, as the GPU has room for them at once, else one, so that rows behind a refusal are not read.
     a.C = 1;
-    while (a.C < kMaxCluster && (int64_t)B * a.C * 2 <= 2 * kSMs && vocab > 4096 * a.C) a.C *= 2;
+    while (a.C < kMaxCluster && (int64_t)B * a.C * 2 <= (a.C < 4 ? 3 : 2) * kSMs && vocab > 4096 * a.C) a.C *= 2;
     a.R = B <= 8 ? kMaxRound : B <= 24 ? 2 : 1;
     constexpr int kSmem = kRing * kPiece * 4;
     static std::atomic<uint64_t> done{0};
