@@ -83,18 +83,21 @@ int32_t take(first_pages* p, int l) {  // (the caller has made sure that there i
 }
 void drop(first_pages* p, int l, int32_t id) {
     if (--p->refs[l][id] > 0) return;
-    bool read = false;
-    for (size_t i = 0; i < p->moves.size();) {
-        Move& m = p->moves[i];
-        if (m.layer == l && m.to == id) {  // nobody wants the copy any more
-            m = p->moves.back();
-            p->moves.pop_back();
-            continue;
+    auto read = [&](int32_t page) {
+        return std::any_of(p->moves.begin(), p->moves.end(), [&](const Move& m) { return m.layer == l && m.from == page; });
+    };
+    const auto copy = std::find_if(p->moves.begin(), p->moves.end(), [&](const Move& m) { return m.layer == l && m.to == id; });
+    if (copy != p->moves.end()) {  // nobody wants the copy any more; its source may have waited for it alone
+        const int32_t from = copy->from;
+        *copy = p->moves.back();
+        p->moves.pop_back();
+        const auto waits = std::find(p->limbo[l].begin(), p->limbo[l].end(), from);
+        if (waits != p->limbo[l].end() && !read(from)) {
+            p->limbo[l].erase(waits);
+            p->free_[l].insert(from);
         }
-        read |= m.layer == l && m.from == id;
-        ++i;
     }
-    if (read) p->limbo[l].push_back(id);
+    if (read(id)) p->limbo[l].push_back(id);
     else p->free_[l].insert(id);
 }
 

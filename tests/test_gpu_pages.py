@@ -402,3 +402,22 @@ def test_imports_wait_for_the_commit():
         for a, b in zip(_read(mgr, l, f, 33), _read(mgr, l, h, 33)):
             assert np.array_equal(a, b)
     mgr.close()
+
+
+def test_a_copy_that_nobody_wants_gives_its_source_back():
+    """A fork takes a page of its own, then both leave before the copy was made: all pages can be had again."""
+    from paper_2410_12513_b200 import FirstPages
+    ctx, _ = _ctx()
+    L = fi.TINY.n_layers
+    mgr = FirstPages(ctx, 3, 4, _caches(fi.TINY, [4] * L, 16, "int8"))
+    a = mgr.join([1] * L)
+    mgr.extend(17, a)
+    mgr.commit()
+    b = mgr.fork(a)
+    mgr.commit()
+    mgr.extend(1, b)
+    mgr.leave(a)
+    mgr.leave(b)
+    mgr.extend(4 * 16, mgr.join([1] * L))
+    mgr.commit()
+    assert (mgr.stats()[0] == 4).all()
