@@ -1517,7 +1517,7 @@ int first_set_pages(first_ctx* c, first_pages* pages) {
     if (!c) return FIRST_E_ARG;
     if (pages) {
         const PagedView v = paged_view(pages);
-        if (v.layers[0].n_kv_heads != c->d.n_kv_heads || v.layers[0].head_dim != c->d.head_dim) return FIRST_E_SHAPE;
+        if (v.L != c->d.n_layers || v.layers[0].n_kv_heads != c->d.n_kv_heads || v.layers[0].head_dim != c->d.head_dim) return FIRST_E_SHAPE;
         if (v.B > c->d.max_batch) return FIRST_E_CAPACITY;
     }
     c->pages = pages;

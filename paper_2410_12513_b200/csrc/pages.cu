@@ -139,6 +139,7 @@ PagedView paged_view(const first_pages* p) {
     PagedView v;
     v.layers = p->layers.data();
     v.pages = p->pages_d;
+    v.L = p->L;
     v.B = p->B;
     v.max_pages = p->max_pages;
     return v;

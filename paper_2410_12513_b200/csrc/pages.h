@@ -7,7 +7,7 @@ namespace first {
 struct PagedView {
     const first_cache8* layers = nullptr;  // [L]
     const int32_t* pages = nullptr;        // dev [L][B][max_pages]
-    int B = 0, max_pages = 0;
+    int L = 0, B = 0, max_pages = 0;
 };
 PagedView paged_view(const first_pages* p);
 

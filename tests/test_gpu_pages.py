@@ -421,3 +421,18 @@ def test_a_copy_that_nobody_wants_gives_its_source_back():
     mgr.extend(4 * 16, mgr.join([1] * L))
     mgr.commit()
     assert (mgr.stats()[0] == 4).all()
+
+
+def test_pages_of_another_model_are_refused():
+    import dataclasses
+    from paper_2410_12513_b200 import FirstError, FirstPages
+    shape = fi.TINY
+    ctx, _ = _ctx()
+    mgr = FirstPages(ctx, 3, 2, _caches(shape, [3] * shape.n_layers, 16, "int8"))
+    for n in (shape.n_layers - 1, shape.n_layers + 2):  # fewer and more layers than there are caches
+        other, _ = _ctx(dataclasses.replace(shape, n_layers=n))
+        with pytest.raises(FirstError) as e:
+            other.set_pages(mgr)
+        assert e.value.status == SHAPE
+    ctx.set_pages(mgr)
+    mgr.close()
