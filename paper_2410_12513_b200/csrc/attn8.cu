@@ -37,6 +37,20 @@ __device__ __forceinline__ void mma_int(uint32_t (&d)[4], const uint32_t (&a)[4]
 __device__ __forceinline__ void e4m3_halves(uint32_t w, uint32_t& a, uint32_t& b) {
     asm("{.reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(a), "=r"(b) : "r"(w));
 }
+// Four 8-bit values as halves, in order.  Integers: 0x64 above a byte is 1024 + byte.
+template <bool E4M3>
+__device__ __forceinline__ void k_halves(uint32_t w, uint32_t& a, uint32_t& b) {
+    if constexpr (E4M3) {
+        e4m3_halves(w, a, b);
+    } else {
+        const __half2 bias = __half2half2(__ushort_as_half(0x6480));  // 1152
+        w ^= 0x80808080u;
+        uint32_t x = __byte_perm(w, 0x64646464u, 0x4140), y = __byte_perm(w, 0x64646464u, 0x4342);
+        const __half2 p = __hsub2(*reinterpret_cast<__half2*>(&x), bias), q = __hsub2(*reinterpret_cast<__half2*>(&y), bias);
+        a = *reinterpret_cast<const uint32_t*>(&p);
+        b = *reinterpret_cast<const uint32_t*>(&q);
+    }
+}
 // Four 8 x 16-byte blocks of shared memory, a row's address a lane (lanes 8 i .. 8 i + 7: block i), whole or with rows and
 // 16-bit columns exchanged.
 __device__ __forceinline__ void blocks(uint32_t at, uint32_t (&r)[4]) {
@@ -115,16 +129,20 @@ constexpr int kRing = 4 / kGroups<NT>;    // steps that a warp has room for: one
 template <int HD, int NT>
 constexpr int kStepBytes = 2 * 16 * kGroups<NT> * HD;
 
-// Integers: a query element in parts of 8 bits, base 256, for products with K as it is: as a multiple of some 2^-14 of its
-// row's largest (2 parts; bfloat16) or 2^-30 (4; float32).  E4M3 has no products of its own on this path, K becomes halves
-// (exactly); a query row is scaled by a power of two into their range and takes one (bfloat16's 8 bits fit) or, PER 1, two (hi + lo).
-template <bool E4M3, bool F32>
-constexpr int kParts = E4M3 ? 2 : F32 ? 4 : 2;
+// How K is multiplied.  Integers with one query row a column pair (PER 1): as they are, a query element in 4 parts of 8 bits, base 256, a
+// multiple of some 2^-30 of its row's largest.  (Two parts were enough for bfloat16's 8 bits only where all elements are of one size:
+// beside a channel of 64 times the others the result was 2e-3 off, of 1024 times 4e-2.)  Otherwise as halves (exactly): E4M3 has no products of its
+// own on this path, and integers with a query row a column take half as many products so (32 sequences x 8 drafts of 4 heads: in parts 164 us, as
+// halves 127).  A query row is scaled by a power of two into their range and takes one (bfloat16's 8 bits fit, down to 2^-30 of the
+// row's largest) or, PER 1, two (hi + lo).
+template <bool E4M3, int PER>
+constexpr bool kHalves = E4M3 || PER == 2;
+constexpr int kParts = 4;
 
 // A cluster takes a tile of query rows (tokens x query heads of a KV head) of one sequence; its CTAs and their warps take
 // its tokens in turns and join (maximum, sum, output) at the end, over shared memory and then over the cluster's.  The
 // tensor cores see tokens as rows: S[16 tokens][8 columns] = K q, O[16 of hd][8 columns] += V' P.
-// S: integers are multiplied as they are, a query row takes a column a part (above), added up in float32; E4M3 as halves.
+// S: by integers as they are a query row takes a column a part (above), added up in float32; by halves a column, or two.
 // O: V in halves (exactly), P in halves, a column a query row (PER 2), or two (PER 1: P = hi + lo, which float32
 // queries need and few rows have room for).  K's page scales act on the float32 products, V's on the weights, relative to the
 // largest that the warp has met (a page far below it, 2^-12, is added apart, so that its weights are not subnormal halves).
@@ -138,17 +156,23 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
           const int Z) {
     constexpr int kThreads = 32 * kWarps;
     constexpr int kRows = NT * 4 * PER, kSteps = HD / 16, kLong = HD / 32;  // steps of 16 (halves) and of 32 (8 bits) along hd
-    constexpr int P = kParts<E4M3, F32>;
-    constexpr int kTiles = E4M3 ? 1 : (P + 1) / 2 * PER;  // S columns' tiles for a tile of O's: integers take two parts of four rows each
+    constexpr int P = kParts;
+    constexpr bool kHalfK = kHalves<E4M3, PER>;
+    constexpr int kTiles = kHalfK ? 1 : P / 2;  // S columns' tiles for a tile of O's: integers take two parts of four rows each
     constexpr int U = kGroups<NT>, kStages = kRing<NT>;
     constexpr int kStride = HD + 16;     // of O in shared memory
-    constexpr bool kHeld = NT * kTiles * (E4M3 ? 2 : 1) <= 3;  // the queries' fragments fit into registers
+    constexpr bool kHeld = NT * kTiles * (kHalfK ? 2 : 1) <= 3;  // the queries' fragments fit into registers
     extern __shared__ __align__(16) uint8_t s_dynamic[];  // [warps][kStages][K | V of a step]; at the end [warps][rows][kStride] float32
     __shared__ uint64_t s_bar[kWarps][kStages];
-    constexpr int kFrag = NT * kTiles * (E4M3 ? kSteps : kLong);  // fragments of the queries
-    __shared__ __align__(16) uint8_t s_q[kRows][E4M3 ? 2 / PER : (P + 1) / 2 * 2][E4M3 ? 2 * HD + 16 : HD + 16];
+    constexpr int kFrag = NT * kTiles * (kHalfK ? kSteps : kLong);  // fragments of the queries
+    // The queries' parts, and, once this CTA has made fragments of them, what the cluster writes.
+    using Parts = uint8_t[kRows][kHalfK ? 2 / PER : P][kHalfK ? 2 * HD + 16 : HD + 16];
+    using Got = float[kRows * HD + kMaxCluster];
+    __shared__ __align__(16) uint8_t s_both[sizeof(Parts) > sizeof(Got) ? sizeof(Parts) : sizeof(Got)];
+    Parts& s_q = *reinterpret_cast<Parts*>(s_both);
+    Got& s_got = *reinterpret_cast<Got*>(s_both);
     __shared__ __align__(16) uint2 s_frag[kHeld ? 1 : kFrag * 32];
-    __shared__ float s_got[kRows * HD + kMaxCluster], s_gm[kMaxCluster][kRows], s_gl[kMaxCluster][kRows];  // written by the cluster
+    __shared__ float s_gm[kMaxCluster][kRows], s_gl[kMaxCluster][kRows];  // written by the cluster
     __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows], s_f[kMaxCluster > kWarps ? kMaxCluster : kWarps][kRows];
     __shared__ float s_rs[kRows], s_inv[kRows];
     __shared__ int s_len[kMaxSorted], s_mine;
@@ -200,7 +224,6 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
     const int tok0 = r0 / p.G;
     const int first_lim = (int)min((int64_t)q.before + tok0 + 1, cap);
     const int end = (int)min((int64_t)q.before + (r0 + rows - 1) / p.G + 1, cap);  // tokens that any row sees
-    if (S > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");  // (waited for before the first remote store)
     const int t1 = (end + 15) / 16;
 
     // ---- the first tokens' values are on their way while the queries are prepared
@@ -289,14 +312,14 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
         amax = __reduce_max_sync(0xffffffffu, amax);
         odd = __any_sync(0xffffffffu, odd);  // (no number among the parts stands for infinities and NaN: the row is NaN)
         // the row's largest magnitude goes to [2^kTop, 2^(kTop+1)); 2^126 times at most, and the inverse is a float32 too
-        constexpr int kTop = E4M3 ? 13 : 8 * P - 3;
+        constexpr int kTop = kHalfK ? 13 : 8 * P - 3;
         const int e = max(min(127 + kTop - (int)(amax >> 23), 126), -126);
         const float up = __int_as_float((e + 127) << 23);
-        if (lane == 0) s_rs[r] = odd ? __int_as_float(0x7fc00000) : __int_as_float((127 - e) << 23) * (E4M3 ? 1.f : (float)(1 << 8 * (P - 1)));
+        if (lane == 0) s_rs[r] = odd ? __int_as_float(0x7fc00000) : __int_as_float((127 - e) << 23) * (kHalfK ? 1.f : (float)(1 << 8 * (P - 1)));
 #pragma unroll
         for (int i = 0; i < HD / 32; ++i) {
             const float x = f[i] * up;
-            if constexpr (E4M3) {
+            if constexpr (kHalfK) {
                 const __half hi = __float2half_rn(x);
                 reinterpret_cast<__half*>(s_q[r][0])[i * 32 + lane] = hi;
                 if constexpr (PER == 1) reinterpret_cast<__half*>(s_q[r][1])[i * 32 + lane] = __float2half_rn(x - __half2float(hi));
@@ -308,25 +331,23 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
                     s_q[r][k][i * 32 + lane] = (uint8_t)digit;
                     n = (n - digit) >> 8;
                 }
-                if constexpr (P % 2) s_q[r][P][i * 32 + lane] = 0;
             }
         }
     }
     __syncthreads();
-    // Fragment of tile n's (k-th) tile of columns, step s.  Integers: column g is row (n, PER*(g/2) + j), part 2k' + g%2, k = (j, k').
-    // E4M3: column g is row (n, g) or, PER 1, half g%2 of row (n, g/2).
+    // Fragment of tile n's (k-th) tile of columns, step s.  In parts: column g is row (n, g/2), part 2k + g%2.
+    // Halves: column g is row (n, g) or, PER 1, half g%2 of row (n, g/2).
     auto query = [&](int n, int k, int s) {
         const uint8_t* x;
-        if constexpr (E4M3) {
+        if constexpr (kHalfK) {
             x = &s_q[n * 4 * PER + (PER == 1 ? g >> 1 : g)][PER == 1 ? g & 1 : 0][(s * 16 + 4 * c) * 2];
             return *reinterpret_cast<const uint2*>(x);
         } else {
-            constexpr int kPairs = (P + 1) / 2;
-            x = &s_q[n * 4 * PER + PER * (g >> 1) + k / kPairs][2 * (k % kPairs) + (g & 1)][s * 32 + 4 * c];
+            x = &s_q[n * 4 + (g >> 1)][2 * k + (g & 1)][s * 32 + 4 * c];
             return make_uint2(*reinterpret_cast<const uint32_t*>(x), *reinterpret_cast<const uint32_t*>(x + 16));
         }
     };
-    constexpr int kQSteps = E4M3 ? kSteps : kLong;
+    constexpr int kQSteps = kHalfK ? kSteps : kLong;
     uint2 qf[kHeld ? kFrag : 1];
     if constexpr (kHeld) {
 #pragma unroll
@@ -335,6 +356,7 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
         for (int i = warp; i < kFrag; i += kWarps) s_frag[i * 32 + lane] = query(i / (kTiles * kQSteps), i / kQSteps % kTiles, i % kQSteps);
         __syncthreads();
     }
+    if (S > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");  // (waited for before the first remote store)
     auto fragment = [&](int i) {
         if constexpr (kHeld) return qf[i];
         else return s_frag[i * 32 + lane];
@@ -416,7 +438,7 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
         uint32_t v0[kAhead ? kAhead : 1][4];
 #pragma unroll
         for (int w = 0; w < kAhead; ++w) blocks_turned(v_in + k_off[w], v0[w]);
-        if constexpr (E4M3) {
+        if constexpr (kHalfK) {
             float d[U][NT][4];
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -432,8 +454,8 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     uint32_t x[4];
-                    e4m3_halves(a[u][s / 2][s % 2 * 2], x[0], x[2]);
-                    e4m3_halves(a[u][s / 2][s % 2 * 2 + 1], x[1], x[3]);
+                    k_halves<E4M3>(a[u][s / 2][s % 2 * 2], x[0], x[2]);
+                    k_halves<E4M3>(a[u][s / 2][s % 2 * 2 + 1], x[1], x[3]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma(d[u][n], x[0], x[1], x[2], x[3], b[n].x, b[n].y);
                 }
@@ -448,38 +470,36 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
                         for (int x = 0; x < 2; ++x)
                             z[u][n][j][x] = (PER == 1 ? d[u][n][2 * x] + d[u][n][2 * x + 1] : d[u][n][2 * x + j]) * (ks[u] * rs[n][j]);
         } else {
-            constexpr int kPairs = (P + 1) / 2;
+            constexpr int kPairs = P / 2;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
+                uint32_t d[U][kPairs][4];
 #pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    uint32_t d[U][kPairs][4];
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
+                    for (int k = 0; k < kPairs; ++k)
 #pragma unroll
-                        for (int k = 0; k < kPairs; ++k)
+                        for (int e = 0; e < 4; ++e) d[u][k][e] = kIntZero;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) d[u][k][e] = kIntZero;
+                for (int s = 0; s < kLong; ++s)
 #pragma unroll
-                    for (int s = 0; s < kLong; ++s)
+                    for (int k = 0; k < kPairs; ++k) {
+                        const uint2 b = fragment((n * kTiles + k) * kLong + s);
 #pragma unroll
-                        for (int k = 0; k < kPairs; ++k) {
-                            const uint2 b = fragment((n * kTiles + j * kPairs + k) * kLong + s);
+                        for (int u = 0; u < U; ++u) mma_int(d[u][k], a[u][s], b);
+                    }
 #pragma unroll
-                            for (int u = 0; u < U; ++u) mma_int(d[u][k], a[u][s], b);
-                        }
+                for (int u = 0; u < U; ++u) {
+                    const float f = ks[u] * rs[n][0];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const float f = ks[u] * rs[n][j];
+                    for (int x = 0; x < 2; ++x) {
+                        float v = 0.f;
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            float v = 0.f;
-#pragma unroll
-                            for (int k = P - 1; k >= 0; --k) v = fmaf(v, 0.00390625f, __uint_as_float(d[u][k / 2][2 * x + (k & 1)]) - 12582912.f);
-                            z[u][n][j][x] = v * f;
-                        }
+                        for (int k = P - 1; k >= 0; --k) v = fmaf(v, 0.00390625f, __uint_as_float(d[u][k / 2][2 * x + (k & 1)]) - 12582912.f);
+                        z[u][n][0][x] = v * f;
                     }
                 }
+            }
         }
         // ---- weights
         if (special) {
@@ -633,7 +653,7 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
     const uint32_t got = (uint32_t)__cvta_generic_to_shared(s_got), gm = (uint32_t)__cvta_generic_to_shared(s_gm),
                    gl = (uint32_t)__cvta_generic_to_shared(s_gl);
     __syncthreads();
-    if (S > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // (all have started)
+    if (S > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // (all have their fragments)
     for (int i = tid; i < S * rows; i += kThreads) {
         const int k = i / rows, r = i % rows;
         float top = -INFINITY, sum = 0.f;
