@@ -496,7 +496,8 @@ int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
  * first_attn8    attention of the new tokens (already appended): new token i of sequence b sees positions 0 .. len[b] + i;
  *                out = sum_t softmax_t(scale * q . k_t) v_t, query head h with KV head h / (n_q_heads / n_kv_heads).
  *                Positions without a page are not there; a row that sees nothing gives zeros.  Products and sums are
- *                float32; weights have 11 bits of mantissa with bfloat16 q and 22 with float32 q; out is rounded once.  The
+ *                float32; a weight times its page's V scale is held to 22 bits, or to 2^-32 of the largest weight times the largest V scale, if
+ *                that is more; out is rounded once.  The
  *                result is the same in every run and depends on nothing but the sequence itself and the launch's sizes (B, max_new, max_pages).  Meant
  *                for one token a sequence and for drafts under verification: the cache is read once for every 32 (float32: 16) query rows of a KV
  *                head.  workspace (dev, 4-byte aligned, or NULL): few long sequences are cut among more of the GPU if it has

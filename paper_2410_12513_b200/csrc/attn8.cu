@@ -143,9 +143,10 @@ constexpr int kParts = 4;
 // its tokens in turns and join (maximum, sum, output) at the end, over shared memory and then over the cluster's.  The
 // tensor cores see tokens as rows: S[16 tokens][8 columns] = K q, O[16 of hd][8 columns] += V' P.
 // S: by integers as they are a query row takes a column a part (above), added up in float32; by halves a column, or two.
-// O: V in halves (exactly), P in halves, a column a query row (PER 2), or two (PER 1: P = hi + lo, which float32
-// queries need and few rows have room for).  K's page scales act on the float32 products, V's on the weights, relative to the
-// largest that the warp has met (a page far below it, 2^-12, is added apart, so that its weights are not subnormal halves).
+// O: V in halves (exactly), P = hi + lo in halves: two columns a query row (PER 1), or one column and a second product (PER 2, where rows are many).
+// (One half, 11 bits, was 2^-12 of the largest value off, visible in bfloat16 where values cancel; the second products cost 16 x 6 drafts 57 -> 63 us.)
+// K's page scales act on the float32 products, V's on the weights, relative to the largest that the warp has met (a page far below it, 2^-12, is added
+// apart, so that its weights are not subnormal halves).
 // Every warp copies its own tokens (TMA, a step ahead) and waits for nobody else until the end.
 // Longer sequences come first, so that the last CTAs are short ones.
 // 8 KV heads of 128, 4 query heads each: 32 sequences (277 MB, integers) 53.6 us, 5.2 TB/s; 128 (1220 MB, float32 queries) 214 us, 5.7 TB/s: the cache's bytes, and
@@ -542,7 +543,7 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
                     }
                 }
         }
-        uint32_t pb[U][NT][2];
+        uint32_t pb[U][NT][2], pl[U][NT][2];  // (pl: PER 2's low halves)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const float f = apart ? 1.f : vr[u];
@@ -560,9 +561,12 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
                     __half2 v;
                     if constexpr (PER == 1) {
                         const __half hi = __float2half_rn(w[0]);
-                        v = __halves2half2(hi, F32 ? __float2half_rn(w[0] - __half2float(hi)) : __ushort_as_half(0));
+                        v = __halves2half2(hi, __float2half_rn(w[0] - __half2float(hi)));
                     } else {
                         v = __floats2half2_rn(w[0], w[PER - 1]);
+                        const float2 hi = __half22float2(v);
+                        const __half2 lo = __floats2half2_rn(w[0] - hi.x, w[PER - 1] - hi.y);
+                        pl[u][n][x] = transpose8(*reinterpret_cast<const uint32_t*>(&lo));
                     }
                     pb[u][n][x] = transpose8(*reinterpret_cast<uint32_t*>(&v));
                 }
@@ -601,7 +605,10 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) mma(o[n][w + y], x[y][0], x[y][1], x[y][2], x[y][3], pb[u][n][0], pb[u][n][1]);
+                        for (int y = 0; y < 2; ++y) {
+                            mma(o[n][w + y], x[y][0], x[y][1], x[y][2], x[y][3], pb[u][n][0], pb[u][n][1]);
+                            if constexpr (PER == 2) mma(o[n][w + y], x[y][0], x[y][1], x[y][2], x[y][3], pl[u][n][0], pl[u][n][1]);
+                        }
                 }
         } else {
 #pragma unroll
@@ -617,6 +624,7 @@ __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12
                         for (int y = 0; y < 2; ++y) {
                             if (u == 0 || apart) t[n][y][0] = t[n][y][1] = t[n][y][2] = t[n][y][3] = 0.f;
                             mma(t[n][y], x[y][0], x[y][1], x[y][2], x[y][3], pb[u][n][0], pb[u][n][1]);
+                            if constexpr (PER == 2) mma(t[n][y], x[y][0], x[y][1], x[y][2], x[y][3], pl[u][n][0], pl[u][n][1]);
                             if (apart || u == U - 1)
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) o[n][w + y][e] = apart ? fmaf(t[n][y][e], vr[u], o[n][w + y][e]) : o[n][w + y][e] + t[n][y][e];
