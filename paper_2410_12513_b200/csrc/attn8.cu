@@ -732,12 +732,26 @@ __global__ void __launch_bounds__(128) attn8_join(const Attn8Args p, const int Z
     __shared__ float s_f[kMaxSplits], s_inv;
     for (int r = blockIdx.z; r < q.n * p.G; r += gridDim.z) {
         const int64_t part = part_of(blockIdx.y, h, r, p.s.max_new * p.G, p.c.H) * Z;
-        if (threadIdx.x < 32) {
-            const int k = threadIdx.x;
-            const float m = k < Z ? p.part_ml[2 * (part + k)] : -INFINITY, top = warp_max(m);
-            const float f = m == -INFINITY ? 1.f : exp2_fast(m - top), sum = warp_sum(k < Z ? p.part_ml[2 * (part + k) + 1] * f : 0.f);
-            s_f[k] = f;
-            if (k == 0) s_inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (threadIdx.x < 32) {  // kEach splits a lane
+            constexpr int kEach = kMaxSplits / 32;
+            static_assert(kMaxSplits % 32 == 0, "every split has a lane");
+            float m[kEach], top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int k = threadIdx.x + 32 * i;
+                m[i] = k < Z ? p.part_ml[2 * (part + k)] : -INFINITY;
+                top = fmaxf(top, m[i]);
+            }
+            top = warp_max(top);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int k = threadIdx.x + 32 * i;
+                const float f = m[i] == -INFINITY ? 1.f : exp2_fast(m[i] - top);
+                s_f[k] = f;
+                if (k < Z) sum += p.part_ml[2 * (part + k) + 1] * f;
+            }
+            sum = warp_sum(sum);
+            if (threadIdx.x == 0) s_inv = sum == 0.f ? 0.f : 1.f / sum;
         }
         __syncthreads();
         for (int d = threadIdx.x; d < hd; d += 128) {
