@@ -13,7 +13,7 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;  // that count; one more warp copies
-constexpr int kMaxCluster = 16, kMaxRound = 8;
+constexpr int kMaxCluster = 16, kMaxRound = 8, kSums = 5;
 
 struct VerifyArgs {
     const float *target, *draft;  // draft NULL: each drafted token had probability 1
@@ -168,7 +168,7 @@ __device__ __forceinline__ void add(Part& p, const float4* piece, const Span& s,
 // the copy's rate, the rest, and the 29-31 us of small batches, is latency: a round's copies, the cluster's joins, the decision, and the 64-bit pass.
 __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs p) {
     __shared__ Part s_warp[2 * kMaxRound][kWarps], s_part[2][2 * kMaxRound];
-    __shared__ double s_sum[4][kWarps], s_all[4][kMaxCluster * kWarps], s_run[kWarps], s_pow[32], s_seg;
+    __shared__ double s_sum[kSums][kWarps], s_all[kSums][kMaxCluster * kWarps], s_run[kWarps], s_pow[32], s_seg;
     __shared__ int s_ok[kMaxRound], s_hit, s_found, s_at;
     __shared__ float s_tops[kMaxRound][2], s_top[2];
     extern __shared__ __align__(128) float4 s_ring[];  // [kRing][kPiece] tokens
@@ -319,8 +319,9 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
         auto of_p = [&](float x, auto& pow32) { return p.probs ? fmax((double)x, 0.0) : weight64(x, tp, sc, pow32); };
         auto of_q = [&](float x, auto& pow32) { return p.probs ? fmax((double)x, 0.0) : td > -INFINITY ? weight64(x, td, sc, pow32) : 0.0; };
         // p - ratio q, ratio = sum of p / sum of q.  Which tokens have something left hardly hangs on it: those of a ratio good to float32
-        // are taken, whose sums, p's and q's apart, then give what is left with the 64-bit ratio (a token on the wrong side
-        // adds 2^-20 of its own weight at most; if no more than 2^-10 of all is left, they are taken anew by that ratio).
+        // are taken, whose sums, p's and q's apart, then give what is left with the 64-bit ratio.  A token on the wrong side is one whose p and
+        // rough q are within the ratios' difference of each other, and is off by that difference times its q: the sum of such q's says whether it
+        // matters (2^-36 of what is left); then the tokens are taken anew by the 64-bit ratio.
         double rough = p.probs ? 1.0 : d && s_run[1] > 0.0 ? s_run[0] / s_run[1] : 0.0;
         double ratio = rough;
         bool sure = p.probs;
@@ -328,8 +329,10 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
             const bool two = d && !again;
             // every warp of the cluster sums a run of tokens
             constexpr int kDeep = 4;
+            constexpr double kNear = 0x1p-19;
             const int span = ((hi - lo + kWarps - 1) / kWarps + 31) & ~31, w0 = min(lo + warp * span, hi), w1 = min(w0 + span, hi);
             double sums[4] = {0.0, 0.0, 0.0, 0.0};  // p and q of the tokens that have something left, of all
+            float close = 0.f;                      // q of those next to the border
 #pragma unroll 1
             for (int base = w0; base < w1; base += 32 * kDeep) {
                 const int e0 = base + lane;
@@ -345,7 +348,9 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
                     const double vx = of_p(x[i], from_lanes), vy = two ? of_q(y[i], from_lanes) : 0.0;
                     sums[2] += vx;
                     sums[3] += vy;
-                    if (two ? vx > rough * vy : e0 + 32 * i != skip || again) {
+                    const double border = rough * vy;
+                    if ((unsigned)(__double2hiint(vx) - __double2hiint(border) + 4) <= 8u) close += (float)vy;  // (within 4 steps of 2^-20 or finer)
+                    if (two ? vx > border : e0 + 32 * i != skip || again) {
                         sums[0] += vx;
                         sums[1] += vy;
                     }
@@ -353,30 +358,35 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) sums[k] = warp_sum64(sums[k]);
+            close = warp_sum(close);
             __syncthreads();
-            if (lane == 0 && warp < kWarps)
+            if (lane == 0 && warp < kWarps) {
                 for (int k = 0; k < 4; ++k) s_sum[k][warp] = sums[k];
+                s_sum[4][warp] = close;
+            }
             cluster.sync();
             const int each_run = (C * kWarps + 31) / 32;
             for (int r = tid; r < C * kWarps; r += kThreads + 32) {
                 const double* from = cluster.map_shared_rank(&s_sum[0][0], r / kWarps) + r % kWarps;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) s_all[k][r % each_run * 32 + r / each_run] = from[k * kWarps];  // (a lane's runs a row apart: other banks)
+                for (int k = 0; k < kSums; ++k) s_all[k][r % each_run * 32 + r / each_run] = from[k * kWarps];  // (a lane's runs a row apart: other banks)
             }
             __syncthreads();
             // which run: the last one that is not empty and starts at or before the target, a lane some neighbouring runs.  (What runs
             // once is kept short: fetching instructions is what takes the time here.)
             if (warp == 0) {
                 const int n = max(0, min(each_run, C * kWarps - lane * each_run));  // of the lane
-                double zp = 0.0, zq = 0.0;
+                double zp = 0.0, zq = 0.0, near = 0.0;
                 if (two && !p.probs) {
 #pragma unroll 1
                     for (int r = 0; r < n; ++r) {
                         zp += s_all[2][r * 32 + lane];
                         zq += s_all[3][r * 32 + lane];
+                        near += s_all[4][r * 32 + lane];
                     }
                     zp = warp_sum64(zp);
                     zq = warp_sum64(zq);
+                    near = warp_sum64(near);
                     ratio = zq > 0.0 ? zp / zq : 0.0;
                 }
                 auto left = [&](int r) {
@@ -399,7 +409,8 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
                 const int last = __reduce_max_sync(0xffffffffu, found);
                 if (last >= 0 && found == last) s_seg = want - start;
                 if (lane == 0) {
-                    s_found = two && !sure && total < 0x1p-10 * zp ? -2 : last;
+                    const double off = fabs(rough - ratio);
+                    s_found = two && !sure && (off > kNear * rough || off * near > 0x1p-36 * total) ? -2 : last;
                     s_run[2] = ratio;
                 }
             }
