@@ -598,7 +598,7 @@ int first_set_pages(first_ctx *ctx, first_pages *pages);
  *   tokens    dev int32 [B][n_draft+1]: the accepted drafts, the new token (-1 if the row has no candidate), then -1
  *   accepted  dev int32 [B]: how many drafts were accepted
  * Sums that decide which token a draw falls on are formed in 64 bits, of weights good to 2^-39 and from the tokens that have something left, those on the
- * border to within 2^-36 of what is left; acceptance has float32's precision.  The result is the same in every run.  (Rows are fetched in whole 16 bytes: up to 12 bytes before and behind a row are read, never used.)  Stateless, no scratch, no
+ * border to within 2^-36 of what is left; acceptance has float32's precision.  The result is the same in every run.  Stateless, no scratch, no
  * wait, one launch; B = 0 does nothing.  accepted[b] = -1: a bounded wait inside the kernel gave up, the sequence's result is void.
  * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides below vocab), FIRST_E_UNSUPPORTED (alignment, n_draft > FIRST_VERIFY_MAX_DRAFTS, vocab >
  * FIRST_SAMPLE_MAX_VOCAB), FIRST_E_CAPACITY, FIRST_E_CUDA. */

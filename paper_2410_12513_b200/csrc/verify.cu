@@ -83,8 +83,8 @@ __device__ __forceinline__ Part warp_join(Part p, const Scale& sc, bool greedy) 
     return p;
 }
 
-// A row's part [lo, hi) comes in pieces of kPiece tokens (whole 16 bytes of memory: what they hold of neighbouring rows is passed over) through
-// a ring in shared memory.
+// A row's part [lo, hi) comes in pieces of kPiece tokens through a ring in shared memory, by copies of its whole 16 bytes of memory; the up to three
+// tokens at either end that share theirs with others are fetched one by one (nothing outside the row is read).
 constexpr int kPiece = 8192, kRing = 3, kEach = kPiece / (4 * kThreads);
 struct Span {
     const float* from;  // 16-byte aligned
@@ -98,9 +98,6 @@ __device__ __forceinline__ Span span_of(const float* row, int lo, int hi) {
     s.pieces = s.n > 0 ? (s.off + s.n + kPiece - 1) / kPiece : 1;
     return s;
 }
-__device__ __forceinline__ uint32_t piece_bytes(const Span& s, int q) {
-    return s.n > 0 ? 16 * min(kPiece / 4, (s.off + s.n + 3) / 4 - q * (kPiece / 4)) : 0;
-}
 constexpr uint32_t kPolls = 1u << 22;
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {  // bounded: false after kPolls tries
     for (uint32_t i = 0; i < kPolls; ++i) {
@@ -111,12 +108,24 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {  // bo
     }
     return false;
 }
+// The tokens of piece q that are not copied, one by one (out of line: few rows have any).
+__device__ __noinline__ void edges(uint32_t dst, const float* from, int off, int all, int q) {
+    const int head = q == 0 && off ? min(4, all) : off, tail = max(all & ~3, head);  // [off, head) and [tail, all) of the span
+#pragma unroll 1
+    for (int i = off; i < head; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + 4 * i), "f"(__ldg(from + i)) : "memory");
+#pragma unroll 1
+    for (int i = tail; i < all && tail / kPiece == q; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + 4 * (i % kPiece)), "f"(__ldg(from + i)) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (the place is copied into again later)
+}
+// (One thread's.)  What it stores itself is there when the barrier completes, like what is copied.
 __device__ __forceinline__ void copy_piece(uint32_t dst, uint32_t bar, const Span& s, int q) {
-    const uint32_t bytes = piece_bytes(s, q);
+    if ((s.off && q == 0) || ((s.off + s.n) & 3)) edges(dst, s.from, s.off, s.off + s.n, q);
+    const int first = q * (kPiece / 4), b0 = max(first, s.off ? 1 : 0), b1 = min(first + kPiece / 4, (s.off + s.n) / 4);  // whole 16 bytes
+    const uint32_t bytes = 16 * max(b1 - b0, 0);
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
     if (bytes)
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     ::"r"(dst), "l"(s.from + (int64_t)q * kPiece), "r"(bytes), "r"(bar) : "memory");
+                     ::"r"(dst + 16 * (b0 - first)), "l"(s.from + 4 * (int64_t)b0), "r"(bytes), "r"(bar) : "memory");
 }
 template <bool GREEDY>
 __device__ __forceinline__ void add(Part& p, const float4* piece, const Span& s, int q, int lo, const Scale& sc) {

@@ -40,3 +40,28 @@ def test_a_draft_model_that_is_almost_the_target():
             if accepted[b] != a or tokens[b].tolist() != out:
                 wrong.append((b, tokens[b].tolist(), out))
     assert not wrong and seen >= 0.9 * B, (seen, wrong)
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 4, 5, 6, 7, 8, 9, 30, 4097, 8191, 8193, 8200, 16390])
+def test_rows_at_every_alignment(V):
+    """Rows that start and end at every place of 16 bytes, the first and the last of their storage among them; their neighbours would win."""
+    import torch
+    B, n = 3, 2
+    g = torch.Generator().manual_seed(V)
+    for off in range(4):
+        for pad in range(4):
+            stride = V + pad
+            rows = []
+            for count in (n + 1, n):
+                store = torch.full((off + B * count * stride - pad,), 1e30)  # (nothing behind the last row)
+                view = store.cuda().as_strided((B, count, V), (count * stride, stride, 1), off)
+                x = torch.randn(B, count, V, generator=g) * 2
+                view.copy_(x)
+                rows.append((x, view))
+            drafted = torch.randint(0, V, (B, n), generator=g).int()
+            u, w = torch.rand(B, n, generator=g) * 0.5, torch.rand(B, generator=g)
+            for temp in (torch.tensor([1.0, 0.5, 0.0]), torch.tensor([0.0, 2.0, 1.0])):
+                tokens, accepted = _verify(rows[0][1], rows[1][1], drafted.cuda(), u.cuda(), w.cuda(), temp.cuda())
+                for b in range(B):
+                    out, a, clear = verified(rows[0][0][b].numpy(), rows[1][0][b].numpy(), drafted[b].tolist(), float(temp[b]), u[b].tolist(), float(w[b]), False)
+                    assert not clear or (int(accepted[b]) == a and tokens[b].tolist() == out), (off, pad, b, tokens[b].tolist(), out)
