@@ -507,7 +507,7 @@ int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
  *                from, to).  All layers alike in format and sizes.  No page may be written twice, nor be both read and
  *                written.  A move outside the caches is left out (FIRST_FLAG_BAD_PAGE).
  * Errors: FIRST_E_ARG, FIRST_E_SHAPE (negative strides, rows that are written overlap, total != B without cu_new, heads),
- * FIRST_E_UNSUPPORTED (page, head_dim, alignment, more than 1024 KV heads, more than 96 layers), FIRST_E_CAPACITY (grid
+ * FIRST_E_UNSUPPORTED (page, head_dim, arrays that do not begin at a multiple of their elements' size, more than 1024 KV heads, more than 96 layers), FIRST_E_CAPACITY (grid
  * sizes: max_pages * page above 2^30, more than 65000 pages or 2^18 query rows a sequence, B above 65535), FIRST_E_CUDA. */
 #define FIRST_CACHE_INT8 0
 #define FIRST_CACHE_E4M3 1
@@ -600,7 +600,7 @@ int first_set_pages(first_ctx *ctx, first_pages *pages);
  * Sums that decide which token a draw falls on are formed in 64 bits, of weights good to 2^-39 and from the tokens that have something left, those on the
  * border to within 2^-36 of what is left; acceptance has float32's precision.  The result is the same in every run.  Stateless, no scratch, no
  * wait, one launch; B = 0 does nothing.  accepted[b] = -1: a bounded wait inside the kernel gave up, the sequence's result is void.
- * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides below vocab), FIRST_E_UNSUPPORTED (alignment, n_draft > FIRST_VERIFY_MAX_DRAFTS, vocab >
+ * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides below vocab), FIRST_E_UNSUPPORTED (an array that is not 4-byte aligned, n_draft > FIRST_VERIFY_MAX_DRAFTS, vocab >
  * FIRST_SAMPLE_MAX_VOCAB), FIRST_E_CAPACITY, FIRST_E_CUDA. */
 #define FIRST_VERIFY_MAX_DRAFTS 32
 int first_verify(const float *target, int64_t target_seq_stride, int64_t target_row_stride, const float *draft,

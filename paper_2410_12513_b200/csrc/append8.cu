@@ -16,15 +16,16 @@ int check_cache8(const first_cache8* c) {
     if (c->n_kv_heads > 1024) return FIRST_E_UNSUPPORTED;
     if ((int64_t)c->n_pages * c->n_kv_heads * c->page > 0x7fffffff) return FIRST_E_CAPACITY;  // (rows are counted in 32 bits)
     if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16) return FIRST_E_UNSUPPORTED;
-    if ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) % 4) return FIRST_E_UNSUPPORTED;
+    if (!words_ok({c->k_scale, c->v_scale})) return FIRST_E_UNSUPPORTED;
     return FIRST_OK;
 }
 
-int check_seqs8(const int32_t* pages, int32_t max_pages, const int32_t* len, const int32_t* cu, int32_t B, int32_t total, int32_t max_new) {
+int check_seqs8(const int32_t* pages, int32_t max_pages, const int32_t* len, const int32_t* cu, int32_t B, int32_t total, int32_t max_new,
+                const uint32_t* flags) {
     if (B < 0 || total < 0 || max_pages < 0 || max_new < 0) return FIRST_E_ARG;
     if (!cu && total != B) return FIRST_E_SHAPE;
     if (B > 0 && total > 0 && max_new > 0 && (!len || (max_pages > 0 && !pages))) return FIRST_E_ARG;
-    return FIRST_OK;
+    return words_ok({pages, len, cu, flags}) ? FIRST_OK : FIRST_E_UNSUPPORTED;
 }
 
 // Rows that are written belong to one (token, head) each; rows that are read may repeat.
@@ -451,7 +452,7 @@ int first_append8(const first_cache8* cache, const void* k, int64_t k_token_stri
                   const int32_t* pages, int32_t max_pages, const int32_t* len, int32_t B, int32_t max_new, uint32_t* flags,
                   void* stream) {
     int rc = check_cache8(cache);
-    if (rc || (rc = check_seqs8(pages, max_pages, len, cu_new, B, total, max_new)) ||
+    if (rc || (rc = check_seqs8(pages, max_pages, len, cu_new, B, total, max_new, flags)) ||
         (rc = check_rows8(k, k_token_stride, k_head_stride, cache->n_kv_heads, cache->head_dim, dtype, total, false)) ||
         (rc = check_rows8(v, v_token_stride, v_head_stride, cache->n_kv_heads, cache->head_dim, dtype, total, false)))
         return rc;
@@ -470,7 +471,7 @@ int first_read8(const first_cache8* cache, const int32_t* pages, int32_t max_pag
                 int32_t B, int32_t total, int32_t max_rows, void* k, int64_t k_token_stride, int64_t k_head_stride, void* v,
                 int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, uint32_t* flags, void* stream) {
     int rc = check_cache8(cache);
-    if (rc || (rc = check_seqs8(pages, max_pages, start, cu, B, total, max_rows)) ||
+    if (rc || (rc = check_seqs8(pages, max_pages, start, cu, B, total, max_rows, flags)) ||
         (rc = check_rows8(k, k_token_stride, k_head_stride, cache->n_kv_heads, cache->head_dim, dtype, total, true)) ||
         (rc = check_rows8(v, v_token_stride, v_head_stride, cache->n_kv_heads, cache->head_dim, dtype, total, true)))
         return rc;
@@ -501,7 +502,7 @@ int first_read8(const first_cache8* cache, const int32_t* pages, int32_t max_pag
 int first_copy_pages(const first_cache8* layers, int32_t n_layers, const int32_t* moves, int64_t n_moves, uint32_t* flags,
                      void* stream) {
     if (!layers || n_layers <= 0 || n_moves < 0 || (n_moves > 0 && !moves)) return FIRST_E_ARG;
-    if (n_layers > kMaxCopyLayers) return FIRST_E_UNSUPPORTED;
+    if (n_layers > kMaxCopyLayers || !words_ok({moves, flags})) return FIRST_E_UNSUPPORTED;
     CopyArgs a{};
     for (int l = 0; l < n_layers; ++l) {
         int rc = check_cache8(layers + l);

@@ -904,9 +904,9 @@ extern "C" int first_attn8(const first_cache8* cache, const void* q, int64_t q_t
     int rc = check_cache8(cache);
     if (rc) return rc;
     const int hd = cache->head_dim;
-    if ((rc = check_seqs8(pages, max_pages, len, cu_new, B, total, max_new))) return rc;
+    if ((rc = check_seqs8(pages, max_pages, len, cu_new, B, total, max_new, flags))) return rc;
     if (n_q_heads <= 0 || workspace_bytes < 0) return FIRST_E_ARG;
-    if (reinterpret_cast<uintptr_t>(workspace) % 4) return FIRST_E_UNSUPPORTED;
+    if (!words_ok({workspace})) return FIRST_E_UNSUPPORTED;
     if (n_q_heads % cache->n_kv_heads) return FIRST_E_SHAPE;
     if ((rc = check_rows8(q, q_token_stride, q_head_stride, n_q_heads, hd, dtype, total, false)) ||
         (rc = check_rows8(out, out_token_stride, out_head_stride, n_q_heads, hd, dtype, total, true)))

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <initializer_list>
 
 #include "first.h"
 
@@ -111,8 +112,14 @@ int64_t attn8_part_floats(int64_t B, int64_t H, int64_t rows, int hd, int64_t lo
 cudaError_t attn8_launch(const Attn8Args& a, cudaStream_t st, bool pdl, int n_sm);
 
 // Checks of arguments: FIRST_OK or an error.
+inline bool words_ok(std::initializer_list<const void*> arrays) {  // arrays of 32-bit values (NULL is fine) begin at a multiple of their size
+    for (const void* p : arrays)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return false;
+    return true;
+}
 int check_cache8(const first_cache8* c);
-int check_seqs8(const int32_t* pages, int32_t max_pages, const int32_t* len, const int32_t* cu, int32_t B, int32_t total, int32_t max_new);
+int check_seqs8(const int32_t* pages, int32_t max_pages, const int32_t* len, const int32_t* cu, int32_t B, int32_t total, int32_t max_new,
+                const uint32_t* flags);
 int check_rows8(const void* p, int64_t tok, int64_t head, int32_t heads, int32_t hd, int32_t dtype, int64_t total, bool written);
 Cache8 cache8_of(const first_cache8& c);
 

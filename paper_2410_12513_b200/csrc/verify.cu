@@ -501,7 +501,7 @@ extern "C" int first_verify(const float* target, int64_t target_seq_stride, int6
     if (!target || !draws || !tokens || !accepted || (n_draft > 0 && (!drafted || !uniforms))) return FIRST_E_ARG;
     if ((n_draft > 0 && target_row_stride < vocab) || (draft && n_draft > 1 && draft_row_stride < vocab)) return FIRST_E_SHAPE;
     if (B > 1 && (target_seq_stride < vocab || (draft && n_draft > 0 && draft_seq_stride < vocab))) return FIRST_E_SHAPE;
-    if ((reinterpret_cast<uintptr_t>(target) | reinterpret_cast<uintptr_t>(draft)) % 4) return FIRST_E_UNSUPPORTED;
+    if (!words_ok({target, draft, drafted, temperature, uniforms, draws, tokens, accepted})) return FIRST_E_UNSUPPORTED;
     VerifyArgs a{};
     a.target = target; a.draft = n_draft > 0 ? draft : nullptr;
     a.t_seq = target_seq_stride; a.t_row = target_row_stride; a.d_seq = draft_seq_stride; a.d_row = draft_row_stride;
