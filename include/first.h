@@ -540,7 +540,7 @@ int first_copy_pages(const first_cache8 *layers, int32_t n_layers, const int32_t
  * cache, belong on one stream; pages freed since the last commit may be handed out again by the next one.
  *
  * first_pages_create  max_seqs <= max_batch slots of at most max_pages pages a layer; layers host [L], alike in format and sizes (n_pages may
- *                     differ), borrowed.  Allocates the device tables.
+ *                     differ), borrowed; every layer has memory of its own (FIRST_E_ARG).  Allocates the device tables.
  * first_pages_join    a sequence enters: mask_row host uint8 [L].  src != NULL: the next commit takes over its first n_tokens keys and values from
  *                     sequence src_seq of a slab cache (per_layer = 0, of the model's dtype, such as a first_prefill call filled; it has to
  *                     stay as it is until then); src == NULL: n_tokens = 0.

@@ -8,6 +8,7 @@
 #include <map>
 #include <new>
 #include <set>
+#include <utility>
 #include <vector>
 
 #include "first.h"
@@ -129,6 +130,22 @@ int free_slot(const first_pages* p) {
     return -1;
 }
 
+// Whether any two of the layers' arrays have memory in common.
+bool overlap(const first_cache8* layers, int L) {
+    std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+    for (int l = 0; l < L; ++l) {
+        const first_cache8& c = layers[l];
+        const uintptr_t heads = (uintptr_t)c.n_pages * c.n_kv_heads, bytes = heads * c.page * c.head_dim;
+        if (!heads) continue;
+        for (const void* x : {c.k, c.v}) spans.emplace_back(reinterpret_cast<uintptr_t>(x), reinterpret_cast<uintptr_t>(x) + bytes);
+        for (const float* x : {c.k_scale, c.v_scale}) spans.emplace_back(reinterpret_cast<uintptr_t>(x), reinterpret_cast<uintptr_t>(x) + 4 * heads);
+    }
+    std::sort(spans.begin(), spans.end());
+    for (size_t i = 1; i < spans.size(); ++i)
+        if (spans[i].first < spans[i - 1].second) return true;
+    return false;
+}
+
 bool is_live(const first_pages* p, int32_t slot) { return slot >= 0 && slot < p->B && p->seq[slot].live; }
 
 }  // namespace
@@ -169,6 +186,10 @@ int first_pages_create(first_ctx* ctx, int32_t max_seqs, int32_t max_pages, cons
     first_pages* p = new (std::nothrow) first_pages();
     if (!p) return FIRST_E_ARG;
     try {
+        if (overlap(layers, d.n_layers)) {
+            delete p;
+            return FIRST_E_ARG;
+        }
         p->ctx = ctx; p->d = d; p->B = max_seqs; p->L = d.n_layers; p->max_pages = max_pages; p->page = layers[0].page;
         p->layers.assign(layers, layers + p->L);
         p->seq.resize(p->B);

@@ -1,0 +1,37 @@
+"""Page managers given caches, plans and imports that do not fit them (B200 only)."""
+import pytest
+
+import first_inputs as fi
+from test_gpu_pages import ARG, _caches, _ctx
+
+pytestmark = pytest.mark.gpu
+
+
+def test_layers_that_share_memory_are_refused():
+    """Each layer hands out page ids of its own: two layers over one memory would overwrite each other."""
+    import torch
+    from paper_2410_12513_b200 import Cache8, FirstError, FirstPages
+    ctx, _ = _ctx()
+    shape = fi.TINY
+    L = shape.n_layers
+    own = _caches(shape, [3] * L, 16, "int8")
+
+    def status(caches):
+        with pytest.raises(FirstError) as e:
+            FirstPages(ctx, 2, 3, caches)
+        return e.value.status
+    assert status([own[0]] * L) == ARG
+    assert status(own[:3] + [own[1]]) == ARG
+    a, b = own[0], own[3]
+    for names in ({"k": a.k}, {"v": a.v}, {"k": a.v}, {"k_scale": a.k_scale}, {"v_scale": a.k_scale}, {"v": b.k}, {"v_scale": b.k_scale}):
+        kw = {"k": b.k, "v": b.v, "k_scale": b.k_scale, "v_scale": b.v_scale} | names
+        assert status(own[:3] + [Cache8(**kw)]) == ARG, list(names)
+    # one memory cut in parts: side by side it is fine, by a page less it is not
+    pool = torch.zeros(2 * L * 3 + 1, *a.k.shape[1:], dtype=torch.int8, device="cuda")
+    scales = torch.zeros(2 * L * 3, shape.n_kv_heads, device="cuda")
+    parts = [Cache8(pool[6 * l:6 * l + 3], pool[6 * l + 3:6 * l + 6], scales[6 * l:6 * l + 3], scales[6 * l + 3:6 * l + 6]) for l in range(L)]
+    FirstPages(ctx, 2, 3, parts).close()
+    over = Cache8(pool[6 * L - 7:6 * L - 4], pool[6 * L - 3:6 * L], scales[6 * L - 6:6 * L - 3], scales[6 * L - 3:])
+    assert status(parts[:3] + [over]) == ARG
+    none = torch.zeros(0, *a.k.shape[1:], dtype=torch.int8, device="cuda")  # (a layer that nobody keeps has no pages)
+    FirstPages(ctx, 2, 3, own[:3] + [Cache8(none, none, scales[:0], scales[:0])]).close()
