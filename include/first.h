@@ -559,8 +559,9 @@ int first_copy_pages(const first_cache8 *layers, int32_t n_layers, const int32_t
  *                     their own; any pointer may be NULL
  * first_pages_stats   per layer: pages in use, the highest id in use (-1: none); live sequences (any pointer may be NULL)
  * first_pages_tokens  the sequence's tokens, by the host's count
- * first_set_pages     first_decode_step with kv == NULL then appends to and attends over this manager's pages (its plan must be the last commit's; free rows need a
- *                     valid token id).  NULL: none.  The manager has to outlive the setting; commit before its first step.
+ * first_set_pages     first_decode_step with kv == NULL then appends to and attends over this manager's pages (FIRST_E_STATE unless the context's plan is the last commit's:
+ *                     first_set_mask, first_prefill or another pool's commit in between ask for a commit; free rows need a valid token id).  FIRST_E_ARG: the
+ *                     manager of another context.  NULL: none.  The manager has to outlive the setting; commit before its first step.
  * Errors: FIRST_E_ARG, FIRST_E_SHAPE (layers differ, or from the model), FIRST_E_CAPACITY (no slot, no pages: nothing is taken then),
  * FIRST_E_STATE (free slot), FIRST_E_UNSUPPORTED (more than 96 layers), FIRST_E_CUDA. */
 typedef struct first_pages first_pages;

@@ -74,6 +74,7 @@ struct first_ctx {
     std::vector<int32_t> cnt_h;
     int B = 0;
     bool has_mask = false;
+    uint64_t plan_serial = 0;  // counts the plans
     int64_t launches = 0;
     // per-kernel-class timing (off unless first_profile enables it)
     bool profiling = false;
@@ -999,6 +1000,8 @@ std::vector<double> plain_freqs(const first_model_desc& d) {
 
 }  // namespace
 
+uint64_t first::plan_serial(const first_ctx* c) { return c->plan_serial; }
+
 extern "C" {
 
 const char* first_status_string(int status) {
@@ -1155,6 +1158,7 @@ int first_set_mask(first_ctx* c, const uint8_t* mask, int32_t B, void* stream) {
     CU_TRY(cudaStreamSynchronize(st));
     if (fl & FIRST_FLAG_BAD_MASK) return FIRST_E_DEVICE_FLAG;
     c->B = B;
+    c->plan_serial += 1;
     c->has_mask = true;  // launch rows = the exact counts; recorded step graphs are looked up by them
     return FIRST_OK;
 }
@@ -1185,6 +1189,7 @@ int first_set_mask_host(first_ctx* c, const uint8_t* mask, int32_t B, void* stre
     // bucket finds its recorded step graph again.
     for (int l = 0; l < L; ++l) c->cnt_h[l] = cnt[l] == 0 ? 0 : std::min<int>(B, (cnt[l] + 15) / 16 * 16);
     c->B = B;
+    c->plan_serial += 1;
     c->has_mask = true;
     return FIRST_OK;
 }
@@ -1208,7 +1213,7 @@ int first_decode_step(first_ctx* c, const int32_t* tokens, const first_kv_cache*
     const PagedView* paged = nullptr;
     if (!kv) {
         view = paged_view(c->pages);
-        if (view.B != c->B) return FIRST_E_STATE;  // (the plan is not that of the manager's last commit)
+        if (view.B != c->B || view.plan != c->plan_serial) return FIRST_E_STATE;  // (the plan is not that of the manager's last commit)
         first_pages_kv(const_cast<first_pages*>(c->pages), &of_pages);
         of_pages.per_layer = 1;  // (capacities by layer; there are no slabs)
         kv = &of_pages;
@@ -1518,6 +1523,7 @@ int first_set_pages(first_ctx* c, first_pages* pages) {
     if (pages) {
         const PagedView v = paged_view(pages);
         if (v.L != c->d.n_layers || v.layers[0].n_kv_heads != c->d.n_kv_heads || v.layers[0].head_dim != c->d.head_dim) return FIRST_E_SHAPE;
+        if (v.ctx != c) return FIRST_E_ARG;  // (its commits set the other context's plan)
         if (v.B > c->d.max_batch) return FIRST_E_CAPACITY;
     }
     c->pages = pages;

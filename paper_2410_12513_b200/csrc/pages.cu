@@ -70,6 +70,7 @@ struct first_pages {
     int32_t *pages_d = nullptr, *cap_d = nullptr, *len_d = nullptr, *pos_d = nullptr, *zero_d = nullptr, *update_d = nullptr, *moves_d = nullptr;
     int64_t* off_d = nullptr;
     int64_t moves_cap = 0;
+    uint64_t plan = 0;  // the context's plan that is this manager's
 };
 
 namespace {
@@ -154,6 +155,8 @@ namespace first {
 
 PagedView paged_view(const first_pages* p) {
     PagedView v;
+    v.ctx = p->ctx;
+    v.plan = p->plan;
     v.layers = p->layers.data();
     v.pages = p->pages_d;
     v.L = p->L;
@@ -407,7 +410,9 @@ int first_pages_commit(first_pages* p, void* stream) {
         std::vector<uint8_t> mask((size_t)p->B * p->L, 0);
         for (int b = 0; b < p->B; ++b)
             if (p->seq[b].live) std::memcpy(&mask[(size_t)b * p->L], p->seq[b].keep.data(), p->L);
-        return first_set_mask_host(p->ctx, mask.data(), p->B, stream);
+        const int rc = first_set_mask_host(p->ctx, mask.data(), p->B, stream);
+        if (rc == FIRST_OK) p->plan = plan_serial(p->ctx);
+        return rc;
     } catch (...) {
         return FIRST_E_ARG;
     }

@@ -1,8 +1,9 @@
 """Page managers given caches, plans and imports that do not fit them (B200 only)."""
+import numpy as np
 import pytest
 
 import first_inputs as fi
-from test_gpu_pages import ARG, _caches, _ctx
+from test_gpu_pages import ARG, STATE, _caches, _ctx
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +36,54 @@ def test_layers_that_share_memory_are_refused():
     assert status(parts[:3] + [over]) == ARG
     none = torch.zeros(0, *a.k.shape[1:], dtype=torch.int8, device="cuda")  # (a layer that nobody keeps has no pages)
     FirstPages(ctx, 2, 3, own[:3] + [Cache8(none, none, scales[:0], scales[:0])]).close()
+
+
+def test_a_step_asks_for_the_managers_own_plan():
+    """Another mask of as many rows, a prompt phase, another manager's commit: the step over pages waits for a commit again."""
+    import torch
+    from harness import GpuKV
+    from paper_2410_12513_b200 import FirstError, FirstPages
+    ctx, _ = _ctx()
+    shape = fi.TINY
+    L = shape.n_layers
+    mgr, other = (FirstPages(ctx, 2, 4, _caches(shape, [6] * L, 16, "int8")) for _ in "12")
+    ctx.set_pages(mgr)
+    s = mgr.join([1, 0, 1, 1])
+    toks, logits = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.empty(2, shape.vocab, device="cuda")
+
+    def steps(n):
+        mgr.extend()
+        mgr.commit()
+        ctx.decode_step(toks, None, logits)
+        assert ctx.device_flags() == 0
+        assert [int(mgr.layer(l)[2][s]) for l in range(L)] == [n, 0, n, n]
+
+    def refused():
+        with pytest.raises(FirstError) as e:
+            ctx.decode_step(toks, None, logits)
+        assert e.value.status == STATE
+    refused()
+    steps(1)
+    ctx.set_mask_host(np.ones((2, L), np.uint8))
+    refused()
+    mgr.commit()
+    ctx.set_mask(torch.ones(2, L, dtype=torch.uint8, device="cuda"))
+    refused()
+    steps(2)
+    stage = GpuKV(shape, [8], False)
+    ctx.prefill(toks, np.array([0, 2], np.int32), stage.c)
+    refused()
+    steps(3)
+    other.join([1] * L)
+    other.commit()
+    refused()
+    steps(4)
+    mgr.compact()
+    steps(5)
+    ctx2, _ = _ctx()
+    with pytest.raises(FirstError) as e:
+        ctx2.set_pages(mgr)
+    assert e.value.status == ARG
+    ctx.set_pages(None)
+    mgr.close()
+    other.close()
