@@ -542,8 +542,9 @@ int first_copy_pages(const first_cache8 *layers, int32_t n_layers, const int32_t
  * first_pages_create  max_seqs <= max_batch slots of at most max_pages pages a layer; layers host [L], alike in format and sizes (n_pages may
  *                     differ), borrowed; every layer has memory of its own (FIRST_E_ARG).  Allocates the device tables.
  * first_pages_join    a sequence enters: mask_row host uint8 [L].  src != NULL: the next commit takes over its first n_tokens keys and values from
- *                     sequence src_seq of a slab cache (per_layer = 0, of the model's dtype, such as a first_prefill call filled; it has to
- *                     stay as it is until then); src == NULL: n_tokens = 0.
+ *                     sequence src_seq (one that src has: its tables are on the device) of a slab cache (per_layer = 0, of the model's dtype, such as a
+ *                     first_prefill call filled; it has to stay as it is until then).  More tokens than its slab holds: the commit's work sets
+ *                     FIRST_FLAG_BAD_SEQ_TABLE in the context's flags, and the pages stay without values.  src == NULL: n_tokens = 0.
  * first_pages_fork    a new slot with the same tokens.  Fork and trim speak of tokens that are there: FIRST_E_STATE while an import, or tokens that the
  *                     sequence was extended by, wait for the commit.
  * first_pages_extend  the sequence (slot -1: every one) is about to gain n_new tokens: pages for them, all or nothing.  After the next commit first_decode_step or

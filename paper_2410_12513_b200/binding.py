@@ -419,6 +419,9 @@ class FirstPages:
         m = np.ascontiguousarray(np.asarray(mask_row), dtype=np.uint8)
         if m.size != self.L:
             raise ValueError(f"mask_row must have {self.L} entries")
+        off = getattr(src, "slab_off", None)
+        if off is not None and not 0 <= int(src_seq) < off.shape[-1]:
+            raise ValueError(f"src has {off.shape[-1]} sequences")
         slot = C.c_int32(-1)
         self._call("first_pages_join", m.ctypes.data, C.byref(src.c) if src is not None else None, int(src_seq), int(n_tokens), C.byref(slot))
         return slot.value

@@ -216,6 +216,14 @@ __global__ void __launch_bounds__(kThreads) append8(const Cache8 c, const Seqs8 
     if (!find_seq(s, blockIdx.z, q)) return;
     const int tid = threadIdx.x, h = blockIdx.x >> 1, hd = c.hd, page = 1 << c.shift;
     const bool is_v = blockIdx.x & 1;
+    int64_t row0 = q.start;
+    if (s.row_off) {
+        row0 += *s.row_off;
+        if (row0 < 0 || row0 + q.n > s.row_total || (s.row_cap && q.n > *s.row_cap)) {  // more than the sequence has there
+            if (s.flags && tid == 0) atomicOr(s.flags, FIRST_FLAG_BAD_SEQ_TABLE);
+            return;
+        }
+    }
     const int64_t first = ((int64_t)(q.before >> c.shift) + blockIdx.y) << c.shift;  // the page's first position
     const int64_t end = (int64_t)q.before + q.n;
     if (first >= end) return;
@@ -227,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) append8(const Cache8 c, const Seqs8 
     const int lo = (int)max((int64_t)q.before - first, (int64_t)0), hi = (int)min(end - first, (int64_t)page);
     const Rows8& r = is_v ? vr : kr;
     // row `lo` of the page
-    const T* src = static_cast<const T*>(r.p) + ((s.row_off ? *s.row_off : 0) + q.start + first + lo - q.before) * r.tok + h * r.head;
+    const T* src = static_cast<const T*>(r.p) + (row0 + first + lo - q.before) * r.tok + h * r.head;
     uint8_t* dst = (is_v ? c.v : c.k) + ((((int64_t)p * c.H + h) << c.shift)) * hd;
     float* scale = (is_v ? c.vs : c.ks) + (int64_t)p * c.H + h;
     const float held = lo > 0 ? *scale : 0.f;

@@ -1000,6 +1000,7 @@ std::vector<double> plain_freqs(const first_model_desc& d) {
 
 }  // namespace
 
+uint32_t* first::device_flags(const first_ctx* c) { return c->flags; }
 uint64_t first::plan_serial(const first_ctx* c) { return c->plan_serial; }
 
 extern "C" {

@@ -86,6 +86,8 @@ struct Seqs8 {
     int B = 0, total = 0, max_new = 1;
     int each = 1;                    // without cu: new tokens of every sequence
     const int64_t* row_off = nullptr;  // dev, or NULL: the sequence's rows start that much later (one sequence alone)
+    int64_t row_total = 0;           // with it: rows that there are,
+    const int32_t* row_cap = nullptr;  // dev, or NULL: of them the sequence's own
     const int32_t *idx = nullptr, *m_dev = nullptr;
     uint32_t* flags = nullptr;       // or NULL
     const float2* cs = nullptr;      // [.][hd/2] by sequence: rotate q and k on the way (the step), or NULL

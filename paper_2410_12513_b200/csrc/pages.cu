@@ -401,6 +401,9 @@ int first_pages_commit(first_pages* p, void* stream) {
                 s.len = p->zero_d;
                 s.B = 1; s.total = s.max_new = s.each = im.n;
                 s.row_off = im.src.slab_off + im.src_seq;
+                s.row_total = im.src.cap_total;
+                s.row_cap = im.src.slab_cap ? im.src.slab_cap + im.src_seq : nullptr;
+                s.flags = device_flags(p->ctx);
                 const bool f32 = p->d.dtype == FIRST_DTYPE_F32;
                 const int64_t hd = p->d.head_dim;
                 const Rows8 k{im.k[l], hd, im.src.cap_total * hd, f32}, v{im.v[l], hd, im.src.cap_total * hd, f32};

@@ -12,6 +12,7 @@ struct PagedView {
     int L = 0, B = 0, max_pages = 0;
 };
 PagedView paged_view(const first_pages* p);
+uint32_t* device_flags(const first_ctx* c);
 uint64_t plan_serial(const first_ctx* c);  // how many plans (masks) the context has been given
 
 }  // namespace first

@@ -87,3 +87,42 @@ def test_a_step_asks_for_the_managers_own_plan():
     ctx.set_pages(None)
     mgr.close()
     other.close()
+
+
+def test_imports_of_more_than_a_slab_holds():
+    """The lengths of slabs are on the device: an import beyond one is left out and flagged, whoever the neighbour is; others arrive."""
+    from harness import GpuKV
+    from paper_2410_12513_b200 import FirstPages
+    from test_gpu_pages import _read
+    ctx, _ = _ctx()
+    shape = fi.TINY
+    L = shape.n_layers
+    stage = GpuKV(shape, [40, 20, 30], False)
+    for l in range(L):
+        stage.k[l].normal_()
+        stage.v[l].normal_()
+    for seq, n, bad in ((0, 40, False), (0, 41, True), (1, 21, True), (1, 20, False), (2, 31, True), (2, 90, True), (2, 30, False)):
+        caches = _caches(shape, [12] * L, 16, "int8")
+        for c in caches:
+            c.k.zero_(), c.v.zero_(), c.k_scale.fill_(2.0), c.v_scale.fill_(2.0)
+        mgr = FirstPages(ctx, 2, 6, caches)
+        if bad:  # (another sequence is not touched by it)
+            mgr.join([1] * L, stage.c, seq, n)
+        s = mgr.join([1] * L, stage.c, 0, 17)
+        good = s if bad else mgr.join([1] * L, stage.c, seq, n)
+        mgr.commit()
+        assert ctx.device_flags() == (32 if bad else 0), (seq, n)
+        o, m = (0, 17) if bad else (int(stage.off[seq]), n)
+        for l in range(L):
+            for got, want in zip(_read(mgr, l, good, m), (stage.k[l], stage.v[l])):
+                want = want[:, o:o + m].permute(1, 0, 2).cpu().numpy()
+                assert np.abs(got - want).max() <= np.abs(want).max() / 127 * 0.501
+            if bad:
+                assert (caches[l].k_scale == 2.0).sum() == 10 * shape.n_kv_heads  # (the good one's two pages alone)
+        mgr.close()
+    mgr = FirstPages(ctx, 2, 6, _caches(shape, [12] * L, 16, "int8"))
+    for seq in (-1, 3):
+        with pytest.raises(ValueError):
+            mgr.join([1] * L, stage.c, seq, 3)
+    assert mgr.stats()[2] == 0
+    mgr.close()
