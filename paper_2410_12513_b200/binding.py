@@ -387,6 +387,7 @@ class FirstPages:
     def __init__(self, ctx, max_seqs, max_pages, caches):
         self._ctx, self.caches = ctx, list(caches)
         self.B, self.L, self.max_pages, self.h = int(max_seqs), len(self.caches), int(max_pages), None
+        self._sources = []  # caches that the next commit imports from
         if self.L != ctx.shape.n_layers:
             raise ValueError(f"one cache a layer: {ctx.shape.n_layers}")
         arr = (Cache8C * self.L)(*[c.c for c in self.caches])
@@ -424,6 +425,8 @@ class FirstPages:
             raise ValueError(f"src has {off.shape[-1]} sequences")
         slot = C.c_int32(-1)
         self._call("first_pages_join", m.ctypes.data, C.byref(src.c) if src is not None else None, int(src_seq), int(n_tokens), C.byref(slot))
+        if src is not None:
+            self._sources.append(src)
         return slot.value
 
     def fork(self, slot):
@@ -442,10 +445,12 @@ class FirstPages:
 
     def commit(self, stream=None):
         self._call("first_pages_commit", _stream(stream))
+        self._sources.clear()
         self._ctx.B = self.B
 
     def compact(self, stream=None):
         self._call("first_pages_compact", _stream(stream))
+        self._sources.clear()
         self._ctx.B = self.B
 
     def tokens(self, slot):

@@ -126,3 +126,35 @@ def test_imports_of_more_than_a_slab_holds():
             mgr.join([1] * L, stage.c, seq, 3)
     assert mgr.stats()[2] == 0
     mgr.close()
+
+
+@pytest.mark.parametrize("commit", ["commit", "compact"])
+def test_a_source_lives_until_its_import(commit):
+    """The cache that a sequence joins from is held on to until the commit has read it, and no longer."""
+    import gc
+    import weakref
+
+    import torch
+    from harness import GpuKV
+    from paper_2410_12513_b200 import FirstPages
+    from test_gpu_pages import _read
+    ctx, _ = _ctx()
+    shape = fi.TINY
+    L = shape.n_layers
+    mgr = FirstPages(ctx, 2, 6, _caches(shape, [12] * L, 16, "int8"))
+    stage = GpuKV(shape, [300], False)
+    for l in range(L):
+        stage.k[l].fill_(0.5)
+        stage.v[l].fill_(0.25)
+    size, ref = stage.k[0].shape, weakref.ref(stage.c)
+    s = mgr.join([1] * L, stage.c, 0, 40)
+    del stage
+    gc.collect()
+    others = [torch.full(size, 9.0, device="cuda") for _ in range(4 * L)]  # (memory that is given back is handed out again)
+    getattr(mgr, commit)()
+    for l in range(L):
+        k, v = _read(mgr, l, s, 40)
+        assert np.allclose(k, 0.5, rtol=1e-6) and np.allclose(v, 0.25, rtol=1e-6)
+    gc.collect()
+    assert ref() is None and len(others) == 4 * L
+    mgr.close()
