@@ -164,8 +164,8 @@ __device__ __forceinline__ bool quotients(const Eight<T>& r, float inv, uint2& o
 }
 
 // Eight finite values exactly (out of line): where a little more and a little less than x * inv have different neighbours, x is compared
-// with the middle between the two, times the scale: a fused product and difference has the exact sign.  (bfloat16 values meet exact ties
-// often: quotients of 8-bit numbers.)
+// with the middle between the two, times the scale: a fused product and difference has the exact sign, as long as it cannot fall below the smallest
+// float32 (a scale from 2^-100 up).  (bfloat16 values meet exact ties often: quotients of 8-bit numbers.)
 template <bool E4M3, typename T>
 __device__ __noinline__ uint2 quotients_exact(const Eight<T> r, float s, float inv) {
     uint32_t w[2] = {0, 0};
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(kThreads) append8(const Cache8 c, const Seqs8 
     }
     const float fresh = __uint_as_float(amax) * (1.f / (E4M3 ? 448.f : 127.f));
     const float now = held >= fresh || held != held ? held : fresh;  // (a NaN stays: what the page holds is none either)
-    const float inv = now > 1e-37f ? 1.f / now : 0.f;
+    const float inv = now >= 0x1p-100f ? 1.f / now : 0.f;
 #pragma unroll
     for (int k = 0; k < kAppendHold; ++k) {
         const int i = tid + k * kThreads;
