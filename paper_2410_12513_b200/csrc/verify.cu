@@ -511,11 +511,14 @@ extern "C" int first_verify(const float* target, int64_t target_seq_stride, int6
     a.B = B; a.K = n_draft; a.V = vocab;
     a.probs = probs != 0;
     // CTAs a sequence: two a multiprocessor in all, what that has room for (24 x 5 of 50257: 8 each 37 us, 16 each 49), or up to three while clusters are
-    // small, as many sequences end early and the next ones shorten the last (180 x 4 of 64000: one each 186 us, two each 121; 80 x 3 of 32000: 57, 49).  Positions a
-    // round: all where there are few sequences, as the GPU has room for them at once, else one, so that rows behind a refusal are not read.
+    // small, as many sequences end early and the next ones shorten the last (180 x 4 of 64000: one each 186 us, two each 121; 80 x 3 of 32000: 57, 49).
+    // Positions of the first round: several where there are few sequences and a round's latency is the time, one where there are many and the rows
+    // behind a refusal cost more (5 drafts of 128256, most of them accepted | half: 1 sequence in rounds of 1, 2, 4, 8: 43, 41, 35, 39 | 27, 29, 35, 39 us;
+    // 8: 51, 51, 49, 49 | 43, 45, 45, 51; 16: 57, 55, 59, 63 | 55, 55, 55, 64; 48: 127, 125, 125, 125 | 123, 121, 117, 127; 64: 127, 129, 123, 133 |
+    // 109, 117, 135, 152; 100: 168, 173, 201, 219 | 152, 170, 203, 238; 24 x 5 looked up of 50257: 39, 38, 37, 37; 48 of them 47, 51, 47, 49 | 41, 37, 43, 49).
     a.C = 1;
     while (a.C < kMaxCluster && (int64_t)B * a.C * 2 <= (a.C < 4 ? 3 : 2) * kSMs && vocab > 4096 * a.C) a.C *= 2;
-    a.R = B <= 8 ? kMaxRound : B <= 24 ? 2 : 1;
+    a.R = B <= 8 ? 4 : B <= 48 ? 2 : 1;
     constexpr int kSmem = kRing * kPiece * 4;
     static std::atomic<uint64_t> done{0};
     if (allow_launch(verify_rows, kSmem, true, done) != cudaSuccess) return FIRST_E_CUDA;
