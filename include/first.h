@@ -473,7 +473,7 @@ int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
  * keys (and values) of head_dim 8-bit numbers, and one float32 scale a (page, head): a key is its number times its page's
  * scale.  Sequences own lists of pages, [B][max_pages] ids, -1 = none: position t of sequence b is token t % page of page
  * pages[b][t / page].  Two sequences may share a page that neither appends to (first_pages_* keeps count of that).  In 8
- * bits a cache takes half of the room and, in decoding, half of the time of a bfloat16 one; rounding: half a 1/127 of the
+ * bits a cache takes half of the room of a bfloat16 one, and decoding reads half of the bytes; rounding: half a 1/127 of the
  * page's largest key (INT8), or 2^-4 of each value (E4M3, 3 bits of mantissa).
  *   k, v              dev [n_pages][n_kv_heads][page][head_dim], 16-byte aligned
  *   k_scale, v_scale  dev float32 [n_pages][n_kv_heads]
@@ -498,7 +498,8 @@ int first_set_rope(first_ctx *ctx, const double *inv_freq, double factor);
  *                Positions without a page are not there; a row that sees nothing gives zeros.  Products and sums are
  *                float32; a weight times its page's V scale is held to 22 bits, or to 2^-32 of the largest weight times the largest V scale, if
  *                that is more; out is rounded once.  The
- *                result is the same in every run and depends on nothing but the sequence itself and the launch's sizes (B, max_new, max_pages).  Meant
+ *                result is the same in every run and depends on nothing but the sequence itself, the launch's sizes (B, max_new, max_pages) and whether there is a
+ *                workspace of the size below: they say how the sums are cut.  Meant
  *                for one token a sequence and for drafts under verification: the cache is read once for every 32 (float32: 16) query rows of a KV
  *                head.  workspace (dev, 4-byte aligned, or NULL): few long sequences are cut among more of the GPU if it has
  *                first_attn8_workspace bytes (host; 0: there is no use for one), and then take a second launch.  Calls that may overlap need workspaces of their own.

@@ -144,13 +144,14 @@ constexpr int kParts = 4;
 // tensor cores see tokens as rows: S[16 tokens][8 columns] = K q, O[16 of hd][8 columns] += V' P.
 // S: by integers as they are a query row takes a column a part (above), added up in float32; by halves a column, or two.
 // O: V in halves (exactly), P = hi + lo in halves: two columns a query row (PER 1), or one column and a second product (PER 2, where rows are many).
-// (One half, 11 bits, was 2^-12 of the largest value off, visible in bfloat16 where values cancel; the second products cost 16 x 6 drafts 57 -> 63 us.)
+// (One half, 11 bits, was 2^-12 of the largest value off, visible in bfloat16 where values cancel; the second products cost 16 x 6 drafts 57 -> 63 us, launched alone.)
 // K's page scales act on the float32 products, V's on the weights, relative to the largest that the warp has met (a page far below it, 2^-12, is added
 // apart, so that its weights are not subnormal halves).
 // Every warp copies its own tokens (TMA, a step ahead) and waits for nobody else until the end.
 // Longer sequences come first, so that the last CTAs are short ones.
-// 8 KV heads of 128, 4 query heads each: 32 sequences (277 MB, integers) 53.6 us, 5.2 TB/s; 128 (1220 MB, float32 queries) 214 us, 5.7 TB/s: the cache's bytes, and
-// the start and join of each item.  16 sequences x 6 drafts (105 MB, E4M3) 53.4 us: conversions and the softmax of 24 columns, at 8 warps an SM.
+// 8 KV heads of 128, 4 query heads each: 32 sequences (277 MB, integers) 55 us, 5.0 TB/s; 128 (1220 MB, float32 queries) 216 to 233 us on several cards, 5.2 to
+// 5.65 TB/s: the cache's bytes, and the start and join of each item.  16 sequences x 6 drafts (105 MB, E4M3) 59.5 us: conversions, the softmax of 24
+// columns and two products with V, at 8 warps an SM.
 template <int HD, int NT, int PER, bool F32, bool E4M3, int kWarps>
 __global__ void __launch_bounds__(32 * kWarps, (NT == 1 ? (kWarps == 8 ? 16 : 12) : 8) / kWarps)
     attn8(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Attn8Args p, const int S,

@@ -173,7 +173,7 @@ __device__ __forceinline__ void add(Part& p, const float4* piece, const Span& s,
 // One cluster a sequence.  Rounds of R positions, then 2 R and so on: every row's sum and largest logit, then the decisions (taken by every
 // CTA alike), until one is refused or all are accepted; the rows of later positions are not read.  Then the new token's
 // distribution, in 64 bits, over the one row (or two) that it comes from: those rows are in L2 by now.
-// 64 sequences x 7 drafts of 128256 tokens, a draft model's logits too: 131 us; the rows up to the refusals (225 MB of 493) would take 34 at
+// 64 sequences x 7 drafts of 128256 tokens, a draft model's logits too: 136 us; the rows up to the refusals (225 MB of 493) would take 34 at
 // the copy's rate, the rest, and the 29-31 us of small batches, is latency: a round's copies, the cluster's joins, the decision, and the 64-bit pass.
 __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs p) {
     __shared__ Part s_warp[2 * kMaxRound][kWarps], s_part[2][2 * kMaxRound];
