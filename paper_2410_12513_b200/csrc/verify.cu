@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) verify_rows(const VerifyArgs
                     sums[2] += vx;
                     sums[3] += vy;
                     const double border = rough * vy;
-                    if ((unsigned)(__double2hiint(vx) - __double2hiint(border) + 4) <= 8u) close += (float)vy;  // (within 4 steps of 2^-20 or finer)
+                    if (two && (unsigned)(__double2hiint(vx) - __double2hiint(border) + 4) <= 8u) close += (float)vy;  // (within 4 steps of 2^-20 or finer)
                     if (two ? vx > border : e0 + 32 * i != skip || again) {
                         sums[0] += vx;
                         sums[1] += vy;
