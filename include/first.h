@@ -600,7 +600,8 @@ int first_set_pages(first_ctx *ctx, first_pages *pages);
  *             float32 below 1)
  *   tokens    dev int32 [B][n_draft+1]: the accepted drafts, the new token (-1 if the row has no candidate), then -1
  *   accepted  dev int32 [B]: how many drafts were accepted
- * Sums that decide which token a draw falls on are formed in 64 bits, of weights good to 2^-39 and from the tokens that have something left, those on the
+ * Sums that decide which token a draw falls on are formed in 64 bits, of weights good to 2^-39 (below 2^-1000 of the row's
+ * largest they count as 0) and from the tokens that have something left, those on the
  * border to within 2^-36 of what is left; acceptance has float32's precision.  The result is the same in every run.  Stateless, no scratch, no
  * wait, one launch; B = 0 does nothing.  accepted[b] = -1: a bounded wait inside the kernel gave up, the sequence's result is void.
  * Errors: FIRST_E_ARG, FIRST_E_SHAPE (strides below vocab), FIRST_E_UNSUPPORTED (an array that is not 4-byte aligned, n_draft > FIRST_VERIFY_MAX_DRAFTS, vocab >
